@@ -223,6 +223,51 @@ int dr_conv2d_bwd_params(const dr_tensor* xd, const void* x, const dr_conv* cd, 
 /* One step of gradient descent on count fp32 parameters: w[i] = w[i] - lr * dw[i]. */
 int dr_sgd_step(size_t count, float* w, const float* dw, float lr, void* stream);
 
+/* ---- layers with a normalisation of their own, and learning them ---------------------------------------------------
+ * Layer normalisation over the channels of every pixel (Ba, Kiros, Hinton 2016), in the place of the LRN or BatchNorm
+ * layer that slimming removes: with the sums over the c channels of one pixel,
+ *   y = gamma_c (x - mean) rstd + beta_c,  mean = sum x / c,  rstd = 1 / sqrt(sum (x - mean)^2 / c + eps),
+ * then max(y, 0) if relu != 0.  Either order, fp32 or bf16; a matrix of rows is {rows, c, 1, 1}.  gamma, beta: fp32 device
+ * vectors of c entries (NULL: ones, zeros).  mean, rstd: fp32 device arrays of n h w entries, in pixel order, that the
+ * gradient reads (NULL: not stored).  Sums are held in fp32.  x == y (in place) is allowed.  eps >= 0. */
+int dr_layernorm_fwd(const dr_tensor* d, const void* x, const float* gamma, const float* beta, float eps, int relu, void* y, float* mean,
+                     float* rstd, void* stream);
+
+/* Its gradient, from dy = dL/dy (behind a ReLU: zero where the ReLU was, as dr_regression_loss_grad leaves it) and the
+ * mean and rstd of the forward pass: with g = dy gamma_c and z = (x - mean) rstd,
+ *   dx = rstd (g - sum g / c - z sum (g z) / c),  dgamma_c = sum over pixels of dy z,  dbeta_c = sum over pixels of dy.
+ * dy, x and dx are tensors of descriptor d; dx == dy (in place) is allowed, dx == x is not.  dx, dgamma and dbeta may each
+ * be NULL (not computed); gamma NULL: ones.  ws: device scratch of at least dr_layernorm_bwd_workspace_bytes, 256-byte
+ * aligned (partial sums over ranges of pixels, added in a fixed order: the result does not depend on scheduling). */
+int dr_layernorm_bwd_workspace_bytes(const dr_tensor* d, size_t* bytes);
+int dr_layernorm_bwd(const dr_tensor* d, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx,
+                     float* dgamma, float* dbeta, void* ws, size_t ws_bytes, void* stream);
+
+/* Orthogonalised matrices: O = f(G) has the singular vectors of G and singular values near one.
+ *   X = G / (|G|_F + eps), on the transpose where G has more rows than columns;
+ *   `steps` times:  A = X X^T,  X = a X + (b A + c A A) X.
+ * count matrices of dtype (DR_F32 or DR_BF16), dense, row by row; ms, g, o: host arrays of count shapes / device
+ * pointers (o[i] == g[i] is allowed).  Products and sums have the precision of fp32 for DR_F32 and of 16 bits and more for
+ * DR_BF16, whatever the matrix units multiply.  A matrix of zeros stays zero; one that holds an infinity or a NaN
+ * becomes NaN and touches no other.  1 <= steps <= DR_MAX_NS_STEPS, eps >= 0.  ws: device scratch of at least
+ * dr_orthogonalise_workspace_bytes, 256-byte aligned. */
+#define DR_MAX_NS_STEPS 64
+typedef struct { int rows, cols; } dr_matrix;
+typedef struct { int steps; float a, b, c, eps; } dr_newton_schulz;
+int dr_orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype, size_t* bytes);
+int dr_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* const* g, void* const* o, const dr_newton_schulz* ns, void* ws,
+                     size_t ws_bytes, void* stream);
+
+/* One descent step with momentum on orthogonalised updates (Muon; Jordan et al. 2024) for count fp32 parameters, each a
+ * matrix of `rows` filters with cols = c r s weights (filters in either order):
+ *   m = momentum m + dw,  u = dw + momentum m,  w = (1 - lr weight_decay) w - lr sqrt(max(1, rows / cols)) f(u)
+ * with f as in dr_orthogonalise.  w and the momentum buffer are updated in place; no two parameters may overlap.
+ * params: host array, read during the call.  ws as above, of at least dr_muon_step_workspace_bytes. */
+typedef struct { int rows, cols; float* w; const float* dw; float* momentum; } dr_muon_param;
+typedef struct { float lr, momentum, weight_decay; dr_newton_schulz ns; } dr_muon;
+int dr_muon_step_workspace_bytes(int count, const dr_muon_param* params, size_t* bytes);
+int dr_muon_step(int count, const dr_muon_param* params, const dr_muon* opt, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- inception module (Sec. 3.2, Fig. 4) ---------------------------------------------------- */
 
 #define DR_MAX_STEPS 4

@@ -72,6 +72,22 @@ class dr_trace_record(C.Structure):
                 ("items", C.c_longlong), ("ms", C.c_float), ("bytes", C.c_longlong)]
 
 
+class dr_matrix(C.Structure):
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int)]
+
+
+class dr_newton_schulz(C.Structure):
+    _fields_ = [("steps", C.c_int)] + [(f, C.c_float) for f in ("a", "b", "c", "eps")]
+
+
+class dr_muon_param(C.Structure):
+    _fields_ = [("rows", C.c_int), ("cols", C.c_int), ("w", C.c_void_p), ("dw", C.c_void_p), ("momentum", C.c_void_p)]
+
+
+class dr_muon(C.Structure):
+    _fields_ = [(f, C.c_float) for f in ("lr", "momentum", "weight_decay")] + [("ns", dr_newton_schulz)]
+
+
 class DeepRebirthError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__("deeprebirth error %d: %s" % (code, msg))
@@ -109,6 +125,13 @@ _SIGNATURES = {
     "dr_conv2d_bwd_params_workspace_bytes": ([_P(dr_tensor), _P(dr_conv), _P(_z)], _i),
     "dr_conv2d_bwd_params": ([_P(dr_tensor), _vp, _P(dr_conv), _P(dr_tensor), _vp, _vp, _vp, _vp, _z, _vp], _i),
     "dr_sgd_step": ([_z, _vp, _vp, _f, _vp], _i),
+    "dr_layernorm_fwd": ([_P(dr_tensor), _vp, _vp, _vp, _f, _i, _vp, _vp, _vp, _vp], _i),
+    "dr_layernorm_bwd_workspace_bytes": ([_P(dr_tensor), _P(_z)], _i),
+    "dr_layernorm_bwd": ([_P(dr_tensor), _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _z, _vp], _i),
+    "dr_orthogonalise_workspace_bytes": ([_i, _P(dr_matrix), _i, _P(_z)], _i),
+    "dr_orthogonalise": ([_i, _P(dr_matrix), _i, _vp, _vp, _P(dr_newton_schulz), _vp, _z, _vp], _i),
+    "dr_muon_step_workspace_bytes": ([_i, _P(dr_muon_param), _P(_z)], _i),
+    "dr_muon_step": ([_i, _P(dr_muon_param), _P(dr_muon), _vp, _z, _vp], _i),
     "dr_inception_workspace_bytes": ([_P(dr_tensor), _P(dr_inception), _P(_z)], _i),
     "dr_inception_fwd": ([_P(dr_tensor), _vp, _P(dr_inception), _vp, _vp, _P(dr_tensor), _vp, _vp, _z, _vp], _i),
     "dr_net_create": ([_P(dr_layer_desc), _i, _P(_vp)], _i),
@@ -212,6 +235,28 @@ def _ptrs(ts, n=1):
     if pack is None:
         pack = _pack_pointers[len(v)] = struct.Struct("%dQ" % len(v)).pack
     return pack(*v)
+
+
+def _vector(t):
+    """Pointer of a contiguous fp32 tensor, or NULL."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32:
+        raise TypeError("vectors are fp32")
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
+
+
+def _like(t, x):
+    """Pointer of a tensor with x's shape, dtype and order, or NULL."""
+    if t is None:
+        return None
+    if isinstance(t, NHWC) != isinstance(x, NHWC) or t.dtype != x.dtype or t.shape != x.shape:
+        raise ValueError("tensors of one call share shape, dtype and order")
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    return t.data_ptr()
 
 
 def _nbytes(t):
@@ -424,6 +469,93 @@ def conv2d_bwd_params(x, cd, dz, dw, db, ws, stream=None):
 def sgd_step(w, dw, lr, stream=None):
     _check(lib().dr_sgd_step(w.numel(), _ptr(w), _ptr(dw), lr, _stream(stream)))
     return w
+
+
+def layernorm_fwd(x, gamma, beta, eps, relu, y, mean=None, rstd=None, stream=None):
+    """y = layer normalisation of x over its channels (then ReLU if relu); mean, rstd: fp32 tensors of n * h * w entries for layernorm_bwd, or None."""
+    _check(lib().dr_layernorm_fwd(desc(x), _ptr(x), _vector(gamma), _vector(beta), eps, int(relu), _like(y, x), _vector(mean), _vector(rstd), _stream(stream)))
+    return y
+
+
+def layernorm_bwd_workspace_bytes(x):
+    n = C.c_size_t(0)
+    _check(lib().dr_layernorm_bwd_workspace_bytes(desc(x), C.byref(n)))
+    return n.value
+
+
+def layernorm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
+    """dx, dgamma, dbeta (each may be None) from dy and the forward pass's x, mean and rstd."""
+    _check(lib().dr_layernorm_bwd(desc(x), _like(dy, x), _ptr(x), _vector(gamma), _vector(mean), _vector(rstd), _like(dx, x), _vector(dgamma), _vector(dbeta),
+                                  _ptr(ws), _nbytes(ws), _stream(stream)))
+    return dx, dgamma, dbeta
+
+
+# The coefficients that Muon is published with: after five steps singular values from 0.01 to 1 lie within 0.7 to 1.2
+NEWTON_SCHULZ = (3.4445, -4.7750, 2.0315)
+
+
+def _matrix_dims(t):
+    """Rows and columns of a contiguous tensor as the matrix of its first dimension by all others."""
+    if t.dim() < 2:
+        raise ValueError("a matrix or a filter tensor is at least 2-d")
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    rows = t.shape[0]
+    return rows, (t.numel() // rows if rows else 0)
+
+
+def _matrices(gs):
+    if len({g.dtype for g in gs}) > 1:
+        raise TypeError("the matrices of one call share a dtype")
+    return (dr_matrix * len(gs))(*[_matrix_dims(g) for g in gs]), (_dtype_code(gs[0]) if gs else DR_F32)
+
+
+def orthogonalise_workspace_bytes(gs):
+    ms, dtype = _matrices(gs)
+    n = C.c_size_t(0)
+    _check(lib().dr_orthogonalise_workspace_bytes(len(gs), ms, dtype, C.byref(n)))
+    return n.value
+
+
+def orthogonalise(gs, os, ws, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, stream=None):
+    """os[i] = the matrix gs[i] with its singular values moved to near one; lists of device tensors (filters: k x everything else)."""
+    ms, dtype = _matrices(gs)
+    if [(o.shape, o.dtype) for o in os] != [(g.shape, g.dtype) for g in gs] or not all(o.is_contiguous() for o in os):
+        raise ValueError("outputs have the inputs' shapes and dtype and are contiguous")
+    _check(lib().dr_orthogonalise(len(gs), ms, dtype, _ptrs(gs), _ptrs(os), dr_newton_schulz(steps, *coefficients, eps), _ptr(ws), _nbytes(ws), _stream(stream)))
+    return os
+
+
+class MuonParams:
+    """A list of (w, dw, momentum) for muon_step: fp32 device tensors of one shape each, kept alive and updated in place."""
+
+    def __init__(self, tensors):
+        self.tensors = [tuple(t) for t in tensors]
+        for w, dw, m in self.tensors:
+            for t in (w, dw, m):
+                if t.dtype != torch.float32:
+                    raise TypeError("muon_step takes fp32 parameters")
+                if t.shape != w.shape:
+                    raise ValueError("parameter, gradient and momentum have one shape")
+        dims = [[_matrix_dims(t) for t in p][0] for p in self.tensors]
+        self.array = (dr_muon_param * len(dims))(*[(r, c, *[t.data_ptr() for t in p]) for (r, c), p in zip(dims, self.tensors)])
+
+
+def muon_params(tensors):
+    return MuonParams(tensors)
+
+
+def muon_step_workspace_bytes(params):
+    n = C.c_size_t(0)
+    _check(lib().dr_muon_step_workspace_bytes(len(params.array), params.array, C.byref(n)))
+    return n.value
+
+
+def muon_step(params, ws, lr, momentum=0.95, weight_decay=0.0, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, stream=None):
+    """One descent step on orthogonalised momentum for every (w, dw, momentum) of muon_params."""
+    _check(lib().dr_muon_step(len(params.array), params.array, dr_muon(lr, momentum, weight_decay, dr_newton_schulz(steps, *coefficients, eps)), _ptr(ws), _nbytes(ws),
+                              _stream(stream)))
+    return params
 
 
 def trace_begin(label_filter="", conv_k=0, conv_c=0, conv_r=0, capacity=4096):

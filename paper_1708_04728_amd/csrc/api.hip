@@ -1528,6 +1528,128 @@ int dr_sgd_step(size_t count, float* w, const float* dw, float lr, void* stream)
     return launch_sgd_step(w, dw, lr, count, (hipStream_t)stream);
 }
 
+// scratch that a call needs: there, large enough, aligned
+static int check_scratch(const char* who, const void* ws, size_t ws_bytes, size_t need)
+{
+    if (need && (!ws || ws_bytes < need)) return fail(DR_ERR_WORKSPACE, "%s: needs %zu bytes of workspace, got %zu", who, need, ws ? ws_bytes : (size_t)0);
+    if (need && ((uintptr_t)ws & 255) != 0) return fail(DR_ERR_WORKSPACE, "%s: workspace must be 256-byte aligned", who);
+    return DR_OK;
+}
+
+int dr_layernorm_fwd(const dr_tensor* d, const void* x, const float* gamma, const float* beta, float eps, int relu, void* y, float* mean, float* rstd, void* stream)
+{
+    const char* who = "dr_layernorm_fwd";
+    DR_TRY(check_tensor(who, "d", d));
+    if (!(eps >= 0.f)) return fail(DR_ERR_SHAPE, "%s: eps must be >= 0", who);
+    if (tensor_elems(*d) == 0) return DR_OK;
+    if (!x || !y) return fail(DR_ERR_NULL, "%s: x or y is NULL", who);
+    return launch_layernorm_fwd(*d, x, gamma, beta, eps, relu, y, mean, rstd, (hipStream_t)stream);
+}
+
+int dr_layernorm_bwd_workspace_bytes(const dr_tensor* d, size_t* bytes)
+{
+    const char* who = "dr_layernorm_bwd_workspace_bytes";
+    DR_TRY(check_tensor(who, "d", d));
+    if (!bytes) return fail(DR_ERR_NULL, "%s: bytes is NULL", who);
+    *bytes = layernorm_bwd_workspace_bytes(*d);
+    return DR_OK;
+}
+
+int dr_layernorm_bwd(const dr_tensor* d, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx, float* dgamma,
+                     float* dbeta, void* ws, size_t ws_bytes, void* stream)
+{
+    const char* who = "dr_layernorm_bwd";
+    DR_TRY(check_tensor(who, "d", d));
+    DR_TRY(check_scratch(who, ws, ws_bytes, dgamma || dbeta ? layernorm_bwd_workspace_bytes(*d) : 0));
+    if (d->c == 0) return DR_OK;
+    if (tensor_elems(*d) && (!dy || !x || !mean || !rstd)) return fail(DR_ERR_NULL, "%s: dy, x, mean or rstd is NULL", who);
+    if (tensor_elems(*d) && dx == x) return fail(DR_ERR_UNSUPPORTED, "%s: dx must not be x", who);
+    return launch_layernorm_bwd(*d, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, (hipStream_t)stream);
+}
+
+static int check_matrix(const char* who, int i, int rows, int cols)
+{
+    if (rows < 0 || cols < 0) return fail(DR_ERR_SHAPE, "%s: matrix %d has a negative dimension (%d,%d)", who, i, rows, cols);
+    if ((double)rows * cols >= 2147483648.0) return fail(DR_ERR_UNSUPPORTED, "%s: matrix %d has more than 2^31-1 elements", who, i);
+    return DR_OK;
+}
+static int check_matrices(const char* who, int count, const dr_matrix* ms, int dtype)
+{
+    if (count < 0) return fail(DR_ERR_SHAPE, "%s: count = %d", who, count);
+    if (dtype != DR_F32 && dtype != DR_BF16) return fail(DR_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
+    if (count && !ms) return fail(DR_ERR_NULL, "%s: ms is NULL", who);
+    double elements = 0;
+    for (int i = 0; i < count; ++i) {
+        DR_TRY(check_matrix(who, i, ms[i].rows, ms[i].cols));
+        elements += (double)ms[i].rows * ms[i].cols;
+    }
+    if (elements >= 2147483648.0) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^31-1 elements in all", who);
+    return DR_OK;
+}
+static int check_muon_params(const char* who, int count, const dr_muon_param* params)
+{
+    if (count < 0) return fail(DR_ERR_SHAPE, "%s: count = %d", who, count);
+    if (count && !params) return fail(DR_ERR_NULL, "%s: params is NULL", who);
+    double elements = 0;
+    for (int i = 0; i < count; ++i) {
+        DR_TRY(check_matrix(who, i, params[i].rows, params[i].cols));
+        elements += (double)params[i].rows * params[i].cols;
+    }
+    if (elements >= 2147483648.0) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^31-1 elements in all", who);
+    return DR_OK;
+}
+static int check_newton_schulz(const char* who, const dr_newton_schulz& ns)
+{
+    if (ns.steps < 1 || ns.steps > DR_MAX_NS_STEPS) return fail(DR_ERR_SHAPE, "%s: %d steps (1..%d supported)", who, ns.steps, DR_MAX_NS_STEPS);
+    if (!(ns.eps >= 0.f)) return fail(DR_ERR_SHAPE, "%s: eps must be >= 0", who);
+    return DR_OK;
+}
+
+int dr_orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype, size_t* bytes)
+{
+    const char* who = "dr_orthogonalise_workspace_bytes";
+    DR_TRY(check_matrices(who, count, ms, dtype));
+    if (!bytes) return fail(DR_ERR_NULL, "%s: bytes is NULL", who);
+    *bytes = orthogonalise_workspace_bytes(count, ms, dtype);
+    return DR_OK;
+}
+
+int dr_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* const* g, void* const* o, const dr_newton_schulz* ns, void* ws, size_t ws_bytes,
+                     void* stream)
+{
+    const char* who = "dr_orthogonalise";
+    DR_TRY(check_matrices(who, count, ms, dtype));
+    if (!ns) return fail(DR_ERR_NULL, "%s: ns is NULL", who);
+    DR_TRY(check_newton_schulz(who, *ns));
+    if (count && (!g || !o)) return fail(DR_ERR_NULL, "%s: g or o is NULL", who);
+    for (int i = 0; i < count; ++i)
+        if (ms[i].rows && ms[i].cols && (!g[i] || !o[i])) return fail(DR_ERR_NULL, "%s: g[%d] or o[%d] is NULL", who, i, i);
+    DR_TRY(check_scratch(who, ws, ws_bytes, orthogonalise_workspace_bytes(count, ms, dtype)));
+    return launch_orthogonalise(count, ms, dtype, g, o, *ns, ws, (hipStream_t)stream);
+}
+
+int dr_muon_step_workspace_bytes(int count, const dr_muon_param* params, size_t* bytes)
+{
+    const char* who = "dr_muon_step_workspace_bytes";
+    DR_TRY(check_muon_params(who, count, params));
+    if (!bytes) return fail(DR_ERR_NULL, "%s: bytes is NULL", who);
+    *bytes = muon_step_workspace_bytes(count, params);
+    return DR_OK;
+}
+
+int dr_muon_step(int count, const dr_muon_param* params, const dr_muon* opt, void* ws, size_t ws_bytes, void* stream)
+{
+    const char* who = "dr_muon_step";
+    DR_TRY(check_muon_params(who, count, params));
+    if (!opt) return fail(DR_ERR_NULL, "%s: opt is NULL", who);
+    DR_TRY(check_newton_schulz(who, opt->ns));
+    for (int i = 0; i < count; ++i)
+        if (params[i].rows && params[i].cols && (!params[i].w || !params[i].dw || !params[i].momentum))
+            return fail(DR_ERR_NULL, "%s: w, dw or momentum of parameter %d is NULL", who, i);
+    DR_TRY(check_scratch(who, ws, ws_bytes, muon_step_workspace_bytes(count, params)));
+    return launch_muon_step(count, params, *opt, ws, (hipStream_t)stream);
+}
+
 int dr_inception_workspace_bytes(const dr_tensor* xd, const dr_inception* desc, size_t* bytes)
 {
     const char* who = "dr_inception_workspace_bytes";

@@ -195,6 +195,19 @@ size_t conv_wgrad_workspace_bytes(const ConvGeom& g);
 int launch_conv_wgrad_f32(const ConvGeom& g, const float* x, const float* dz, float* dw, float* db, void* ws, hipStream_t st);
 int launch_sgd_step(float* w, const float* dw, float lr, size_t count, hipStream_t st);
 
+// layernorm.hip: layer normalisation over the channels of every pixel, either order, and its gradient
+int launch_layernorm_fwd(const dr_tensor& d, const void* x, const float* gamma, const float* beta, float eps, int relu, void* y, float* mean, float* rstd,
+                         hipStream_t st);
+size_t layernorm_bwd_workspace_bytes(const dr_tensor& d);
+int launch_layernorm_bwd(const dr_tensor& d, const void* dy, const void* x, const float* gamma, const float* mean, const float* rstd, void* dx, float* dgamma,
+                         float* dbeta, void* ws, hipStream_t st);
+
+// orthogonal.hip: Newton-Schulz products on a list of matrices, and the descent step on them
+size_t orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype);
+int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* const* g, void* const* o, const dr_newton_schulz& ns, void* ws, hipStream_t st);
+size_t muon_step_workspace_bytes(int count, const dr_muon_param* ps);
+int launch_muon_step(int count, const dr_muon_param* ps, const dr_muon& opt, void* ws, hipStream_t st);
+
 // pointwise.hip
 int launch_pack_filters(int dtype, const void* w_kcrs, void* w_krsc, int K, int C, int RS, hipStream_t st);
 int launch_relu(int dtype, const void* x, void* y, size_t count, hipStream_t st);
