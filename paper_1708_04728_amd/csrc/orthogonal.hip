@@ -20,6 +20,7 @@
 
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "dr_internal.h"
 #include "f32_pieces.h"
@@ -51,6 +52,7 @@ struct Jobs {
 
 struct Call {
     double* squares;
+    float* partial;                          // sums of workgroups that share a tile
     unsigned char* ws;
     int count;
     float a, b, c, eps;
@@ -315,20 +317,23 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[P], const u32x4 (&b)[P
 }
 
 // A product of small matrices: W waves share a tile of T x T blocks, every wave a W-th of the contraction.  Operands go straight to registers, AHEAD k-blocks of them
-// while as many are multiplied: what such a product waits for is its first operands.
+// while as many are multiplied: what such a product waits for is its first operands.  splits > 1: as many workgroups share a tile, and leave sums for sum_kernel.
+template <int T> constexpr int ahead() { return T == 1 ? 4 : 2; }
 template <typename E, int P, int WHAT, int T, int W, bool MUON>
-__global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs j, int turn, int last)
+__global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs j, int turn, int last, int splits)
 {
-    constexpr int AHEAD = T == 1 ? 4 : 2;
+    constexpr int AHEAD = ahead<T>();
     __shared__ __attribute__((aligned(16))) float sums[W][T * T][32 * PITCH];
-    const Mat m = find_matrix(j, c.count, blockIdx.x);
+    const int unit = splits > 1 ? (int)blockIdx.x / splits : (int)blockIdx.x, part = (int)blockIdx.x - unit * splits;
+    const Mat m = find_matrix(j, c.count, unit);
     const Operands<P> op(c, j, m);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     int bi, bj;
-    tile_blocks<WHAT, T>(m, (int)blockIdx.x - j.first[m.k], bi, bj);
+    tile_blocks<WHAT, T>(m, unit - j.first[m.k], bi, bj);
     const unsigned char* const left = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : op.q;
     const unsigned char* const right = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : turn ? op.xt1 : op.xt0;
     const int kblocks = 2 * (WHAT == GRAM ? m.nb : m.mb), lrows = m.mb, rrows = WHAT == APPLY ? m.nb : m.mb;
+    const int step = W * splits, mine = wave + part * W;      // this wave's k-blocks: mine, mine + step, ...
     const unsigned char *lp[T], *rp[T];
 #pragma unroll
     for (int i = 0; i < T; ++i) {            // (a block beyond the last is the last again, and is not stored)
@@ -347,7 +352,7 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
         constexpr int S = decltype(set)::value;
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
-            const size_t at = (size_t)min(kb0 + n * W, kblocks - 1) * P * BLOCK;
+            const size_t at = (size_t)min(kb0 + n * step, kblocks - 1) * P * BLOCK;
 #pragma unroll
             for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -361,7 +366,7 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
         constexpr int S = decltype(set)::value;
 #pragma unroll
         for (int n = 0; n < AHEAD; ++n) {
-            if (kb0 + n * W >= kblocks) break;
+            if (kb0 + n * step >= kblocks) break;
 #pragma unroll
             for (int i = 0; i < T; ++i)
 #pragma unroll
@@ -369,12 +374,12 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
         }
     };
     using std::integral_constant;
-    fetch(wave, integral_constant<int, 0>{});
-    for (int kb = wave; kb < kblocks; kb += 2 * AHEAD * W) {
-        if (kb + AHEAD * W < kblocks) fetch(kb + AHEAD * W, integral_constant<int, 1>{});
+    fetch(mine, integral_constant<int, 0>{});
+    for (int kb = mine; kb < kblocks; kb += 2 * AHEAD * step) {
+        if (kb + AHEAD * step < kblocks) fetch(kb + AHEAD * step, integral_constant<int, 1>{});
         products(kb, integral_constant<int, 0>{});
-        if (kb + 2 * AHEAD * W < kblocks) fetch(kb + 2 * AHEAD * W, integral_constant<int, 0>{});
-        products(kb + AHEAD * W, integral_constant<int, 1>{});
+        if (kb + 2 * AHEAD * step < kblocks) fetch(kb + 2 * AHEAD * step, integral_constant<int, 0>{});
+        products(kb + AHEAD * step, integral_constant<int, 1>{});
     }
     // register v holds row 8 (v / 4) + 4 half + v % 4 of column lane % 32
 #pragma unroll
@@ -391,8 +396,10 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < W; ++w) s += sums[w][blk][at];
-        sums[0][blk][at] = s;
+        if (splits > 1) c.partial[(size_t)blockIdx.x * (T * T * 1024) + i] = s;
+        else sums[0][blk][at] = s;
     }
+    if (splits > 1) return;
     __syncthreads();
     if (WHAT == APPLY && last) {
         for (int blk = 0; blk < T * T; ++blk) {
@@ -407,37 +414,468 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
     }
 }
 
-// ---- the plan of a call: made in the same way to size the workspace and to run
-struct Plan { size_t operands, total; };      // in the workspace; squares come first
+// A product of larger matrices: WM x WN waves share a tile, TM x TN blocks of 32 x 32 each.  A stage is one k-block (16 k) of the tile's operands in LDS; of three stages
+// one is multiplied, one is complete, one is written, from registers that were loaded DEPTH iterations before, with a barrier an iteration.  A wave keeps one k-block of
+// its operands in registers.  The products of pieces come in an order in which every piece of the next k-block is read between the last product that needs the present one
+// and the first that needs it; reads, writes and loads are issued one by one between matrix instructions, which cover them: one wave per SIMD keeps its unit busy.
+template <int P, int BM, int BN> constexpr int tile_lds() { return 3 * (BM + BN) * P * BLOCK; }
+
+__device__ __forceinline__ void lds_barrier()        // orders LDS traffic only
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Adds the sums that the workgroups of a tile have left, in their order
+template <typename E, int P, int WHAT, int T, bool MUON>
+__global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs j, int turn, int last, int splits)
+{
+    __shared__ __attribute__((aligned(16))) float tile[32 * PITCH];
+    const int unit = (int)blockIdx.x / (T * T), blk = (int)blockIdx.x - unit * (T * T);
+    const Mat m = find_matrix(j, c.count, unit);
+    const Operands<P> op(c, j, m);
+    int bi, bj;
+    tile_blocks<WHAT, T>(m, unit - j.first[m.k], bi, bj);
+    bi += blk / T;
+    bj += blk % T;
+    if (bi >= m.mb || bj >= (WHAT == APPLY ? m.nb : m.mb) || (WHAT != APPLY && bi < bj)) return;
+    const float* const from = c.partial + ((size_t)unit * splits * (T * T) + blk) * 1024;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < splits; ++k)
+#pragma unroll
+        for (int n = 0; n < 4; ++n) s[n] += from[(size_t)k * (T * T * 1024) + n * 256 + threadIdx.x];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) tile[(n * 8 + (threadIdx.x >> 5)) * PITCH + (threadIdx.x & 31)] = s[n];
+    __syncthreads();
+    if (WHAT == APPLY && last) finish_result<E, MUON>(c, j, m, tile, bi, bj, threadIdx.x >> 5, 8);
+    else finish_task<P, WHAT>(c, m, op, tile, bi, bj, turn, threadIdx.x >> 6);
+}
+
+// f(0), ..., f(N - 1), as constants
+template <class F, int... I>
+__device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
+template <int N, class F>
+__device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
+
+template <typename E, int P, int WHAT, int WM, int WN, int TM, int TN, int DEPTH, bool APART, bool MUON>
+__global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const Jobs j, int turn, int last)
+{
+    constexpr int W = WM * WN, BM = WM * TM, BN = WN * TN, STAGE = (BM + BN) * P * BLOCK, LOADS = (BM + BN) * P / W;
+    static_assert((BM + BN) * P % W == 0 && BM == BN && (DEPTH == 1 || DEPTH == 2) && tile_lds<P, BM, BN>() >= W * 32 * PITCH * 4, "a tile's operands");
+    __shared__ __attribute__((aligned(16))) unsigned char lds[tile_lds<P, BM, BN>()];
+    // workgroup b runs on die b & 7: a die takes a contiguous range of tiles, which share operands
+    const int die = blockIdx.x & 7, share = (int)gridDim.x >> 3, odd = gridDim.x & 7, id = die * share + min(die, odd) + (int)(blockIdx.x >> 3);
+    const Mat m = find_matrix(j, c.count, id);
+    const Operands<P> op(c, j, m);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
+    const int wm = wave / WN, wn = wave % WN;
+    int bi, bj;
+    tile_blocks<WHAT, BM>(m, id - j.first[m.k], bi, bj);
+    const unsigned char* const left = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : op.q;
+    const unsigned char* const right = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : turn ? op.xt1 : op.xt0;
+    const int kblocks = 2 * (WHAT == GRAM ? m.nb : m.mb), lrows = m.mb, rrows = WHAT == APPLY ? m.nb : m.mb;
+
+    // load n of a wave: KiB wave + n W of the stage: piece % P of row of blocks / P
+    const unsigned char* from[LOADS];
+#pragma unroll
+    for (int n = 0; n < LOADS; ++n) {
+        const int q = wave + n * W, row = q / P, piece = q % P;
+        from[n] = (row < BM ? left + (size_t)min(bi + row, lrows - 1) * kblocks * P * BLOCK : right + (size_t)min(bj + row - BM, rrows - 1) * kblocks * P * BLOCK) + piece * BLOCK;
+    }
+    u32x4 in[DEPTH][LOADS];
+    auto fetch = [&](auto set, int n) __attribute__((always_inline)) {
+        in[decltype(set)::value][n] = *reinterpret_cast<const u32x4*>(from[n] + lane * 16);
+        from[n] += P * BLOCK;
+    };
+    auto put = [&](auto set, int stage, int n) __attribute__((always_inline)) {
+        *reinterpret_cast<u32x4*>(lds + stage + (wave + n * W) * BLOCK + lane * 16) = in[decltype(set)::value][n];
+    };
+    u32x4 a[TM][P], b[TN][P];
+    const unsigned char* const mine_a = lds + wm * TM * P * BLOCK + lane * 16;
+    const unsigned char* const mine_b = lds + (BM + wn * TN) * P * BLOCK + lane * 16;
+    auto read_a = [&](int stage, int i, int e) __attribute__((always_inline)) { a[i][e] = *reinterpret_cast<const u32x4*>(mine_a + stage + (i * P + e) * BLOCK); };
+    auto read_b = [&](int stage, int i, int e) __attribute__((always_inline)) { b[i][e] = *reinterpret_cast<const u32x4*>(mine_b + stage + (i * P + e) * BLOCK); };
+    f32x16 acc[TM][TN], small[APART ? TM : 1][APART ? TN : 1];      // APART: the small products in sums of their own
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int k = 0; k < TN; ++k)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                acc[i][k][v] = 0.f;
+                if constexpr (APART) small[i][k][v] = 0.f;
+            }
+
+    using std::integral_constant;
+    typedef integral_constant<int, 0> First;
+    typedef integral_constant<int, DEPTH - 1> Second;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {            // (k-blocks come in pairs)
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) fetch(First{}, n);
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) put(First{}, k * STAGE, n);
+    }
+    if (kblocks > 2) {
+#pragma unroll
+        for (int n = 0; n < LOADS; ++n) fetch(First{}, n);
+        if constexpr (DEPTH == 2) {
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) fetch(Second{}, n);
+        }
+    }
+    lds_barrier();
+    // (pieces of the first k-block that are not read where it is multiplied)
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int e = 0; e < P - 1; ++e) read_a(0, i, e);
+#pragma unroll
+    for (int k = 0; k < TN; ++k)
+#pragma unroll
+        for (int e = 1; e < P; ++e) read_b(0, k, e);
+
+    int here = 0, next = STAGE, write = 2 * STAGE;       // the stages of k-blocks kb, kb + 1 and kb + 2
+    auto iteration = [&](auto set, bool putting, bool fetching) __attribute__((always_inline)) {
+        constexpr int G = TM * TN, PAIRS = P == 3 ? 6 : 3;
+        // products of pieces: first the one that needs neither b's first piece nor a's last, which are read meanwhile
+        constexpr int X[6] = {0, 0, 0, 1, 1, 2}, Y[6] = {2, 1, 0, 1, 0, 0};
+        constexpr int X2[3] = {0, 0, 1}, Y2[3] = {1, 0, 0};
+        each<PAIRS * G>([&](auto slot) __attribute__((always_inline)) {
+            constexpr int t = decltype(slot)::value, g = t / G, i = t % G / TN, k = t % TN, x = P == 3 ? X[g] : X2[g % 3], y = P == 3 ? Y[g] : Y2[g % 3];
+            if constexpr (APART && x + y != 0) small[i][k] = mfma(a[i][x], b[k][y], small[i][k]);
+            else acc[i][k] = mfma(a[i][x], b[k][y], acc[i][k]);
+            __builtin_amdgcn_sched_barrier(0);
+            // this k-block's pieces that come last
+            if constexpr (t < TN) read_b(here, t, 0);
+            else if constexpr (t < TN + TM) read_a(here, t - TN, P - 1);
+            // the next one's
+            constexpr int u = t - g * G;
+            if constexpr (P == 3 && g == 1 && u < TN) read_b(next, u, 2);
+            if constexpr (P == 3 && g == 3 && u < TM) read_a(next, u, 0);
+            if constexpr (P == 3 && g == 4 && u < TN) read_b(next, u, 1);
+            if constexpr (P == 3 && g == 5 && u < TM) read_a(next, u, 1);
+            if constexpr (P == 2 && g == 1 && u < TN) read_b(next, u, 1);
+            if constexpr (P == 2 && g == 2 && u < TM) read_a(next, u, 0);
+            // the one behind, and the loads of the one DEPTH behind that
+            constexpr int FROM = G / 2, SPAN = (P == 3 ? 3 : 2) * G - FROM;
+#pragma unroll
+            for (int n = 0; n < LOADS; ++n) {
+                if (putting && t == FROM + n * SPAN / LOADS) put(set, write, n);
+                if (fetching && t == FROM + n * SPAN / LOADS + 1) fetch(set, n);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        lds_barrier();
+        const int done = here;
+        here = next;
+        next = write;
+        write = done;
+    };
+    int kb = 0;
+    for (; kb + 2 + DEPTH < kblocks; kb += DEPTH) {
+        iteration(First{}, true, true);
+        if constexpr (DEPTH == 2) iteration(Second{}, true, true);
+    }
+    // the last k-blocks: nothing more to load, then nothing more to write
+    for (; kb + 2 < kblocks; kb += DEPTH) {
+        iteration(First{}, true, false);
+        if constexpr (DEPTH == 2) iteration(Second{}, true, false);
+    }
+    iteration(First{}, false, false);
+    iteration(First{}, false, false);
+    // block by block through LDS, each wave in its own part
+    float* const tile = reinterpret_cast<float*>(lds) + wave * 32 * PITCH;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int k = 0; k < TN; ++k) {
+            const int ri = bi + wm * TM + i, rk = bj + wn * TN + k;
+            if (ri >= lrows || rk >= rrows || (WHAT != APPLY && ri < rk)) continue;
+            // register v holds row 8 (v / 4) + 4 half + v % 4 of column lane % 32
+#pragma unroll
+            for (int v = 0; v < 16; ++v) tile[(8 * (v >> 2) + 4 * half + (v & 3)) * PITCH + l32] = APART ? acc[i][k][v] + small[APART ? i : 0][APART ? k : 0][v] : acc[i][k][v];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+            __builtin_amdgcn_wave_barrier();
+            if (WHAT == APPLY && last) finish_result<E, MUON>(c, j, m, tile, ri, rk, half, 2);
+            else {
+#pragma unroll 1
+                for (int t = 0; t < 4; ++t) finish_task<P, WHAT>(c, m, op, tile, ri, rk, turn, t);
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+            __builtin_amdgcn_wave_barrier();
+        }
+}
+
+// ---- matrices small enough for one workgroup's LDS: the whole iteration there, X, A and Q in fp32, cut into pieces where they are multiplied
+// 64 rows and 448 columns, or 32 and 896: eight waves.  Nothing but the matrix is read or written, and a step is nine barriers instead of three launches.
+constexpr int WHOLE_FLOATS = 38912;
+__host__ __device__ inline bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 14; }
+
+template <typename E, int P, bool MUON>
+__global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs j, int steps)
+{
+    __shared__ __attribute__((aligned(16))) float lds[WHOLE_FLOATS];
+    __shared__ double red[8];
+    const int k = blockIdx.x, mb = j.mb[k], nb = j.nb[k], rows = j.rows[k], cols = j.cols[k];
+    const bool tall = rows > cols;
+    const int XP = nb * 32 + 4, AP = mb * 32 + 4;
+    float* const X = lds;
+    float* const A = X + mb * 32 * XP;
+    float* const Q = A + mb * 32 * AP;       // and partial sums, whose time is another
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
+
+    // element i of the matrix, i = tid, tid + 512, ...: f(i, its place in X)
+    const int total = rows * cols, step_r = 512 / cols, step_c = 512 - step_r * cols;
+    auto elements = [&](auto f) __attribute__((always_inline)) {
+        int r = tid / cols, col = tid - r * cols;
+        for (int i = tid; i < total; i += 512) {
+            f(i, tall ? col * XP + r : r * XP + col);
+            r += step_r;
+            col += step_c;
+            if (col >= cols) { col -= cols; ++r; }
+        }
+    };
+    for (int i = tid; i < mb * 32 * XP; i += 512) X[i] = 0.f;
+    __syncthreads();
+    double s = 0.0;
+    elements([&](int i, int at) {
+        float u = Store<E>::ld((const E*)j.g[k] + i);
+        if constexpr (MUON) {
+            const float v = c.mu * j.momentum[k][i] + u;
+            j.momentum[k][i] = v;
+            u += c.mu * v;
+        }
+        X[at] = u;
+        s += (double)u * (double)u;
+    });
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
+    if (lane == 0) red[wave] = s;
+    __syncthreads();
+    const double inv = 1.0 / (sqrt(((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]))) + (double)c.eps);
+    for (int i = tid; i < mb * 32 * XP; i += 512) X[i] = (float)((double)X[i] * inv);
+    __syncthreads();
+
+    // eight values along a row of M, cut; down a column of X
+    auto along = [&](const float* M, int pitch, int row, int k0, u32x4 (&p)[P]) __attribute__((always_inline)) {
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 t = *reinterpret_cast<const f32x4*>(M + row * pitch + k0 + half * 8 + 4 * h);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * h + e] = t[e];
+        }
+        cut8<P>(v, p);
+    };
+    auto down = [&](int col, int k0, u32x4 (&p)[P]) __attribute__((always_inline)) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = X[(k0 + half * 8 + e) * XP + col];
+        cut8<P>(v, p);
+    };
+    auto zero = [](f32x16& a, f32x16& b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) a[v] = b[v] = 0.f;
+    };
+    // register v holds row 8 (v / 4) + 4 half + v % 4 of column lane % 32
+    auto row_of = [&](int v) __attribute__((always_inline)) { return 8 * (v >> 2) + 4 * half + (v & 3); };
+    for (int step = 0; step < steps; ++step) {
+        f32x16 large, small;
+        // A = X X^T: the first wave of a block leaves its sum in A, the others theirs beside it
+        if (mb == 1 || wave < 6) {
+            const int blk = mb == 1 ? 0 : wave >> 1, split = mb == 1 ? wave : wave & 1, splits = mb == 1 ? 8 : 2, bi = blk ? 1 : 0, bj = blk == 2 ? 1 : 0;
+            zero(large, small);
+            for (int kb = split; kb < 2 * nb; kb += splits) {
+                u32x4 a[P], b[P];
+                along(X, XP, bi * 32 + l32, kb * 16, a);
+                if (bi == bj) multiply<P>(a, a, large, small);
+                else {
+                    along(X, XP, bj * 32 + l32, kb * 16, b);
+                    multiply<P>(a, b, large, small);
+                }
+            }
+            float* const to = split ? Q + (mb == 1 ? split - 1 : blk) * 32 * PITCH : A + bi * 32 * AP + bj * 32;
+            const int pitch = split ? PITCH : AP;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) to[row_of(v) * pitch + l32] = large[v] + small[v];
+        }
+        __syncthreads();
+        for (int i = tid; i < (mb == 1 ? 1024 : 3072); i += 512) {
+            const int blk = i >> 10, r = (i >> 5) & 31, cl = i & 31, bi = blk ? 1 : 0, bj = blk == 2 ? 1 : 0;
+            float* const at = A + (bi * 32 + r) * AP + bj * 32 + cl;
+            float t = *at;
+            if (mb == 1) {
+#pragma unroll
+                for (int w = 0; w < 7; ++w) t += Q[w * 32 * PITCH + r * PITCH + cl];
+            } else t += Q[blk * 32 * PITCH + r * PITCH + cl];
+            *at = t;
+            if (blk == 1) A[cl * AP + 32 + r] = t;
+        }
+        __syncthreads();
+        // Q = a I + b A + c A A
+        if (wave < mb * mb) {
+            const int bi = wave >> (mb - 1), bj = wave & (mb - 1);
+            zero(large, small);
+            for (int kb = 0; kb < 2 * mb; ++kb) {
+                u32x4 a[P], b[P];
+                along(A, AP, bi * 32 + l32, kb * 16, a);
+                along(A, AP, bj * 32 + l32, kb * 16, b);
+                multiply<P>(a, b, large, small);
+            }
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int at = (bi * 32 + row_of(v)) * AP + bj * 32 + l32;
+                Q[at] = c.b * A[at] + c.c * (large[v] + small[v]) + (bi == bj && row_of(v) == l32 ? c.a : 0.f);
+            }
+        }
+        __syncthreads();
+        // X = Q X: a wave has whole columns, which it replaces
+        auto apply = [&](auto blocks) __attribute__((always_inline)) {
+            constexpr int MB = decltype(blocks)::value;
+            for (int bj = wave; bj < nb; bj += 8) {
+                f32x16 big[MB], little[MB];
+#pragma unroll
+                for (int i = 0; i < MB; ++i) zero(big[i], little[i]);
+#pragma unroll 2
+                for (int kb = 0; kb < 2 * MB; ++kb) {
+                    u32x4 b[P];
+                    down(bj * 32 + l32, kb * 16, b);
+#pragma unroll
+                    for (int i = 0; i < MB; ++i) {
+                        u32x4 q[P];
+                        along(Q, AP, i * 32 + l32, kb * 16, q);
+                        multiply<P>(q, b, big[i], little[i]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) X[(i * 32 + row_of(v)) * XP + bj * 32 + l32] = big[i][v] + little[i][v];
+            }
+        };
+        if (mb == 1) apply(std::integral_constant<int, 1>{});
+        else apply(std::integral_constant<int, 2>{});
+        __syncthreads();
+    }
+    elements([&](int i, int at) {
+        if constexpr (MUON) {
+            float* const w = (float*)j.o[k];
+            w[i] = c.keep * w[i] - j.scale[k] * X[at];
+        } else Store<E>::st((E*)j.o[k] + i, X[at]);
+    });
+}
+
+// ---- which kernel multiplies
+// Kernels for a product, by the blocks of a tile's side
+enum { FINE, DIRECT, TILE4, TILE6, TILE8, KERNELS };
+constexpr int SIDE[KERNELS] = {1, 2, 4, 6, 8};
 
 int tiles_of(int what, int mb, int nb, int T)
 {
     const int tm = (mb + T - 1) / T, tn = (nb + T - 1) / T;
     return what == APPLY ? tm * tn : tm * (tm + 1) / 2;
 }
-size_t operand_bytes(int rows, int cols, int P)
+
+// What one launch of a product has to do: tiles and tiles x k-blocks for each side of a tile, the longest contraction
+struct Work {
+    int tiles[KERNELS], longest;
+    double blocks[KERNELS];
+    void add(int what, int mb, int nb)
+    {
+        const int kblocks = 2 * (what == GRAM ? nb : mb);
+        longest = std::max(longest, kblocks);
+        for (int k = 0; k < KERNELS; ++k) {
+            const int n = tiles_of(what, mb, nb, SIDE[k]);
+            tiles[k] += n;
+            blocks[k] += (double)n * kblocks;
+        }
+    }
+};
+
+// Microseconds that a launch takes, from 36 square and oblong shapes of 64 to 4096 rows in either number of pieces: what a round of workgroups costs beside its products;
+// a k-block on a compute unit by itself; what all of them multiply together, in blocks of 32 x 32 x 16 a microsecond; workgroups per compute unit.
+struct Cost { float round, kblock, rate; int slots; };
+constexpr Cost COSTS[2][KERNELS] = {
+    {{3.f, 0.065f, 3900.f, 1}, {5.f, 0.2f, 5100.f, 1}, {7.f, 0.42f, 6600.f, 2}, {12.f, 0.8f, 7450.f, 1}, {18.f, 1.45f, 7150.f, 1}},           // three pieces
+    {{2.6f, 0.045f, 5700.f, 1}, {4.f, 0.12f, 8500.f, 1}, {5.5f, 0.24f, 10200.f, 2}, {9.f, 0.45f, 12700.f, 1}, {12.5f, 0.8f, 13900.f, 1}},     // two
+};
+float cost_of(int P, int kernel, double tiles, double blocks, double longest)
 {
-    const size_t mb = (std::min(rows, cols) + 31) / 32, nb = (std::max(rows, cols) + 31) / 32;
-    return (3 * mb * nb + 2 * mb * mb) * 2 * P * BLOCK;
+    const Cost& c = COSTS[P == 3 ? 0 : 1][kernel];
+    const double area = SIDE[kernel] * SIDE[kernel], slots = (double)c.slots * device_cus(), each = blocks / tiles;
+    const double full = floor(tiles / slots), rest = tiles - full * slots;
+    auto time = [&](double n) { return n > 0 ? c.round + std::max(each * c.kblock, n * each * area / (c.rate * device_cus() / 256.0)) : 0.0; };
+    return (float)(1.0 + std::max(full * time(slots) + time(rest), (double)c.round + longest * c.kblock));
 }
 
-template <class Shape>
-Plan make_plan(int count, int P, Shape shape)
+struct Choice { int kernel, splits; };
+Choice choose(int P, int what, const Work& w)
 {
-    size_t squares = 0, at = 0;
+    Choice best{FINE, 1};
+    float least = 0.f;
+    for (int k = 0; k < KERNELS; ++k) {
+        const float t = cost_of(P, k, w.tiles[k], w.blocks[k], w.longest);
+        if (k == 0 || t < least) { least = t; best = Choice{k, 1}; }
+    }
+    if (what != GRAM) return best;
+    // few tiles of long rows: up to a workgroup per compute unit, with eight waves' (four waves') k-blocks in flight at once at least; the sums take a launch of 4 us
+    for (int k = FINE; k <= DIRECT; ++k) {
+        const int waves = k == FINE ? 8 : 4, splits = std::min(device_cus() / std::max(w.tiles[k], 1), w.longest / (waves * (k == FINE ? ahead<1>() : ahead<2>())));
+        if (splits < 2) continue;
+        const float t = 4.f + cost_of(P, k, (double)w.tiles[k] * splits, w.blocks[k], (double)w.longest / splits);
+        if (t < least) { least = t; best = Choice{k, splits}; }
+    }
+    return best;
+}
+size_t partial_bytes(const Choice& c, const Work& w) { return c.splits > 1 ? (size_t)w.tiles[c.kernel] * c.splits * SIDE[c.kernel] * SIDE[c.kernel] * 1024 * sizeof(float) : 0; }
+
+// ---- the plan of a call: made in the same way to size the workspace and to run
+size_t operand_bytes(int mb, int nb, int P) { return ((size_t)3 * mb * nb + (size_t)2 * mb * mb) * 2 * P * BLOCK; }
+
+// The matrices that one sequence of launches works on: JOBS of a list, its empty ones left out
+struct Group {
+    Work work[PRODUCTS];
+    int count;
+    bool whole;                              // all of them fit the LDS of a workgroup
+    size_t squares, operands, partial;       // bytes
+    void start() { *this = Group{}; whole = true; }
+    void add(int rows, int cols, int P)
+    {
+        const int mb = (std::min(rows, cols) + 31) / 32, nb = (std::max(rows, cols) + 31) / 32;
+        for (int w = 0; w < PRODUCTS; ++w) work[w].add(w, mb, nb);
+        ++count;
+        whole = whole && whole_fits(mb, nb);
+        squares += squares_of(rows, cols) * sizeof(double);
+        operands += operand_bytes(mb, nb, P);
+    }
+    size_t bytes(int P) const
+    {
+        if (whole) return 256;               // (none is used)
+        return align_up(squares, 1024) + operands + partial_bytes(choose(P, GRAM, work[GRAM]), work[GRAM]);
+    }
+};
+
+template <class Shape>
+size_t workspace_bytes(int count, int P, Shape shape)
+{
+    size_t most = 0;
+    Group g;
+    g.start();
     for (int i = 0; i < count; ++i) {
         int rows, cols;
         shape(i, rows, cols);
-        squares += squares_of(rows, cols);
-        at += operand_bytes(rows, cols, P);
+        if (rows && cols) g.add(rows, cols, P);
+        if (g.count == JOBS || (i + 1 == count && g.count)) {
+            most = std::max(most, g.bytes(P));
+            g.start();
+        }
     }
-    Plan p;
-    p.operands = align_up(squares * sizeof(double), 1024);
-    p.total = p.operands + at;
-    return p;
+    return most;
 }
 
-// count entries of j, for launches whose matrix i has `units(mb, nb, rows, cols)` workgroups
+// the first workgroups of j's matrices, for launches whose matrix i has `units(mb, nb, rows, cols)` of them; their number
 template <class Units>
 unsigned number(Jobs& j, int count, Units units)
 {
@@ -450,82 +888,95 @@ unsigned number(Jobs& j, int count, Units units)
 }
 
 template <typename E, int P, bool MUON>
-int run(Call c, Jobs& j, int count, int steps, hipStream_t st)
+int run_group(const Group& group, Call c, Jobs& j, int steps, void* ws, hipStream_t st)
 {
-    c.count = count;
-    const unsigned squares = number(j, count, [](int, int, int r, int co) { return squares_of(r, co); });
-    if (squares == 0) return DR_OK;
+    c.count = group.count;
+    if (group.whole) {
+        hipLaunchKernelGGL((whole_kernel<E, P, MUON>), dim3(group.count), dim3(512), 0, st, c, j, steps);
+        return check_launch("orthogonalise");
+    }
+    c.squares = (double*)ws;
+    c.ws = (unsigned char*)ws + align_up(group.squares, 1024);
+    c.partial = (float*)(c.ws + group.operands);
+    size_t operands = 0;
+    int squares_at = 0;
+    for (int i = 0; i < group.count; ++i) {
+        j.operands[i] = (unsigned)(operands / 1024);
+        j.squares[i] = squares_at;
+        operands += operand_bytes(j.mb[i], j.nb[i], P);
+        squares_at += squares_of(j.rows[i], j.cols[i]);
+    }
+    const unsigned squares = number(j, group.count, [](int, int, int r, int co) { return squares_of(r, co); });
     hipLaunchKernelGGL((squares_kernel<E, MUON>), dim3(squares), dim3(256), 0, st, c, j);
-    const unsigned cuts = number(j, count, [](int mb, int nb, int, int) { return (mb * nb + 3) / 4; });
+    const unsigned cuts = number(j, group.count, [](int mb, int nb, int, int) { return (mb * nb + 3) / 4; });
     hipLaunchKernelGGL((cut_kernel<E, P, MUON>), dim3(cuts), dim3(256), 0, st, c, j);
+    using std::integral_constant;
     auto product = [&](auto what, int turn, int last) {
         constexpr int WHAT = decltype(what)::value;
         constexpr bool END = WHAT == APPLY && MUON;      // (the other products are the same for every result)
         typedef std::conditional_t<WHAT == APPLY, E, float> R;
-        const unsigned fine = number(j, count, [](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, 1); });
-        if (fine <= 2u * device_cus()) hipLaunchKernelGGL((product_kernel<R, P, WHAT, 1, 8, END>), dim3(fine), dim3(512), 0, st, c, j, turn, last);
-        else {
-            const unsigned units = number(j, count, [](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, 2); });
-            hipLaunchKernelGGL((product_kernel<R, P, WHAT, 2, 4, END>), dim3(units), dim3(256), 0, st, c, j, turn, last);
-        }
+        const Choice choice = choose(P, WHAT, group.work[WHAT]);
+        const unsigned tiles = number(j, group.count, [&](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, SIDE[choice.kernel]); });
+        auto direct = [&](auto side, auto waves) {
+            constexpr int T = decltype(side)::value, W = decltype(waves)::value;
+            hipLaunchKernelGGL((product_kernel<R, P, WHAT, T, W, END>), dim3(tiles * choice.splits), dim3(W * 64), 0, st, c, j, turn, last, choice.splits);
+            if constexpr (WHAT == GRAM) {
+                if (choice.splits > 1) hipLaunchKernelGGL((sum_kernel<R, P, WHAT, T, END>), dim3(tiles * T * T), dim3(256), 0, st, c, j, turn, last, choice.splits);
+            }
+        };
+        auto tile = [&](auto side, auto depth, auto apart) {
+            constexpr int T = decltype(side)::value;
+            hipLaunchKernelGGL((tile_kernel<R, P, WHAT, 2, 2, T / 2, T / 2, decltype(depth)::value, decltype(apart)::value, END>), dim3(tiles), dim3(256), 0, st, c, j, turn, last);
+        };
+        if (choice.kernel == FINE) direct(integral_constant<int, 1>{}, integral_constant<int, 8>{});
+        else if (choice.kernel == DIRECT) direct(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+        else if (choice.kernel == TILE4) tile(integral_constant<int, 4>{}, integral_constant<int, 2>{}, std::bool_constant<P == 3>{});
+        else if (choice.kernel == TILE6) tile(integral_constant<int, 6>{}, integral_constant<int, 2>{}, std::false_type{});
+        else tile(integral_constant<int, 8>{}, integral_constant<int, P == 3 ? 1 : 2>{}, std::false_type{});      // (registers: three pieces two deep 658 us for 590)
     };
     for (int s = 0; s < steps; ++s) {
         const int last = s + 1 == steps;
-        product(std::integral_constant<int, GRAM>{}, s & 1, last);
-        product(std::integral_constant<int, POLY>{}, s & 1, last);
-        product(std::integral_constant<int, APPLY>{}, s & 1, last);
+        product(integral_constant<int, GRAM>{}, s & 1, last);
+        product(integral_constant<int, POLY>{}, s & 1, last);
+        product(integral_constant<int, APPLY>{}, s & 1, last);
     }
     return check_launch("orthogonalise");
 }
 
-// The list, JOBS matrices that are not empty at a time.  fill(i, rows, cols, j, k): matrix i's shape and, with j, its entry k
+// fill(i, rows, cols, j, k): matrix i's shape, and entry k of j but for its shape and places
 template <typename E, int P, bool MUON, class Fill>
-int run_list(const Plan& p, Call c, int count, int steps, hipStream_t st, Fill fill)
+int run_list(Call c, int count, const dr_newton_schulz& ns, void* ws, hipStream_t st, Fill fill)
 {
+    c.a = ns.a; c.b = ns.b; c.c = ns.c; c.eps = ns.eps;
     Jobs j;
-    int n = 0, squares = 0;
-    size_t at = p.operands;
+    Group g;
+    g.start();
     for (int i = 0; i < count; ++i) {
         int rows, cols;
-        fill(i, rows, cols, j, n);
+        fill(i, rows, cols, j, g.count);
         if (rows && cols) {
-            j.rows[n] = rows; j.cols[n] = cols;
-            j.mb[n] = (std::min(rows, cols) + 31) / 32;
-            j.nb[n] = (std::max(rows, cols) + 31) / 32;
-            j.operands[n] = (unsigned)(at / 1024);
-            j.squares[n] = squares;
-            at += operand_bytes(rows, cols, P);
-            squares += squares_of(rows, cols);
-            ++n;
+            j.rows[g.count] = rows; j.cols[g.count] = cols;
+            j.mb[g.count] = (std::min(rows, cols) + 31) / 32;
+            j.nb[g.count] = (std::max(rows, cols) + 31) / 32;
+            g.add(rows, cols, P);
         }
-        if (n == JOBS || (i + 1 == count && n)) {
-            if (const int rc = run<E, P, MUON>(c, j, n, steps, st)) return rc;
-            n = 0;
+        if (g.count == JOBS || (i + 1 == count && g.count)) {
+            if (const int rc = run_group<E, P, MUON>(g, c, j, ns.steps, ws, st)) return rc;
+            g.start();
         }
     }
     return DR_OK;
-}
-
-Call make_call(const dr_newton_schulz& ns, void* ws)
-{
-    Call c{};
-    c.ws = (unsigned char*)ws;
-    c.squares = (double*)ws;
-    c.a = ns.a; c.b = ns.b; c.c = ns.c; c.eps = ns.eps;
-    return c;
 }
 
 }  // namespace
 
 size_t orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype)
 {
-    return make_plan(count, dtype == DR_F32 ? 3 : 2, [&](int i, int& r, int& c) { r = ms[i].rows; c = ms[i].cols; }).total;
+    return workspace_bytes(count, dtype == DR_F32 ? 3 : 2, [&](int i, int& r, int& c) { r = ms[i].rows; c = ms[i].cols; });
 }
 
 int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* const* g, void* const* o, const dr_newton_schulz& ns, void* ws, hipStream_t st)
 {
-    const Plan p = make_plan(count, dtype == DR_F32 ? 3 : 2, [&](int i, int& r, int& c) { r = ms[i].rows; c = ms[i].cols; });
-    const Call c = make_call(ns, ws);
     TraceScope trace("orthogonalise", nullptr, count, st);
     auto fill = [&](int i, int& r, int& cols, Jobs& j, int k) {
         r = ms[i].rows; cols = ms[i].cols;
@@ -534,22 +985,21 @@ int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* 
         j.o[k] = o[i];
         j.scale[k] = 0.f;
     };
-    return dtype == DR_F32 ? run_list<float, 3, false>(p, c, count, ns.steps, st, fill) : run_list<uint16_t, 2, false>(p, c, count, ns.steps, st, fill);
+    return dtype == DR_F32 ? run_list<float, 3, false>(Call{}, count, ns, ws, st, fill) : run_list<uint16_t, 2, false>(Call{}, count, ns, ws, st, fill);
 }
 
 size_t muon_step_workspace_bytes(int count, const dr_muon_param* ps)
 {
-    return make_plan(count, 3, [&](int i, int& r, int& c) { r = ps[i].rows; c = ps[i].cols; }).total;
+    return workspace_bytes(count, 3, [&](int i, int& r, int& c) { r = ps[i].rows; c = ps[i].cols; });
 }
 
 int launch_muon_step(int count, const dr_muon_param* ps, const dr_muon& opt, void* ws, hipStream_t st)
 {
-    const Plan p = make_plan(count, 3, [&](int i, int& r, int& c) { r = ps[i].rows; c = ps[i].cols; });
-    Call c = make_call(opt.ns, ws);
+    Call c{};
     c.mu = opt.momentum;
     c.keep = (float)(1.0 - (double)opt.lr * opt.weight_decay);
     TraceScope trace("muon_step", nullptr, count, st);
-    return run_list<float, 3, true>(p, c, count, opt.ns.steps, st, [&](int i, int& r, int& cols, Jobs& j, int k) {
+    return run_list<float, 3, true>(c, count, opt.ns, ws, st, [&](int i, int& r, int& cols, Jobs& j, int k) {
         r = ps[i].rows; cols = ps[i].cols;
         j.g[k] = ps[i].dw;
         j.momentum[k] = ps[i].momentum;
