@@ -39,7 +39,8 @@ enum { GRAM = 0, POLY = 1, APPLY = 2, PRODUCTS = 3 };
 // The matrices of a launch; arrays by what is looked up together.  A list is worked on JOBS at a time.
 constexpr int JOBS = 64;
 struct Jobs {
-    int first[JOBS];                         // first workgroup; INT_MAX behind the last matrix
+    int first[JOBS];                         // first workgroup of the launch's k-th matrix; INT_MAX behind the last
+    int which[JOBS];                         // the launch's k-th matrix
     unsigned operands[JOBS];                 // its operands' place in the workspace, in KiB
     int mb[JOBS], nb[JOBS];                  // blocks of 32 of the short and of the long side
     int rows[JOBS], cols[JOBS];
@@ -61,7 +62,7 @@ struct Call {
 
 // A matrix of a launch as its kernels see it
 struct Mat {
-    int k, mb, nb, rows, cols;
+    int k, first, mb, nb, rows, cols;        // first: its first workgroup
     bool tall;                               // rows > cols: X is the transpose
 };
 __device__ __forceinline__ Mat find_matrix(const Jobs& j, int count, int id)
@@ -72,7 +73,8 @@ __device__ __forceinline__ Mat find_matrix(const Jobs& j, int count, int id)
         for (int i = 1; i < JOBS; ++i) k += j.first[i] <= id ? 1 : 0;
     }
     k = __builtin_amdgcn_readfirstlane(k);
-    return Mat{k, j.mb[k], j.nb[k], j.rows[k], j.cols[k], j.rows[k] > j.cols[k]};
+    const int i = j.which[k];
+    return Mat{i, j.first[k], j.mb[i], j.nb[i], j.rows[i], j.cols[i], j.rows[i] > j.cols[i]};
 }
 
 // Operands of a matrix: X, X^T twice (a product reads one and writes the other), A, Q
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(256) void squares_kernel(const Call c, const Jobs j
     const Mat m = find_matrix(j, c.count, blockIdx.x);
     const T* const g = (const T*)j.g[m.k];
     float* const mom = j.momentum[m.k];
-    const int me = (int)blockIdx.x - j.first[m.k];
+    const int me = (int)blockIdx.x - m.first;
     const size_t total = (size_t)m.rows * m.cols, step = (size_t)squares_of(m.rows, m.cols) * 256;
     double s = 0.0;
     for (size_t i = (size_t)me * 256 + threadIdx.x; i < total; i += step * 8) {
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs j)
     const T* const g = (const T*)j.g[m.k];
     const float* const mom = j.momentum[m.k];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
-    const int b = ((int)blockIdx.x - j.first[m.k]) * 4 + wave;
+    const int b = ((int)blockIdx.x - m.first) * 4 + wave;
     const bool on = b < m.mb * m.nb;
     const int bi = on ? b / m.nb : 0, bj = on ? b - bi * m.nb : 0;
     float* const tile = tiles[wave];
@@ -329,7 +331,7 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
     const Operands<P> op(c, j, m);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     int bi, bj;
-    tile_blocks<WHAT, T>(m, unit - j.first[m.k], bi, bj);
+    tile_blocks<WHAT, T>(m, unit - m.first, bi, bj);
     const unsigned char* const left = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : op.q;
     const unsigned char* const right = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : turn ? op.xt1 : op.xt0;
     const int kblocks = 2 * (WHAT == GRAM ? m.nb : m.mb), lrows = m.mb, rrows = WHAT == APPLY ? m.nb : m.mb;
@@ -436,7 +438,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs j, in
     const Mat m = find_matrix(j, c.count, unit);
     const Operands<P> op(c, j, m);
     int bi, bj;
-    tile_blocks<WHAT, T>(m, unit - j.first[m.k], bi, bj);
+    tile_blocks<WHAT, T>(m, unit - m.first, bi, bj);
     bi += blk / T;
     bj += blk % T;
     if (bi >= m.mb || bj >= (WHAT == APPLY ? m.nb : m.mb) || (WHAT != APPLY && bi < bj)) return;
@@ -464,14 +466,16 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
     constexpr int W = WM * WN, BM = WM * TM, BN = WN * TN, STAGE = (BM + BN) * P * BLOCK, LOADS = (BM + BN) * P / W;
     static_assert((BM + BN) * P % W == 0 && BM == BN && (DEPTH == 1 || DEPTH == 2) && tile_lds<P, BM, BN>() >= W * 32 * PITCH * 4, "a tile's operands");
     __shared__ __attribute__((aligned(16))) unsigned char lds[tile_lds<P, BM, BN>()];
-    // workgroup b runs on die b & 7: a die takes a contiguous range of tiles, which share operands
-    const int die = blockIdx.x & 7, share = (int)gridDim.x >> 3, odd = gridDim.x & 7, id = die * share + min(die, odd) + (int)(blockIdx.x >> 3);
+    // workgroup b runs on die b & 7: of one matrix a die takes a contiguous range of tiles, which share operands (of a list, whose long contractions come first, that
+    // would give one die the most work)
+    const int die = blockIdx.x & 7, share = (int)gridDim.x >> 3, odd = gridDim.x & 7;
+    const int id = c.count > 1 ? (int)blockIdx.x : die * share + min(die, odd) + (int)(blockIdx.x >> 3);
     const Mat m = find_matrix(j, c.count, id);
     const Operands<P> op(c, j, m);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wm = wave / WN, wn = wave % WN;
     int bi, bj;
-    tile_blocks<WHAT, BM>(m, id - j.first[m.k], bi, bj);
+    tile_blocks<WHAT, BM>(m, id - m.first, bi, bj);
     const unsigned char* const left = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : op.q;
     const unsigned char* const right = WHAT == GRAM ? op.x : WHAT == POLY ? op.a : turn ? op.xt1 : op.xt0;
     const int kblocks = 2 * (WHAT == GRAM ? m.nb : m.mb), lrows = m.mb, rrows = WHAT == APPLY ? m.nb : m.mb;
@@ -875,14 +879,32 @@ size_t workspace_bytes(int count, int P, Shape shape)
     return most;
 }
 
-// the first workgroups of j's matrices, for launches whose matrix i has `units(mb, nb, rows, cols)` of them; their number
+// The order of a launch's matrices: those with the largest length(mb, nb) first, so that what is started last is short
+struct Order { int which[JOBS]; };
+template <class Length>
+Order order_by(const Jobs& j, int count, Length length)
+{
+    Order o;
+    for (int i = 0; i < count; ++i) {
+        int at = i;
+        for (; at > 0 && length(j.mb[o.which[at - 1]], j.nb[o.which[at - 1]]) < length(j.mb[i], j.nb[i]); --at) o.which[at] = o.which[at - 1];
+        o.which[at] = i;
+    }
+    return o;
+}
+
+// the first workgroups of j's matrices, for launches whose matrix has `units(mb, nb, rows, cols)` of them; their number
 template <class Units>
-unsigned number(Jobs& j, int count, Units units)
+unsigned number(Jobs& j, int count, const Order& order, Units units)
 {
     unsigned at = 0;
-    for (int i = 0; i < JOBS; ++i) {
-        j.first[i] = i < count ? (int)at : 0x7FFFFFFF;
-        if (i < count) at += units(j.mb[i], j.nb[i], j.rows[i], j.cols[i]);
+    for (int k = 0; k < JOBS; ++k) {
+        j.first[k] = 0x7FFFFFFF;
+        if (k >= count) continue;
+        const int i = order.which[k];
+        j.which[k] = i;
+        j.first[k] = (int)at;
+        at += units(j.mb[i], j.nb[i], j.rows[i], j.cols[i]);
     }
     return at;
 }
@@ -906,9 +928,11 @@ int run_group(const Group& group, Call c, Jobs& j, int steps, void* ws, hipStrea
         operands += operand_bytes(j.mb[i], j.nb[i], P);
         squares_at += squares_of(j.rows[i], j.cols[i]);
     }
-    const unsigned squares = number(j, group.count, [](int, int, int r, int co) { return squares_of(r, co); });
+    const Order orders[PRODUCTS] = {order_by(j, group.count, [](int, int nb) { return nb; }), order_by(j, group.count, [](int mb, int) { return mb; }),
+                                    order_by(j, group.count, [](int mb, int) { return mb; })};
+    const unsigned squares = number(j, group.count, orders[GRAM], [](int, int, int r, int co) { return squares_of(r, co); });
     hipLaunchKernelGGL((squares_kernel<E, MUON>), dim3(squares), dim3(256), 0, st, c, j);
-    const unsigned cuts = number(j, group.count, [](int mb, int nb, int, int) { return (mb * nb + 3) / 4; });
+    const unsigned cuts = number(j, group.count, orders[GRAM], [](int mb, int nb, int, int) { return (mb * nb + 3) / 4; });
     hipLaunchKernelGGL((cut_kernel<E, P, MUON>), dim3(cuts), dim3(256), 0, st, c, j);
     using std::integral_constant;
     auto product = [&](auto what, int turn, int last) {
@@ -916,7 +940,7 @@ int run_group(const Group& group, Call c, Jobs& j, int steps, void* ws, hipStrea
         constexpr bool END = WHAT == APPLY && MUON;      // (the other products are the same for every result)
         typedef std::conditional_t<WHAT == APPLY, E, float> R;
         const Choice choice = choose(P, WHAT, group.work[WHAT]);
-        const unsigned tiles = number(j, group.count, [&](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, SIDE[choice.kernel]); });
+        const unsigned tiles = number(j, group.count, orders[WHAT], [&](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, SIDE[choice.kernel]); });
         auto direct = [&](auto side, auto waves) {
             constexpr int T = decltype(side)::value, W = decltype(waves)::value;
             hipLaunchKernelGGL((product_kernel<R, P, WHAT, T, W, END>), dim3(tiles * choice.splits), dim3(W * 64), 0, st, c, j, turn, last, choice.splits);
