@@ -252,7 +252,11 @@ def _like(t, x):
     """Pointer of a tensor with x's shape, dtype and order, or NULL."""
     if t is None:
         return None
-    if isinstance(t, NHWC) != isinstance(x, NHWC) or t.dtype != x.dtype or t.shape != x.shape:
+    if isinstance(t, NHWC) != isinstance(x, NHWC):
+        raise ValueError("tensors of one call share shape, dtype and order")
+    if isinstance(t, NHWC):
+        t, x = t.t, x.t
+    if t.dtype is not x.dtype or t.shape != x.shape:
         raise ValueError("tensors of one call share shape, dtype and order")
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")

@@ -124,28 +124,37 @@ __global__ __launch_bounds__(256) void norm_vectors_any_kernel(const Pixels px, 
 }
 
 // dgamma and dbeta from the partial sums of `ranges` ranges of pixels, in a fixed order, in double
-__global__ __launch_bounds__(256) void norm_vectors_sum_kernel(const float* __restrict__ partial, int ranges, int C, float* __restrict__ dgamma, float* __restrict__ dbeta)
+__global__ __launch_bounds__(1024) void norm_vectors_sum_kernel(const float* __restrict__ partial, int ranges, int C, float* __restrict__ dgamma, float* __restrict__ dbeta)
 {
-    __shared__ double red[16][16];
-    const int col = blockIdx.x * 16 + (threadIdx.x & 15), row = threadIdx.x >> 4;
+    __shared__ double red[64][17];
+    const int lane = threadIdx.x & 15, col = blockIdx.x * 16 + lane, row = threadIdx.x >> 4;
     double s = 0.0;
     if (col < 2 * C) {
-#pragma unroll 4
-        for (int r = row; r < ranges; r += 16) s += (double)partial[(size_t)r * 2 * C + col];
+#pragma unroll 8
+        for (int r = row; r < ranges; r += 64) s += (double)partial[(size_t)r * 2 * C + col];
     }
-    red[row][threadIdx.x & 15] = s;
+    red[row][lane] = s;
     __syncthreads();
-    if (threadIdx.x < 16 && col < 2 * C) {
+    if (row < 4) {
         s = 0.0;
-        for (int r = 0; r < 16; ++r) s += red[r][threadIdx.x];
-        if (col < C) { if (dgamma) dgamma[col] = (float)s; }
-        else if (dbeta) dbeta[col - C] = (float)s;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += red[row * 16 + r][lane];
+    }
+    __syncthreads();
+    if (row < 4) red[row][lane] = s;
+    __syncthreads();
+    if (row == 0 && col < 2 * C) {
+        const float v = (float)((red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]));
+        if (col < C) { if (dgamma) dgamma[col] = v; }
+        else if (dbeta) dbeta[col - C] = v;
     }
 }
 
 // ---- sums over lanes
 template <int CTRL>
-__device__ __forceinline__ float add_dpp(float v) { return v + __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)); }
+__device__ __forceinline__ float dpp(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true)); }
+template <int CTRL>
+__device__ __forceinline__ float add_dpp(float v) { return v + dpp<CTRL>(v); }
 
 // over groups of G lanes (a power of two), the same value in every lane of a group
 template <int G>
@@ -166,8 +175,24 @@ __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
-// ---- channels last, 16-byte aligned rows of a multiple of 16 bytes: a row in the registers of G lanes, NV vectors of 16 bytes each.  G > 64: G / 64 waves.
-// The workgroup's THREADS / G groups walk the rows together.
+// ---- channels last, rows of 16 bytes and more: a row in the registers of G lanes, NV vectors of 16 bytes each.  G > 64: G / 64 waves.  The workgroup's THREADS / G
+// groups walk the rows together.  Rows may start anywhere: 16-byte loads and stores need no alignment.  RAGGED: where 16 bytes do not divide a row, its last vector ends where
+// the row ends and holds some elements of the one before it again, which count once and are stored twice, with the same value.
+__device__ __forceinline__ uint4 load16(const void* p)
+{
+    uint4 v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+template <typename T>
+__device__ __forceinline__ void store16(T* p, const float* v)
+{
+    uint4 t;
+    if constexpr (sizeof(T) == 4) t = uint4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    else t = uint4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+    __builtin_memcpy(p, &t, 16);
+}
+
 template <typename T>
 __device__ __forceinline__ void unpack(const uint4& r, float* v)
 {
@@ -213,20 +238,34 @@ __device__ __forceinline__ void load_vector(const float* p, int at, float other,
     for (int e = 0; e < VN; ++e) v[e] = p ? p[at + e] : other;
 }
 
-template <typename T, int G, int NV, int THREADS>
+// Where vector k of a row of C elements starts, and how many of its elements the vector before it holds too
+template <int VN, bool RAGGED>
+struct Place {
+    int first, skip;
+    __device__ __forceinline__ Place(int k, int C) : first(k * VN), skip(0)
+    {
+        if (RAGGED && first + VN > C) {
+            skip = first + VN - C;
+            first = C - VN;
+        }
+    }
+};
+
+template <typename T, int G, int NV, int THREADS, bool RAGGED>
 __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
                                                             int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
 {
     constexpr int VN = Store<T>::VN, GROUPS = THREADS / G;
     __shared__ float red[2][THREADS / 64][1];
     int turn = 0;
-    const int lane = threadIdx.x % G, group = threadIdx.x / G, nvec = C / VN;
+    const int lane = threadIdx.x % G, group = threadIdx.x / G, nvec = (C + VN - 1) / VN;
     const float down = square_scale(C);
     uint4 next[NV];
+    auto at = [&](int j) __attribute__((always_inline)) { return Place<VN, RAGGED>(lane + j * G, C); };
     auto fetch = [&](size_t row) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < NV; ++j)
-            if (lane + j * G < nvec && row < rows) next[j] = reinterpret_cast<const uint4*>(x + row * C)[lane + j * G];
+            if (lane + j * G < nvec && row < rows) next[j] = load16(x + row * C + at(j).first);
     };
     size_t row = (size_t)blockIdx.x * GROUPS + group;
     const size_t stride = (size_t)gridDim.x * GROUPS;
@@ -237,8 +276,8 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, 
 #pragma unroll
     for (int j = 0; j < NV; ++j)
         if (lane + j * G < nvec) {
-            load_vector<VN>(gamma, (lane + j * G) * VN, 1.f, g[j]);
-            load_vector<VN>(beta, (lane + j * G) * VN, 0.f, b[j]);
+            load_vector<VN>(gamma, at(j).first, 1.f, g[j]);
+            load_vector<VN>(beta, at(j).first, 0.f, b[j]);
         }
     for (size_t first = (size_t)blockIdx.x * GROUPS; first < rows; first += stride, row += stride) {      // (the same rounds for all lanes)
         float v[NV][VN], s[1] = {0.f};
@@ -246,7 +285,7 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, 
         for (int j = 0; j < NV; ++j) {
             unpack<T>(next[j], v[j]);                  // (zero beyond the row)
 #pragma unroll
-            for (int e = 0; e < VN; ++e) s[0] += v[j][e];
+            for (int e = 0; e < VN; ++e) s[0] += !RAGGED || e >= at(j).skip ? v[j][e] : 0.f;
         }
         fetch(row + stride);
         group_sums<G, THREADS, 1>(s, red, turn);
@@ -258,7 +297,7 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, 
 #pragma unroll
                 for (int e = 0; e < VN; ++e) {
                     v[j][e] -= mean;
-                    s[0] = __builtin_fmaf(v[j][e] * down, v[j][e], s[0]);
+                    s[0] = __builtin_fmaf(!RAGGED || e >= at(j).skip ? v[j][e] * down : 0.f, v[j][e], s[0]);
                 }
             }
         group_sums<G, THREADS, 1>(s, red, turn);
@@ -272,7 +311,7 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, 
                         const float t = v[j][e] * rstd * g[j][e] + b[j][e];
                         v[j][e] = relu ? fmaxf(t, 0.f) : t;
                     }
-                    Store<T>::stv(y + row * C + (size_t)(lane + j * G) * VN, v[j]);
+                    store16<T>(y + row * C + at(j).first, v[j]);
                 }
             if (lane == 0) {
                 if (mean_out) mean_out[row] = mean;
@@ -283,7 +322,7 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, 
 }
 
 // ... and the gradient: every lane adds its columns of dgamma and dbeta over the workgroup's rows; partial[workgroup][2][C]
-template <typename T, int G, int NV, int THREADS>
+template <typename T, int G, int NV, int THREADS, bool RAGGED>
 __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, int C, const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
                                                                  const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
 {
@@ -291,16 +330,17 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
     __shared__ float red[2][THREADS / 64][2];
     extern __shared__ float columns[];                 // [2][C]
     int turn = 0;
-    const int lane = threadIdx.x % G, group = threadIdx.x / G, nvec = C / VN;
+    const int lane = threadIdx.x % G, group = threadIdx.x / G, nvec = (C + VN - 1) / VN;
     uint4 nx[NV], nd[NV];
     float n_mean = 0.f, n_rstd = 0.f;
+    auto at = [&](int j) __attribute__((always_inline)) { return Place<VN, RAGGED>(lane + j * G, C); };
     auto fetch = [&](size_t row) __attribute__((always_inline)) {
         if (row >= rows) return;
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             if (lane + j * G < nvec) {
-                nd[j] = reinterpret_cast<const uint4*>(dy + row * C)[lane + j * G];
-                nx[j] = reinterpret_cast<const uint4*>(x + row * C)[lane + j * G];
+                nd[j] = load16(dy + row * C + at(j).first);
+                nx[j] = load16(x + row * C + at(j).first);
             }
         n_mean = mean[row];
         n_rstd = rstd[row];
@@ -315,7 +355,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
     for (int j = 0; j < NV; ++j) {
 #pragma unroll
         for (int e = 0; e < VN; ++e) dg[j][e] = db[j][e] = g[j][e] = 0.f;
-        if (lane + j * G < nvec) load_vector<VN>(gamma, (lane + j * G) * VN, 1.f, g[j]);
+        if (lane + j * G < nvec) load_vector<VN>(gamma, at(j).first, 1.f, g[j]);
     }
     for (size_t first = (size_t)blockIdx.x * GROUPS; first < rows; first += stride, row += stride) {
         float z[NV][VN], d[NV][VN], s[2] = {0.f, 0.f};
@@ -329,11 +369,11 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
 #pragma unroll
                 for (int e = 0; e < VN; ++e) {
                     z[j][e] = (z[j][e] - mu) * r;
-                    const float u = d[j][e] * g[j][e];
+                    const float once = !RAGGED || e >= at(j).skip ? d[j][e] : 0.f, u = once * g[j][e];
                     s[0] += u;
                     s[1] += u * z[j][e];
-                    db[j][e] += d[j][e];
-                    dg[j][e] += d[j][e] * z[j][e];
+                    db[j][e] += once;
+                    dg[j][e] += once * z[j][e];
                 }
             }
         }
@@ -346,7 +386,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
                 if (lane + j * G < nvec) {
 #pragma unroll
                     for (int e = 0; e < VN; ++e) d[j][e] = r * (d[j][e] * g[j][e] - s0 - z[j][e] * s1);
-                    Store<T>::stv(dx + row * C + (size_t)(lane + j * G) * VN, d[j]);
+                    store16<T>(dx + row * C + at(j).first, d[j]);
                 }
         }
     }
@@ -368,7 +408,8 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
                 if (lane + j * G < nvec) {
 #pragma unroll
                     for (int e = 0; e < VN; ++e) {
-                        const int c = (lane + j * G) * VN + e;
+                        if (RAGGED && e < at(j).skip) continue;
+                        const int c = at(j).first + e;
                         columns[c] = t ? columns[c] + dg[j][e] : dg[j][e];
                         columns[C + c] = t ? columns[C + c] + db[j][e] : db[j][e];
                     }
@@ -379,176 +420,131 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
     for (int i = threadIdx.x; i < 2 * C; i += THREADS) partial[(size_t)blockIdx.x * 2 * C + i] = columns[i];
 }
 
-// ---- channels last, any row length and alignment: runs of whole rows go through LDS, fetched and written in aligned 16-byte pieces
-// A run's first byte lies (address % 16) into LDS, so that every piece is 16 bytes of memory and of LDS.
+// ---- channels last, rows shorter than 16 bytes: a lane has a whole row
+constexpr int NARROW = 8;
 template <typename T>
-__device__ __forceinline__ int run_in(const T* base, size_t total, size_t at, int count, unsigned char* lds)
+__global__ __launch_bounds__(256) void norm_narrow_kernel(size_t rows, int C, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps, int relu, T* y,
+                                                          float* __restrict__ mean_out, float* __restrict__ rstd_out)
 {
-    const uintptr_t lo = (uintptr_t)base, hi = lo + total * sizeof(T), from = lo + at * sizeof(T), first = from & ~(uintptr_t)15;
-    const int shift = (int)(from - first), pieces = (shift + count * (int)sizeof(T) + 15) >> 4;
-    for (int i = threadIdx.x; i < pieces; i += 256) {
-        const uintptr_t p = first + (uintptr_t)i * 16;
-        if (p >= lo && p + 16 <= hi) reinterpret_cast<uint4*>(lds)[i] = *reinterpret_cast<const uint4*>(p);
-        else {
-#pragma unroll
-            for (int e = 0; e < (int)(16 / sizeof(T)); ++e) {
-                const uintptr_t q = p + e * sizeof(T);
-                if (q >= lo && q < hi) reinterpret_cast<T*>(lds)[i * (16 / sizeof(T)) + e] = *reinterpret_cast<const T*>(q);
-            }
-        }
-    }
-    return shift / (int)sizeof(T);
-}
-template <typename T>
-__device__ __forceinline__ void run_out(T* base, size_t at, int count, const unsigned char* lds)      // lds: laid out as for this address
-{
-    const uintptr_t from = (uintptr_t)(base + at), to = from + (size_t)count * sizeof(T), first = from & ~(uintptr_t)15;
-    const int pieces = (int)((to - first + 15) >> 4);
-    for (int i = threadIdx.x; i < pieces; i += 256) {
-        const uintptr_t p = first + (uintptr_t)i * 16;
-        if (p >= from && p + 16 <= to) *reinterpret_cast<uint4*>(p) = reinterpret_cast<const uint4*>(lds)[i];
-        else {
-#pragma unroll
-            for (int e = 0; e < (int)(16 / sizeof(T)); ++e) {
-                const uintptr_t q = p + e * sizeof(T);
-                if (q >= from && q < to) *reinterpret_cast<T*>(q) = reinterpret_cast<const T*>(lds)[i * (16 / sizeof(T)) + e];
-            }
-        }
-    }
-}
-
-constexpr int RUN_BYTES = 16384;         // most bytes of a run (of each tensor)
-template <typename T> constexpr int run_bytes() { return RUN_BYTES + 32; }
-
-template <typename T, int G>
-__global__ __launch_bounds__(256) void norm_runs_kernel(size_t rows, int C, int run, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
-                                                        int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
-{
-    __shared__ __attribute__((aligned(16))) unsigned char in[run_bytes<T>()], out[run_bytes<T>()];
-    const int lane = threadIdx.x % G, group = threadIdx.x / G;
     const float down = square_scale(C);
-    const size_t runs = (rows + run - 1) / run;
-    for (size_t k = blockIdx.x; k < runs; k += gridDim.x) {
-        const size_t row0 = k * run;
-        const int here = (int)(rows - row0 < (size_t)run ? rows - row0 : (size_t)run);
-        const int shift = run_in<T>(x, rows * C, row0 * C, here * C, in);
-        const int out_shift = (int)(((uintptr_t)(y + row0 * C) & 15) / sizeof(T));
-        __syncthreads();
-        for (int r = group; r < here; r += 256 / G) {
-            const T* v = reinterpret_cast<const T*>(in) + shift + r * C;
-            T* o = reinterpret_cast<T*>(out) + out_shift + r * C;
-            float s = 0.f;
-            for (int c = lane; c < C; c += G) s += Store<T>::ld(v + c);
-            const float mean = lanes_sum<G>(s) / (float)C;
-            s = 0.f;
-            for (int c = lane; c < C; c += G) {
-                const float d = Store<T>::ld(v + c) - mean;
-                s = __builtin_fmaf(d * down, d, s);
-            }
-            const float rstd = 1.f / sqrtf(lanes_sum<G>(s) / ((float)C * down) + eps);
-            for (int c = lane; c < C; c += G) {
-                const float t = (Store<T>::ld(v + c) - mean) * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f);
-                Store<T>::st(o + c, relu ? fmaxf(t, 0.f) : t);
-            }
-            if (lane == 0) {
-                if (mean_out) mean_out[row0 + r] = mean;
-                if (rstd_out) rstd_out[row0 + r] = rstd;
-            }
+    for (size_t row = (size_t)blockIdx.x * 256 + threadIdx.x; row < rows; row += (size_t)gridDim.x * 256) {
+        float v[NARROW], s = 0.f;
+#pragma unroll
+        for (int c = 0; c < NARROW; ++c) {
+            v[c] = c < C ? Store<T>::ld(x + row * C + c) : 0.f;
+            s += v[c];
         }
-        __syncthreads();
-        run_out<T>(y, row0 * C, here * C, out);
-        // (the next run's rows are written behind the barrier that follows its fetch)
+        const float mean = s / (float)C;
+        s = 0.f;
+#pragma unroll
+        for (int c = 0; c < NARROW; ++c)
+            if (c < C) {
+                v[c] -= mean;
+                s = __builtin_fmaf(v[c] * down, v[c], s);
+            }
+        const float rstd = 1.f / sqrtf(s / ((float)C * down) + eps);
+#pragma unroll
+        for (int c = 0; c < NARROW; ++c)
+            if (c < C) {
+                const float t = v[c] * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f);
+                Store<T>::st(y + row * C + c, relu ? fmaxf(t, 0.f) : t);
+            }
+        if (mean_out) mean_out[row] = mean;
+        if (rstd_out) rstd_out[row] = rstd;
     }
 }
 
-// ... and the gradient: the sums row by row, then column by column (thread t: columns t, t + 256, ...) what needs both
-constexpr int RUN_COLUMNS = 8;           // most columns of a thread
-template <typename T, int G, int NC>
-__global__ __launch_bounds__(256) void norm_grad_runs_kernel(size_t rows, int C, int run, const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
-                                                             const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
+template <typename T>
+__global__ __launch_bounds__(256) void norm_grad_narrow_kernel(size_t rows, int C, const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
+                                                               const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
 {
-    __shared__ __attribute__((aligned(16))) unsigned char in_d[run_bytes<T>()], in_x[run_bytes<T>()], out[run_bytes<T>()];
-    __shared__ float4 of_row[512];       // mean, rstd, sum g / C, sum g z / C
-    const int lane = threadIdx.x % G, group = threadIdx.x / G;
-    const size_t runs = (rows + run - 1) / run;
-    float g[NC], dg[NC], db[NC];
+    __shared__ float red[4][2 * NARROW];
+    float dg[NARROW], db[NARROW];
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int c = threadIdx.x + j * 256;
-        g[j] = gamma && c < C ? gamma[c] : 1.f;
-        dg[j] = db[j] = 0.f;
-    }
-    for (size_t k = blockIdx.x; k < runs; k += gridDim.x) {
-        const size_t row0 = k * run;
-        const int here = (int)(rows - row0 < (size_t)run ? rows - row0 : (size_t)run);
-        const int sd = run_in<T>(dy, rows * C, row0 * C, here * C, in_d), sx = run_in<T>(x, rows * C, row0 * C, here * C, in_x);
-        const int so = dx ? (int)(((uintptr_t)(dx + row0 * C) & 15) / sizeof(T)) : 0;
-        __syncthreads();
-        for (int r = group; r < here; r += 256 / G) {
-            const T *vd = reinterpret_cast<const T*>(in_d) + sd + r * C, *vx = reinterpret_cast<const T*>(in_x) + sx + r * C;
-            const float mu = mean[row0 + r], rs = rstd[row0 + r];
-            float s = 0.f, t = 0.f;
-            for (int c = lane; c < C; c += G) {
-                const float u = Store<T>::ld(vd + c) * (gamma ? gamma[c] : 1.f);
-                s += u;
-                t += u * ((Store<T>::ld(vx + c) - mu) * rs);
-            }
-            s = lanes_sum<G>(s) / (float)C;
-            t = lanes_sum<G>(t) / (float)C;
-            if (lane == 0) of_row[r] = make_float4(mu, rs, s, t);
-        }
-        __syncthreads();
+    for (int c = 0; c < NARROW; ++c) dg[c] = db[c] = 0.f;
+    for (size_t row = (size_t)blockIdx.x * 256 + threadIdx.x; row < rows; row += (size_t)gridDim.x * 256) {
+        const float mu = mean[row], r = rstd[row];
+        float d[NARROW], z[NARROW], s = 0.f, t = 0.f;
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            const int c = threadIdx.x + j * 256;
-            if (c >= C) break;
-            const T *vd = reinterpret_cast<const T*>(in_d) + sd + c, *vx = reinterpret_cast<const T*>(in_x) + sx + c;
-            T* o = reinterpret_cast<T*>(out) + so + c;
-            for (int r = 0; r < here; ++r) {
-                const float4 q = of_row[r];
-                const float d = Store<T>::ld(vd + r * C), z = (Store<T>::ld(vx + r * C) - q.x) * q.y;
-                db[j] += d;
-                dg[j] += d * z;
-                if (dx) Store<T>::st(o + r * C, q.y * (d * g[j] - q.z - z * q.w));
-            }
+        for (int c = 0; c < NARROW; ++c) {
+            d[c] = c < C ? Store<T>::ld(dy + row * C + c) : 0.f;
+            z[c] = c < C ? (Store<T>::ld(x + row * C + c) - mu) * r : 0.f;
+            db[c] += d[c];
+            dg[c] += d[c] * z[c];
+            const float u = d[c] * (gamma && c < C ? gamma[c] : 1.f);
+            s += u;
+            t += u * z[c];
         }
-        __syncthreads();
-        if (dx) run_out<T>(dx, row0 * C, here * C, out);
+        s /= (float)C;
+        t /= (float)C;
+        if (dx) {
+#pragma unroll
+            for (int c = 0; c < NARROW; ++c)
+                if (c < C) Store<T>::st(dx + row * C + c, r * (d[c] * (gamma ? gamma[c] : 1.f) - s - z[c] * t));
+        }
     }
     if (!partial) return;
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int c = threadIdx.x + j * 256;
-        if (c >= C) break;
-        partial[(size_t)blockIdx.x * 2 * C + c] = dg[j];
-        partial[(size_t)blockIdx.x * 2 * C + C + c] = db[j];
+    for (int c = 0; c < NARROW; ++c) {
+        dg[c] = lanes_sum<64>(dg[c]);
+        db[c] = lanes_sum<64>(db[c]);
+        if ((threadIdx.x & 63) == 0) {
+            red[threadIdx.x >> 6][c] = dg[c];
+            red[threadIdx.x >> 6][NARROW + c] = db[c];
+        }
+    }
+    __syncthreads();
+    if (threadIdx.x < 2 * NARROW) {
+        const int c = threadIdx.x % NARROW, which = threadIdx.x / NARROW;
+        if (c < C) partial[(size_t)blockIdx.x * 2 * C + which * C + c] = (red[0][threadIdx.x] + red[1][threadIdx.x]) + (red[2][threadIdx.x] + red[3][threadIdx.x]);
     }
 }
 
-// ---- channel planes: a lane per pixel, 64 pixels a workgroup (of any images), wave w of W takes channels w, w + W, ..., NC of them at most, in registers
-template <typename T, int NC, int W>
-__global__ __launch_bounds__(W * 64) void norm_planes_kernel(const Pixels px, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps, int relu,
-                                                             T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
+// ---- channel planes: a lane per pixel, 64 pixels of any images a workgroup; its W waves (16 at most) take channels w, w + W, ..., NC of them at most, in registers.
+// An element's address is a plane's, the same for the wave, and the lane's 32-bit distance from it: with 64-bit addresses of their own the loads wait for arithmetic
+// (192 channels of 28 x 28 x 32 pixels fp32: 11.6 us for ...).
+constexpr int PLANES_WAVES = 16;
+template <typename T>
+struct Planes {
+    size_t step, at;         // elements from channel to channel; of the first pixel's image
+    size_t pixel;
+    unsigned off;            // bytes from `at` to this lane's pixel in its channel 0
+    bool on;
+    __device__ __forceinline__ Planes(const Pixels& px, size_t group)
+    {
+        const size_t first = group * 64, img0 = first / px.HW;
+        const unsigned in0 = (unsigned)(first - img0 * px.HW);      // (wave-uniform)
+        pixel = first + (threadIdx.x & 63);
+        on = pixel < px.count;
+        const unsigned p = in0 + (on ? threadIdx.x & 63 : (unsigned)(px.count - 1 - first)), img = p / (unsigned)px.HW;
+        step = px.HW;
+        at = img0 * px.C * px.HW;
+        off = (img * (unsigned)px.C * px.HW + (p - img * px.HW)) * (unsigned)sizeof(T);
+        if (!on) pixel = px.count - 1;
+    }
+    __device__ __forceinline__ float ld(const T* base, int c) const { return Store<T>::ld(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base + at + c * step) + off)); }
+    __device__ __forceinline__ void st(T* base, int c, float v) const { Store<T>::st(reinterpret_cast<T*>(reinterpret_cast<char*>(base + at + c * step) + off), v); }
+};
+// the distances above fit 32 bits
+bool planes_near(const Pixels& px, int size) { return (double)(64 / px.HW + 2) * px.C * px.HW * size < 4294967296.0; }
+
+template <typename T, int NC>
+__global__ __launch_bounds__(PLANES_WAVES * 64) void norm_planes_kernel(const Pixels px, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
+                                                                        int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
 {
-    __shared__ float red[2][W][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = px.C;
+    __shared__ float red[2][PLANES_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, C = px.C;
     const float down = square_scale(C);
-    const size_t pixel = (size_t)blockIdx.x * 64 + lane;
-    const bool on = pixel < px.count;
-    const size_t at = px.base(on ? pixel : px.count - 1), step = px.step();
+    const Planes<T> p(px, blockIdx.x);
     float v[NC], s = 0.f;
 #pragma unroll
-    for (int j = 0; j < NC; ++j) {
-        const int c = wave + j * W;
-        v[j] = c < C ? Store<T>::ld(x + at + c * step) : 0.f;
-    }
+    for (int j = 0; j < NC; ++j) v[j] = p.ld(x, min(wave + j * W, C - 1));
 #pragma unroll
-    for (int j = 0; j < NC; ++j) s += v[j];
+    for (int j = 0; j < NC; ++j) s += wave + j * W < C ? v[j] : 0.f;
     auto sum = [&](float mine, int turn) __attribute__((always_inline)) {
         red[turn][wave][lane] = mine;
         __syncthreads();
         float t = 0.f;
-#pragma unroll
         for (int w = 0; w < W; ++w) t += red[turn][w][lane];
         return t;
     };
@@ -561,114 +557,115 @@ __global__ __launch_bounds__(W * 64) void norm_planes_kernel(const Pixels px, co
             s = __builtin_fmaf(v[j] * down, v[j], s);
         }
     const float rstd = 1.f / sqrtf(sum(s, 1) / ((float)C * down) + eps);
-    if (!on) return;
+    if (!p.on) return;
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
         const int c = wave + j * W;
         if (c < C) {
             const float t = v[j] * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f);
-            Store<T>::st(y + at + c * step, relu ? fmaxf(t, 0.f) : t);
+            p.st(y, c, relu ? fmaxf(t, 0.f) : t);
         }
     }
     if (wave == 0) {
-        if (mean_out) mean_out[pixel] = mean;
-        if (rstd_out) rstd_out[pixel] = rstd;
+        if (mean_out) mean_out[p.pixel] = mean;
+        if (rstd_out) rstd_out[p.pixel] = rstd;
     }
 }
 
-// Sums over the 64 lanes of N values each, N a power of two from 4 to 32: every lane gets the sum of value lane * N / 64.  A step hands half of a lane's values to the
-// lane it meets and takes the others' in return: about two instructions a value in all, in the place of twelve.
-template <int N, int M, int D, int CTRL>
+// Sums over the 64 lanes of N <= 64 values each, N a power of two: every lane gets the sum of value lane N / 64.  A step hands half of a lane's values to the lane it
+// meets and takes the others' in return: about two instructions a value in all, in the place of twelve.
+template <int N, int M, int D>
 __device__ __forceinline__ void transpose_step(float (&v)[N])      // M values left; lanes meet across bit D
 {
-    auto met = [](float f) __attribute__((always_inline)) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, f), CTRL, 0xF, 0xF, true)); };
-    if constexpr (M > 1) {
-        const bool high = (threadIdx.x & D) != 0;
+    if constexpr (D >= 16) {
+        auto sum = [](float a, float b) __attribute__((always_inline)) {      // lanes without bit D: a of both lanes; with it: b
+            if constexpr (D == 32) {
+                const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+                return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+            } else {
+                const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(a), __float_as_uint(b), false, false);
+                return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+            }
+        };
+        if constexpr (M > 1) {
 #pragma unroll
-        for (int i = 0; i < M / 2; ++i) {
-            const float keep = high ? v[i + M / 2] : v[i], give = high ? v[i] : v[i + M / 2];
-            v[i] = keep + met(give);
-        }
-    } else v[0] += met(v[0]);
+            for (int i = 0; i < M / 2; ++i) v[i] = sum(v[i], v[i + M / 2]);
+        } else v[0] = sum(v[0], v[0]);
+    } else {
+        // lane +- 8 of sixteen; 7 - lane of eight (a lane's later partners have met the others of the eight); lane ^ 2; lane ^ 1
+        constexpr int CTRL = D == 8 ? 0x128 : D == 4 ? 0x141 : D == 2 ? 0x4E : 0xB1;
+        if constexpr (M > 1) {
+            const bool high = (threadIdx.x & D) != 0;
+#pragma unroll
+            for (int i = 0; i < M / 2; ++i) {
+                const float keep = high ? v[i + M / 2] : v[i], give = high ? v[i] : v[i + M / 2];
+                v[i] = keep + dpp<CTRL>(give);
+            }
+        } else v[0] += dpp<CTRL>(v[0]);
+    }
+    if constexpr (D > 1) transpose_step<N, (M > 1 ? M / 2 : 1), D / 2>(v);
 }
 template <int N>
 __device__ __forceinline__ float transpose_sum(float (&v)[N])
 {
-    static_assert(N >= 4 && N <= 32, "values of a lane");
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        const auto t = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 2]), false, false);
-        v[i] = __uint_as_float(t[0]) + __uint_as_float(t[1]);
-    }
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-        const auto t = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + N / 4]), false, false);
-        v[i] = __uint_as_float(t[0]) + __uint_as_float(t[1]);
-    }
-    constexpr int A = N / 4, B = A > 1 ? A / 2 : 1, C = B > 1 ? B / 2 : 1, D = C > 1 ? C / 2 : 1;
-    transpose_step<N, A, 8, 0x128>(v);      // lane +- 8 of sixteen
-    transpose_step<N, B, 4, 0x141>(v);      // 7 - lane of eight (a lane's later partners have met the others of the eight)
-    transpose_step<N, C, 2, 0x4E>(v);
-    transpose_step<N, D, 1, 0xB1>(v);
+    static_assert(N <= 64, "a value for a lane at most");
+    transpose_step<N, N, 32>(v);
     return v[0];
 }
 
 // The gradient on planes: a workgroup walks groups of 64 pixels; the sums over a group's pixels by transpose_sum, so that a lane holds the running sums of one channel
-template <typename T, int NC, int W>
-__global__ __launch_bounds__(W * 64) void norm_grad_planes_kernel(const Pixels px, const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
-                                                                  const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
+template <typename T, int NC>
+__global__ __launch_bounds__(PLANES_WAVES * 64) void norm_grad_planes_kernel(const Pixels px, const T* dy, const T* x, const float* __restrict__ gamma,
+                                                                             const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
 {
-    __shared__ float red[2][2][W][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = px.C;
-    const size_t step = px.step(), groups = (px.count + 63) / 64;
+    __shared__ float red[2][2][PLANES_WAVES][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, C = px.C;
+    const size_t groups = (px.count + 63) / 64;
     float dg = 0.f, db = 0.f;
     int turn = 0;
     for (size_t k = blockIdx.x; k < groups; k += gridDim.x, turn ^= 1) {
-        const size_t pixel = k * 64 + lane;
-        const bool on = pixel < px.count;
-        const size_t q = on ? pixel : px.count - 1, at = px.base(q);
-        const float mu = mean[q], r = rstd[q];
+        const Planes<T> p(px, k);
         float z[NC], d[NC], s = 0.f, t = 0.f;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const int c = wave + j * W;
-            d[j] = c < C ? Store<T>::ld(dy + at + c * step) : 0.f;
-            z[j] = c < C ? Store<T>::ld(x + at + c * step) : 0.f;
+            d[j] = p.ld(dy, min(wave + j * W, C - 1));
+            z[j] = p.ld(x, min(wave + j * W, C - 1));
         }
+        const float mu = mean[p.pixel], r = rstd[p.pixel];
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
             const int c = wave + j * W;
-            z[j] = c < C ? (z[j] - mu) * r : 0.f;
-            const float u = d[j] * (gamma && c < C ? gamma[c] : 1.f);
-            s += u;
-            t += u * z[j];
+            const float g = gamma ? gamma[min(c, C - 1)] : 1.f;
+            d[j] = c < C ? d[j] : 0.f;
+            z[j] = (z[j] - mu) * r;
+            s += d[j] * g;
+            t += d[j] * g * z[j];
         }
         red[turn][0][wave][lane] = s;
         red[turn][1][wave][lane] = t;
         __syncthreads();
         s = t = 0.f;
-#pragma unroll
         for (int w = 0; w < W; ++w) {
             s += red[turn][0][w][lane];
             t += red[turn][1][w][lane];
         }
         s /= (float)C;
         t /= (float)C;
-        if (dx && on) {
+        if (dx && p.on) {
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
                 const int c = wave + j * W;
-                if (c < C) Store<T>::st(dx + at + c * step, r * (d[j] * (gamma ? gamma[c] : 1.f) - s - z[j] * t));
+                if (c < C) p.st(dx, c, r * (d[j] * (gamma ? gamma[c] : 1.f) - s - z[j] * t));
             }
         }
         if (partial) {
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                d[j] = on ? d[j] : 0.f;
-                z[j] = on ? d[j] * z[j] : 0.f;
+                d[j] = p.on ? d[j] : 0.f;
+                z[j] = p.on && wave + j * W < C ? d[j] * z[j] : 0.f;
             }
-            dg += transpose_sum<NC>(z);
-            db += transpose_sum<NC>(d);
+            dg += transpose_sum(z);
+            db += transpose_sum(d);
         }
     }
     const int c = wave + lane * NC / 64 * W;
@@ -787,7 +784,7 @@ __global__ __launch_bounds__(LONG_W * 64) void norm_grad_long_planes_kernel(cons
                 z[j] = on ? d[j] * z[j] : 0.f;
             }
             if (partial) {
-                const float dg = transpose_sum<CHUNK>(z), db = transpose_sum<CHUNK>(d);
+                const float dg = transpose_sum(z), db = transpose_sum(d);
                 const int c = c0 + lane * CHUNK / 64 * LONG_W;
                 if (lane % (64 / CHUNK) == 0 && c < C) {
                     columns[c] += dg;
@@ -815,7 +812,13 @@ Pixels pixels_of(const dr_tensor& d)
 int norm_ranges(const dr_tensor& d)
 {
     const size_t pixels = (size_t)d.n * d.h * d.w;
-    return (int)std::min<size_t>(d.c > 1024 ? 256 : 512, std::max<size_t>(1, pixels / 4));
+    return (int)std::min<size_t>(d.c <= 256 ? 1024 : d.c <= 1024 ? 512 : 256, std::max<size_t>(1, pixels / 4));
+}
+// workgroups for `groups` groups of pixels, `most` at most: every one has the same number of them, or one less
+int even_blocks(size_t groups, int most)
+{
+    const size_t each = (groups + most - 1) / most;
+    return (int)((groups + each - 1) / each);
 }
 
 // f(G, NV) for rows of nvec vectors: the fewest lanes that hold a row in at most `most` vectors each; more of them while the rows are too few to give every compute unit
@@ -839,71 +842,45 @@ void with_lanes(int nvec, int most, size_t rows, F f)
     else with_nv(IC<64>{});
 }
 
-// f(NC, W): channels of a wave, waves
+// f(NC): channels of a lane; as many waves as that takes
 template <class F>
 void with_planes(int C, F f)
 {
-    if (C <= 16) f(IC<4>{}, IC<4>{});
-    else if (C <= 64) f(IC<8>{}, IC<8>{});
-    else if (C <= 128) f(IC<16>{}, IC<8>{});
-    else if (C <= 256) f(IC<32>{}, IC<8>{});
-    else f(IC<32>{}, IC<16>{});
+    if (C <= 128) f(IC<8>{});
+    else if (C <= 256) f(IC<16>{});
+    else f(IC<32>{});
 }
 constexpr int PLANES_MOST = 512, COLUMNS_MOST = 8192;      // channels: in registers; sums in LDS (64 KB)
-
-template <class F>
-void with_run_lanes(int C, F f)
-{
-    if (C <= 64) f(IC<8>{});
-    else if (C <= 160) f(IC<16>{});
-    else f(IC<64>{});
-}
-
-// rows of a run: as many as fit, but a run for every other compute unit at least; in eights, so that only the first and the last run of a tensor have pieces of their own
-int rows_of_run(size_t rows, int C, int size)
-{
-    int r = (int)std::min<size_t>(std::min(512, RUN_BYTES / (C * size)), std::max<size_t>(1, rows / (2 * device_cus())));
-    if (r >= 8) r &= ~7;
-    return r;
-}
 
 template <typename T>
 int norm_fwd(const dr_tensor& d, const T* x, const float* gamma, const float* beta, float eps, int relu, T* y, float* mean, float* rstd, hipStream_t st)
 {
     constexpr int VN = Store<T>::VN;
     const Pixels px = pixels_of(d);
-    const int C = d.c, nvec = C / VN;
-    const bool vectors = C % VN == 0 && aligned16(x) && aligned16(y);
+    const int C = d.c, nvec = (C + VN - 1) / VN;
     TraceScope trace("layernorm", nullptr, (long long)tensor_elems(d), st, 2ll * tensor_bytes(d));
     auto rows = [&](auto g, auto nv, auto threads) {
         constexpr int G = decltype(g)::value, NV = decltype(nv)::value, TH = decltype(threads)::value;
         const unsigned grid = blocks_for(px.count, TH / G, (size_t)device_cus() * (2048 / TH));
-        hipLaunchKernelGGL((norm_rows_kernel<T, G, NV, TH>), dim3(grid), dim3(TH), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
+        if (C % VN == 0) hipLaunchKernelGGL((norm_rows_kernel<T, G, NV, TH, false>), dim3(grid), dim3(TH), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
+        else hipLaunchKernelGGL((norm_rows_kernel<T, G, NV, TH, true>), dim3(grid), dim3(TH), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
     };
     if (px.planes) {
         const unsigned grid = (unsigned)((px.count + 63) / 64);
-        if (C <= PLANES_MOST)
-            with_planes(C, [&](auto nc, auto w) {
-                constexpr int NC = decltype(nc)::value, W = decltype(w)::value;
-                hipLaunchKernelGGL((norm_planes_kernel<T, NC, W>), dim3(grid), dim3(W * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
+        if (C <= PLANES_MOST && planes_near(px, sizeof(T)))
+            with_planes(C, [&](auto nc) {
+                constexpr int NC = decltype(nc)::value;
+                hipLaunchKernelGGL((norm_planes_kernel<T, NC>), dim3(grid), dim3((C + NC - 1) / NC * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
             });
         else hipLaunchKernelGGL((norm_long_planes_kernel<T>), dim3(grid), dim3(LONG_W * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
-    } else if (vectors && nvec <= 4 * 64) {
-        with_lanes(nvec, 4, px.count, [&](auto g, auto nv) { rows(g, nv, IC<256>{}); });
-    } else if (vectors && nvec <= 4 * 256) {
-        if (nvec <= 2 * 256) rows(IC<256>{}, IC<2>{}, IC<256>{});
-        else rows(IC<256>{}, IC<4>{}, IC<256>{});
-    } else if (vectors && nvec <= 4 * 1024) {
-        if (nvec <= 2 * 1024) rows(IC<1024>{}, IC<2>{}, IC<1024>{});
-        else rows(IC<1024>{}, IC<4>{}, IC<1024>{});
-    } else if (C * (int)sizeof(T) <= RUN_BYTES && C <= RUN_BYTES) {
-        const int run = rows_of_run(px.count, C, sizeof(T));
-        with_run_lanes(C, [&](auto g) {
-            constexpr int G = decltype(g)::value;
-            hipLaunchKernelGGL((norm_runs_kernel<T, G>), dim3(blocks_for(px.count, run, (size_t)device_cus() * 4)), dim3(256), 0, st, px.count, C, run, x, gamma, beta, eps, relu, y,
-                               mean, rstd);
-        });
-    } else
+    } else if (C < VN)
+        hipLaunchKernelGGL((norm_narrow_kernel<T>), dim3(blocks_for(px.count, 256, 4096)), dim3(256), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
+    else if (nvec <= 4 * 64) with_lanes(nvec, 4, px.count, [&](auto g, auto nv) { rows(g, nv, IC<256>{}); });
+    else if (nvec <= 2 * 256) rows(IC<256>{}, IC<2>{}, IC<256>{});
+    else if (nvec <= 4 * 256) rows(IC<256>{}, IC<4>{}, IC<256>{});
+    else if (nvec <= 2 * 1024) rows(IC<1024>{}, IC<2>{}, IC<1024>{});
+    else if (nvec <= 4 * 1024) rows(IC<1024>{}, IC<4>{}, IC<1024>{});
+    else
         hipLaunchKernelGGL((norm_any_kernel<T>), dim3(blocks_for(px.count, 1, 16384)), dim3(256), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
     return check_launch("layernorm_fwd");
 }
@@ -914,53 +891,40 @@ int norm_bwd(const dr_tensor& d, const T* dy, const T* x, const float* gamma, co
 {
     constexpr int VN = Store<T>::VN;
     const Pixels px = pixels_of(d);
-    const int C = d.c, nvec = C / VN, most = norm_ranges(d);
+    const int C = d.c, nvec = (C + VN - 1) / VN, most = norm_ranges(d);
     float* const partial = dgamma || dbeta ? ws : nullptr;
-    const bool vectors = C % VN == 0 && aligned16(x) && aligned16(dy) && (!dx || aligned16(dx));
     TraceScope trace("layernorm_bwd", nullptr, (long long)tensor_elems(d), st, 3ll * tensor_bytes(d));
     int ranges = 0;                                      // partial sums made; 0: by no kernel yet
     if (px.count) {
         auto rows = [&](auto g, auto nv, auto threads) {
             constexpr int G = decltype(g)::value, NV = decltype(nv)::value, TH = decltype(threads)::value;
             ranges = (int)blocks_for(px.count, TH / G, std::min(most, device_cus() * (TH > 256 ? 1 : 2)));
-            hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH>), dim3(ranges), dim3(TH), 2 * C * sizeof(float), st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
+            if (C % VN == 0) hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH, false>), dim3(ranges), dim3(TH), 2 * C * sizeof(float), st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
+            else hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH, true>), dim3(ranges), dim3(TH), 2 * C * sizeof(float), st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
         };
-        if (px.planes && C <= COLUMNS_MOST) {
-            ranges = (int)blocks_for(px.count, 64, most);
-            if (C <= PLANES_MOST)
-                with_planes(C, [&](auto nc, auto w) {
-                    constexpr int NC = decltype(nc)::value, W = decltype(w)::value;
-                    hipLaunchKernelGGL((norm_grad_planes_kernel<T, NC, W>), dim3(ranges), dim3(W * 64), 0, st, px, dy, x, gamma, mean, rstd, dx, partial);
+        if (px.planes) {
+            if (C <= COLUMNS_MOST) ranges = even_blocks((px.count + 63) / 64, most);
+            if (C <= PLANES_MOST && planes_near(px, sizeof(T)))
+                with_planes(C, [&](auto nc) {
+                    constexpr int NC = decltype(nc)::value;
+                    hipLaunchKernelGGL((norm_grad_planes_kernel<T, NC>), dim3(ranges), dim3((C + NC - 1) / NC * 64), 0, st, px, dy, x, gamma, mean, rstd, dx, partial);
                 });
-            else hipLaunchKernelGGL((norm_grad_long_planes_kernel<T>), dim3(ranges), dim3(LONG_W * 64), 2 * C * sizeof(float), st, px, dy, x, gamma, mean, rstd, dx, partial);
-        } else if (!px.planes && vectors && nvec <= 2 * 64) {
-            with_lanes(nvec, VN == 4 ? 4 : 3, px.count, [&](auto g, auto nv) { rows(g, nv, IC<256>{}); });
-        } else if (!px.planes && vectors && nvec <= 2 * 256) {
-            rows(IC<256>{}, IC<2>{}, IC<512>{});
-        } else if (!px.planes && vectors && nvec <= 2 * 1024 && C <= COLUMNS_MOST) {
-            rows(IC<1024>{}, IC<2>{}, IC<1024>{});
-        } else if (!px.planes && C <= 256 * RUN_COLUMNS && C * (int)sizeof(T) <= RUN_BYTES) {
-            const int run = rows_of_run(px.count, C, sizeof(T));
-            ranges = (int)blocks_for(px.count, run, most);
-            with_run_lanes(C, [&](auto g) {
-                constexpr int G = decltype(g)::value;
-                auto launch = [&](auto nc) {
-                    hipLaunchKernelGGL((norm_grad_runs_kernel<T, G, decltype(nc)::value>), dim3(ranges), dim3(256), 0, st, px.count, C, run, dy, x, gamma, mean, rstd, dx, partial);
-                };
-                if constexpr (G < 64) launch(IC<1>{});
-                else if (C <= 256) launch(IC<1>{});
-                else if (C <= 512) launch(IC<2>{});
-                else if (C <= 1024) launch(IC<4>{});
-                else launch(IC<RUN_COLUMNS>{});
-            });
-        }
+            else if (C <= COLUMNS_MOST) {
+                hipLaunchKernelGGL((norm_grad_long_planes_kernel<T>), dim3(ranges), dim3(LONG_W * 64), 2 * C * sizeof(float), st, px, dy, x, gamma, mean, rstd, dx, partial);
+            }
+        } else if (C < VN) {
+            ranges = (int)blocks_for(px.count, 256, most);
+            hipLaunchKernelGGL((norm_grad_narrow_kernel<T>), dim3(ranges), dim3(256), 0, st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
+        } else if (nvec <= 2 * 64) with_lanes(nvec, VN == 4 ? 4 : 3, px.count, [&](auto g, auto nv) { rows(g, nv, IC<256>{}); });
+        else if (nvec <= 2 * 256) rows(IC<256>{}, IC<2>{}, IC<512>{});
+        else if (nvec <= 2 * 1024 && C <= COLUMNS_MOST) rows(IC<1024>{}, IC<2>{}, IC<1024>{});
     }
     if (ranges == 0) {
         ranges = most;
         if (partial) hipLaunchKernelGGL((norm_vectors_any_kernel<T>), dim3((C + 63) / 64, ranges), dim3(256), 0, st, px, dy, x, mean, rstd, ws);
         if (dx && px.count) hipLaunchKernelGGL((norm_grad_any_kernel<T>), dim3(blocks_for(px.count, 1, 16384)), dim3(256), 0, st, px, dy, x, gamma, mean, rstd, dx);
     }
-    if (partial) hipLaunchKernelGGL(norm_vectors_sum_kernel, dim3((2 * C + 15) / 16), dim3(256), 0, st, ws, ranges, C, dgamma, dbeta);
+    if (partial) hipLaunchKernelGGL(norm_vectors_sum_kernel, dim3((2 * C + 15) / 16), dim3(1024), 0, st, ws, ranges, C, dgamma, dbeta);
     return check_launch("layernorm_bwd");
 }
 
