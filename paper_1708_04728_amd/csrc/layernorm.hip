@@ -500,80 +500,104 @@ __global__ __launch_bounds__(256) void norm_grad_narrow_kernel(size_t rows, int 
     }
 }
 
-// ---- channel planes: a lane per pixel, 64 pixels of any images a workgroup; its W waves (16 at most) take channels w, w + W, ..., NC of them at most, in registers.
-// An element's address is a plane's, the same for the wave, and the lane's 32-bit distance from it: with 64-bit addresses of their own the loads wait for arithmetic
-// (192 channels of 28 x 28 x 32 pixels fp32: 11.6 us for ...).
+// ---- channel planes: LP pixels of any images a workgroup, a lane for each in 64 / LP channels at a time; its waves (16 at most) share the channels, NC of them at most in a
+// lane's registers.  An element's address is a plane's, the same for the wave, and the lane's 32-bit distance from it: with 64-bit addresses of their own the loads wait for
+// arithmetic (the gradient of 192 channels on 28 x 28 x 32 pixels fp32 22.8 us for 17.2).
 constexpr int PLANES_WAVES = 16;
-template <typename T>
+template <typename T, int LP>
 struct Planes {
+    static constexpr int SUB = 64 / LP;
     size_t step, at;         // elements from channel to channel; of the first pixel's image
     size_t pixel;
-    unsigned off;            // bytes from `at` to this lane's pixel in its channel 0
+    unsigned off0, off;      // bytes from `at` to this lane's pixel in channel 0, and in its own of the SUB channels
+    int sub, C;
     bool on;
     __device__ __forceinline__ Planes(const Pixels& px, size_t group)
     {
-        const size_t first = group * 64, img0 = first / px.HW;
-        const unsigned in0 = (unsigned)(first - img0 * px.HW);      // (wave-uniform)
-        pixel = first + (threadIdx.x & 63);
+        const size_t first = group * LP, img0 = first / px.HW;
+        const unsigned in0 = (unsigned)(first - img0 * px.HW), lane = threadIdx.x % LP;      // (in0: wave-uniform)
+        pixel = first + lane;
         on = pixel < px.count;
-        const unsigned p = in0 + (on ? threadIdx.x & 63 : (unsigned)(px.count - 1 - first)), img = p / (unsigned)px.HW;
+        if (!on) pixel = px.count - 1;
+        const unsigned p = in0 + (unsigned)(pixel - first), img = p / (unsigned)px.HW;
         step = px.HW;
         at = img0 * px.C * px.HW;
-        off = (img * (unsigned)px.C * px.HW + (p - img * px.HW)) * (unsigned)sizeof(T);
-        if (!on) pixel = px.count - 1;
+        C = px.C;
+        sub = (threadIdx.x & 63) / LP;
+        off0 = (img * (unsigned)px.C * px.HW + (p - img * px.HW)) * (unsigned)sizeof(T);
+        off = off0 + sub * (unsigned)px.HW * (unsigned)sizeof(T);
     }
-    __device__ __forceinline__ float ld(const T* base, int c) const { return Store<T>::ld(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base + at + c * step) + off)); }
-    __device__ __forceinline__ void st(T* base, int c, float v) const { Store<T>::st(reinterpret_cast<T*>(reinterpret_cast<char*>(base + at + c * step) + off), v); }
+    // channel c0 + sub, c0 the same for the wave.  Of a channel that does not exist: another's value.
+    __device__ __forceinline__ float ld(const T* base, int c0) const
+    {
+        c0 = min(c0, C - 1);
+        const unsigned o = SUB == 1 || c0 + sub < C ? off : off0;
+        return Store<T>::ld(reinterpret_cast<const T*>(reinterpret_cast<const char*>(base + at + c0 * step) + o));
+    }
+    __device__ __forceinline__ void st(T* base, int c0, float v) const
+    {
+        if (on && c0 + sub < C) Store<T>::st(reinterpret_cast<T*>(reinterpret_cast<char*>(base + at + c0 * step) + off), v);
+    }
 };
 // the distances above fit 32 bits
-bool planes_near(const Pixels& px, int size) { return (double)(64 / px.HW + 2) * px.C * px.HW * size < 4294967296.0; }
+bool planes_near(const Pixels& px, int size) { return (double)(64 / px.HW + 2) * px.C * px.HW * size + 4.0 * px.HW * size < 4294967296.0; }
 
-template <typename T, int NC>
+// sums over a pixel's channels: its lanes' in all waves of the workgroup
+template <int LP, int N>
+__device__ __forceinline__ void pixel_sums(float (&v)[N], float (*red)[PLANES_WAVES][64])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, W = blockDim.x >> 6;
+#pragma unroll
+    for (int n = 0; n < N; ++n) red[n][wave][lane] = v[n];
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        float t = 0.f;
+        for (int w = 0; w < W; ++w)
+#pragma unroll
+            for (int u = 0; u < 64 / LP; ++u) t += red[n][w][u * LP + lane % LP];
+        v[n] = t;
+    }
+}
+
+template <typename T, int LP, int NC>
 __global__ __launch_bounds__(PLANES_WAVES * 64) void norm_planes_kernel(const Pixels px, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
                                                                         int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
 {
+    constexpr int SUB = 64 / LP;
     __shared__ float red[2][PLANES_WAVES][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, C = px.C;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), step = (blockDim.x >> 6) * SUB, C = px.C;
     const float down = square_scale(C);
-    const Planes<T> p(px, blockIdx.x);
-    float v[NC], s = 0.f;
+    const Planes<T, LP> p(px, blockIdx.x);
+    float v[NC], s[1] = {0.f};
 #pragma unroll
-    for (int j = 0; j < NC; ++j) v[j] = p.ld(x, min(wave + j * W, C - 1));
+    for (int j = 0; j < NC; ++j) v[j] = p.ld(x, wave * SUB + j * step);
 #pragma unroll
-    for (int j = 0; j < NC; ++j) s += wave + j * W < C ? v[j] : 0.f;
-    auto sum = [&](float mine, int turn) __attribute__((always_inline)) {
-        red[turn][wave][lane] = mine;
-        __syncthreads();
-        float t = 0.f;
-        for (int w = 0; w < W; ++w) t += red[turn][w][lane];
-        return t;
-    };
-    const float mean = sum(s, 0) / (float)C;
-    s = 0.f;
-#pragma unroll
-    for (int j = 0; j < NC; ++j)
-        if (wave + j * W < C) {
-            v[j] -= mean;
-            s = __builtin_fmaf(v[j] * down, v[j], s);
-        }
-    const float rstd = 1.f / sqrtf(sum(s, 1) / ((float)C * down) + eps);
-    if (!p.on) return;
+    for (int j = 0; j < NC; ++j) s[0] += wave * SUB + p.sub + j * step < C ? v[j] : 0.f;
+    pixel_sums<LP>(s, red);
+    const float mean = s[0] / (float)C;
+    s[0] = 0.f;
 #pragma unroll
     for (int j = 0; j < NC; ++j) {
-        const int c = wave + j * W;
-        if (c < C) {
-            const float t = v[j] * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f);
-            p.st(y, c, relu ? fmaxf(t, 0.f) : t);
-        }
+        v[j] -= mean;
+        s[0] = __builtin_fmaf(wave * SUB + p.sub + j * step < C ? v[j] * down : 0.f, v[j], s[0]);
     }
-    if (wave == 0) {
+    pixel_sums<LP>(s, red + 1);
+    const float rstd = 1.f / sqrtf(s[0] / ((float)C * down) + eps);
+#pragma unroll
+    for (int j = 0; j < NC; ++j) {
+        const int c0 = wave * SUB + j * step, c = min(c0 + p.sub, C - 1);
+        const float t = v[j] * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f);
+        p.st(y, c0, relu ? fmaxf(t, 0.f) : t);
+    }
+    if (threadIdx.x < LP && p.on) {
         if (mean_out) mean_out[p.pixel] = mean;
         if (rstd_out) rstd_out[p.pixel] = rstd;
     }
 }
 
-// Sums over the 64 lanes of N <= 64 values each, N a power of two: every lane gets the sum of value lane N / 64.  A step hands half of a lane's values to the lane it
-// meets and takes the others' in return: about two instructions a value in all, in the place of twelve.
+// Sums over groups of LP lanes of N <= LP values each, both powers of two: every lane gets the sum of value (lane % LP) N / LP.  A step hands half of a lane's values to the
+// lane it meets and takes the others' in return: about two instructions a value in all, in the place of twelve.
 template <int N, int M, int D>
 __device__ __forceinline__ void transpose_step(float (&v)[N])      // M values left; lanes meet across bit D
 {
@@ -605,188 +629,167 @@ __device__ __forceinline__ void transpose_step(float (&v)[N])      // M values l
     }
     if constexpr (D > 1) transpose_step<N, (M > 1 ? M / 2 : 1), D / 2>(v);
 }
-template <int N>
+template <int LP, int N>
 __device__ __forceinline__ float transpose_sum(float (&v)[N])
 {
-    static_assert(N <= 64, "a value for a lane at most");
-    transpose_step<N, N, 32>(v);
+    static_assert(N <= LP, "a value for a lane at most");
+    transpose_step<N, N, LP / 2>(v);
     return v[0];
 }
-
-// The gradient on planes: a workgroup walks groups of 64 pixels; the sums over a group's pixels by transpose_sum, so that a lane holds the running sums of one channel
-template <typename T, int NC>
+// The gradient on planes: a workgroup walks groups of LP pixels; the sums over a group's pixels by transpose_sum, so that a lane holds the running sums of a channel
+template <typename T, int LP, int NC>
 __global__ __launch_bounds__(PLANES_WAVES * 64) void norm_grad_planes_kernel(const Pixels px, const T* dy, const T* x, const float* __restrict__ gamma,
                                                                              const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
 {
+    constexpr int SUB = 64 / LP;
     __shared__ float red[2][2][PLANES_WAVES][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = blockDim.x >> 6, C = px.C;
-    const size_t groups = (px.count + 63) / 64;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), step = (blockDim.x >> 6) * SUB, C = px.C;
+    const size_t groups = (px.count + LP - 1) / LP;
     float dg = 0.f, db = 0.f;
     int turn = 0;
     for (size_t k = blockIdx.x; k < groups; k += gridDim.x, turn ^= 1) {
-        const Planes<T> p(px, k);
-        float z[NC], d[NC], s = 0.f, t = 0.f;
+        const Planes<T, LP> p(px, k);
+        float z[NC], d[NC], s[2] = {0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            d[j] = p.ld(dy, min(wave + j * W, C - 1));
-            z[j] = p.ld(x, min(wave + j * W, C - 1));
+            d[j] = p.ld(dy, wave * SUB + j * step);
+            z[j] = p.ld(x, wave * SUB + j * step);
         }
         const float mu = mean[p.pixel], r = rstd[p.pixel];
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-            const int c = wave + j * W;
-            const float g = gamma ? gamma[min(c, C - 1)] : 1.f;
+            const int c = wave * SUB + p.sub + j * step;
             d[j] = c < C ? d[j] : 0.f;
-            z[j] = (z[j] - mu) * r;
-            s += d[j] * g;
-            t += d[j] * g * z[j];
+            z[j] = c < C ? (z[j] - mu) * r : 0.f;
+            const float u = d[j] * (gamma ? gamma[min(c, C - 1)] : 1.f);
+            s[0] += u;
+            s[1] += u * z[j];
         }
-        red[turn][0][wave][lane] = s;
-        red[turn][1][wave][lane] = t;
-        __syncthreads();
-        s = t = 0.f;
-        for (int w = 0; w < W; ++w) {
-            s += red[turn][0][w][lane];
-            t += red[turn][1][w][lane];
-        }
-        s /= (float)C;
-        t /= (float)C;
-        if (dx && p.on) {
+        pixel_sums<LP>(s, red[turn]);
+        s[0] /= (float)C;
+        s[1] /= (float)C;
+        if (dx) {
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-                const int c = wave + j * W;
-                if (c < C) p.st(dx, c, r * (d[j] * (gamma ? gamma[c] : 1.f) - s - z[j] * t));
+                const int c0 = wave * SUB + j * step;
+                p.st(dx, c0, r * (d[j] * (gamma ? gamma[min(c0 + p.sub, C - 1)] : 1.f) - s[0] - z[j] * s[1]));
             }
         }
         if (partial) {
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
                 d[j] = p.on ? d[j] : 0.f;
-                z[j] = p.on && wave + j * W < C ? d[j] * z[j] : 0.f;
+                z[j] = p.on ? d[j] * z[j] : 0.f;
             }
-            dg += transpose_sum(z);
-            db += transpose_sum(d);
+            dg += transpose_sum<LP>(z);
+            db += transpose_sum<LP>(d);
         }
     }
-    const int c = wave + lane * NC / 64 * W;
-    if (partial && lane % (64 / NC) == 0 && c < C) {
+    const int lane = threadIdx.x % LP, c = wave * SUB + (int)(threadIdx.x & 63) / LP + lane * NC / LP * step;
+    if (partial && lane % (LP / NC) == 0 && c < C) {
         partial[(size_t)blockIdx.x * 2 * C + c] = dg;
         partial[(size_t)blockIdx.x * 2 * C + C + c] = db;
     }
 }
 
-// ... of more channels than registers hold: read again for each use (from the caches), CHUNK channels a wave at a time
-constexpr int LONG_W = 16, CHUNK = 16;
-template <typename T>
-__global__ __launch_bounds__(LONG_W * 64) void norm_long_planes_kernel(const Pixels px, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
-                                                                       int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
+// ... of more channels than registers hold: read again for each use (from the caches), CHUNK channels of a lane at a time, by 16 waves
+constexpr int CHUNK = 16;
+template <typename T, int LP>
+__global__ __launch_bounds__(PLANES_WAVES * 64) void norm_long_planes_kernel(const Pixels px, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta,
+                                                                             float eps, int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
 {
-    __shared__ float red[2][LONG_W][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = px.C;
+    constexpr int SUB = 64 / LP, LONG_STEP = PLANES_WAVES * SUB;
+    __shared__ float red[2][PLANES_WAVES][64];
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = px.C;
     const float down = square_scale(C);
-    const size_t pixel = (size_t)blockIdx.x * 64 + lane;
-    const bool on = pixel < px.count;
-    const size_t at = px.base(on ? pixel : px.count - 1), step = px.step();
-    auto sum = [&](float mine, int turn) __attribute__((always_inline)) {
-        red[turn][wave][lane] = mine;
-        __syncthreads();
-        float t = 0.f;
-#pragma unroll
-        for (int w = 0; w < LONG_W; ++w) t += red[turn][w][lane];
-        return t;
-    };
-    auto each = [&](auto f) __attribute__((always_inline)) {
-        for (int c0 = wave; c0 < C; c0 += LONG_W * CHUNK) {
+    const Planes<T, LP> p(px, blockIdx.x);
+    auto chunks = [&](auto f) __attribute__((always_inline)) {
+        for (int c0 = wave * SUB; c0 < C; c0 += LONG_STEP * CHUNK) {
             float v[CHUNK];
 #pragma unroll
-            for (int j = 0; j < CHUNK; ++j) v[j] = c0 + j * LONG_W < C ? Store<T>::ld(x + at + (c0 + j * LONG_W) * step) : 0.f;
+            for (int j = 0; j < CHUNK; ++j) v[j] = p.ld(x, c0 + j * LONG_STEP);
 #pragma unroll
-            for (int j = 0; j < CHUNK; ++j)
-                if (c0 + j * LONG_W < C) f(c0 + j * LONG_W, v[j]);
+            for (int j = 0; j < CHUNK; ++j) f(c0 + j * LONG_STEP, v[j]);
         }
     };
-    float s = 0.f;
-    each([&](int, float v) { s += v; });
-    const float mean = sum(s, 0) / (float)C;
-    s = 0.f;
-    each([&](int, float v) {
+    float s[1] = {0.f};
+    chunks([&](int c0, float v) { s[0] += c0 + p.sub < C ? v : 0.f; });
+    pixel_sums<LP>(s, red);
+    const float mean = s[0] / (float)C;
+    s[0] = 0.f;
+    chunks([&](int c0, float v) {
         const float d = v - mean;
-        s = __builtin_fmaf(d * down, d, s);
+        s[0] = __builtin_fmaf(c0 + p.sub < C ? d * down : 0.f, d, s[0]);
     });
-    const float rstd = 1.f / sqrtf(sum(s, 1) / ((float)C * down) + eps);
-    each([&](int c, float v) {
+    pixel_sums<LP>(s, red + 1);
+    const float rstd = 1.f / sqrtf(s[0] / ((float)C * down) + eps);
+    chunks([&](int c0, float v) {
+        const int c = min(c0 + p.sub, C - 1);
         const float t = (v - mean) * rstd * (gamma ? gamma[c] : 1.f) + (beta ? beta[c] : 0.f);
-        if (on) Store<T>::st(y + at + c * step, relu ? fmaxf(t, 0.f) : t);
+        p.st(y, c0, relu ? fmaxf(t, 0.f) : t);
     });
-    if (on && wave == 0) {
-        if (mean_out) mean_out[pixel] = mean;
-        if (rstd_out) rstd_out[pixel] = rstd;
+    if (threadIdx.x < LP && p.on) {
+        if (mean_out) mean_out[p.pixel] = mean;
+        if (rstd_out) rstd_out[p.pixel] = rstd;
     }
 }
 
-template <typename T>
-__global__ __launch_bounds__(LONG_W * 64) void norm_grad_long_planes_kernel(const Pixels px, const T* dy, const T* x, const float* __restrict__ gamma,
-                                                                            const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
+template <typename T, int LP>
+__global__ __launch_bounds__(PLANES_WAVES * 64) void norm_grad_long_planes_kernel(const Pixels px, const T* dy, const T* x, const float* __restrict__ gamma,
+                                                                                  const float* __restrict__ mean, const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
 {
-    __shared__ float red[2][2][LONG_W][64];
+    constexpr int SUB = 64 / LP, LONG_STEP = PLANES_WAVES * SUB;
+    __shared__ float red[2][2][PLANES_WAVES][64];
     extern __shared__ float columns[];       // [2][C]: running sums, each touched by one lane
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = px.C;
-    const size_t step = px.step(), groups = (px.count + 63) / 64;
-    for (int i = threadIdx.x; i < 2 * C; i += LONG_W * 64) columns[i] = 0.f;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), C = px.C;
+    const size_t groups = (px.count + LP - 1) / LP;
+    for (int i = threadIdx.x; i < 2 * C; i += PLANES_WAVES * 64) columns[i] = 0.f;
     __syncthreads();
     int turn = 0;
     for (size_t k = blockIdx.x; k < groups; k += gridDim.x, turn ^= 1) {
-        const size_t pixel = k * 64 + lane;
-        const bool on = pixel < px.count;
-        const size_t q = on ? pixel : px.count - 1, at = px.base(q);
-        const float mu = mean[q], r = rstd[q];
-        auto each = [&](auto f) __attribute__((always_inline)) {
-            for (int c0 = wave; c0 < C; c0 += LONG_W * CHUNK) {
+        const Planes<T, LP> p(px, k);
+        const float mu = mean[p.pixel], r = rstd[p.pixel];
+        auto chunks = [&](auto f) __attribute__((always_inline)) {
+            for (int c0 = wave * SUB; c0 < C; c0 += LONG_STEP * CHUNK) {
                 float d[CHUNK], z[CHUNK];
 #pragma unroll
                 for (int j = 0; j < CHUNK; ++j) {
-                    const int c = c0 + j * LONG_W;
-                    d[j] = c < C ? Store<T>::ld(dy + at + c * step) : 0.f;
-                    z[j] = c < C ? Store<T>::ld(x + at + c * step) : mu;
+                    d[j] = p.ld(dy, c0 + j * LONG_STEP);
+                    z[j] = p.ld(x, c0 + j * LONG_STEP);
                 }
 #pragma unroll
-                for (int j = 0; j < CHUNK; ++j) z[j] = (z[j] - mu) * r;
+                for (int j = 0; j < CHUNK; ++j) {
+                    const bool in = c0 + p.sub + j * LONG_STEP < C;
+                    d[j] = in ? d[j] : 0.f;
+                    z[j] = in ? (z[j] - mu) * r : 0.f;
+                }
                 f(c0, d, z);
             }
         };
-        float s = 0.f, t = 0.f;
-        each([&](int c0, float (&d)[CHUNK], float (&z)[CHUNK]) {
+        float s[2] = {0.f, 0.f};
+        chunks([&](int c0, float (&d)[CHUNK], float (&z)[CHUNK]) {
 #pragma unroll
             for (int j = 0; j < CHUNK; ++j) {
-                const int c = c0 + j * LONG_W;
-                const float u = d[j] * (gamma && c < C ? gamma[c] : 1.f);
-                s += u;
-                t += u * z[j];
+                const float u = d[j] * (gamma ? gamma[min(c0 + p.sub + j * LONG_STEP, C - 1)] : 1.f);
+                s[0] += u;
+                s[1] += u * z[j];
             }
         });
-        red[turn][0][wave][lane] = s;
-        red[turn][1][wave][lane] = t;
-        __syncthreads();
-        s = t = 0.f;
-#pragma unroll
-        for (int w = 0; w < LONG_W; ++w) {
-            s += red[turn][0][w][lane];
-            t += red[turn][1][w][lane];
-        }
-        s /= (float)C;
-        t /= (float)C;
-        each([&](int c0, float (&d)[CHUNK], float (&z)[CHUNK]) {
+        pixel_sums<LP>(s, red[turn]);
+        s[0] /= (float)C;
+        s[1] /= (float)C;
+        chunks([&](int c0, float (&d)[CHUNK], float (&z)[CHUNK]) {
 #pragma unroll
             for (int j = 0; j < CHUNK; ++j) {
-                const int c = c0 + j * LONG_W;
-                if (dx && on && c < C) Store<T>::st(dx + at + c * step, r * (d[j] * (gamma ? gamma[c] : 1.f) - s - z[j] * t));
-                d[j] = on ? d[j] : 0.f;
-                z[j] = on ? d[j] * z[j] : 0.f;
+                const int c = c0 + j * LONG_STEP;
+                if (dx) p.st(dx, c, r * (d[j] * (gamma ? gamma[min(c + p.sub, C - 1)] : 1.f) - s[0] - z[j] * s[1]));
+                d[j] = p.on ? d[j] : 0.f;
+                z[j] = p.on ? d[j] * z[j] : 0.f;
             }
             if (partial) {
-                const float dg = transpose_sum(z), db = transpose_sum(d);
-                const int c = c0 + lane * CHUNK / 64 * LONG_W;
-                if (lane % (64 / CHUNK) == 0 && c < C) {
+                const float dg = transpose_sum<LP>(z), db = transpose_sum<LP>(d);
+                const int c = c0 + p.sub + (int)(threadIdx.x % LP) * CHUNK / LP * LONG_STEP;
+                if (threadIdx.x % (LP / CHUNK) == 0 && c < C) {
                     columns[c] += dg;
                     columns[C + c] += db;
                 }
@@ -795,7 +798,7 @@ __global__ __launch_bounds__(LONG_W * 64) void norm_grad_long_planes_kernel(cons
     }
     if (!partial) return;
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * C; i += LONG_W * 64) partial[(size_t)blockIdx.x * 2 * C + i] = columns[i];
+    for (int i = threadIdx.x; i < 2 * C; i += PLANES_WAVES * 64) partial[(size_t)blockIdx.x * 2 * C + i] = columns[i];
 }
 
 // ---- which kernel
@@ -842,15 +845,22 @@ void with_lanes(int nvec, int most, size_t rows, F f)
     else with_nv(IC<64>{});
 }
 
-// f(NC): channels of a lane; as many waves as that takes
+// f(LP, NC): pixels of a workgroup, channels of a lane; NC = 0: more channels than registers hold (`most` of a lane).  64 pixels, a whole 256 bytes of a plane, but where they
+// make fewer workgroups than half of the compute units: 16 (832 channels of 7 x 7 x 128 fp32 33.5 us with 64, 22.8 with 16; 192 of 28 x 28 x 32 11.2 and 14.2 with 32).
 template <class F>
-void with_planes(int C, F f)
+void with_planes(const Pixels& px, int most, F f)
 {
-    if (C <= 128) f(IC<8>{});
-    else if (C <= 256) f(IC<16>{});
-    else f(IC<32>{});
+    auto with_nc = [&](auto lp) {
+        constexpr int LP = decltype(lp)::value, GROUPS = PLANES_WAVES * (64 / LP);      // lanes of a pixel at most
+        if (px.C <= 8 * GROUPS / 2) f(lp, IC<8>{});
+        else if (px.C <= 16 * GROUPS) f(lp, IC<16>{});
+        else if (px.C <= std::min(most, 32) * GROUPS) f(lp, IC<32>{});
+        else f(lp, IC<0>{});
+    };
+    if (px.count >= 32 * (size_t)device_cus()) with_nc(IC<64>{});
+    else with_nc(IC<16>{});
 }
-constexpr int PLANES_MOST = 512, COLUMNS_MOST = 8192;      // channels: in registers; sums in LDS (64 KB)
+constexpr int COLUMNS_MOST = 8192;      // channels whose sums fit LDS (64 KB)
 
 template <typename T>
 int norm_fwd(const dr_tensor& d, const T* x, const float* gamma, const float* beta, float eps, int relu, T* y, float* mean, float* rstd, hipStream_t st)
@@ -865,15 +875,16 @@ int norm_fwd(const dr_tensor& d, const T* x, const float* gamma, const float* be
         if (C % VN == 0) hipLaunchKernelGGL((norm_rows_kernel<T, G, NV, TH, false>), dim3(grid), dim3(TH), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
         else hipLaunchKernelGGL((norm_rows_kernel<T, G, NV, TH, true>), dim3(grid), dim3(TH), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
     };
-    if (px.planes) {
-        const unsigned grid = (unsigned)((px.count + 63) / 64);
-        if (C <= PLANES_MOST && planes_near(px, sizeof(T)))
-            with_planes(C, [&](auto nc) {
-                constexpr int NC = decltype(nc)::value;
-                hipLaunchKernelGGL((norm_planes_kernel<T, NC>), dim3(grid), dim3((C + NC - 1) / NC * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
-            });
-        else hipLaunchKernelGGL((norm_long_planes_kernel<T>), dim3(grid), dim3(LONG_W * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
-    } else if (C < VN)
+    if (px.planes && planes_near(px, sizeof(T))) {
+        with_planes(px, 32, [&](auto lp, auto nc) {
+            constexpr int LP = decltype(lp)::value, NC = decltype(nc)::value, EACH = NC * (64 / LP);
+            const dim3 grid((unsigned)((px.count + LP - 1) / LP));
+            if constexpr (NC == 0) hipLaunchKernelGGL((norm_long_planes_kernel<T, LP>), grid, dim3(PLANES_WAVES * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
+            else hipLaunchKernelGGL((norm_planes_kernel<T, LP, NC>), grid, dim3((C + EACH - 1) / EACH * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
+        });
+    } else if (px.planes)
+        hipLaunchKernelGGL((norm_any_kernel<T>), dim3(blocks_for(px.count, 1, 16384)), dim3(256), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
+    else if (C < VN)
         hipLaunchKernelGGL((norm_narrow_kernel<T>), dim3(blocks_for(px.count, 256, 4096)), dim3(256), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
     else if (nvec <= 4 * 64) with_lanes(nvec, 4, px.count, [&](auto g, auto nv) { rows(g, nv, IC<256>{}); });
     else if (nvec <= 2 * 256) rows(IC<256>{}, IC<2>{}, IC<256>{});
@@ -903,15 +914,15 @@ int norm_bwd(const dr_tensor& d, const T* dy, const T* x, const float* gamma, co
             else hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH, true>), dim3(ranges), dim3(TH), 2 * C * sizeof(float), st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
         };
         if (px.planes) {
-            if (C <= COLUMNS_MOST) ranges = even_blocks((px.count + 63) / 64, most);
-            if (C <= PLANES_MOST && planes_near(px, sizeof(T)))
-                with_planes(C, [&](auto nc) {
-                    constexpr int NC = decltype(nc)::value;
-                    hipLaunchKernelGGL((norm_grad_planes_kernel<T, NC>), dim3(ranges), dim3((C + NC - 1) / NC * 64), 0, st, px, dy, x, gamma, mean, rstd, dx, partial);
+            if (planes_near(px, sizeof(T)) && C <= COLUMNS_MOST)
+                with_planes(px, px.count >= 32 * (size_t)device_cus() ? 32 : 16, [&](auto lp, auto nc) {
+                    constexpr int LP = decltype(lp)::value, NC = decltype(nc)::value, EACH = NC * (64 / LP);
+                    ranges = even_blocks((px.count + LP - 1) / LP, most);
+                    if constexpr (NC == 0)
+                        hipLaunchKernelGGL((norm_grad_long_planes_kernel<T, LP>), dim3(ranges), dim3(PLANES_WAVES * 64), 2 * C * sizeof(float), st, px, dy, x, gamma, mean, rstd, dx, partial);
+                    else if constexpr (NC <= 16 || LP == 64)
+                        hipLaunchKernelGGL((norm_grad_planes_kernel<T, LP, NC>), dim3(ranges), dim3((C + EACH - 1) / EACH * 64), 0, st, px, dy, x, gamma, mean, rstd, dx, partial);
                 });
-            else if (C <= COLUMNS_MOST) {
-                hipLaunchKernelGGL((norm_grad_long_planes_kernel<T>), dim3(ranges), dim3(LONG_W * 64), 2 * C * sizeof(float), st, px, dy, x, gamma, mean, rstd, dx, partial);
-            }
         } else if (C < VN) {
             ranges = (int)blocks_for(px.count, 256, most);
             hipLaunchKernelGGL((norm_grad_narrow_kernel<T>), dim3(ranges), dim3(256), 0, st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
