@@ -612,47 +612,66 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
         }
 }
 
-// ---- matrices small enough for one workgroup's LDS: the whole iteration there, X, A and Q in fp32, cut into pieces where they are multiplied
-// 64 rows and 448 columns, or 32 and 896: eight waves.  Nothing but the matrix is read or written, and a step is nine barriers instead of three launches.
-constexpr int WHOLE_FLOATS = 38912;
-__host__ __device__ inline bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 14; }
+// ---- matrices small enough for one workgroup's LDS: the whole iteration there, X in fp32, cut into pieces where it is multiplied, A and Q in pieces, as operands
+// 64 rows and 352 columns, or 32 and 896: eight waves.  Nothing but the matrix is read or written, and a step is four barriers instead of three launches.  Vector
+// instructions bound it, most of them the cutting: with A and Q in fp32 too, cut by every wave that multiplies them, a step on 64 x 64 took 5.8 us, 1650 of them on its path.
+constexpr int WHOLE_BYTES = 163840 - 256;
+__host__ __device__ inline bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 11; }
 
 template <typename E, int P, bool MUON>
 __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs j, int steps)
 {
-    __shared__ __attribute__((aligned(16))) float lds[WHOLE_FLOATS];
+    __shared__ __attribute__((aligned(16))) unsigned char lds[WHOLE_BYTES];
     __shared__ double red[8];
     const int k = blockIdx.x, mb = j.mb[k], nb = j.nb[k], rows = j.rows[k], cols = j.cols[k];
     const bool tall = rows > cols;
-    const int XP = nb * 32 + 4, AP = mb * 32 + 4;
-    float* const X = lds;
-    float* const A = X + mb * 32 * XP;
-    float* const Q = A + mb * 32 * AP;       // and partial sums, whose time is another
+    // X; A as operand, 2 mb k-blocks for each 32 rows; Q likewise; sums of A's blocks on and below the diagonal that single waves have made, in the place of Q and behind it
+    const int XP = nb * 32 + 4;
+    float* const X = (float*)lds;
+    unsigned char* const A = lds + mb * 32 * XP * 4;
+    unsigned char* const Q = A + 2 * mb * mb * P * BLOCK;
+    float* const sums = (float*)Q;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l32 = lane & 31, half = lane >> 5;
 
-    // element i of the matrix, i = tid, tid + 512, ...: f(i, its place in X)
+    // elements i = tid, tid + 512, ... of the matrix, AT_ONCE at a time: f(the first's number, their places in X)
+    constexpr int AT_ONCE = 16;
     const int total = rows * cols, step_r = 512 / cols, step_c = 512 - step_r * cols;
     auto elements = [&](auto f) __attribute__((always_inline)) {
         int r = tid / cols, col = tid - r * cols;
-        for (int i = tid; i < total; i += 512) {
-            f(i, tall ? col * XP + r : r * XP + col);
-            r += step_r;
-            col += step_c;
-            if (col >= cols) { col -= cols; ++r; }
+        for (int i = tid; i < total; i += AT_ONCE * 512) {
+            int at[AT_ONCE];
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) {
+                at[e] = tall ? col * XP + r : r * XP + col;
+                r += step_r;
+                col += step_c;
+                if (col >= cols) { col -= cols; ++r; }
+            }
+            f(i, at);
         }
     };
     for (int i = tid; i < mb * 32 * XP; i += 512) X[i] = 0.f;
     __syncthreads();
     double s = 0.0;
-    elements([&](int i, int at) {
-        float u = Store<E>::ld((const E*)j.g[k] + i);
-        if constexpr (MUON) {
-            const float v = c.mu * j.momentum[k][i] + u;
-            j.momentum[k][i] = v;
-            u += c.mu * v;
+    elements([&](int i, const int (&at)[AT_ONCE]) {
+        float u[AT_ONCE], v[AT_ONCE];
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) {
+            const bool in = i + e * 512 < total;
+            u[e] = in ? Store<E>::ld((const E*)j.g[k] + i + e * 512) : 0.f;
+            if constexpr (MUON) v[e] = in ? j.momentum[k][i + e * 512] : 0.f;
         }
-        X[at] = u;
-        s += (double)u * (double)u;
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) {
+            if (i + e * 512 >= total) break;
+            if constexpr (MUON) {
+                v[e] = c.mu * v[e] + u[e];
+                j.momentum[k][i + e * 512] = v[e];
+                u[e] += c.mu * v[e];
+            }
+            X[at[e]] = u[e];
+            s += (double)u[e] * (double)u[e];
+        }
     });
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
@@ -662,12 +681,12 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs j, 
     for (int i = tid; i < mb * 32 * XP; i += 512) X[i] = (float)((double)X[i] * inv);
     __syncthreads();
 
-    // eight values along a row of M, cut; down a column of X
-    auto along = [&](const float* M, int pitch, int row, int k0, u32x4 (&p)[P]) __attribute__((always_inline)) {
+    // eight values along a row of X, cut; down a column
+    auto along = [&](int row, int k0, u32x4 (&p)[P]) __attribute__((always_inline)) {
         float v[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const f32x4 t = *reinterpret_cast<const f32x4*>(M + row * pitch + k0 + half * 8 + 4 * h);
+            const f32x4 t = *reinterpret_cast<const f32x4*>(X + row * XP + k0 + half * 8 + 4 * h);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[4 * h + e] = t[e];
         }
@@ -679,77 +698,125 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs j, 
         for (int e = 0; e < 8; ++e) v[e] = X[(k0 + half * 8 + e) * XP + col];
         cut8<P>(v, p);
     };
+    auto read = [&](const unsigned char* M, int rb, int kb, u32x4 (&p)[P]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < P; ++e) p[e] = *reinterpret_cast<const u32x4*>(M + ((rb * 2 * mb + kb) * P + e) * BLOCK + lane * 16);
+    };
     auto zero = [](f32x16& a, f32x16& b) __attribute__((always_inline)) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) a[v] = b[v] = 0.f;
     };
     // register v holds row 8 (v / 4) + 4 half + v % 4 of column lane % 32
     auto row_of = [&](int v) __attribute__((always_inline)) { return 8 * (v >> 2) + 4 * half + (v & 3); };
-    for (int step = 0; step < steps; ++step) {
-        f32x16 large, small;
-        // A = X X^T: the first wave of a block leaves its sum in A, the others theirs beside it
-        if (mb == 1 || wave < 6) {
-            const int blk = mb == 1 ? 0 : wave >> 1, split = mb == 1 ? wave : wave & 1, splits = mb == 1 ? 8 : 2, bi = blk ? 1 : 0, bj = blk == 2 ? 1 : 0;
-            zero(large, small);
-            for (int kb = split; kb < 2 * nb; kb += splits) {
-                u32x4 a[P], b[P];
-                along(X, XP, bi * 32 + l32, kb * 16, a);
-                if (bi == bj) multiply<P>(a, a, large, small);
-                else {
-                    along(X, XP, bj * 32 + l32, kb * 16, b);
-                    multiply<P>(a, b, large, small);
+    auto iterate = [&](auto blocks) __attribute__((always_inline)) {
+        constexpr int MB = decltype(blocks)::value, SPLITS = MB == 1 ? 8 : 2;      // waves that share a block of A
+        f32x16 large[2], small[2];
+        auto multiply2 = [&](int which, const u32x4 (&a)[P], const u32x4 (&b)[P]) __attribute__((always_inline)) { multiply<P>(a, b, large[which], small[which]); };
+        auto sum = [&](int v) __attribute__((always_inline)) { return (large[0][v] + large[1][v]) + (small[0][v] + small[1][v]); };
+        for (int step = 0; step < steps; ++step) {
+            // A = X X^T
+            if (MB == 1 || wave < 6) {
+                const int blk = MB == 1 ? 0 : wave >> 1, split = MB == 1 ? wave : wave & 1, bi = blk ? 1 : 0, bj = blk == 2 ? 1 : 0;
+                zero(large[0], small[0]);
+                zero(large[1], small[1]);
+                // (two k-blocks at a time, in sums of their own: what a product waits for is the one before it)
+                for (int kb = split; kb < 2 * nb; kb += 2 * SPLITS) {
+                    u32x4 a[2][P], b[2][P];
+                    const bool two = kb + SPLITS < 2 * nb;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) along(bi * 32 + l32, (h && two ? kb + SPLITS : kb) * 16, a[h]);
+                    if (bi == bj) {
+                        multiply2(0, a[0], a[0]);
+                        if (two) multiply2(1, a[1], a[1]);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) along(bj * 32 + l32, (h && two ? kb + SPLITS : kb) * 16, b[h]);
+                        multiply2(0, a[0], b[0]);
+                        if (two) multiply2(1, a[1], b[1]);
+                    }
+                }
+                float* const to = sums + (blk * SPLITS + split) * 32 * PITCH;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) to[row_of(v) * PITCH + l32] = sum(v);
+            }
+            __syncthreads();
+            // ... as operand: a wave per k-block of 32 rows
+            if (wave < 2 * MB * MB) {
+                const int rb = wave / (2 * MB), kb = wave % (2 * MB), cb = kb >> 1, blk = rb + cb, k0 = (kb & 1) * 16 + half * 8;
+                const float* const from = sums + blk * SPLITS * 32 * PITCH;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll
+                for (int w = 0; w < SPLITS; ++w) {
+                    if (rb < cb) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] += from[w * 32 * PITCH + (k0 + e) * PITCH + l32];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] += from[w * 32 * PITCH + l32 * PITCH + k0 + e];
+                    }
+                }
+                u32x4 p[P];
+                cut8<P>(v, p);
+#pragma unroll
+                for (int e = 0; e < P; ++e) *reinterpret_cast<u32x4*>(A + (wave * P + e) * BLOCK + lane * 16) = p[e];
+            }
+            __syncthreads();
+            // Q = a I + b A + c A A, which is symmetric: element (row, column) is stored as (column, row), four of a lane's one after the other
+            if (wave < MB * MB) {
+                const int bi = wave / MB, bj = wave % MB;
+                zero(large[0], small[0]);
+                zero(large[1], small[1]);
+#pragma unroll
+                for (int kb = 0; kb < 2 * MB; ++kb) {
+                    u32x4 a[P], b[P];
+                    read(A, bi, kb, a);
+                    read(A, bj, kb, b);
+                    multiply2(kb & 1, a, b);
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {             // rows 16 h .. 16 h + 15 of the block: a k-block
+                    float v[8];
+                    u32x2 p[2][P];
+                    const int block = ((bj * 2 * MB + bi * 2 + h) * P) * BLOCK + l32 * 16 + half * 8;
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                        for (int e = 0; e < P; ++e) p[q][e] = *reinterpret_cast<const u32x2*>(A + block + q * 512 + e * BLOCK);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const int n = (2 * h + q) * 4 + r;
+                            float w = 0.f;
+#pragma unroll
+                            for (int e = P - 1; e >= 0; --e) w += __uint_as_float(r & 1 ? p[q][e][r >> 1] & 0xFFFF0000u : p[q][e][r >> 1] << 16);
+                            v[q * 4 + r] = c.b * w + c.c * sum(n) + (bi == bj && row_of(n) == l32 ? c.a : 0.f);
+                        }
+                    u32x4 t[P];
+                    cut8<P>(v, t);
+#pragma unroll
+                    for (int q = 0; q < 2; ++q)
+#pragma unroll
+                        for (int e = 0; e < P; ++e) *reinterpret_cast<u32x2*>(Q + block + q * 512 + e * BLOCK) = u32x2{t[e][2 * q], t[e][2 * q + 1]};
                 }
             }
-            float* const to = split ? Q + (mb == 1 ? split - 1 : blk) * 32 * PITCH : A + bi * 32 * AP + bj * 32;
-            const int pitch = split ? PITCH : AP;
-#pragma unroll
-            for (int v = 0; v < 16; ++v) to[row_of(v) * pitch + l32] = large[v] + small[v];
-        }
-        __syncthreads();
-        for (int i = tid; i < (mb == 1 ? 1024 : 3072); i += 512) {
-            const int blk = i >> 10, r = (i >> 5) & 31, cl = i & 31, bi = blk ? 1 : 0, bj = blk == 2 ? 1 : 0;
-            float* const at = A + (bi * 32 + r) * AP + bj * 32 + cl;
-            float t = *at;
-            if (mb == 1) {
-#pragma unroll
-                for (int w = 0; w < 7; ++w) t += Q[w * 32 * PITCH + r * PITCH + cl];
-            } else t += Q[blk * 32 * PITCH + r * PITCH + cl];
-            *at = t;
-            if (blk == 1) A[cl * AP + 32 + r] = t;
-        }
-        __syncthreads();
-        // Q = a I + b A + c A A
-        if (wave < mb * mb) {
-            const int bi = wave >> (mb - 1), bj = wave & (mb - 1);
-            zero(large, small);
-            for (int kb = 0; kb < 2 * mb; ++kb) {
-                u32x4 a[P], b[P];
-                along(A, AP, bi * 32 + l32, kb * 16, a);
-                along(A, AP, bj * 32 + l32, kb * 16, b);
-                multiply<P>(a, b, large, small);
-            }
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int at = (bi * 32 + row_of(v)) * AP + bj * 32 + l32;
-                Q[at] = c.b * A[at] + c.c * (large[v] + small[v]) + (bi == bj && row_of(v) == l32 ? c.a : 0.f);
-            }
-        }
-        __syncthreads();
-        // X = Q X: a wave has whole columns, which it replaces
-        auto apply = [&](auto blocks) __attribute__((always_inline)) {
-            constexpr int MB = decltype(blocks)::value;
+            __syncthreads();
+            // X = Q X: a wave has whole columns, which it replaces
             for (int bj = wave; bj < nb; bj += 8) {
                 f32x16 big[MB], little[MB];
 #pragma unroll
                 for (int i = 0; i < MB; ++i) zero(big[i], little[i]);
-#pragma unroll 2
+#pragma unroll
                 for (int kb = 0; kb < 2 * MB; ++kb) {
                     u32x4 b[P];
                     down(bj * 32 + l32, kb * 16, b);
 #pragma unroll
                     for (int i = 0; i < MB; ++i) {
                         u32x4 q[P];
-                        along(Q, AP, i * 32 + l32, kb * 16, q);
+                        read(Q, i, kb, q);
                         multiply<P>(q, b, big[i], little[i]);
                     }
                 }
@@ -758,16 +825,23 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs j, 
 #pragma unroll
                     for (int v = 0; v < 16; ++v) X[(i * 32 + row_of(v)) * XP + bj * 32 + l32] = big[i][v] + little[i][v];
             }
-        };
-        if (mb == 1) apply(std::integral_constant<int, 1>{});
-        else apply(std::integral_constant<int, 2>{});
-        __syncthreads();
-    }
-    elements([&](int i, int at) {
+            __syncthreads();
+        }
+    };
+    if (mb == 1) iterate(std::integral_constant<int, 1>{});
+    else iterate(std::integral_constant<int, 2>{});
+    elements([&](int i, const int (&at)[AT_ONCE]) {
+        float w[AT_ONCE];
         if constexpr (MUON) {
-            float* const w = (float*)j.o[k];
-            w[i] = c.keep * w[i] - j.scale[k] * X[at];
-        } else Store<E>::st((E*)j.o[k] + i, X[at]);
+#pragma unroll
+            for (int e = 0; e < AT_ONCE; ++e) w[e] = i + e * 512 < total ? ((const float*)j.o[k])[i + e * 512] : 0.f;
+        }
+#pragma unroll
+        for (int e = 0; e < AT_ONCE; ++e) {
+            if (i + e * 512 >= total) break;
+            if constexpr (MUON) ((float*)j.o[k])[i + e * 512] = c.keep * w[e] - j.scale[k] * X[at[e]];
+            else Store<E>::st((E*)j.o[k] + i + e * 512, X[at[e]]);
+        }
     });
 }
 
