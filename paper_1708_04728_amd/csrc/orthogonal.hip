@@ -36,26 +36,27 @@ constexpr int PITCH = 36;                    // floats of a row of 32 in LDS
 constexpr int SQUARES = 1024;                // most workgroups (and partial sums of squares) of a matrix
 enum { GRAM = 0, POLY = 1, APPLY = 2, PRODUCTS = 3 };
 
-// The matrices of a launch; arrays by what is looked up together.  A list is worked on JOBS at a time.
+// The matrices of a launch; arrays by what is looked up together.  A list is worked on JOBS at a time.  (N: room for as many.  A launch reads its arguments from memory, one after
+// the other where an index is among them: a single matrix has kernels whose arguments are its own.)
 constexpr int JOBS = 64;
+template <int N>
 struct Jobs {
-    int first[JOBS];                         // first workgroup of the launch's k-th matrix; INT_MAX behind the last
-    int which[JOBS];                         // the launch's k-th matrix
-    unsigned operands[JOBS];                 // its operands' place in the workspace, in KiB
-    int mb[JOBS], nb[JOBS];                  // blocks of 32 of the short and of the long side
-    int rows[JOBS], cols[JOBS];
-    int squares[JOBS];                       // its first partial sum of squares
-    const void* g[JOBS];
-    float* momentum[JOBS];                   // (descent step only)
-    void* o[JOBS];                           // the result, or the weights
-    float scale[JOBS];                       // descent step: lr sqrt(max(1, rows / cols))
+    int first[N];                         // first workgroup of the launch's k-th matrix; INT_MAX behind the last
+    int which[N];                         // the launch's k-th matrix
+    unsigned operands[N];                 // its operands' place in the workspace, in KiB
+    int mb[N], nb[N];                  // blocks of 32 of the short and of the long side
+    int rows[N], cols[N];
+    int squares[N];                       // its first partial sum of squares
+    const void* g[N];
+    float* momentum[N];                   // (descent step only)
+    void* o[N];                           // the result, or the weights
+    float scale[N];                       // descent step: lr sqrt(max(1, rows / cols))
 };
 
 struct Call {
     double* squares;
     float* partial;                          // sums of workgroups that share a tile
     unsigned char* ws;
-    int count;
     float a, b, c, eps;
     float mu, keep;                          // descent step: momentum; 1 - lr decay
 };
@@ -65,13 +66,13 @@ struct Mat {
     int k, first, mb, nb, rows, cols;        // first: its first workgroup
     bool tall;                               // rows > cols: X is the transpose
 };
-__device__ __forceinline__ Mat find_matrix(const Jobs& j, int count, int id)
+template <int N>
+__device__ __forceinline__ Mat find_matrix(const Jobs<N>& j, int id)
 {
+    if constexpr (N == 1) return Mat{0, 0, j.mb[0], j.nb[0], j.rows[0], j.cols[0], j.rows[0] > j.cols[0]};
     int k = 0;
-    if (count > 1) {
 #pragma unroll
-        for (int i = 1; i < JOBS; ++i) k += j.first[i] <= id ? 1 : 0;
-    }
+    for (int i = 1; i < N; ++i) k += j.first[i] <= id ? 1 : 0;
     k = __builtin_amdgcn_readfirstlane(k);
     const int i = j.which[k];
     return Mat{i, j.first[k], j.mb[i], j.nb[i], j.rows[i], j.cols[i], j.rows[i] > j.cols[i]};
@@ -81,7 +82,8 @@ __device__ __forceinline__ Mat find_matrix(const Jobs& j, int count, int id)
 template <int P>
 struct Operands {
     unsigned char *x, *xt0, *xt1, *a, *q;
-    __device__ __forceinline__ Operands(const Call& c, const Jobs& j, const Mat& m)
+    template <int N>
+    __device__ __forceinline__ Operands(const Call& c, const Jobs<N>& j, const Mat& m)
     {
         const size_t wide = (size_t)m.mb * m.nb * (2 * P * BLOCK), square = (size_t)m.mb * m.mb * (2 * P * BLOCK);
         x = c.ws + (size_t)j.operands[m.k] * 1024;
@@ -112,11 +114,11 @@ __device__ __forceinline__ double sum256(double v, double* red)
 }
 
 // Momentum (descent step), and the sums of the squares of U's elements, in double: a square of 1e20 or 1e-30 is no fp32 number
-template <typename T, bool MUON>
-__global__ __launch_bounds__(256) void squares_kernel(const Call c, const Jobs j)
+template <typename T, bool MUON, int N>
+__global__ __launch_bounds__(256) void squares_kernel(const Call c, const Jobs<N> j)
 {
     __shared__ double red[256];
-    const Mat m = find_matrix(j, c.count, blockIdx.x);
+    const Mat m = find_matrix(j, blockIdx.x);
     const T* const g = (const T*)j.g[m.k];
     float* const mom = j.momentum[m.k];
     const int me = (int)blockIdx.x - m.first;
@@ -199,12 +201,12 @@ __device__ __forceinline__ void put8(const float (&v)[8], unsigned char* block, 
 }
 
 // X = U / (|U| + eps) in both orders, cut into pieces: a wave per 32 x 32 block
-template <typename T, int P, bool MUON>
-__global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs j)
+template <typename T, int P, bool MUON, int N>
+__global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs<N> j)
 {
     __shared__ __attribute__((aligned(16))) float tiles[4][32 * PITCH];
     __shared__ double red[256];
-    const Mat m = find_matrix(j, c.count, blockIdx.x);
+    const Mat m = find_matrix(j, blockIdx.x);
     const Operands<P> op(c, j, m);
     const T* const g = (const T*)j.g[m.k];
     const float* const mom = j.momentum[m.k];
@@ -215,22 +217,23 @@ __global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs j)
     float* const tile = tiles[wave];
     // lanes along the matrix's own columns; the tile's rows are X's
     const int r0 = (m.tall ? bj : bi) * 32, col = (m.tall ? bi : bj) * 32 + l32;
-    float u[16];
+    float u[16], v[16];
+    auto at = [&](int r) __attribute__((always_inline)) { return (size_t)min(r0 + 2 * r + half, m.rows - 1) * m.cols + min(col, m.cols - 1); };
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int row = r0 + 2 * r + half;
-        const size_t i = (size_t)row * m.cols + col;
-        u[r] = 0.f;
-        if (on && row < m.rows && col < m.cols) {
-            u[r] = Store<T>::ld(g + i);
-            if constexpr (MUON) u[r] += c.mu * mom[i];
-        }
+    for (int r = 0; r < 16; ++r) u[r] = Store<T>::ld(g + at(r));
+    if constexpr (MUON) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) v[r] = mom[at(r)];
     }
     double s = 0.0;
     for (int i = threadIdx.x; i < squares_of(m.rows, m.cols); i += 256) s += c.squares[j.squares[m.k] + i];
     const double inv = 1.0 / (sqrt(sum256(s, red)) + (double)c.eps);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) tile[m.tall ? l32 * PITCH + 2 * r + half : (2 * r + half) * PITCH + l32] = (float)((double)u[r] * inv);
+    for (int r = 0; r < 16; ++r) {
+        if constexpr (MUON) u[r] += c.mu * v[r];
+        const bool in = r0 + 2 * r + half < m.rows && col < m.cols;
+        tile[m.tall ? l32 * PITCH + 2 * r + half : (2 * r + half) * PITCH + l32] = in ? (float)((double)u[r] * inv) : 0.f;
+    }
     __syncthreads();
     if (!on) return;
 #pragma unroll
@@ -271,20 +274,25 @@ __device__ __forceinline__ void finish_task(const Call& c, const Mat& m, const O
     }
 }
 // ... of the last product: the result, or the weights; rows r0, r0 + step, ... of the matrix' own 32 x 32 block
-template <typename T, bool MUON>
-__device__ __forceinline__ void finish_result(const Call& c, const Jobs& j, const Mat& m, const float* tile, int bi, int bj, int r0, int step)
+template <typename T, bool MUON, int N>
+__device__ __forceinline__ void finish_result(const Call& c, const Jobs<N>& j, const Mat& m, const float* tile, int bi, int bj, int r0, int step)
 {
-    const int l32 = threadIdx.x & 31;
-#pragma unroll 4
-    for (int r = r0; r < 32; r += step) {
-        const int row = (m.tall ? bj : bi) * 32 + r, col = (m.tall ? bi : bj) * 32 + l32;
-        if (row >= m.rows || col >= m.cols) continue;
-        const float v = tile[m.tall ? l32 * PITCH + r : r * PITCH + l32];
-        const size_t i = (size_t)row * m.cols + col;
+    const int l32 = threadIdx.x & 31, row0 = (m.tall ? bj : bi) * 32, col = (m.tall ? bi : bj) * 32 + l32;
+    for (int r8 = r0; r8 < 32; r8 += 8 * step) {         // (eight weights at a time: loads behind stores would wait for each other)
+        float old[8];
         if constexpr (MUON) {
-            float* const w = (float*)j.o[m.k];
-            w[i] = c.keep * w[i] - j.scale[m.k] * v;
-        } else Store<T>::st((T*)j.o[m.k] + i, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) old[e] = ((const float*)j.o[m.k])[(size_t)min(row0 + r8 + e * step, m.rows - 1) * m.cols + min(col, m.cols - 1)];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int r = r8 + e * step;
+            if (r >= 32 || row0 + r >= m.rows || col >= m.cols) continue;
+            const float v = tile[m.tall ? l32 * PITCH + r : r * PITCH + l32];
+            const size_t i = (size_t)(row0 + r) * m.cols + col;
+            if constexpr (MUON) ((float*)j.o[m.k])[i] = c.keep * old[e] - j.scale[m.k] * v;
+            else Store<T>::st((T*)j.o[m.k] + i, v);
+        }
     }
 }
 
@@ -321,13 +329,13 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[P], const u32x4 (&b)[P
 // A product of small matrices: W waves share a tile of T x T blocks, every wave a W-th of the contraction.  Operands go straight to registers, AHEAD k-blocks of them
 // while as many are multiplied: what such a product waits for is its first operands.  splits > 1: as many workgroups share a tile, and leave sums for sum_kernel.
 template <int T> constexpr int ahead() { return T == 1 ? 4 : 2; }
-template <typename E, int P, int WHAT, int T, int W, bool MUON>
-__global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs j, int turn, int last, int splits)
+template <typename E, int P, int WHAT, int T, int W, bool MUON, int N>
+__global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs<N> j, int turn, int last, int splits)
 {
     constexpr int AHEAD = ahead<T>();
     __shared__ __attribute__((aligned(16))) float sums[W][T * T][32 * PITCH];
     const int unit = splits > 1 ? (int)blockIdx.x / splits : (int)blockIdx.x, part = (int)blockIdx.x - unit * splits;
-    const Mat m = find_matrix(j, c.count, unit);
+    const Mat m = find_matrix(j, unit);
     const Operands<P> op(c, j, m);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     int bi, bj;
@@ -406,7 +414,7 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
     if (WHAT == APPLY && last) {
         for (int blk = 0; blk < T * T; ++blk) {
             const int i = bi + blk / T, k = bj + blk % T;
-            if (i < lrows && k < rrows) finish_result<E, MUON>(c, j, m, sums[0][blk], i, k, wave * 2 + half, 2 * W);
+            if (i < lrows && k < rrows) finish_result<E, MUON, N>(c, j, m, sums[0][blk], i, k, wave * 2 + half, 2 * W);
         }
         return;
     }
@@ -430,12 +438,12 @@ __device__ __forceinline__ void lds_barrier()        // orders LDS traffic only
 }
 
 // Adds the sums that the workgroups of a tile have left, in their order
-template <typename E, int P, int WHAT, int T, bool MUON>
-__global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs j, int turn, int last, int splits)
+template <typename E, int P, int WHAT, int T, bool MUON, int N>
+__global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j, int turn, int last, int splits)
 {
     __shared__ __attribute__((aligned(16))) float tile[32 * PITCH];
     const int unit = (int)blockIdx.x / (T * T), blk = (int)blockIdx.x - unit * (T * T);
-    const Mat m = find_matrix(j, c.count, unit);
+    const Mat m = find_matrix(j, unit);
     const Operands<P> op(c, j, m);
     int bi, bj;
     tile_blocks<WHAT, T>(m, unit - m.first, bi, bj);
@@ -450,7 +458,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs j, in
 #pragma unroll
     for (int n = 0; n < 4; ++n) tile[(n * 8 + (threadIdx.x >> 5)) * PITCH + (threadIdx.x & 31)] = s[n];
     __syncthreads();
-    if (WHAT == APPLY && last) finish_result<E, MUON>(c, j, m, tile, bi, bj, threadIdx.x >> 5, 8);
+    if (WHAT == APPLY && last) finish_result<E, MUON, N>(c, j, m, tile, bi, bj, threadIdx.x >> 5, 8);
     else finish_task<P, WHAT>(c, m, op, tile, bi, bj, turn, threadIdx.x >> 6);
 }
 
@@ -460,8 +468,8 @@ __device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
 template <int N, class F>
 __device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
-template <typename E, int P, int WHAT, int WM, int WN, int TM, int TN, int DEPTH, bool APART, bool MUON>
-__global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const Jobs j, int turn, int last)
+template <typename E, int P, int WHAT, int WM, int WN, int TM, int TN, int DEPTH, bool APART, bool MUON, int N>
+__global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const Jobs<N> j, int turn, int last)
 {
     constexpr int W = WM * WN, BM = WM * TM, BN = WN * TN, STAGE = (BM + BN) * P * BLOCK, LOADS = (BM + BN) * P / W;
     static_assert((BM + BN) * P % W == 0 && BM == BN && (DEPTH == 1 || DEPTH == 2) && tile_lds<P, BM, BN>() >= W * 32 * PITCH * 4, "a tile's operands");
@@ -469,8 +477,8 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
     // workgroup b runs on die b & 7: of one matrix a die takes a contiguous range of tiles, which share operands (of a list, whose long contractions come first, that
     // would give one die the most work)
     const int die = blockIdx.x & 7, share = (int)gridDim.x >> 3, odd = gridDim.x & 7;
-    const int id = c.count > 1 ? (int)blockIdx.x : die * share + min(die, odd) + (int)(blockIdx.x >> 3);
-    const Mat m = find_matrix(j, c.count, id);
+    const int id = N > 1 ? (int)blockIdx.x : die * share + min(die, odd) + (int)(blockIdx.x >> 3);
+    const Mat m = find_matrix(j, id);
     const Operands<P> op(c, j, m);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wm = wave / WN, wn = wave % WN;
@@ -602,7 +610,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
             for (int v = 0; v < 16; ++v) tile[(8 * (v >> 2) + 4 * half + (v & 3)) * PITCH + l32] = APART ? acc[i][k][v] + small[APART ? i : 0][APART ? k : 0][v] : acc[i][k][v];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
             __builtin_amdgcn_wave_barrier();
-            if (WHAT == APPLY && last) finish_result<E, MUON>(c, j, m, tile, ri, rk, half, 2);
+            if (WHAT == APPLY && last) finish_result<E, MUON, N>(c, j, m, tile, ri, rk, half, 2);
             else {
 #pragma unroll 1
                 for (int t = 0; t < 4; ++t) finish_task<P, WHAT>(c, m, op, tile, ri, rk, turn, t);
@@ -618,8 +626,8 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
 constexpr int WHOLE_BYTES = 163840 - 256;
 __host__ __device__ inline bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 11; }
 
-template <typename E, int P, bool MUON>
-__global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs j, int steps)
+template <typename E, int P, bool MUON, int N>
+__global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> j, int steps)
 {
     __shared__ __attribute__((aligned(16))) unsigned char lds[WHOLE_BYTES];
     __shared__ double red[8];
@@ -955,8 +963,8 @@ size_t workspace_bytes(int count, int P, Shape shape)
 
 // The order of a launch's matrices: those with the largest length(mb, nb) first, so that what is started last is short
 struct Order { int which[JOBS]; };
-template <class Length>
-Order order_by(const Jobs& j, int count, Length length)
+template <int N, class Length>
+Order order_by(const Jobs<N>& j, int count, Length length)
 {
     Order o;
     for (int i = 0; i < count; ++i) {
@@ -968,11 +976,11 @@ Order order_by(const Jobs& j, int count, Length length)
 }
 
 // the first workgroups of j's matrices, for launches whose matrix has `units(mb, nb, rows, cols)` of them; their number
-template <class Units>
-unsigned number(Jobs& j, int count, const Order& order, Units units)
+template <int N, class Units>
+unsigned number(Jobs<N>& j, int count, const Order& order, Units units)
 {
     unsigned at = 0;
-    for (int k = 0; k < JOBS; ++k) {
+    for (int k = 0; k < N; ++k) {
         j.first[k] = 0x7FFFFFFF;
         if (k >= count) continue;
         const int i = order.which[k];
@@ -983,12 +991,11 @@ unsigned number(Jobs& j, int count, const Order& order, Units units)
     return at;
 }
 
-template <typename E, int P, bool MUON>
-int run_group(const Group& group, Call c, Jobs& j, int steps, void* ws, hipStream_t st)
+template <typename E, int P, bool MUON, int N>
+int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipStream_t st)
 {
-    c.count = group.count;
     if (group.whole) {
-        hipLaunchKernelGGL((whole_kernel<E, P, MUON>), dim3(group.count), dim3(512), 0, st, c, j, steps);
+        hipLaunchKernelGGL((whole_kernel<E, P, MUON, N>), dim3(group.count), dim3(512), 0, st, c, j, steps);
         return check_launch("orthogonalise");
     }
     c.squares = (double*)ws;
@@ -1005,9 +1012,9 @@ int run_group(const Group& group, Call c, Jobs& j, int steps, void* ws, hipStrea
     const Order orders[PRODUCTS] = {order_by(j, group.count, [](int, int nb) { return nb; }), order_by(j, group.count, [](int mb, int) { return mb; }),
                                     order_by(j, group.count, [](int mb, int) { return mb; })};
     const unsigned squares = number(j, group.count, orders[GRAM], [](int, int, int r, int co) { return squares_of(r, co); });
-    hipLaunchKernelGGL((squares_kernel<E, MUON>), dim3(squares), dim3(256), 0, st, c, j);
+    hipLaunchKernelGGL((squares_kernel<E, MUON, N>), dim3(squares), dim3(256), 0, st, c, j);
     const unsigned cuts = number(j, group.count, orders[GRAM], [](int mb, int nb, int, int) { return (mb * nb + 3) / 4; });
-    hipLaunchKernelGGL((cut_kernel<E, P, MUON>), dim3(cuts), dim3(256), 0, st, c, j);
+    hipLaunchKernelGGL((cut_kernel<E, P, MUON, N>), dim3(cuts), dim3(256), 0, st, c, j);
     using std::integral_constant;
     auto product = [&](auto what, int turn, int last) {
         constexpr int WHAT = decltype(what)::value;
@@ -1017,14 +1024,14 @@ int run_group(const Group& group, Call c, Jobs& j, int steps, void* ws, hipStrea
         const unsigned tiles = number(j, group.count, orders[WHAT], [&](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, SIDE[choice.kernel]); });
         auto direct = [&](auto side, auto waves) {
             constexpr int T = decltype(side)::value, W = decltype(waves)::value;
-            hipLaunchKernelGGL((product_kernel<R, P, WHAT, T, W, END>), dim3(tiles * choice.splits), dim3(W * 64), 0, st, c, j, turn, last, choice.splits);
+            hipLaunchKernelGGL((product_kernel<R, P, WHAT, T, W, END, N>), dim3(tiles * choice.splits), dim3(W * 64), 0, st, c, j, turn, last, choice.splits);
             if constexpr (WHAT == GRAM) {
-                if (choice.splits > 1) hipLaunchKernelGGL((sum_kernel<R, P, WHAT, T, END>), dim3(tiles * T * T), dim3(256), 0, st, c, j, turn, last, choice.splits);
+                if (choice.splits > 1) hipLaunchKernelGGL((sum_kernel<R, P, WHAT, T, END, N>), dim3(tiles * T * T), dim3(256), 0, st, c, j, turn, last, choice.splits);
             }
         };
         auto tile = [&](auto side, auto depth, auto apart) {
             constexpr int T = decltype(side)::value;
-            hipLaunchKernelGGL((tile_kernel<R, P, WHAT, 2, 2, T / 2, T / 2, decltype(depth)::value, decltype(apart)::value, END>), dim3(tiles), dim3(256), 0, st, c, j, turn, last);
+            hipLaunchKernelGGL((tile_kernel<R, P, WHAT, 2, 2, T / 2, T / 2, decltype(depth)::value, decltype(apart)::value, END, N>), dim3(tiles), dim3(256), 0, st, c, j, turn, last);
         };
         if (choice.kernel == FINE) direct(integral_constant<int, 1>{}, integral_constant<int, 8>{});
         else if (choice.kernel == DIRECT) direct(integral_constant<int, 2>{}, integral_constant<int, 4>{});
@@ -1042,11 +1049,10 @@ int run_group(const Group& group, Call c, Jobs& j, int steps, void* ws, hipStrea
 }
 
 // fill(i, rows, cols, j, k): matrix i's shape, and entry k of j but for its shape and places
-template <typename E, int P, bool MUON, class Fill>
-int run_list(Call c, int count, const dr_newton_schulz& ns, void* ws, hipStream_t st, Fill fill)
+template <typename E, int P, bool MUON, int N, class Fill>
+int run_jobs(Call c, int count, int steps, void* ws, hipStream_t st, Fill fill)
 {
-    c.a = ns.a; c.b = ns.b; c.c = ns.c; c.eps = ns.eps;
-    Jobs j;
+    Jobs<N> j;
     Group g;
     g.start();
     for (int i = 0; i < count; ++i) {
@@ -1058,12 +1064,18 @@ int run_list(Call c, int count, const dr_newton_schulz& ns, void* ws, hipStream_
             j.nb[g.count] = (std::max(rows, cols) + 31) / 32;
             g.add(rows, cols, P);
         }
-        if (g.count == JOBS || (i + 1 == count && g.count)) {
-            if (const int rc = run_group<E, P, MUON>(g, c, j, ns.steps, ws, st)) return rc;
+        if (g.count == N || (i + 1 == count && g.count)) {
+            if (const int rc = run_group<E, P, MUON>(g, c, j, steps, ws, st)) return rc;
             g.start();
         }
     }
     return DR_OK;
+}
+template <typename E, int P, bool MUON, class Fill>
+int run_list(Call c, int count, const dr_newton_schulz& ns, void* ws, hipStream_t st, Fill fill)
+{
+    c.a = ns.a; c.b = ns.b; c.c = ns.c; c.eps = ns.eps;
+    return count == 1 ? run_jobs<E, P, MUON, 1>(c, count, ns.steps, ws, st, fill) : run_jobs<E, P, MUON, JOBS>(c, count, ns.steps, ws, st, fill);
 }
 
 }  // namespace
@@ -1076,7 +1088,7 @@ size_t orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype)
 int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* const* g, void* const* o, const dr_newton_schulz& ns, void* ws, hipStream_t st)
 {
     TraceScope trace("orthogonalise", nullptr, count, st);
-    auto fill = [&](int i, int& r, int& cols, Jobs& j, int k) {
+    auto fill = [&](int i, int& r, int& cols, auto& j, int k) {
         r = ms[i].rows; cols = ms[i].cols;
         j.g[k] = g[i];
         j.momentum[k] = nullptr;
@@ -1097,7 +1109,7 @@ int launch_muon_step(int count, const dr_muon_param* ps, const dr_muon& opt, voi
     c.mu = opt.momentum;
     c.keep = (float)(1.0 - (double)opt.lr * opt.weight_decay);
     TraceScope trace("muon_step", nullptr, count, st);
-    return run_list<float, 3, true>(c, count, opt.ns, ws, st, [&](int i, int& r, int& cols, Jobs& j, int k) {
+    return run_list<float, 3, true>(c, count, opt.ns, ws, st, [&](int i, int& r, int& cols, auto& j, int k) {
         r = ps[i].rows; cols = ps[i].cols;
         j.g[k] = ps[i].dw;
         j.momentum[k] = ps[i].momentum;
