@@ -230,6 +230,7 @@ int dr_sgd_step(size_t count, float* w, const float* dw, float lr, void* stream)
  * then max(y, 0) if relu != 0.  Either order, fp32 or bf16; a matrix of rows is {rows, c, 1, 1}.  gamma, beta: fp32 device
  * vectors of c entries (NULL: ones, zeros).  mean, rstd: fp32 device arrays of n h w entries, in pixel order, that the
  * gradient reads (NULL: not stored).  Sums are held in fp32.  x == y (in place) is allowed.  eps >= 0. */
+typedef struct { float eps; int relu; } dr_layernorm;      /* of a network's layer */
 int dr_layernorm_fwd(const dr_tensor* d, const void* x, const float* gamma, const float* beta, float eps, int relu, void* y, float* mean,
                      float* rstd, void* stream);
 
@@ -330,7 +331,8 @@ typedef enum {
     DR_LAYER_BOTTLENECK, DR_LAYER_AVGPOOL, DR_LAYER_FC, DR_LAYER_SOFTMAX,
     DR_LAYER_LRN_MAXPOOL,    /* dr_lrn_maxpool_fwd: uses .lrn and .pool */
     DR_LAYER_MAXPOOL_LRN,    /* dr_maxpool_lrn_fwd: uses .pool and .lrn */
-    DR_LAYER_CONV_LRN_MAXPOOL /* dr_conv_lrn_maxpool_fwd: uses .conv, .lrn and .pool; parameters: filters, bias */
+    DR_LAYER_CONV_LRN_MAXPOOL,/* dr_conv_lrn_maxpool_fwd: uses .conv, .lrn and .pool; parameters: filters, bias */
+    DR_LAYER_LAYERNORM        /* dr_layernorm_fwd: uses .layernorm; parameters: gamma, beta */
 } dr_layer_kind;
 
 /* ResNet bottleneck (Sec. 4.2): 1x1 (mid) - 3x3 (mid) - 1x1 (out), each followed by BatchNorm
@@ -347,12 +349,13 @@ typedef struct {
     dr_inception inception;  /* DR_LAYER_INCEPTION */
     dr_bottleneck bottleneck;/* DR_LAYER_BOTTLENECK */
     int fc_out;              /* DR_LAYER_FC */
+    dr_layernorm layernorm;  /* DR_LAYER_LAYERNORM */
 } dr_layer_desc;
 
 typedef struct dr_net dr_net;   /* host-side object: a validated copy of the layer list */
 
 /* Builds a network from n_layers descriptors (copied).  Parameter order expected by dr_net_fwd:
- * forward order; conv: w, bias; inception: per branch, per conv step: w, bias; bottleneck:
+ * forward order; conv: w, bias; layer normalisation: gamma, beta; inception: per branch, per conv step: w, bias; bottleneck:
  * conv a, [bn a], conv b, [bn b], conv c, [bn c], then projection conv, [bn] if present, where a
  * conv is (w, bias) and a bn is (gamma, beta, mean, var) and the bn entries are absent when
  * folded; fc: w, bias. */

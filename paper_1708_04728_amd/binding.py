@@ -25,7 +25,8 @@ DR_MAX_BRANCHES, DR_MAX_STEPS = 8, 4
 DR_STEP_CONV, DR_STEP_MAXPOOL = 0, 1
 DR_FUSE_RELU, DR_FUSE_CONCAT, DR_FUSE_STACK, DR_CONCURRENT_BRANCHES = 1, 2, 4, 8
 (DR_LAYER_CONV, DR_LAYER_RELU, DR_LAYER_LRN, DR_LAYER_MAXPOOL, DR_LAYER_INCEPTION, DR_LAYER_BOTTLENECK,
- DR_LAYER_AVGPOOL, DR_LAYER_FC, DR_LAYER_SOFTMAX, DR_LAYER_LRN_MAXPOOL, DR_LAYER_MAXPOOL_LRN, DR_LAYER_CONV_LRN_MAXPOOL) = range(12)
+ DR_LAYER_AVGPOOL, DR_LAYER_FC, DR_LAYER_SOFTMAX, DR_LAYER_LRN_MAXPOOL, DR_LAYER_MAXPOOL_LRN, DR_LAYER_CONV_LRN_MAXPOOL,
+ DR_LAYER_LAYERNORM) = range(13)
 
 
 class dr_tensor(C.Structure):
@@ -62,9 +63,14 @@ class dr_bottleneck(C.Structure):
                 ("filter_layout", C.c_int)]
 
 
+class dr_layernorm(C.Structure):
+    _fields_ = [("eps", C.c_float), ("relu", C.c_int)]
+
+
 class dr_layer_desc(C.Structure):
     _fields_ = [("kind", C.c_int), ("conv", dr_conv), ("lrn", dr_lrn), ("pool", dr_pool),
-                ("inception", dr_inception), ("bottleneck", dr_bottleneck), ("fc_out", C.c_int)]
+                ("inception", dr_inception), ("bottleneck", dr_bottleneck), ("fc_out", C.c_int),
+                ("layernorm", dr_layernorm)]
 
 
 class dr_trace_record(C.Structure):

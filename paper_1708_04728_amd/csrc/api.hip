@@ -890,6 +890,7 @@ int param_count(const dr_layer_desc& L)
     case DR_LAYER_CONV: return 2;
     case DR_LAYER_CONV_LRN_MAXPOOL: return 2;
     case DR_LAYER_FC: return 2;
+    case DR_LAYER_LAYERNORM: return 2;
     case DR_LAYER_INCEPTION: {
         int n = 0;
         for (int b = 0; b < L.inception.n_branches; ++b)
@@ -1014,6 +1015,10 @@ int layer_out(const dr_layer_desc& L, const dr_tensor& t, dr_tensor* o)
         *o = conv_out(t, L.conv);
         return DR_OK;
     case DR_LAYER_RELU: *o = t; return DR_OK;
+    case DR_LAYER_LAYERNORM:
+        if (!(L.layernorm.eps >= 0.f)) return fail(DR_ERR_SHAPE, "%s: layer normalisation's eps must be >= 0", who);
+        *o = t;
+        return DR_OK;
     case DR_LAYER_LRN:
         if (L.lrn.local_size < 1) return fail(DR_ERR_SHAPE, "%s: LRN local_size %d", who, L.lrn.local_size);
         *o = t;
@@ -1697,7 +1702,7 @@ int dr_net_create(const dr_layer_desc* layers, int n_layers, dr_net** out)
     if (!net) return fail(DR_ERR_HIP, "%s: out of host memory", who);
     net->layers.assign(layers, layers + n_layers);
     for (const dr_layer_desc& L : net->layers) {
-        if (L.kind < DR_LAYER_CONV || L.kind > DR_LAYER_CONV_LRN_MAXPOOL) {
+        if (L.kind < DR_LAYER_CONV || L.kind > DR_LAYER_LAYERNORM) {
             delete net;
             return fail(DR_ERR_UNSUPPORTED, "%s: unknown layer kind %d", who, L.kind);
         }
@@ -1806,8 +1811,8 @@ int dr_net_fwd(dr_net* net, const dr_tensor* xd, const void* x, const void* cons
         const dr_layer_desc& L = net->layers[i];
         const dr_tensor& od = plan.outs[i];
         const bool last = i + 1 == nl;
-        // ReLU runs in place unless it would overwrite the caller's input or is the last layer
-        const bool inplace = L.kind == DR_LAYER_RELU && cur_buf >= 0 && !last;
+        // ReLU and layer normalisation run in place unless they would overwrite the caller's input or are the last layer
+        const bool inplace = (L.kind == DR_LAYER_RELU || L.kind == DR_LAYER_LAYERNORM) && cur_buf >= 0 && !last;
         const int dst_buf = inplace ? cur_buf : (cur_buf == 0 ? 1 : 0);
         void* dst = last ? y : (void*)buf[dst_buf];
         Arena ar(scratch, plan.scratch_bytes, false);
@@ -1839,6 +1844,10 @@ int dr_net_fwd(dr_net* net, const dr_tensor* xd, const void* x, const void* cons
             break;
         case DR_LAYER_RELU: DR_TRY(launch_relu(t.dtype, cur, dst, tensor_elems(t), st)); break;
         case DR_LAYER_LRN: DR_TRY(launch_lrn(t, cur, dst, L.lrn, st)); break;
+        case DR_LAYER_LAYERNORM:
+            if (tensor_elems(t))
+                DR_TRY(launch_layernorm_fwd(t, cur, (const float*)params[pi], (const float*)params[pi + 1], L.layernorm.eps, L.layernorm.relu, dst, nullptr, nullptr, st));
+            break;
         case DR_LAYER_MAXPOOL: DR_TRY(launch_maxpool(t, cur, od, dst, L.pool, st)); break;
         case DR_LAYER_LRN_MAXPOOL:
         case DR_LAYER_MAXPOOL_LRN:

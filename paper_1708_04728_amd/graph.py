@@ -96,7 +96,7 @@ def net_descs(layers, c_in, inception_mode=0, fuse_relu=False, folded=False, pac
                conv - relu - lrn - maxpool run (3x3 pooling at stride 2, at most 192 filters, bf16) becomes the one
                kernel of dr_conv_lrn_maxpool_fwd, and a maxpool - lrn pair one pass as with True.
 
-    fuse_relu: a conv directly followed by a relu becomes one conv with the ReLU in its store
+    fuse_relu: a conv or a layernorm directly followed by a relu becomes one layer with the ReLU in its store
                (the slim form always runs this way; for the original form it is the "fused"
                variant reported next to the layer-by-layer one)."""
     out, c, i = [], c_in, 0
@@ -120,6 +120,11 @@ def net_descs(layers, c_in, inception_mode=0, fuse_relu=False, folded=False, pac
                 i += 1
         elif kind == "relu":
             L.kind = B.DR_LAYER_RELU
+        elif kind == "layernorm":
+            relu = fuse_relu and i + 1 < len(layers) and layers[i + 1][0] == "relu"
+            L.kind, L.layernorm = B.DR_LAYER_LAYERNORM, B.dr_layernorm(p["eps"], int(relu))
+            if relu:
+                i += 1
         elif kind == "lrn":
             L.kind, L.lrn = B.DR_LAYER_LRN, B.dr_lrn(p["n"], p["alpha"], p["beta"], p["k"])
             if fuse_nontensor == "all" and i + 1 < len(layers) and layers[i + 1][0] == "maxpool":
@@ -161,7 +166,7 @@ def stack_first_steps(layers, flat):
     buffer).  `flat` is the list flat_params returned for `layers` (w, bias per convolution / fc)."""
     out, i = list(flat), 0
     for kind, p in layers:
-        if kind in ("conv", "fc"):
+        if kind in ("conv", "fc", "layernorm"):
             i += 2
         elif kind == "inception":
             first, j = [], i
@@ -187,7 +192,7 @@ def stack_first_steps(layers, flat):
 
 def flat_params(params, dtype="f32", device="cuda", pack=False):
     """Device tensors in the order dr_net_fwd expects: conv/fc -> w, bias; bn -> gamma, beta,
-    mean, var (all fp32 except w).  pack: convolution filters whose channel count allows it are
+    mean, var; layernorm -> gamma, beta (all fp32 except w).  pack: convolution filters whose channel count allows it are
     reordered to KRSC by the library (must match the `pack` given to the descriptor builders)."""
     out = []
     for q in params:
@@ -197,5 +202,5 @@ def flat_params(params, dtype="f32", device="cuda", pack=False):
                 w = B.pack_filters(w)
             out += [w, to_device(q["b"], "f32", device)]
         else:
-            out += [to_device(q[k], "f32", device) for k in ("gamma", "beta", "mean", "var")]
+            out += [to_device(q[k], "f32", device) for k in ("gamma", "beta", "mean", "var") if k in q]
     return out

@@ -94,3 +94,15 @@ def test_binding_refuses():
         B.muon_params([(torch.zeros(3, 4), torch.zeros(3, 4, dtype=torch.bfloat16), torch.zeros(3, 4))])
     with pytest.raises(ValueError):
         B.muon_params([(torch.zeros(3, 4), torch.zeros(4, 3), torch.zeros(3, 4))])
+
+
+def test_networks_with_a_layer_normalisation():
+    from paper_1708_04728_amd import graph as G
+    layers = [("conv", {"k": 6, "r": 3, "s": 3, "stride": 1, "pad": 1}), ("layernorm", {"eps": 1e-5}), ("relu", {}), ("maxpool", {"k": 3, "stride": 2, "pad": 0})]
+    net, fused = B.Net(G.net_descs(layers, 4)), B.Net(G.net_descs(layers, 4, fuse_relu=True))
+    assert net.n_layers == 4 and fused.n_layers == 3 and net.num_params() == fused.num_params() == 4
+    d = net.output_desc(tensor(2, 4, 9, 9))
+    assert (d.n, d.c, d.h, d.w) == (2, 6, 4, 4)
+    bad = B.Net(G.net_descs([("layernorm", {"eps": -1.0})], 4))
+    with pytest.raises(B.DeepRebirthError):
+        bad.output_desc(tensor(2, 4, 9, 9))
