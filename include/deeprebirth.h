@@ -227,7 +227,8 @@ int dr_sgd_step(size_t count, float* w, const float* dw, float lr, void* stream)
  * Layer normalisation over the channels of every pixel (Ba, Kiros, Hinton 2016), in the place of the LRN or BatchNorm
  * layer that slimming removes: with the sums over the c channels of one pixel,
  *   y = gamma_c (x - mean) rstd + beta_c,  mean = sum x / c,  rstd = 1 / sqrt(sum (x - mean)^2 / c + eps),
- * then max(y, 0) if relu != 0.  Either order, fp32 or bf16; a matrix of rows is {rows, c, 1, 1}.  gamma, beta: fp32 device
+ * then max(y, 0) if relu != 0 (0 for a NaN, as in dr_relu).  Either order, fp32 or bf16; a matrix of rows is
+ * {rows, c, 1, 1}.  gamma, beta: fp32 device
  * vectors of c entries (NULL: ones, zeros).  mean, rstd: fp32 device arrays of n h w entries, in pixel order, that the
  * gradient reads (NULL: not stored).  Sums are held in fp32.  x == y (in place) is allowed.  eps >= 0. */
 typedef struct { float eps; int relu; } dr_layernorm;      /* of a network's layer */
@@ -250,7 +251,8 @@ int dr_layernorm_bwd(const dr_tensor* d, const void* dy, const void* x, const fl
  * count matrices of dtype (DR_F32 or DR_BF16), dense, row by row; ms, g, o: host arrays of count shapes / device
  * pointers (o[i] == g[i] is allowed).  Products and sums have the precision of fp32 for DR_F32 and of 16 bits and more for
  * DR_BF16, whatever the matrix units multiply.  A matrix of zeros stays zero; one that holds an infinity or a NaN
- * becomes NaN and touches no other.  1 <= steps <= DR_MAX_NS_STEPS, eps >= 0.  ws: device scratch of at least
+ * becomes NaN and touches no other.  1 <= steps <= DR_MAX_NS_STEPS, eps >= 0.  A matrix has at most 2^31-1 elements, a
+ * list less than 2^23 blocks of 32 x 32 (matrices padded to them).  ws: device scratch of at least
  * dr_orthogonalise_workspace_bytes, 256-byte aligned. */
 #define DR_MAX_NS_STEPS 64
 typedef struct { int rows, cols; } dr_matrix;

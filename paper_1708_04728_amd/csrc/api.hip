@@ -13,6 +13,7 @@
 
 #include "dr_internal.h"
 #include "inception_levels.h"
+#include "orthogonal_plan.h"
 
 namespace dr {
 
@@ -1572,10 +1573,13 @@ int dr_layernorm_bwd(const dr_tensor* d, const void* dy, const void* x, const fl
     return launch_layernorm_bwd(*d, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, (hipStream_t)stream);
 }
 
-static int check_matrix(const char* who, int i, int rows, int cols)
+// blocks: of the list's matrices so far, padded
+static int check_matrix(const char* who, int i, int rows, int cols, double* blocks)
 {
     if (rows < 0 || cols < 0) return fail(DR_ERR_SHAPE, "%s: matrix %d has a negative dimension (%d,%d)", who, i, rows, cols);
     if ((double)rows * cols >= 2147483648.0) return fail(DR_ERR_UNSUPPORTED, "%s: matrix %d has more than 2^31-1 elements", who, i);
+    *blocks += (double)(((size_t)rows + 31) / 32) * (((size_t)cols + 31) / 32);
+    if (*blocks > NS_MOST_BLOCKS) return fail(DR_ERR_UNSUPPORTED, "%s: matrices of more than 2^23 blocks of 32 x 32", who);
     return DR_OK;
 }
 static int check_matrices(const char* who, int count, const dr_matrix* ms, int dtype)
@@ -1583,24 +1587,16 @@ static int check_matrices(const char* who, int count, const dr_matrix* ms, int d
     if (count < 0) return fail(DR_ERR_SHAPE, "%s: count = %d", who, count);
     if (dtype != DR_F32 && dtype != DR_BF16) return fail(DR_ERR_UNSUPPORTED, "%s: unknown dtype %d", who, dtype);
     if (count && !ms) return fail(DR_ERR_NULL, "%s: ms is NULL", who);
-    double elements = 0;
-    for (int i = 0; i < count; ++i) {
-        DR_TRY(check_matrix(who, i, ms[i].rows, ms[i].cols));
-        elements += (double)ms[i].rows * ms[i].cols;
-    }
-    if (elements >= 2147483648.0) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^31-1 elements in all", who);
+    double blocks = 0;
+    for (int i = 0; i < count; ++i) DR_TRY(check_matrix(who, i, ms[i].rows, ms[i].cols, &blocks));
     return DR_OK;
 }
 static int check_muon_params(const char* who, int count, const dr_muon_param* params)
 {
     if (count < 0) return fail(DR_ERR_SHAPE, "%s: count = %d", who, count);
     if (count && !params) return fail(DR_ERR_NULL, "%s: params is NULL", who);
-    double elements = 0;
-    for (int i = 0; i < count; ++i) {
-        DR_TRY(check_matrix(who, i, params[i].rows, params[i].cols));
-        elements += (double)params[i].rows * params[i].cols;
-    }
-    if (elements >= 2147483648.0) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^31-1 elements in all", who);
+    double blocks = 0;
+    for (int i = 0; i < count; ++i) DR_TRY(check_matrix(who, i, params[i].rows, params[i].cols, &blocks));
     return DR_OK;
 }
 static int check_newton_schulz(const char* who, const dr_newton_schulz& ns)

@@ -24,6 +24,7 @@
 
 #include "dr_internal.h"
 #include "f32_pieces.h"
+#include "orthogonal_plan.h"
 
 namespace dr {
 namespace {
@@ -31,10 +32,8 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int BLOCK = 1024;                  // bytes of a block of 32 rows x 16 k of one piece
+constexpr int BLOCK = NS_BLOCK;
 constexpr int PITCH = 36;                    // floats of a row of 32 in LDS
-constexpr int SQUARES = 1024;                // most workgroups (and partial sums of squares) of a matrix
-enum { GRAM = 0, POLY = 1, APPLY = 2, PRODUCTS = 3 };
 
 // The matrices of a launch; arrays by what is looked up together.  A list is worked on JOBS at a time.  (N: room for as many.  A launch reads its arguments from memory, one after
 // the other where an index is among them: a single matrix has kernels whose arguments are its own.)
@@ -94,13 +93,6 @@ struct Operands {
     }
 };
 __device__ __forceinline__ size_t block_at(int P, int rb, int kblocks32, int kb32) { return ((size_t)rb * kblocks32 + kb32) * (2 * P * BLOCK); }
-
-// partial sums of squares of a matrix: workgroups of 256 threads, 16 elements each and more
-__host__ __device__ inline int squares_of(int rows, int cols)
-{
-    const size_t n = ((size_t)rows * cols + 4095) / 4096;
-    return (int)(n < SQUARES ? n : SQUARES);
-}
 
 __device__ __forceinline__ double sum256(double v, double* red)
 {
@@ -326,13 +318,13 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[P], const u32x4 (&b)[P
     }
 }
 
-// A product of small matrices: W waves share a tile of T x T blocks, every wave a W-th of the contraction.  Operands go straight to registers, AHEAD k-blocks of them
+// A product of small matrices: W waves share a tile of T x T blocks, every wave a W-th of the contraction.  Operands go straight to registers, some k-blocks of them
 // while as many are multiplied: what such a product waits for is its first operands.  splits > 1: as many workgroups share a tile, and leave sums for sum_kernel.
-template <int T> constexpr int ahead() { return T == 1 ? 4 : 2; }
 template <typename E, int P, int WHAT, int T, int W, bool MUON, int N>
 __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs<N> j, int turn, int last, int splits)
 {
-    constexpr int AHEAD = ahead<T>();
+    constexpr int KEEP = AHEAD[T == 1 ? FINE : DIRECT];
+    static_assert(W == WAVES[T == 1 ? FINE : DIRECT], "the plan's waves");
     __shared__ __attribute__((aligned(16))) float sums[W][T * T][32 * PITCH];
     const int unit = splits > 1 ? (int)blockIdx.x / splits : (int)blockIdx.x, part = (int)blockIdx.x - unit * splits;
     const Mat m = find_matrix(j, unit);
@@ -357,11 +349,11 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
         for (int k = 0; k < T; ++k)
 #pragma unroll
             for (int v = 0; v < 16; ++v) large[i][k][v] = small[i][k][v] = 0.f;
-    u32x4 a[2][AHEAD][T][P], b[2][AHEAD][T][P];
+    u32x4 a[2][KEEP][T][P], b[2][KEEP][T][P];
     auto fetch = [&](int kb0, auto set) __attribute__((always_inline)) {
         constexpr int S = decltype(set)::value;
 #pragma unroll
-        for (int n = 0; n < AHEAD; ++n) {
+        for (int n = 0; n < KEEP; ++n) {
             const size_t at = (size_t)min(kb0 + n * step, kblocks - 1) * P * BLOCK;
 #pragma unroll
             for (int i = 0; i < T; ++i)
@@ -375,7 +367,7 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
     auto products = [&](int kb0, auto set) __attribute__((always_inline)) {
         constexpr int S = decltype(set)::value;
 #pragma unroll
-        for (int n = 0; n < AHEAD; ++n) {
+        for (int n = 0; n < KEEP; ++n) {
             if (kb0 + n * step >= kblocks) break;
 #pragma unroll
             for (int i = 0; i < T; ++i)
@@ -385,11 +377,11 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
     };
     using std::integral_constant;
     fetch(mine, integral_constant<int, 0>{});
-    for (int kb = mine; kb < kblocks; kb += 2 * AHEAD * step) {
-        if (kb + AHEAD * step < kblocks) fetch(kb + AHEAD * step, integral_constant<int, 1>{});
+    for (int kb = mine; kb < kblocks; kb += 2 * KEEP * step) {
+        if (kb + KEEP * step < kblocks) fetch(kb + KEEP * step, integral_constant<int, 1>{});
         products(kb, integral_constant<int, 0>{});
-        if (kb + 2 * AHEAD * step < kblocks) fetch(kb + 2 * AHEAD * step, integral_constant<int, 0>{});
-        products(kb + AHEAD * step, integral_constant<int, 1>{});
+        if (kb + 2 * KEEP * step < kblocks) fetch(kb + 2 * KEEP * step, integral_constant<int, 0>{});
+        products(kb + KEEP * step, integral_constant<int, 1>{});
     }
     // register v holds row 8 (v / 4) + 4 half + v % 4 of column lane % 32
 #pragma unroll
@@ -624,7 +616,6 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
 // 64 rows and 352 columns, or 32 and 896: eight waves.  Nothing but the matrix is read or written, and a step is four barriers instead of three launches.  Vector
 // instructions bound it, most of them the cutting: with A and Q in fp32 too, cut by every wave that multiplies them, a step on 64 x 64 took 5.8 us, 1650 of them on its path.
 constexpr int WHOLE_BYTES = 163840 - 256;
-__host__ __device__ inline bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 11; }
 
 template <typename E, int P, bool MUON, int N>
 __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> j, int steps)
@@ -853,96 +844,7 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
     });
 }
 
-// ---- which kernel multiplies
-// Kernels for a product, by the blocks of a tile's side
-enum { FINE, DIRECT, TILE4, TILE6, TILE8, KERNELS };
-constexpr int SIDE[KERNELS] = {1, 2, 4, 6, 8};
-
-int tiles_of(int what, int mb, int nb, int T)
-{
-    const int tm = (mb + T - 1) / T, tn = (nb + T - 1) / T;
-    return what == APPLY ? tm * tn : tm * (tm + 1) / 2;
-}
-
-// What one launch of a product has to do: tiles and tiles x k-blocks for each side of a tile, the longest contraction
-struct Work {
-    int tiles[KERNELS], longest;
-    double blocks[KERNELS];
-    void add(int what, int mb, int nb)
-    {
-        const int kblocks = 2 * (what == GRAM ? nb : mb);
-        longest = std::max(longest, kblocks);
-        for (int k = 0; k < KERNELS; ++k) {
-            const int n = tiles_of(what, mb, nb, SIDE[k]);
-            tiles[k] += n;
-            blocks[k] += (double)n * kblocks;
-        }
-    }
-};
-
-// Microseconds that a launch takes, from 36 square and oblong shapes of 64 to 4096 rows in either number of pieces: what a round of workgroups costs beside its products;
-// a k-block on a compute unit by itself; what all of them multiply together, in blocks of 32 x 32 x 16 a microsecond; workgroups per compute unit.
-struct Cost { float round, kblock, rate; int slots; };
-constexpr Cost COSTS[2][KERNELS] = {
-    {{3.f, 0.065f, 3900.f, 1}, {5.f, 0.2f, 5100.f, 1}, {7.f, 0.42f, 6600.f, 2}, {12.f, 0.8f, 7450.f, 1}, {18.f, 1.45f, 7150.f, 1}},           // three pieces
-    {{2.6f, 0.045f, 5700.f, 1}, {4.f, 0.12f, 8500.f, 1}, {5.5f, 0.24f, 10200.f, 2}, {9.f, 0.45f, 12700.f, 1}, {12.5f, 0.8f, 13900.f, 1}},     // two
-};
-float cost_of(int P, int kernel, double tiles, double blocks, double longest)
-{
-    const Cost& c = COSTS[P == 3 ? 0 : 1][kernel];
-    const double area = SIDE[kernel] * SIDE[kernel], slots = (double)c.slots * device_cus(), each = blocks / tiles;
-    const double full = floor(tiles / slots), rest = tiles - full * slots;
-    auto time = [&](double n) { return n > 0 ? c.round + std::max(each * c.kblock, n * each * area / (c.rate * device_cus() / 256.0)) : 0.0; };
-    return (float)(1.0 + std::max(full * time(slots) + time(rest), (double)c.round + longest * c.kblock));
-}
-
-struct Choice { int kernel, splits; };
-Choice choose(int P, int what, const Work& w)
-{
-    Choice best{FINE, 1};
-    float least = 0.f;
-    for (int k = 0; k < KERNELS; ++k) {
-        const float t = cost_of(P, k, w.tiles[k], w.blocks[k], w.longest);
-        if (k == 0 || t < least) { least = t; best = Choice{k, 1}; }
-    }
-    if (what != GRAM) return best;
-    // few tiles of long rows: up to a workgroup per compute unit, with eight waves' (four waves') k-blocks in flight at once at least; the sums take a launch of 4 us
-    for (int k = FINE; k <= DIRECT; ++k) {
-        const int waves = k == FINE ? 8 : 4, splits = std::min(device_cus() / std::max(w.tiles[k], 1), w.longest / (waves * (k == FINE ? ahead<1>() : ahead<2>())));
-        if (splits < 2) continue;
-        const float t = 4.f + cost_of(P, k, (double)w.tiles[k] * splits, w.blocks[k], (double)w.longest / splits);
-        if (t < least) { least = t; best = Choice{k, splits}; }
-    }
-    return best;
-}
-size_t partial_bytes(const Choice& c, const Work& w) { return c.splits > 1 ? (size_t)w.tiles[c.kernel] * c.splits * SIDE[c.kernel] * SIDE[c.kernel] * 1024 * sizeof(float) : 0; }
-
-// ---- the plan of a call: made in the same way to size the workspace and to run
-size_t operand_bytes(int mb, int nb, int P) { return ((size_t)3 * mb * nb + (size_t)2 * mb * mb) * 2 * P * BLOCK; }
-
-// The matrices that one sequence of launches works on: JOBS of a list, its empty ones left out
-struct Group {
-    Work work[PRODUCTS];
-    int count;
-    bool whole;                              // all of them fit the LDS of a workgroup
-    size_t squares, operands, partial;       // bytes
-    void start() { *this = Group{}; whole = true; }
-    void add(int rows, int cols, int P)
-    {
-        const int mb = (std::min(rows, cols) + 31) / 32, nb = (std::max(rows, cols) + 31) / 32;
-        for (int w = 0; w < PRODUCTS; ++w) work[w].add(w, mb, nb);
-        ++count;
-        whole = whole && whole_fits(mb, nb);
-        squares += squares_of(rows, cols) * sizeof(double);
-        operands += operand_bytes(mb, nb, P);
-    }
-    size_t bytes(int P) const
-    {
-        if (whole) return 256;               // (none is used)
-        return align_up(squares, 1024) + operands + partial_bytes(choose(P, GRAM, work[GRAM]), work[GRAM]);
-    }
-};
-
+// ---- a call
 template <class Shape>
 size_t workspace_bytes(int count, int P, Shape shape)
 {
@@ -954,7 +856,7 @@ size_t workspace_bytes(int count, int P, Shape shape)
         shape(i, rows, cols);
         if (rows && cols) g.add(rows, cols, P);
         if (g.count == JOBS || (i + 1 == count && g.count)) {
-            most = std::max(most, g.bytes(P));
+            most = std::max(most, g.bytes(P, device_cus()));
             g.start();
         }
     }
@@ -999,7 +901,7 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
         return check_launch("orthogonalise");
     }
     c.squares = (double*)ws;
-    c.ws = (unsigned char*)ws + align_up(group.squares, 1024);
+    c.ws = (unsigned char*)ws + group.squares_bytes();
     c.partial = (float*)(c.ws + group.operands);
     size_t operands = 0;
     int squares_at = 0;
@@ -1020,7 +922,7 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
         constexpr int WHAT = decltype(what)::value;
         constexpr bool END = WHAT == APPLY && MUON;      // (the other products are the same for every result)
         typedef std::conditional_t<WHAT == APPLY, E, float> R;
-        const Choice choice = choose(P, WHAT, group.work[WHAT]);
+        const Choice choice = choose(P, WHAT, group.work[WHAT], device_cus());
         const unsigned tiles = number(j, group.count, orders[WHAT], [&](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, SIDE[choice.kernel]); });
         auto direct = [&](auto side, auto waves) {
             constexpr int T = decltype(side)::value, W = decltype(waves)::value;

@@ -1,0 +1,117 @@
+// Which kernel multiplies the matrices of a launch of orthogonal.hip, and how much scratch they take.  Plain C++, so that the same lines run in the launcher and in a test
+// on the host.
+#pragma once
+#include <math.h>
+#include <stddef.h>
+
+#include <algorithm>
+
+namespace dr {
+
+constexpr int NS_BLOCK = 1024;               // bytes of a block of 32 rows x 16 k of one piece of an operand
+constexpr int SQUARES = 1024;                // most workgroups (and partial sums of squares) of a matrix
+enum { GRAM = 0, POLY = 1, APPLY = 2, PRODUCTS = 3 };
+
+// partial sums of squares of a matrix: workgroups of 256 threads, 16 elements each and more
+constexpr int squares_of(int rows, int cols)
+{
+    return (int)std::min<size_t>(SQUARES, ((size_t)rows * cols + 4095) / 4096);
+}
+
+// matrices that fit the LDS of one workgroup: blocks of 32 of the short and of the long side
+constexpr bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 11; }
+
+// blocks of 32 x 32 that a launch may have: its workgroups of 512 threads are counted in 32 bits
+constexpr double NS_MOST_BLOCKS = 8388607;
+
+// Kernels for a product, by the blocks of a tile's side; k-blocks that a wave of the first two has in flight, and their waves
+enum { FINE, DIRECT, TILE4, TILE6, TILE8, KERNELS };
+constexpr int SIDE[KERNELS] = {1, 2, 4, 6, 8}, AHEAD[] = {4, 2}, WAVES[] = {8, 4};
+
+inline int tiles_of(int what, int mb, int nb, int T)
+{
+    const int tm = (mb + T - 1) / T, tn = (nb + T - 1) / T;
+    return what == APPLY ? tm * tn : tm * (tm + 1) / 2;
+}
+
+// What one launch of a product has to do: tiles and tiles x k-blocks for each side of a tile, the longest contraction
+struct Work {
+    int tiles[KERNELS], longest;
+    double blocks[KERNELS];
+    void add(int what, int mb, int nb)
+    {
+        const int kblocks = 2 * (what == GRAM ? nb : mb);
+        longest = std::max(longest, kblocks);
+        for (int k = 0; k < KERNELS; ++k) {
+            const int n = tiles_of(what, mb, nb, SIDE[k]);
+            tiles[k] += n;
+            blocks[k] += (double)n * kblocks;
+        }
+    }
+};
+
+// Microseconds that a launch takes, from 36 square and oblong shapes of 64 to 4096 rows in either number of pieces: what a round of workgroups costs beside its products;
+// a k-block on a compute unit by itself; what all of them multiply together, in blocks of 32 x 32 x 16 a microsecond; workgroups per compute unit.
+struct Cost { float round, kblock, rate; int slots; };
+constexpr Cost COSTS[2][KERNELS] = {
+    {{3.f, 0.065f, 3900.f, 1}, {5.f, 0.2f, 5100.f, 1}, {7.f, 0.42f, 6600.f, 2}, {12.f, 0.8f, 7450.f, 1}, {18.f, 1.45f, 7150.f, 1}},           // three pieces
+    {{2.6f, 0.045f, 5700.f, 1}, {4.f, 0.12f, 8500.f, 1}, {5.5f, 0.24f, 10200.f, 2}, {9.f, 0.45f, 12700.f, 1}, {12.5f, 0.8f, 13900.f, 1}},     // two
+};
+inline float cost_of(int P, int kernel, double tiles, double blocks, double longest, int cus)
+{
+    const Cost& c = COSTS[P == 3 ? 0 : 1][kernel];
+    const double area = SIDE[kernel] * SIDE[kernel], slots = (double)c.slots * cus, each = blocks / tiles;
+    const double full = floor(tiles / slots), rest = tiles - full * slots;
+    auto time = [&](double n) { return n > 0 ? c.round + std::max(each * c.kblock, n * each * area / (c.rate * cus / 256.0)) : 0.0; };
+    return (float)(1.0 + std::max(full * time(slots) + time(rest), (double)c.round + longest * c.kblock));
+}
+
+struct Choice { int kernel, splits; };
+inline Choice choose(int P, int what, const Work& w, int cus)
+{
+    Choice best{FINE, 1};
+    float least = 0.f;
+    for (int k = 0; k < KERNELS; ++k) {
+        const float t = cost_of(P, k, w.tiles[k], w.blocks[k], w.longest, cus);
+        if (k == 0 || t < least) { least = t; best = Choice{k, 1}; }
+    }
+    if (what != GRAM) return best;
+    // few tiles of long rows: up to a workgroup per compute unit, with eight waves' (four waves') k-blocks in flight at once at least; the sums take a launch of 4 us
+    for (int k = FINE; k <= DIRECT; ++k) {
+        const int splits = std::min(cus / std::max(w.tiles[k], 1), w.longest / (WAVES[k] * AHEAD[k]));
+        if (splits < 2) continue;
+        const float t = 4.f + cost_of(P, k, (double)w.tiles[k] * splits, w.blocks[k], (double)w.longest / splits, cus);
+        if (t < least) { least = t; best = Choice{k, splits}; }
+    }
+    return best;
+}
+inline size_t partial_bytes(const Choice& c, const Work& w) { return c.splits > 1 ? (size_t)w.tiles[c.kernel] * c.splits * SIDE[c.kernel] * SIDE[c.kernel] * 1024 * sizeof(float) : 0; }
+
+// Operands of a matrix: X, X^T twice, A, Q
+inline size_t operand_bytes(int mb, int nb, int P) { return ((size_t)3 * mb * nb + (size_t)2 * mb * mb) * 2 * P * NS_BLOCK; }
+
+// The matrices that one sequence of launches works on: some of a list, its empty ones left out; made in the same way to size the workspace and to run
+struct Group {
+    Work work[PRODUCTS];
+    int count;
+    bool whole;                              // all of them fit the LDS of a workgroup
+    size_t squares, operands, partial;       // bytes
+    size_t squares_bytes() const { return (squares + 1023) / 1024 * 1024; }
+    void start() { *this = Group{}; whole = true; }
+    void add(int rows, int cols, int P)
+    {
+        const int mb = (std::min(rows, cols) + 31) / 32, nb = (std::max(rows, cols) + 31) / 32;
+        for (int w = 0; w < PRODUCTS; ++w) work[w].add(w, mb, nb);
+        ++count;
+        whole = whole && whole_fits(mb, nb);
+        squares += squares_of(rows, cols) * sizeof(double);
+        operands += operand_bytes(mb, nb, P);
+    }
+    size_t bytes(int P, int cus) const
+    {
+        if (whole) return 256;               // (none is used)
+        return squares_bytes() + operands + partial_bytes(choose(P, GRAM, work[GRAM], cus), work[GRAM]);
+    }
+};
+
+}  // namespace dr

@@ -259,6 +259,48 @@ def test_rows_that_are_hard(dtype, order, c):
     assert torch.equal(a[1][1:], b[1][1:]) and torch.equal(a[2][1:], b[2][1:]) and not torch.isfinite(b[2][0])
 
 
+@pytest.mark.parametrize("n,c,hw,dtype,order", ((1, 1030, (2 ** 20 + 3, 1), "f32", "nhwc"), (1, 1030, (2 ** 20 + 5, 1), "bf16", "nhwc"), (2, 8192, (301, 300), "f32", "nchw"), (6000, 192, (31, 31), "f32", "nchw")))
+def test_offsets_beyond_32_bits(n, c, hw, dtype, order):
+    """More than 4 GiB (2 GiB in bf16), and planes whose 64 pixels reach that far: pixels from all over against the formulas, dgamma and dbeta against sums in 64 bits on the GPU."""
+    k = Case(n, c, *hw, dtype, order)
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x, dy = (torch.empty(k.shape, dtype=k.dtype, device="cuda").normal_(generator=gen) for _ in range(2))
+    rng = np.random.default_rng(5)
+    gamma, beta = vectors(c, rng)
+    pixels = n * hw[0] * hw[1]
+    at = torch.from_numpy(np.unique(np.concatenate([[0, 1, pixels - 2, pixels - 1], rng.integers(0, pixels, 400)]))).cuda()
+    some = Case(len(at), c, 1, 1, dtype, "nhwc")
+
+    def chosen(t):
+        t = t.view(pixels, c)[at] if order == "nhwc" else t.view(n, c, -1)[at // (hw[0] * hw[1]), :, at % (hw[0] * hw[1])]
+        return t.view(some.shape)
+
+    y, mean, rstd = forward(k, x, gamma, beta, True)
+    check_forward(some, chosen(x), gamma, beta, True, chosen(y), mean[at], rstd[at])
+    del y
+    dx, dgamma, dbeta = gradient(k, dy, x, gamma, mean, rstd)
+    check_gradient(some, chosen(dy), chosen(x), gamma, mean[at], rstd[at], chosen(dx), None, None)
+    del dx
+    refs, mags = torch.zeros((2, c), dtype=torch.float64, device="cuda"), torch.zeros((3, c), dtype=torch.float64, device="cuda")
+    flat = [t.view(1, pixels, c) if order == "nhwc" else t.view(n, c, -1) for t in (x, dy)]
+    stats = [t.double().view(n, -1) for t in (mean, rstd)]
+    step = 2 ** 15 if order == "nhwc" else 2 ** 13
+    for i in range(flat[0].shape[0]):
+        length = pixels // flat[0].shape[0]
+        for p in range(0, length, step):
+            if order == "nhwc":
+                a, b = (t[0, p:p + step].double() for t in flat)
+            else:
+                a, b = (t[i, :, p:p + step].t().double() for t in flat)
+            m, r = (t[i, p:p + step, None] for t in stats)
+            z = (a - m) * r
+            refs += torch.stack(((b * z).sum(0), b.sum(0)))
+            mags += torch.stack(((b * z).abs().sum(0), b.abs().sum(0), (b.abs() * (3 * U * z.abs() + U * a.abs() * r)).sum(0)))
+    chains = 32 + pixels / 256 + 16
+    assert note("dgamma", ((dgamma.double() - refs[0]).abs() / (chains * U * mags[0] + mags[2])).max().item(), 1.0)
+    assert note("dbeta", ((dbeta.double() - refs[1]).abs() / (chains * U * mags[1])).max().item(), 1.0)
+
+
 def test_tensors_without_elements():
     for shape in ((0, 8, 3, 3), (2, 8, 0, 3), (0, 8, 1, 1)):
         for k in (Case(*shape, "f32", "nchw"), Case(*shape, "bf16", "nhwc")):

@@ -72,6 +72,29 @@ SHAPES = [(1, 1), (1, 7), (7, 1), (2, 3), (16, 16), (31, 33), (32, 32), (33, 31)
           (129, 129), (500, 301), (256, 2400), (384, 864), (700, 1300), (1300, 700), (1000, 1024), (64, 20000), (1500, 1501)]
 
 
+# shared contractions and the largest tiles, the reference in 64 bits on the GPU (products of torch)
+LARGE = [(500, 6000), (33000, 250), (1024, 4000), (2049, 2500), (2700, 2600), (3300, 3700), (4160, 4100), (4300, 4500)]
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("shape", LARGE)
+def test_orthogonalise_large(shape, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(case_seed(shape))
+    pixels = min(shape) + 500
+    g = ((torch.randn((shape[0], pixels), device="cuda", generator=gen) @ torch.randn((pixels, shape[1]), device="cuda", generator=gen).abs())).to(DTYPES[dtype])
+    got, = run([g])
+    a, b, c = COEFFICIENTS
+    x = g.double().t() if shape[0] > shape[1] else g.double()
+    x = x / (x.norm() + EPS)
+    for _ in range(5):
+        p = x @ x.t()
+        x = a * x + (b * p + c * (p @ p)) @ x
+    ref = x.t() if shape[0] > shape[1] else x
+    tol = 6 * a ** 5 * (2.0 ** -17 if dtype == "bf16" else 2.0 ** -23) + (2.0 ** -8 * ref.norm().item() if dtype == "bf16" else 0)
+    again, = run([g])
+    assert torch.equal(got, again)
+
+
 @pytest.mark.parametrize("dtype", ("f32", "bf16"))
 @pytest.mark.parametrize("shape", SHAPES)
 def test_orthogonalise(shape, dtype):
