@@ -429,6 +429,120 @@ __device__ __forceinline__ void lds_barrier()        // orders LDS traffic only
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
+__device__ __forceinline__ void wave_lds()           // orders a wave's LDS traffic between its lanes
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Q and Q X in one launch, for matrices of few rows: a workgroup makes one block of X, and for it the blocks of Q of its rows, a wave each, which stay in LDS.  A's rows that
+// all of these share come through LDS (each wave loading them for itself, 192 x 576 takes 92 us for 87: a compute unit reads 64 bytes a cycle from beyond it), the other
+// factor straight to registers, KEEP k-blocks of it while as many are multiplied.  Waits in a row bound it: loads, the products of a wave, a barrier, products, a barrier.
+template <typename E, int P, bool MUON, int N>
+__global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Jobs<N> j, int turn, int last)
+{
+    constexpr int W = 8, KEEP = 4;
+    static_assert(NS_JOINED_ROWS <= W, "a wave for each block of Q");
+    __shared__ __attribute__((aligned(16))) float sums[W][32 * PITCH];
+    __shared__ __attribute__((aligned(16))) unsigned char q[2 * NS_JOINED_ROWS * P * BLOCK], arows[2 * NS_JOINED_ROWS * P * BLOCK];
+    const Mat m = find_matrix(j, blockIdx.x);
+    const Operands<P> op(c, j, m);
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5, kblocks = 2 * m.mb;
+    int bi, bj;
+    tile_blocks<APPLY, 1>(m, (int)blockIdx.x - m.first, bi, bj);
+    const unsigned char* const rows = op.a + (size_t)bi * kblocks * P * BLOCK + lane * 16;
+    const unsigned char* const others = op.a + (size_t)min(wave, m.mb - 1) * kblocks * P * BLOCK + lane * 16;
+    const unsigned char* const right = (turn ? op.xt1 : op.xt0) + (size_t)bj * kblocks * P * BLOCK + lane * 16;
+    auto load = [](const unsigned char* from, int kb, u32x4 (&to)[P]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < P; ++e) to[e] = *reinterpret_cast<const u32x4*>(from + (kb * P + e) * BLOCK);
+    };
+    f32x16 large, small;
+    auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) large[v] = small[v] = 0.f;
+    };
+    auto leave = [&]() __attribute__((always_inline)) {      // register v holds row 8 (v / 4) + 4 half + v % 4 of column lane % 32
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sums[wave][(8 * (v >> 2) + 4 * half + (v & 3)) * PITCH + l32] = large[v] + small[v];
+    };
+    u32x4 mine[2][P], b[2][KEEP][P], x[2][P];      // k-blocks wave and wave + 8 of A's rows; A's rows that give this wave's block of Q; k-blocks wave and wave + 8 of X
+    auto fetch = [&](int kb0, auto set) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < KEEP; ++n) load(others, min(kb0 + n, kblocks - 1), b[decltype(set)::value][n]);
+    };
+    using std::integral_constant;
+#pragma unroll
+    for (int n = 0; n < 2; ++n) load(rows, min(wave + n * W, kblocks - 1), mine[n]);
+    fetch(0, integral_constant<int, 0>{});
+#pragma unroll
+    for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+            if (wave + n * W < kblocks) *reinterpret_cast<u32x4*>(arows + ((wave + n * W) * P + e) * BLOCK + lane * 16) = mine[n][e];
+    lds_barrier();
+    if (wave < m.mb) {
+        clear();
+        auto products = [&](int kb0, auto set) __attribute__((always_inline)) {
+#pragma unroll
+            for (int n = 0; n < KEEP; ++n) {
+                if (kb0 + n >= kblocks) break;
+                u32x4 a[P];
+                load(arows + lane * 16, kb0 + n, a);
+                multiply<P>(a, b[decltype(set)::value][n], large, small);
+            }
+        };
+        for (int kb = 0; kb < kblocks; kb += 2 * KEEP) {
+            if (kb + KEEP < kblocks) fetch(kb + KEEP, integral_constant<int, 1>{});
+            products(kb, integral_constant<int, 0>{});
+            if (kb + 2 * KEEP < kblocks) fetch(kb + 2 * KEEP, integral_constant<int, 0>{});
+            products(kb + KEEP, integral_constant<int, 1>{});
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < 2; ++n) load(right, min(wave + n * W, kblocks - 1), x[n]);
+    if (wave < m.mb) {
+        leave();
+        wave_lds();
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+            float v[8], w[8];
+            const int diagonal = wave * 32 + n * 16 + half * 8 - bi * 32 - l32;
+            u32x4 own[P];
+            load(arows + lane * 16, 2 * wave + n, own);
+            operand8<false>(sums[wave], n, v);
+            join8<P>(own, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = c.b * w[e] + c.c * v[e] + (diagonal + e == 0 ? c.a : 0.f);
+            put8<P>(v, q + 2 * wave * P * BLOCK, n);
+        }
+    }
+    __syncthreads();
+    clear();
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int kb = wave + n * W;
+        if (kb >= kblocks) break;
+        u32x4 a[P];
+#pragma unroll
+        for (int e = 0; e < P; ++e) a[e] = *reinterpret_cast<const u32x4*>(q + (kb * P + e) * BLOCK + lane * 16);
+        multiply<P>(a, x[n], large, small);
+    }
+    leave();
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        const int i = n * 512 + threadIdx.x, at = (i >> 5) * PITCH + (i & 31);
+        float s = 0.f;
+#pragma unroll
+        for (int w = 0; w < W; ++w) s += sums[w][at];
+        sums[0][at] = s;
+    }
+    __syncthreads();
+    if (last) finish_result<E, MUON, N>(c, j, m, sums[0], bi, bj, wave * 2 + half, 2 * W);
+    else if (wave < 4) finish_task<P, APPLY>(c, m, op, sums[0], bi, bj, turn, wave);
+}
+
 // Adds the sums that the workgroups of a tile have left, in their order
 template <typename E, int P, int WHAT, int T, bool MUON, int N>
 __global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j, int turn, int last, int splits)
@@ -944,6 +1058,11 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
     for (int s = 0; s < steps; ++s) {
         const int last = s + 1 == steps;
         product(integral_constant<int, GRAM>{}, s & 1, last);
+        if (group.joined(device_cus())) {
+            const unsigned tiles = number(j, group.count, orders[APPLY], [](int mb, int nb, int, int) { return mb * nb; });
+            hipLaunchKernelGGL((poly_apply_kernel<E, P, MUON, N>), dim3(tiles), dim3(512), 0, st, c, j, s & 1, last);
+            continue;
+        }
         product(integral_constant<int, POLY>{}, s & 1, last);
         product(integral_constant<int, APPLY>{}, s & 1, last);
     }

@@ -21,6 +21,9 @@ constexpr int squares_of(int rows, int cols)
 // matrices that fit the LDS of one workgroup: blocks of 32 of the short and of the long side
 constexpr bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 11; }
 
+// a matrix whose products Q and Q X may be one launch has as many blocks of 32 rows at most
+constexpr int NS_JOINED_ROWS = 8;
+
 // blocks of 32 x 32 that a launch may have: its workgroups of 512 threads are counted in 32 bits
 constexpr double NS_MOST_BLOCKS = 8388607;
 
@@ -93,7 +96,7 @@ inline size_t operand_bytes(int mb, int nb, int P) { return ((size_t)3 * mb * nb
 // The matrices that one sequence of launches works on: some of a list, its empty ones left out; made in the same way to size the workspace and to run
 struct Group {
     Work work[PRODUCTS];
-    int count;
+    int count, most_mb;
     bool whole;                              // all of them fit the LDS of a workgroup
     size_t squares, operands, partial;       // bytes
     size_t squares_bytes() const { return (squares + 1023) / 1024 * 1024; }
@@ -103,10 +106,15 @@ struct Group {
         const int mb = (std::min(rows, cols) + 31) / 32, nb = (std::max(rows, cols) + 31) / 32;
         for (int w = 0; w < PRODUCTS; ++w) work[w].add(w, mb, nb);
         ++count;
+        most_mb = std::max(most_mb, mb);
         whole = whole && whole_fits(mb, nb);
         squares += squares_of(rows, cols) * sizeof(double);
         operands += operand_bytes(mb, nb, P);
     }
+    // Q and Q X in one launch, a workgroup for each 32 x 32 of X: each makes its rows of Q for itself, which costs less than a launch as long as the workgroups come in one
+    // round (two, where Q has 64 rows).  Measured, two launches -> one, fp32: 64 x 1728 101 -> 81 us, 64 x 8192 122 -> 112, 128 x 2048 107 -> 93, 128 x 6144 (768 workgroups)
+    // 139 -> 160, 192 x 576 95 -> 87, 256 x 1024 108 -> 108, 256 x 1536 (384) 133 -> 152; bf16: 192 x 576 75 -> 69, 256 x 1024 88 -> 81
+    bool joined(int cus) const { return !whole && most_mb <= NS_JOINED_ROWS && work[APPLY].tiles[FINE] <= (most_mb <= 2 ? 2 : 1) * cus; }
     size_t bytes(int P, int cus) const
     {
         if (whole) return 256;               // (none is used)

@@ -22,7 +22,7 @@ int main()
             if (scanf("%d %d", &rows, &cols) != 2) return 1;
             g.add(rows, cols, pieces);
         }
-        printf("%d %zu", g.whole, g.bytes(pieces, cus));
+        printf("%d %d %zu", g.whole, g.joined(cus), g.bytes(pieces, cus));
         for (int w = 0; w < dr::PRODUCTS; ++w) {
             const dr::Choice c = dr::choose(pieces, w, g.work[w], cus);
             printf(" %d %d %d %d", c.kernel, c.splits, g.work[w].tiles[c.kernel], g.work[w].longest);
@@ -55,8 +55,10 @@ def blocks(v):
 
 def check(case, plan):
     cus, pieces, shapes = case
-    whole, need, *products = plan
+    whole, joined, need, *products = plan
     assert bool(whole) == all((blocks(min(s)) == 1 and blocks(max(s)) <= 28) or (blocks(min(s)) == 2 and blocks(max(s)) <= 11) for s in shapes), case
+    if joined:
+        assert not whole and all(blocks(min(s)) <= 8 for s in shapes) and sum(blocks(min(s)) * blocks(max(s)) for s in shapes) <= 2 * cus, case
     square = lambda s: -(-min(s[0] * s[1], 4096 * 1024) // 4096)
     operands = sum((3 * blocks(min(s)) * blocks(max(s)) + 2 * blocks(min(s)) ** 2) * 2 * pieces * 1024 for s in shapes)
     for w in range(3):
@@ -72,7 +74,7 @@ def check(case, plan):
         squares = -(-8 * sum(square(s) for s in shapes) // 1024) * 1024
         kernel, splits, tiles, _ = products[:4]
         assert need == squares + operands + (tiles * splits * SIDE[kernel] ** 2 * 4096 if splits > 1 else 0), case
-    return products
+    return joined, products
 
 
 def test_choices_are_consistent(ask):
@@ -87,12 +89,12 @@ def test_the_gpu_tests_reach_every_kernel(ask):
     """... in either number of pieces, for a symmetric product and for the other, and with a contraction that workgroups share."""
     from test_gpu_orthogonal import LARGE, SHAPES
     for pieces in (2, 3):
-        seen, shared, whole = set(), set(), False
+        seen, shared, whole, together = set(), set(), False, False
         for shape, plan in zip(SHAPES + LARGE, ask([(256, pieces, [s]) for s in SHAPES + LARGE])):
-            products = check((256, pieces, [shape]), plan)
-            whole = whole or plan[0]
+            joined, products = check((256, pieces, [shape]), plan)
+            whole, together = whole or plan[0], together or joined
             if not plan[0]:
-                seen |= {(products[4 * w], w == 2) for w in range(3)}
+                seen |= {(products[4 * w], w == 2) for w in ((0,) if joined else range(3))}
                 shared |= {products[0]} if products[1] > 1 else set()
-        assert whole and seen == {(k, w) for k in range(5) for w in (False, True)}, (pieces, sorted(seen))
+        assert whole and together and seen == {(k, w) for k in range(5) for w in (False, True)}, (pieces, sorted(seen))
         assert shared == {0, 1}, (pieces, shared)
