@@ -243,30 +243,57 @@ def _ptrs(ts, n=1):
     return pack(*v)
 
 
-def _vector(t):
-    """Pointer of a contiguous fp32 tensor, or NULL."""
-    if t is None:
-        return None
-    if t.dtype != torch.float32:
-        raise TypeError("vectors are fp32")
-    if not t.is_contiguous():
-        raise ValueError("tensor must be contiguous")
-    return t.data_ptr()
+_ALIKE = "tensors of one call share shape, dtype and order"
 
 
-def _like(t, x):
-    """Pointer of a tensor with x's shape, dtype and order, or NULL."""
-    if t is None:
-        return None
-    if isinstance(t, NHWC) != isinstance(x, NHWC):
-        raise ValueError("tensors of one call share shape, dtype and order")
-    if isinstance(t, NHWC):
-        t, x = t.t, x.t
-    if t.dtype is not x.dtype or t.shape != x.shape:
-        raise ValueError("tensors of one call share shape, dtype and order")
-    if not t.is_contiguous():
+def _alike(x, *others):
+    """dr_tensor of x, then the pointers of x and of others like it (None: NULL)."""
+    if isinstance(x, NHWC):
+        x = x.t
+        n, h, w, c = shape = x.shape
+        layout, kind = DR_NHWC, NHWC
+    else:
+        shape = x.shape
+        n, c, h, w = shape if len(shape) == 4 else (tuple(shape) + (1, 1, 1, 1))[:4]
+        layout, kind = DR_NCHW, None
+    dtype = x.dtype
+    if not x.is_contiguous():
         raise ValueError("tensor must be contiguous")
-    return t.data_ptr()
+    out = [dr_tensor(n, c, h, w, _dtype_code(x), layout), x.data_ptr()]
+    for t in others:
+        if t is None:
+            out.append(None)
+            continue
+        if kind is None:
+            if isinstance(t, NHWC):
+                raise ValueError(_ALIKE)
+        elif isinstance(t, NHWC):
+            t = t.t
+        else:
+            raise ValueError(_ALIKE)
+        if t.dtype is not dtype or t.shape != shape:
+            raise ValueError(_ALIKE)
+        if not t.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+        out.append(t.data_ptr())
+    return out
+
+
+def _vectors(n, *ts):
+    """Pointers of contiguous fp32 tensors of n entries (None: NULL)."""
+    out = []
+    for t in ts:
+        if t is None:
+            out.append(None)
+            continue
+        if t.dtype is not torch.float32:
+            raise TypeError("vectors are fp32")
+        if t.numel() != n:
+            raise ValueError("vectors have an entry for each channel, statistics one for each pixel")
+        if not t.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+        out.append(t.data_ptr())
+    return out
 
 
 def _nbytes(t):
@@ -483,7 +510,12 @@ def sgd_step(w, dw, lr, stream=None):
 
 def layernorm_fwd(x, gamma, beta, eps, relu, y, mean=None, rstd=None, stream=None):
     """y = layer normalisation of x over its channels (then ReLU if relu); mean, rstd: fp32 tensors of n * h * w entries for layernorm_bwd, or None."""
-    _check(lib().dr_layernorm_fwd(desc(x), _ptr(x), _vector(gamma), _vector(beta), eps, int(relu), _like(y, x), _vector(mean), _vector(rstd), _stream(stream)))
+    d, px, py = _alike(x, y)
+    g, b = _vectors(d.c, gamma, beta)
+    m, r = _vectors(d.n * d.h * d.w, mean, rstd) if mean is not None or rstd is not None else (None, None)
+    rc = lib().dr_layernorm_fwd(d, px, g, b, eps, int(relu), py, m, r, _stream(stream))
+    if rc:
+        _check(rc)
     return y
 
 
@@ -495,8 +527,10 @@ def layernorm_bwd_workspace_bytes(x):
 
 def layernorm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
     """dx, dgamma, dbeta (each may be None) from dy and the forward pass's x, mean and rstd."""
-    _check(lib().dr_layernorm_bwd(desc(x), _like(dy, x), _ptr(x), _vector(gamma), _vector(mean), _vector(rstd), _like(dx, x), _vector(dgamma), _vector(dbeta),
-                                  _ptr(ws), _nbytes(ws), _stream(stream)))
+    d, px, pdy, pdx = _alike(x, dy, dx)
+    g, dg, db = _vectors(d.c, gamma, dgamma, dbeta)
+    m, r = _vectors(d.n * d.h * d.w, mean, rstd)
+    _check(lib().dr_layernorm_bwd(d, pdy, px, g, m, r, pdx, dg, db, _ptr(ws), _nbytes(ws), _stream(stream)))
     return dx, dgamma, dbeta
 
 

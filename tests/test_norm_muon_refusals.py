@@ -82,6 +82,17 @@ def test_binding_refuses():
         B.layernorm_fwd(t, None, None, 1e-5, False, B.NHWC(t))
     with pytest.raises(TypeError):
         B.layernorm_fwd(t, torch.zeros(4, dtype=torch.float64), None, 1e-5, False, t)
+    for vectors in ((torch.zeros(3), None), (None, torch.zeros(5)), (torch.zeros(8)[::2], None)):
+        with pytest.raises(ValueError):
+            B.layernorm_fwd(t, *vectors, 1e-5, False, t)
+    pixels = torch.zeros(2, 3, 3)
+    for mean, rstd in ((pixels, torch.zeros(17)), (torch.zeros(19), pixels)):
+        with pytest.raises(ValueError):
+            B.layernorm_fwd(t, None, None, 1e-5, False, t, mean, rstd)
+        with pytest.raises(ValueError):
+            B.layernorm_bwd(t, t, None, mean, rstd, t.clone(), None, None, None)
+    with pytest.raises(ValueError):
+        B.layernorm_bwd(t, t, None, pixels, pixels, t.clone(), torch.zeros(5), None, None)
     with pytest.raises(ValueError):
         B.orthogonalise([torch.zeros(3, 4)], [torch.zeros(4, 3)], None)
     with pytest.raises(TypeError):
