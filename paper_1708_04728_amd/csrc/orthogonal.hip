@@ -726,9 +726,11 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
         }
 }
 
-// ---- matrices small enough for one workgroup's LDS: the whole iteration there, X in fp32, cut into pieces where it is multiplied, A and Q in pieces, as operands
-// 64 rows and 352 columns, or 32 and 896: eight waves.  Nothing but the matrix is read or written, and a step is four barriers instead of three launches.  Vector
+// ---- matrices small enough for one workgroup's LDS: the whole iteration there, X in fp32, cut into pieces where it is multiplied, A and Q in pieces, as operands.
+// 64 rows and 352 columns, or 32 and 896: eight waves.  Nothing but the matrix is read or written, and a step is four barriers instead of two or three launches.  Vector
 // instructions bound it, most of them the cutting: with A and Q in fp32 too, cut by every wave that multiplies them, a step on 64 x 64 took 5.8 us, 1650 of them on its path.
+// fp32, all of five steps: 16 x 16 17 us, 64 x 64 29, 64 x 147 40 (6.4 a step), 64 x 352 64, 32 x 800 47; bf16 14, 23, 32, 53 and 38.  (Four waves for A's block below the
+// diagonal, where both operands are cut, and two for each on it cost registers and gain nothing: 64 x 147 42 us, 64 x 352 65 for 66 then.)
 constexpr int WHOLE_BYTES = 163840 - 256;
 
 template <typename E, int P, bool MUON, int N>
@@ -749,30 +751,32 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
     // elements i = tid, tid + 512, ... of the matrix, AT_ONCE at a time: f(the first's number, their places in X)
     constexpr int AT_ONCE = 16;
     const int total = rows * cols, step_r = 512 / cols, step_c = 512 - step_r * cols;
+    const int row_at = tall ? 1 : XP, col_at = tall ? XP : 1, step_at = step_r * row_at + step_c * col_at, wrap_at = row_at - cols * col_at;
     auto elements = [&](auto f) __attribute__((always_inline)) {
-        int r = tid / cols, col = tid - r * cols;
+        int col = tid % cols, place = tid / cols * row_at + col * col_at;
         for (int i = tid; i < total; i += AT_ONCE * 512) {
             int at[AT_ONCE];
 #pragma unroll
             for (int e = 0; e < AT_ONCE; ++e) {
-                at[e] = tall ? col * XP + r : r * XP + col;
-                r += step_r;
+                at[e] = place;
                 col += step_c;
-                if (col >= cols) { col -= cols; ++r; }
+                place += step_at;
+                if (col >= cols) { col -= cols; place += wrap_at; }
             }
             f(i, at);
         }
     };
-    for (int i = tid; i < mb * 32 * XP; i += 512) X[i] = 0.f;
+    const int pieces = mb * 8 * XP;          // of 16 bytes of X
+    for (int i = tid; i < pieces; i += 512) reinterpret_cast<f32x4*>(X)[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     __syncthreads();
     double s = 0.0;
     elements([&](int i, const int (&at)[AT_ONCE]) {
         float u[AT_ONCE], v[AT_ONCE];
 #pragma unroll
         for (int e = 0; e < AT_ONCE; ++e) {
-            const bool in = i + e * 512 < total;
-            u[e] = in ? Store<E>::ld((const E*)j.g[k] + i + e * 512) : 0.f;
-            if constexpr (MUON) v[e] = in ? j.momentum[k][i + e * 512] : 0.f;
+            const int n = min(i + e * 512, total - 1);
+            u[e] = Store<E>::ld((const E*)j.g[k] + n);
+            if constexpr (MUON) v[e] = j.momentum[k][n];
         }
 #pragma unroll
         for (int e = 0; e < AT_ONCE; ++e) {
@@ -791,7 +795,21 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
     if (lane == 0) red[wave] = s;
     __syncthreads();
     const double inv = 1.0 / (sqrt(((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]))) + (double)c.eps);
-    for (int i = tid; i < mb * 32 * XP; i += 512) X[i] = (float)((double)X[i] * inv);
+    // (inv as factor 2^exponent: inv itself may be no fp32 number, and a product in double is four times the work)
+    int exponent;
+    const float factor = (float)frexp(inv, &exponent);
+    for (int i = tid; i < pieces; i += 4 * 512) {          // (four at once: a pass that waits for every read takes 5 us of 32 x 800)
+        f32x4 v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = reinterpret_cast<const f32x4*>(X)[min(i + e * 512, pieces - 1)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (i + e * 512 >= pieces) break;
+#pragma unroll
+            for (int n = 0; n < 4; ++n) v[e][n] = ldexpf(v[e][n], exponent) * factor;
+            reinterpret_cast<f32x4*>(X)[i + e * 512] = v[e];
+        }
+    }
     __syncthreads();
 
     // eight values along a row of X, cut; down a column
@@ -947,7 +965,7 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
         float w[AT_ONCE];
         if constexpr (MUON) {
 #pragma unroll
-            for (int e = 0; e < AT_ONCE; ++e) w[e] = i + e * 512 < total ? ((const float*)j.o[k])[i + e * 512] : 0.f;
+            for (int e = 0; e < AT_ONCE; ++e) w[e] = ((const float*)j.o[k])[min(i + e * 512, total - 1)];
         }
 #pragma unroll
         for (int e = 0; e < AT_ONCE; ++e) {
