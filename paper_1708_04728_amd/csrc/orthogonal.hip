@@ -94,22 +94,21 @@ struct Operands {
 };
 __device__ __forceinline__ size_t block_at(int P, int rb, int kblocks32, int kb32) { return ((size_t)rb * kblocks32 + kb32) * (2 * P * BLOCK); }
 
+// The sum over 256 threads, added in the same order in every run
 __device__ __forceinline__ double sum256(double v, double* red)
 {
-    red[threadIdx.x] = v;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    for (int d = 128; d >= 1; d >>= 1) {
-        if ((int)threadIdx.x < d) red[threadIdx.x] += red[threadIdx.x + d];
-        __syncthreads();
-    }
-    return red[0];
+    return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
 // Momentum (descent step), and the sums of the squares of U's elements, in double: a square of 1e20 or 1e-30 is no fp32 number
 template <typename T, bool MUON, int N>
 __global__ __launch_bounds__(256) void squares_kernel(const Call c, const Jobs<N> j)
 {
-    __shared__ double red[256];
+    __shared__ double red[4];
     const Mat m = find_matrix(j, blockIdx.x);
     const T* const g = (const T*)j.g[m.k];
     float* const mom = j.momentum[m.k];
@@ -120,14 +119,16 @@ __global__ __launch_bounds__(256) void squares_kernel(const Call c, const Jobs<N
         float u[8], v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            u[e] = i + e * step < total ? Store<T>::ld(g + i + e * step) : 0.f;
-            if constexpr (MUON) v[e] = i + e * step < total ? mom[i + e * step] : 0.f;
+            const size_t n = i + e * step < total ? i + e * step : total - 1;      // (a load under a condition waits for the one before it)
+            u[e] = Store<T>::ld(g + n);
+            if constexpr (MUON) v[e] = mom[n];
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
+            if (i + e * step >= total) break;
             if constexpr (MUON) {
                 v[e] = c.mu * v[e] + u[e];
-                if (i + e * step < total) mom[i + e * step] = v[e];
+                mom[i + e * step] = v[e];
                 u[e] += c.mu * v[e];
             }
             s += (double)u[e] * (double)u[e];
@@ -197,7 +198,7 @@ template <typename T, int P, bool MUON, int N>
 __global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs<N> j)
 {
     __shared__ __attribute__((aligned(16))) float tiles[4][32 * PITCH];
-    __shared__ double red[256];
+    __shared__ double red[4];
     const Mat m = find_matrix(j, blockIdx.x);
     const Operands<P> op(c, j, m);
     const T* const g = (const T*)j.g[m.k];
