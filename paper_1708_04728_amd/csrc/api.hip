@@ -1611,7 +1611,7 @@ int dr_orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype, 
     const char* who = "dr_orthogonalise_workspace_bytes";
     DR_TRY(check_matrices(who, count, ms, dtype));
     if (!bytes) return fail(DR_ERR_NULL, "%s: bytes is NULL", who);
-    *bytes = orthogonalise_workspace_bytes(count, ms, dtype);
+    *bytes = orthogonalise_workspace_bytes(count, ms);
     return DR_OK;
 }
 
@@ -1625,7 +1625,7 @@ int dr_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* cons
     if (count && (!g || !o)) return fail(DR_ERR_NULL, "%s: g or o is NULL", who);
     for (int i = 0; i < count; ++i)
         if (ms[i].rows && ms[i].cols && (!g[i] || !o[i])) return fail(DR_ERR_NULL, "%s: g[%d] or o[%d] is NULL", who, i, i);
-    DR_TRY(check_scratch(who, ws, ws_bytes, orthogonalise_workspace_bytes(count, ms, dtype)));
+    DR_TRY(check_scratch(who, ws, ws_bytes, orthogonalise_workspace_bytes(count, ms)));
     return launch_orthogonalise(count, ms, dtype, g, o, *ns, ws, (hipStream_t)stream);
 }
 

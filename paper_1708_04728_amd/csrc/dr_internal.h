@@ -203,7 +203,7 @@ int launch_layernorm_bwd(const dr_tensor& d, const void* dy, const void* x, cons
                          float* dbeta, void* ws, hipStream_t st);
 
 // orthogonal.hip: Newton-Schulz products on a list of matrices, and the descent step on them
-size_t orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype);
+size_t orthogonalise_workspace_bytes(int count, const dr_matrix* ms);
 int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* const* g, void* const* o, const dr_newton_schulz& ns, void* ws, hipStream_t st);
 size_t muon_step_workspace_bytes(int count, const dr_muon_param* ps);
 int launch_muon_step(int count, const dr_muon_param* ps, const dr_muon& opt, void* ws, hipStream_t st);

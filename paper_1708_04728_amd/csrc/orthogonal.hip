@@ -5,8 +5,10 @@
 //
 // The polynomial moves every singular value of X towards one and leaves the singular vectors, so that X ends near U V^T of U = U S V^T.  It multiplies
 // small singular values by a = 3.4 in every step, and with them what roundings of X leave there: 64 to 512 rows of a filter's gradient end 1e-2 off with X, A and Q
-// in bf16, 2e-5 with two bf16 pieces of each value (16 bits), 2e-6 to 3e-5 in fp32.  So matrices are held as bf16 pieces whose sum is the value, three for fp32 (all
-// of its bits) and two for bf16 results, and multiplied on the bf16 matrix cores: six and three products of pieces for each product (f32_pieces.h).
+// in bf16, and 1e-6 to 1e-5 in fp32.  So matrices are held as two fp16 pieces whose sum is the value to 2^-23 (11 bits each, the lower one with a sign of its own), at
+// scales that keep them in fp16's range, and multiplied on the matrix cores: three products of pieces, with sums in fp32, for each product; the fourth, of the lower
+// pieces, is 2^-24 of it.  They end where fp32 ends (4096 x 4096: 3.5e-6 off, in fp32 4.3e-6) in half the time of three bf16 pieces, whose six products hold all of fp32's bits
+// and all of its range: polynomials whose values could pass fp16's take those (f32_pieces.h).  Results in bf16 go the same way: 16 bits would do, and two fp16 pieces cost no more.
 //
 // A and A A are symmetric: only blocks on and below the diagonal are computed, and stored on both sides.
 //
@@ -30,14 +32,25 @@ namespace dr {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int BLOCK = NS_BLOCK;
 constexpr int PITCH = 36;                    // floats of a row of 32 in LDS
 
+// Powers of two that operands are held multiplied by: fp16 has 11 bits from 2^-14 on, so that two pieces of X's have 22 bits from 2^-17 on, and A's and Q's from 2^-15 on.
+// (bf16 reaches as far as fp32.)  A sum of products becomes the operand A, Q or X, or the result, multiplied by what is below.
+template <int P> constexpr float X_SCALE = P == 2 ? NS_X_SCALE : 1.f;
+template <int P> constexpr float A_SCALE = P == 2 ? NS_A_SCALE : 1.f;
+template <int P> constexpr float FROM_GRAM = A_SCALE<P> / (X_SCALE<P> * X_SCALE<P>);
+template <int P> constexpr float FROM_APPLY = 1.f / A_SCALE<P>;
+template <int P> constexpr float TO_RESULT = 1.f / X_SCALE<P>;
+
 // The matrices of a launch; arrays by what is looked up together.  A list is worked on JOBS at a time.  (N: room for as many.  A launch reads its arguments from memory, one after
 // the other where an index is among them: a single matrix has kernels whose arguments are its own.)
-constexpr int JOBS = 64;
+constexpr int JOBS = NS_JOBS;
 template <int N>
 struct Jobs {
     int first[N];                         // first workgroup of the launch's k-th matrix; INT_MAX behind the last
@@ -54,9 +67,11 @@ struct Jobs {
 
 struct Call {
     double* squares;
+    int* shifts;                             // of the matrices (pieces of fp16): X is held multiplied by 2^held_at(shift, growth, step)
+    int growth;
     float* partial;                          // sums of workgroups that share a tile
     unsigned char* ws;
-    float a, b, c, eps;
+    float a, b, c, eps;                      // a times, c by the scale of A and Q: Q's scale times (a I + b A + c A A) of A's sums
     float mu, keep;                          // descent step: momentum; 1 - lr decay
 };
 
@@ -75,6 +90,30 @@ __device__ __forceinline__ Mat find_matrix(const Jobs<N>& j, int id)
     k = __builtin_amdgcn_readfirstlane(k);
     const int i = j.which[k];
     return Mat{i, j.first[k], j.mb[i], j.nb[i], j.rows[i], j.cols[i], j.rows[i] > j.cols[i]};
+}
+
+// What a product of step `step` makes of its sums
+template <int P>
+struct Scales {
+    float gram, b, c, apply;
+    int down;                                // the result, times 2^-down
+    __device__ __forceinline__ Scales(const Call& call, int shift, int step)
+    {
+        const int now = P == 2 ? held_at(shift, call.growth, step) : 0, next = P == 2 ? held_at(shift, call.growth, step + 1) : 0;
+        gram = FROM_GRAM<P>;
+        b = P == 2 ? ldexpf(call.b, -2 * now) : call.b;
+        c = P == 2 ? ldexpf(call.c, -4 * now) : call.c;
+        apply = P == 2 ? ldexpf(FROM_APPLY<P>, next - now) : 1.f;
+        down = now;
+    }
+    __device__ __forceinline__ float result_of(float v) const { return P == 2 ? ldexpf(v * (FROM_APPLY<P> * TO_RESULT<P>), -down) : v; }
+};
+// 2^shift times a norm of `norm` after the division is below 1; from 2^-200 on nothing of it is left in fp32 either way
+__device__ __forceinline__ int shift_of(double norm)
+{
+    int exponent = 0;
+    if (norm > 0.0 && norm < 0.5) frexp(norm, &exponent);
+    return min(-exponent, 200);
 }
 
 // Operands of a matrix: X, X^T twice (a product reads one and writes the other), A, Q
@@ -138,7 +177,7 @@ __global__ __launch_bounds__(256) void squares_kernel(const Call c, const Jobs<N
     if (threadIdx.x == 0) c.squares[j.squares[m.k] + me] = s;
 }
 
-// Eight values as P bf16 pieces
+// Eight values as P pieces: two of fp16, three of bf16
 template <int P>
 __device__ __forceinline__ void cut8(const float (&v)[8], u32x4 (&p)[P])
 {
@@ -146,25 +185,37 @@ __device__ __forceinline__ void cut8(const float (&v)[8], u32x4 (&p)[P])
     else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const unsigned h = pack_bf16x2(v[2 * i], v[2 * i + 1]);
-            p[0][i] = h;
-            p[1][i] = pack_bf16x2(v[2 * i] - __uint_as_float(h << 16), v[2 * i + 1] - __uint_as_float(h & 0xFFFF0000u));
+            const f32x2 x = {v[2 * i], v[2 * i + 1]};
+            const f16x2 high = __builtin_convertvector(x, f16x2);
+            const f32x2 back = __builtin_convertvector(high, f32x2), rest = {x[0] - back[0], x[1] - back[1]};
+            p[0][i] = __builtin_bit_cast(unsigned, high);
+            p[1][i] = __builtin_bit_cast(unsigned, __builtin_convertvector(rest, f16x2));
         }
     }
 }
 
 template <int P>
+__device__ __forceinline__ float value_of(unsigned pair, int n)      // of the n-th piece of a pair
+{
+    if constexpr (P == 3) return __uint_as_float(n ? pair & 0xFFFF0000u : pair << 16);
+    else return (float)__builtin_bit_cast(f16x2, pair)[n];
+}
+template <int P>
 __device__ __forceinline__ void join8(const u32x4 (&p)[P], float (&v)[8])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = v[2 * i + 1] = 0.f;
+    for (int i = 0; i < 8; ++i) {
+        v[i] = 0.f;
 #pragma unroll
-        for (int e = P - 1; e >= 0; --e) {
-            v[2 * i] += __uint_as_float(p[e][i] << 16);
-            v[2 * i + 1] += __uint_as_float(p[e][i] & 0xFFFF0000u);
-        }
+        for (int e = P - 1; e >= 0; --e) v[i] += value_of<P>(p[e][i >> 1], i & 1);
     }
+}
+
+template <int P>
+__device__ __forceinline__ f32x16 mfma_of(u32x4 a, u32x4 b, f32x16 c)
+{
+    if constexpr (P == 3) return mfma(a, b, c);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
 // Half of a 32 x 32 block that is in LDS, k from 16 kb on, as this lane's 16 bytes of an operand block: rows = the tile's rows (COLUMNS: its columns)
@@ -220,12 +271,18 @@ __global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs<N> j)
     }
     double s = 0.0;
     for (int i = threadIdx.x; i < squares_of(m.rows, m.cols); i += 256) s += c.squares[j.squares[m.k] + i];
-    const double inv = 1.0 / (sqrt(sum256(s, red)) + (double)c.eps);
+    const double norm = sqrt(sum256(s, red)), inv = 1.0 / (norm + (double)c.eps);
+    double scale = inv;
+    if constexpr (P == 2) {
+        const int shift = shift_of(norm * inv);
+        scale = ldexp(inv * X_SCALE<P>, shift);
+        if ((int)blockIdx.x == m.first && threadIdx.x == 0) c.shifts[m.k] = shift;
+    }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         if constexpr (MUON) u[r] += c.mu * v[r];
         const bool in = r0 + 2 * r + half < m.rows && col < m.cols;
-        tile[m.tall ? l32 * PITCH + 2 * r + half : (2 * r + half) * PITCH + l32] = in ? (float)((double)u[r] * inv) : 0.f;
+        tile[m.tall ? l32 * PITCH + 2 * r + half : (2 * r + half) * PITCH + l32] = in ? (float)((double)u[r] * scale) : 0.f;
     }
     __syncthreads();
     if (!on) return;
@@ -241,7 +298,7 @@ __global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs<N> j)
 
 // What becomes of a 32 x 32 block (bi, bj) of a product, which is in LDS: task t = 0 .. 3 stores a half of it in one of the two orders
 template <int P, int WHAT>
-__device__ __forceinline__ void finish_task(const Call& c, const Mat& m, const Operands<P>& op, const float* tile, int bi, int bj, int turn, int t)
+__device__ __forceinline__ void finish_task(const Call& c, const Mat& m, const Operands<P>& op, const float* tile, int bi, int bj, const Scales<P>& by, int turn, int t)
 {
     const int kb = t & 1;
     const bool flip = t >= 2;
@@ -249,6 +306,10 @@ __device__ __forceinline__ void finish_task(const Call& c, const Mat& m, const O
     if (WHAT != APPLY && flip && bi == bj) return;
     if (flip) operand8<true>(tile, kb, v);
     else operand8<false>(tile, kb, v);
+    if (P == 2 && WHAT != POLY) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= WHAT == GRAM ? by.gram : by.apply;
+    }
     const int rb = flip ? bj : bi, cb = flip ? bi : bj;
     if constexpr (WHAT == APPLY) put8<P>(v, flip ? (turn ? op.xt0 : op.xt1) + block_at(P, rb, m.mb, cb) : op.x + block_at(P, rb, m.nb, cb), kb);
     else if constexpr (WHAT == GRAM) put8<P>(v, op.a + block_at(P, rb, m.mb, cb), kb);
@@ -262,13 +323,13 @@ __device__ __forceinline__ void finish_task(const Call& c, const Mat& m, const O
         join8<P>(p, w);
         // (also on the diagonal of the rows that pad X: what they multiply is zero)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = c.b * w[e] + c.c * v[e] + (diagonal + e == 0 ? c.a : 0.f);
+        for (int e = 0; e < 8; ++e) v[e] = by.b * w[e] + by.c * v[e] + (diagonal + e == 0 ? c.a : 0.f);
         put8<P>(v, op.q + block_at(P, rb, m.mb, cb), kb);
     }
 }
 // ... of the last product: the result, or the weights; rows r0, r0 + step, ... of the matrix' own 32 x 32 block
-template <typename T, bool MUON, int N>
-__device__ __forceinline__ void finish_result(const Call& c, const Jobs<N>& j, const Mat& m, const float* tile, int bi, int bj, int r0, int step)
+template <typename T, int P, bool MUON, int N>
+__device__ __forceinline__ void finish_result(const Call& c, const Jobs<N>& j, const Mat& m, const float* tile, int bi, int bj, const Scales<P>& by, int r0, int step)
 {
     const int l32 = threadIdx.x & 31, row0 = (m.tall ? bj : bi) * 32, col = (m.tall ? bi : bj) * 32 + l32;
     for (int r8 = r0; r8 < 32; r8 += 8 * step) {         // (eight weights at a time: loads behind stores would wait for each other)
@@ -281,7 +342,7 @@ __device__ __forceinline__ void finish_result(const Call& c, const Jobs<N>& j, c
         for (int e = 0; e < 8; ++e) {
             const int r = r8 + e * step;
             if (r >= 32 || row0 + r >= m.rows || col >= m.cols) continue;
-            const float v = tile[m.tall ? l32 * PITCH + r : r * PITCH + l32];
+            const float v = by.result_of(tile[m.tall ? l32 * PITCH + r : r * PITCH + l32]);
             const size_t i = (size_t)(row0 + r) * m.cols + col;
             if constexpr (MUON) ((float*)j.o[m.k])[i] = c.keep * old[e] - j.scale[m.k] * v;
             else Store<T>::st((T*)j.o[m.k] + i, v);
@@ -309,20 +370,20 @@ __device__ __forceinline__ void tile_blocks(const Mat& m, int t, int& bi, int& b
 template <int P>
 __device__ __forceinline__ void multiply(const u32x4 (&a)[P], const u32x4 (&b)[P], f32x16& large, f32x16& small)
 {
-    large = mfma(a[0], b[0], large);
-    small = mfma(a[0], b[1], small);
-    small = mfma(a[1], b[0], small);
+    large = mfma_of<P>(a[0], b[0], large);
+    small = mfma_of<P>(a[0], b[1], small);
+    small = mfma_of<P>(a[1], b[0], small);
     if constexpr (P == 3) {
-        small = mfma(a[1], b[1], small);
-        small = mfma(a[0], b[2], small);
-        small = mfma(a[2], b[0], small);
+        small = mfma_of<P>(a[1], b[1], small);
+        small = mfma_of<P>(a[0], b[2], small);
+        small = mfma_of<P>(a[2], b[0], small);
     }
 }
 
 // A product of small matrices: W waves share a tile of T x T blocks, every wave a W-th of the contraction.  Operands go straight to registers, some k-blocks of them
 // while as many are multiplied: what such a product waits for is its first operands.  splits > 1: as many workgroups share a tile, and leave sums for sum_kernel.
 template <typename E, int P, int WHAT, int T, int W, bool MUON, int N>
-__global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs<N> j, int turn, int last, int splits)
+__global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs<N> j, int nth, int last, int splits)
 {
     constexpr int KEEP = AHEAD[T == 1 ? FINE : DIRECT];
     static_assert(W == WAVES[T == 1 ? FINE : DIRECT], "the plan's waves");
@@ -330,6 +391,8 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
     const int unit = splits > 1 ? (int)blockIdx.x / splits : (int)blockIdx.x, part = (int)blockIdx.x - unit * splits;
     const Mat m = find_matrix(j, unit);
     const Operands<P> op(c, j, m);
+    const int turn = nth & 1;
+    const Scales<P> by(c, P == 2 ? c.shifts[m.k] : 0, nth);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     int bi, bj;
     tile_blocks<WHAT, T>(m, unit - m.first, bi, bj);
@@ -407,13 +470,13 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
     if (WHAT == APPLY && last) {
         for (int blk = 0; blk < T * T; ++blk) {
             const int i = bi + blk / T, k = bj + blk % T;
-            if (i < lrows && k < rrows) finish_result<E, MUON, N>(c, j, m, sums[0][blk], i, k, wave * 2 + half, 2 * W);
+            if (i < lrows && k < rrows) finish_result<E, P, MUON, N>(c, j, m, sums[0][blk], i, k, by, wave * 2 + half, 2 * W);
         }
         return;
     }
     for (int t = wave; t < T * T * 4; t += W) {
         const int blk = t >> 2, i = bi + blk / T, k = bj + blk % T;
-        if (i < lrows && k < rrows && (WHAT == APPLY || i >= k)) finish_task<P, WHAT>(c, m, op, sums[0][blk], i, k, turn, t & 3);
+        if (i < lrows && k < rrows && (WHAT == APPLY || i >= k)) finish_task<P, WHAT>(c, m, op, sums[0][blk], i, k, by, turn, t & 3);
     }
 }
 
@@ -437,10 +500,10 @@ __device__ __forceinline__ void wave_lds()           // orders a wave's LDS traf
 }
 
 // Q and Q X in one launch, for matrices of few rows: a workgroup makes one block of X, and for it the blocks of Q of its rows, a wave each, which stay in LDS.  A's rows that
-// all of these share come through LDS (each wave loading them for itself, 192 x 576 takes 92 us for 87: a compute unit reads 64 bytes a cycle from beyond it), the other
+// all of these share come through LDS (each wave loading them for itself, 192 x 576 takes 92 us for 87 with three pieces, 71 for 69 with two: a compute unit reads 64 bytes a cycle from beyond it), the other
 // factor straight to registers, KEEP k-blocks of it while as many are multiplied.  Waits in a row bound it: loads, the products of a wave, a barrier, products, a barrier.
 template <typename E, int P, bool MUON, int N>
-__global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Jobs<N> j, int turn, int last)
+__global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Jobs<N> j, int nth, int last)
 {
     constexpr int W = 8, KEEP = 4;
     static_assert(NS_JOINED_ROWS <= W, "a wave for each block of Q");
@@ -448,6 +511,8 @@ __global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Job
     __shared__ __attribute__((aligned(16))) unsigned char q[2 * NS_JOINED_ROWS * P * BLOCK], arows[2 * NS_JOINED_ROWS * P * BLOCK];
     const Mat m = find_matrix(j, blockIdx.x);
     const Operands<P> op(c, j, m);
+    const int turn = nth & 1;
+    const Scales<P> by(c, P == 2 ? c.shifts[m.k] : 0, nth);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5, kblocks = 2 * m.mb;
     int bi, bj;
     tile_blocks<APPLY, 1>(m, (int)blockIdx.x - m.first, bi, bj);
@@ -514,7 +579,7 @@ __global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Job
             operand8<false>(sums[wave], n, v);
             join8<P>(own, w);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = c.b * w[e] + c.c * v[e] + (diagonal + e == 0 ? c.a : 0.f);
+            for (int e = 0; e < 8; ++e) v[e] = by.b * w[e] + by.c * v[e] + (diagonal + e == 0 ? c.a : 0.f);
             put8<P>(v, q + 2 * wave * P * BLOCK, n);
         }
     }
@@ -540,18 +605,20 @@ __global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Job
         sums[0][at] = s;
     }
     __syncthreads();
-    if (last) finish_result<E, MUON, N>(c, j, m, sums[0], bi, bj, wave * 2 + half, 2 * W);
-    else if (wave < 4) finish_task<P, APPLY>(c, m, op, sums[0], bi, bj, turn, wave);
+    if (last) finish_result<E, P, MUON, N>(c, j, m, sums[0], bi, bj, by, wave * 2 + half, 2 * W);
+    else if (wave < 4) finish_task<P, APPLY>(c, m, op, sums[0], bi, bj, by, turn, wave);
 }
 
 // Adds the sums that the workgroups of a tile have left, in their order
 template <typename E, int P, int WHAT, int T, bool MUON, int N>
-__global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j, int turn, int last, int splits)
+__global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j, int nth, int last, int splits)
 {
     __shared__ __attribute__((aligned(16))) float tile[32 * PITCH];
     const int unit = (int)blockIdx.x / (T * T), blk = (int)blockIdx.x - unit * (T * T);
     const Mat m = find_matrix(j, unit);
     const Operands<P> op(c, j, m);
+    const int turn = nth & 1;
+    const Scales<P> by(c, P == 2 ? c.shifts[m.k] : 0, nth);
     int bi, bj;
     tile_blocks<WHAT, T>(m, unit - m.first, bi, bj);
     bi += blk / T;
@@ -565,8 +632,8 @@ __global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j,
 #pragma unroll
     for (int n = 0; n < 4; ++n) tile[(n * 8 + (threadIdx.x >> 5)) * PITCH + (threadIdx.x & 31)] = s[n];
     __syncthreads();
-    if (WHAT == APPLY && last) finish_result<E, MUON, N>(c, j, m, tile, bi, bj, threadIdx.x >> 5, 8);
-    else finish_task<P, WHAT>(c, m, op, tile, bi, bj, turn, threadIdx.x >> 6);
+    if (WHAT == APPLY && last) finish_result<E, P, MUON, N>(c, j, m, tile, bi, bj, by, threadIdx.x >> 5, 8);
+    else finish_task<P, WHAT>(c, m, op, tile, bi, bj, by, turn, threadIdx.x >> 6);
 }
 
 // f(0), ..., f(N - 1), as constants
@@ -576,7 +643,7 @@ template <int N, class F>
 __device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
 template <typename E, int P, int WHAT, int WM, int WN, int TM, int TN, int DEPTH, bool APART, bool MUON, int N>
-__global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const Jobs<N> j, int turn, int last)
+__global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const Jobs<N> j, int nth, int last)
 {
     constexpr int W = WM * WN, BM = WM * TM, BN = WN * TN, STAGE = (BM + BN) * P * BLOCK, LOADS = (BM + BN) * P / W;
     static_assert((BM + BN) * P % W == 0 && BM == BN && (DEPTH == 1 || DEPTH == 2) && tile_lds<P, BM, BN>() >= W * 32 * PITCH * 4, "a tile's operands");
@@ -587,6 +654,8 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
     const int id = N > 1 ? (int)blockIdx.x : die * share + min(die, odd) + (int)(blockIdx.x >> 3);
     const Mat m = find_matrix(j, id);
     const Operands<P> op(c, j, m);
+    const int turn = nth & 1;
+    const Scales<P> by(c, P == 2 ? c.shifts[m.k] : 0, nth);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, half = lane >> 5;
     const int wm = wave / WN, wn = wave % WN;
     int bi, bj;
@@ -663,8 +732,8 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
         constexpr int X2[3] = {0, 0, 1}, Y2[3] = {1, 0, 0};
         each<PAIRS * G>([&](auto slot) __attribute__((always_inline)) {
             constexpr int t = decltype(slot)::value, g = t / G, i = t % G / TN, k = t % TN, x = P == 3 ? X[g] : X2[g % 3], y = P == 3 ? Y[g] : Y2[g % 3];
-            if constexpr (APART && x + y != 0) small[i][k] = mfma(a[i][x], b[k][y], small[i][k]);
-            else acc[i][k] = mfma(a[i][x], b[k][y], acc[i][k]);
+            if constexpr (APART && x + y != 0) small[i][k] = mfma_of<P>(a[i][x], b[k][y], small[i][k]);
+            else acc[i][k] = mfma_of<P>(a[i][x], b[k][y], acc[i][k]);
             __builtin_amdgcn_sched_barrier(0);
             // this k-block's pieces that come last
             if constexpr (t < TN) read_b(here, t, 0);
@@ -717,10 +786,10 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
             for (int v = 0; v < 16; ++v) tile[(8 * (v >> 2) + 4 * half + (v & 3)) * PITCH + l32] = APART ? acc[i][k][v] + small[APART ? i : 0][APART ? k : 0][v] : acc[i][k][v];
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
             __builtin_amdgcn_wave_barrier();
-            if (WHAT == APPLY && last) finish_result<E, MUON, N>(c, j, m, tile, ri, rk, half, 2);
+            if (WHAT == APPLY && last) finish_result<E, P, MUON, N>(c, j, m, tile, ri, rk, by, half, 2);
             else {
 #pragma unroll 1
-                for (int t = 0; t < 4; ++t) finish_task<P, WHAT>(c, m, op, tile, ri, rk, turn, t);
+                for (int t = 0; t < 4; ++t) finish_task<P, WHAT>(c, m, op, tile, ri, rk, by, turn, t);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
             __builtin_amdgcn_wave_barrier();
@@ -730,8 +799,8 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
 // ---- matrices small enough for one workgroup's LDS: the whole iteration there, X in fp32, cut into pieces where it is multiplied, A and Q in pieces, as operands.
 // 64 rows and 352 columns, or 32 and 896: eight waves.  Nothing but the matrix is read or written, and a step is four barriers instead of two or three launches.  Vector
 // instructions bound it, most of them the cutting: with A and Q in fp32 too, cut by every wave that multiplies them, a step on 64 x 64 took 5.8 us, 1650 of them on its path.
-// fp32, all of five steps: 16 x 16 17 us, 64 x 64 29, 64 x 147 40 (6.4 a step), 64 x 352 64, 32 x 800 47; bf16 14, 23, 32, 53 and 38.  (Four waves for A's block below the
-// diagonal, where both operands are cut, and two for each on it cost registers and gain nothing: 64 x 147 42 us, 64 x 352 65 for 66 then.)
+// All of five steps, fp32 or bf16: 16 x 16 15 us, 64 x 64 25, 64 x 147 34 (5.2 a step), 64 x 352 55, 32 x 800 41; three pieces 17, 29, 40, 64 and 47.  (Four waves for A's block below the
+// diagonal, where both operands are cut, and two for each on it cost registers and gain nothing: with three pieces 64 x 147 42 us for 41, 64 x 352 65 for 66.)
 constexpr int WHOLE_BYTES = 163840 - 256;
 
 template <typename E, int P, bool MUON, int N>
@@ -795,10 +864,12 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
     if (lane == 0) red[wave] = s;
     __syncthreads();
-    const double inv = 1.0 / (sqrt(((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]))) + (double)c.eps);
+    const double norm = sqrt(((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]))), inv = 1.0 / (norm + (double)c.eps);
+    const int shift = P == 2 ? shift_of(norm * inv) : 0;
     // (inv as factor 2^exponent: inv itself may be no fp32 number, and a product in double is four times the work)
     int exponent;
-    const float factor = (float)frexp(inv, &exponent);
+    const float factor = (float)frexp(inv * X_SCALE<P>, &exponent);
+    exponent += shift;
     for (int i = tid; i < pieces; i += 4 * 512) {          // (four at once: a pass that waits for every read takes 5 us of 32 x 800)
         f32x4 v[4];
 #pragma unroll
@@ -846,6 +917,7 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
         auto multiply2 = [&](int which, const u32x4 (&a)[P], const u32x4 (&b)[P]) __attribute__((always_inline)) { multiply<P>(a, b, large[which], small[which]); };
         auto sum = [&](int v) __attribute__((always_inline)) { return (large[0][v] + large[1][v]) + (small[0][v] + small[1][v]); };
         for (int step = 0; step < steps; ++step) {
+            const Scales<P> by(c, shift, step);
             // A = X X^T
             if (MB == 1 || wave < 6) {
                 const int blk = MB == 1 ? 0 : wave >> 1, split = MB == 1 ? wave : wave & 1, bi = blk ? 1 : 0, bj = blk == 2 ? 1 : 0;
@@ -889,6 +961,8 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
                         for (int e = 0; e < 8; ++e) v[e] += from[w * 32 * PITCH + l32 * PITCH + k0 + e];
                     }
                 }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] *= by.gram;
                 u32x4 p[P];
                 cut8<P>(v, p);
 #pragma unroll
@@ -924,8 +998,8 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
                             const int n = (2 * h + q) * 4 + r;
                             float w = 0.f;
 #pragma unroll
-                            for (int e = P - 1; e >= 0; --e) w += __uint_as_float(r & 1 ? p[q][e][r >> 1] & 0xFFFF0000u : p[q][e][r >> 1] << 16);
-                            v[q * 4 + r] = c.b * w + c.c * sum(n) + (bi == bj && row_of(n) == l32 ? c.a : 0.f);
+                            for (int e = P - 1; e >= 0; --e) w += value_of<P>(p[q][e][r >> 1], r & 1);
+                            v[q * 4 + r] = by.b * w + by.c * sum(n) + (bi == bj && row_of(n) == l32 ? c.a : 0.f);
                         }
                     u32x4 t[P];
                     cut8<P>(v, t);
@@ -955,13 +1029,15 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
 #pragma unroll
                 for (int i = 0; i < MB; ++i)
 #pragma unroll
-                    for (int v = 0; v < 16; ++v) X[(i * 32 + row_of(v)) * XP + bj * 32 + l32] = big[i][v] + little[i][v];
+                    for (int v = 0; v < 16; ++v) X[(i * 32 + row_of(v)) * XP + bj * 32 + l32] = (big[i][v] + little[i][v]) * by.apply;
             }
             __syncthreads();
         }
     };
     if (mb == 1) iterate(std::integral_constant<int, 1>{});
     else iterate(std::integral_constant<int, 2>{});
+    const int held = held_at(shift, c.growth, steps);
+    auto result_of = [&](float v) __attribute__((always_inline)) { return P == 2 ? ldexpf(v * TO_RESULT<P>, -held) : v; };
     elements([&](int i, const int (&at)[AT_ONCE]) {
         float w[AT_ONCE];
         if constexpr (MUON) {
@@ -971,15 +1047,15 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
 #pragma unroll
         for (int e = 0; e < AT_ONCE; ++e) {
             if (i + e * 512 >= total) break;
-            if constexpr (MUON) ((float*)j.o[k])[i + e * 512] = c.keep * w[e] - j.scale[k] * X[at[e]];
-            else Store<E>::st((E*)j.o[k] + i + e * 512, X[at[e]]);
+            if constexpr (MUON) ((float*)j.o[k])[i + e * 512] = c.keep * w[e] - j.scale[k] * result_of(X[at[e]]);
+            else Store<E>::st((E*)j.o[k] + i + e * 512, result_of(X[at[e]]));
         }
     });
 }
 
 // ---- a call
 template <class Shape>
-size_t workspace_bytes(int count, int P, Shape shape)
+size_t workspace_bytes(int count, Shape shape)
 {
     size_t most = 0;
     Group g;
@@ -987,9 +1063,9 @@ size_t workspace_bytes(int count, int P, Shape shape)
     for (int i = 0; i < count; ++i) {
         int rows, cols;
         shape(i, rows, cols);
-        if (rows && cols) g.add(rows, cols, P);
+        if (rows && cols) g.add(rows, cols);
         if (g.count == JOBS || (i + 1 == count && g.count)) {
-            most = std::max(most, g.bytes(P, device_cus()));
+            for (int pieces = 2; pieces <= 3; ++pieces) most = std::max(most, g.bytes(pieces, device_cus()));      // (whatever the polynomial)
             g.start();
         }
     }
@@ -1034,8 +1110,9 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
         return check_launch("orthogonalise");
     }
     c.squares = (double*)ws;
+    c.shifts = (int*)((unsigned char*)ws + group.squares);
     c.ws = (unsigned char*)ws + group.squares_bytes();
-    c.partial = (float*)(c.ws + group.operands);
+    c.partial = (float*)(c.ws + group.operands_bytes(P));
     size_t operands = 0;
     int squares_at = 0;
     for (int i = 0; i < group.count; ++i) {
@@ -1051,7 +1128,7 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
     const unsigned cuts = number(j, group.count, orders[GRAM], [](int mb, int nb, int, int) { return (mb * nb + 3) / 4; });
     hipLaunchKernelGGL((cut_kernel<E, P, MUON, N>), dim3(cuts), dim3(256), 0, st, c, j);
     using std::integral_constant;
-    auto product = [&](auto what, int turn, int last) {
+    auto product = [&](auto what, int nth, int last) {
         constexpr int WHAT = decltype(what)::value;
         constexpr bool END = WHAT == APPLY && MUON;      // (the other products are the same for every result)
         typedef std::conditional_t<WHAT == APPLY, E, float> R;
@@ -1059,14 +1136,14 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
         const unsigned tiles = number(j, group.count, orders[WHAT], [&](int mb, int nb, int, int) { return tiles_of(WHAT, mb, nb, SIDE[choice.kernel]); });
         auto direct = [&](auto side, auto waves) {
             constexpr int T = decltype(side)::value, W = decltype(waves)::value;
-            hipLaunchKernelGGL((product_kernel<R, P, WHAT, T, W, END, N>), dim3(tiles * choice.splits), dim3(W * 64), 0, st, c, j, turn, last, choice.splits);
+            hipLaunchKernelGGL((product_kernel<R, P, WHAT, T, W, END, N>), dim3(tiles * choice.splits), dim3(W * 64), 0, st, c, j, nth, last, choice.splits);
             if constexpr (WHAT == GRAM) {
-                if (choice.splits > 1) hipLaunchKernelGGL((sum_kernel<R, P, WHAT, T, END, N>), dim3(tiles * T * T), dim3(256), 0, st, c, j, turn, last, choice.splits);
+                if (choice.splits > 1) hipLaunchKernelGGL((sum_kernel<R, P, WHAT, T, END, N>), dim3(tiles * T * T), dim3(256), 0, st, c, j, nth, last, choice.splits);
             }
         };
         auto tile = [&](auto side, auto depth, auto apart) {
             constexpr int T = decltype(side)::value;
-            hipLaunchKernelGGL((tile_kernel<R, P, WHAT, 2, 2, T / 2, T / 2, decltype(depth)::value, decltype(apart)::value, END, N>), dim3(tiles), dim3(256), 0, st, c, j, turn, last);
+            hipLaunchKernelGGL((tile_kernel<R, P, WHAT, 2, 2, T / 2, T / 2, decltype(depth)::value, decltype(apart)::value, END, N>), dim3(tiles), dim3(256), 0, st, c, j, nth, last);
         };
         if (choice.kernel == FINE) direct(integral_constant<int, 1>{}, integral_constant<int, 8>{});
         else if (choice.kernel == DIRECT) direct(integral_constant<int, 2>{}, integral_constant<int, 4>{});
@@ -1076,14 +1153,14 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
     };
     for (int s = 0; s < steps; ++s) {
         const int last = s + 1 == steps;
-        product(integral_constant<int, GRAM>{}, s & 1, last);
+        product(integral_constant<int, GRAM>{}, s, last);
         if (group.joined(device_cus())) {
             const unsigned tiles = number(j, group.count, orders[APPLY], [](int mb, int nb, int, int) { return mb * nb; });
-            hipLaunchKernelGGL((poly_apply_kernel<E, P, MUON, N>), dim3(tiles), dim3(512), 0, st, c, j, s & 1, last);
+            hipLaunchKernelGGL((poly_apply_kernel<E, P, MUON, N>), dim3(tiles), dim3(512), 0, st, c, j, s, last);
             continue;
         }
-        product(integral_constant<int, POLY>{}, s & 1, last);
-        product(integral_constant<int, APPLY>{}, s & 1, last);
+        product(integral_constant<int, POLY>{}, s, last);
+        product(integral_constant<int, APPLY>{}, s, last);
     }
     return check_launch("orthogonalise");
 }
@@ -1102,7 +1179,7 @@ int run_jobs(Call c, int count, int steps, void* ws, hipStream_t st, Fill fill)
             j.rows[g.count] = rows; j.cols[g.count] = cols;
             j.mb[g.count] = (std::min(rows, cols) + 31) / 32;
             j.nb[g.count] = (std::max(rows, cols) + 31) / 32;
-            g.add(rows, cols, P);
+            g.add(rows, cols);
         }
         if (g.count == N || (i + 1 == count && g.count)) {
             if (const int rc = run_group<E, P, MUON>(g, c, j, steps, ws, st)) return rc;
@@ -1111,18 +1188,23 @@ int run_jobs(Call c, int count, int steps, void* ws, hipStream_t st, Fill fill)
     }
     return DR_OK;
 }
-template <typename E, int P, bool MUON, class Fill>
+template <typename E, bool MUON, class Fill>
 int run_list(Call c, int count, const dr_newton_schulz& ns, void* ws, hipStream_t st, Fill fill)
 {
-    c.a = ns.a; c.b = ns.b; c.c = ns.c; c.eps = ns.eps;
-    return count == 1 ? run_jobs<E, P, MUON, 1>(c, count, ns.steps, ws, st, fill) : run_jobs<E, P, MUON, JOBS>(c, count, ns.steps, ws, st, fill);
+    c.b = ns.b; c.eps = ns.eps;
+    auto run = [&](auto pieces) {
+        constexpr int P = decltype(pieces)::value;
+        c.a = ns.a * A_SCALE<P>; c.c = ns.c / A_SCALE<P>;
+        return count == 1 ? run_jobs<E, P, MUON, 1>(c, count, ns.steps, ws, st, fill) : run_jobs<E, P, MUON, JOBS>(c, count, ns.steps, ws, st, fill);
+    };
+    return stays_small(ns.steps, ns.a, ns.b, ns.c, &c.growth) ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 3>{});
 }
 
 }  // namespace
 
-size_t orthogonalise_workspace_bytes(int count, const dr_matrix* ms, int dtype)
+size_t orthogonalise_workspace_bytes(int count, const dr_matrix* ms)
 {
-    return workspace_bytes(count, dtype == DR_F32 ? 3 : 2, [&](int i, int& r, int& c) { r = ms[i].rows; c = ms[i].cols; });
+    return workspace_bytes(count, [&](int i, int& r, int& c) { r = ms[i].rows; c = ms[i].cols; });
 }
 
 int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* const* g, void* const* o, const dr_newton_schulz& ns, void* ws, hipStream_t st)
@@ -1135,12 +1217,12 @@ int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* 
         j.o[k] = o[i];
         j.scale[k] = 0.f;
     };
-    return dtype == DR_F32 ? run_list<float, 3, false>(Call{}, count, ns, ws, st, fill) : run_list<uint16_t, 2, false>(Call{}, count, ns, ws, st, fill);
+    return dtype == DR_F32 ? run_list<float, false>(Call{}, count, ns, ws, st, fill) : run_list<uint16_t, false>(Call{}, count, ns, ws, st, fill);
 }
 
 size_t muon_step_workspace_bytes(int count, const dr_muon_param* ps)
 {
-    return workspace_bytes(count, 3, [&](int i, int& r, int& c) { r = ps[i].rows; c = ps[i].cols; });
+    return workspace_bytes(count, [&](int i, int& r, int& c) { r = ps[i].rows; c = ps[i].cols; });
 }
 
 int launch_muon_step(int count, const dr_muon_param* ps, const dr_muon& opt, void* ws, hipStream_t st)
@@ -1149,7 +1231,7 @@ int launch_muon_step(int count, const dr_muon_param* ps, const dr_muon& opt, voi
     c.mu = opt.momentum;
     c.keep = (float)(1.0 - (double)opt.lr * opt.weight_decay);
     TraceScope trace("muon_step", nullptr, count, st);
-    return run_list<float, 3, true>(c, count, opt.ns, ws, st, [&](int i, int& r, int& cols, auto& j, int k) {
+    return run_list<float, true>(c, count, opt.ns, ws, st, [&](int i, int& r, int& cols, auto& j, int k) {
         r = ps[i].rows; cols = ps[i].cols;
         j.g[k] = ps[i].dw;
         j.momentum[k] = ps[i].momentum;

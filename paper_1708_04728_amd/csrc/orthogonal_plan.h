@@ -8,6 +8,7 @@
 
 namespace dr {
 
+constexpr int NS_JOBS = 64;                  // most matrices of a launch
 constexpr int NS_BLOCK = 1024;               // bytes of a block of 32 rows x 16 k of one piece of an operand
 constexpr int SQUARES = 1024;                // most workgroups (and partial sums of squares) of a matrix
 enum { GRAM = 0, POLY = 1, APPLY = 2, PRODUCTS = 3 };
@@ -17,6 +18,40 @@ constexpr int squares_of(int rows, int cols)
 {
     return (int)std::min<size_t>(SQUARES, ((size_t)rows * cols + 4095) / 4096);
 }
+
+// Scales of the fp16 pieces of X and of A and Q, and whether those suffice: no element of X, A = X X^T or Q = a I + b A + c A A may pass 65504 by far.  Elements are at
+// most the largest singular value, 1 at the start (|X|_F <= 1), which each step takes to at most the largest |a s + b s^3 + c s^5| of s up to it; that of Q is at most the
+// largest |a + b t + c t^2| of t = s^2.  Beyond 3, 9 and 12 (a quarter left for roundings) the pieces are of bf16, three of them.  growth: log2 of what a step multiplies
+// a singular value by, at most.
+constexpr float NS_X_SCALE = 16384.f, NS_A_SCALE = 4096.f;
+inline bool stays_small(int steps, double a, double b, double c, int* growth)
+{
+    double most = 1.0;
+    *growth = 0;
+    for (int i = 0; i < steps; ++i) {
+        const double end = most * most;
+        double x = 0, q = fabs(a);
+        auto look = [&](double t) {
+            if (!(t >= 0 && t <= end)) return;
+            q = std::max(q, fabs(a + b * t + c * t * t));
+            x = std::max(x, sqrt(t) * fabs(a + b * t + c * t * t));
+        };
+        look(end);
+        if (c != 0) {
+            look(-b / (2 * c));                                      // where the derivative of Q's is zero
+            const double d = 9 * b * b - 20 * a * c;                 // ... of X's: a + 3 b t + 5 c t^2 = 0
+            if (d >= 0) { look((-3 * b + sqrt(d)) / (10 * c)); look((-3 * b - sqrt(d)) / (10 * c)); }
+        } else if (b != 0) look(-a / (3 * b));
+        if (!(x <= 3 && q <= 12)) return false;
+        while (q * 1.001 > (1 << *growth)) ++*growth;
+        most = x * 1.001;                                            // (roundings)
+    }
+    return true;
+}
+
+// A matrix whose norm is far below eps starts from an X as small, which fp16 does not hold: it is held multiplied by 2^shift, at step k by 2^(what is left), as much less as
+// the steps before may have multiplied it by
+constexpr int held_at(int shift, int growth, int step) { return shift > growth * step ? shift - growth * step : 0; }
 
 // matrices that fit the LDS of one workgroup: blocks of 32 of the short and of the long side
 constexpr bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 11; }
@@ -53,7 +88,7 @@ struct Work {
     }
 };
 
-// Microseconds that a launch takes, from 36 square and oblong shapes of 64 to 4096 rows in either number of pieces: what a round of workgroups costs beside its products;
+// Microseconds that a launch takes, from 36 square and oblong shapes of 64 to 4096 rows with either number of pieces (of bf16 then, which multiply as fast): what a round of workgroups costs beside its products;
 // a k-block on a compute unit by itself; what all of them multiply together, in blocks of 32 x 32 x 16 a microsecond; workgroups per compute unit.
 struct Cost { float round, kblock, rate; int slots; };
 constexpr Cost COSTS[2][KERNELS] = {
@@ -98,10 +133,11 @@ struct Group {
     Work work[PRODUCTS];
     int count, most_mb;
     bool whole;                              // all of them fit the LDS of a workgroup
-    size_t squares, operands, partial;       // bytes
-    size_t squares_bytes() const { return (squares + 1023) / 1024 * 1024; }
+    size_t squares, operands;                // bytes, of a piece
+    size_t operands_bytes(int P) const { return operands * P; }
+    size_t squares_bytes() const { return (squares + NS_JOBS * sizeof(int) + 1023) / 1024 * 1024; }     // ... and a shift for each matrix
     void start() { *this = Group{}; whole = true; }
-    void add(int rows, int cols, int P)
+    void add(int rows, int cols)
     {
         const int mb = (std::min(rows, cols) + 31) / 32, nb = (std::max(rows, cols) + 31) / 32;
         for (int w = 0; w < PRODUCTS; ++w) work[w].add(w, mb, nb);
@@ -109,16 +145,16 @@ struct Group {
         most_mb = std::max(most_mb, mb);
         whole = whole && whole_fits(mb, nb);
         squares += squares_of(rows, cols) * sizeof(double);
-        operands += operand_bytes(mb, nb, P);
+        operands += operand_bytes(mb, nb, 1);
     }
     // Q and Q X in one launch, a workgroup for each 32 x 32 of X: each makes its rows of Q for itself, which costs less than a launch as long as the workgroups come in one
-    // round (two, where Q has 64 rows).  Measured, two launches -> one, fp32: 64 x 1728 101 -> 81 us, 64 x 8192 122 -> 112, 128 x 2048 107 -> 93, 128 x 6144 (768 workgroups)
-    // 139 -> 160, 192 x 576 95 -> 87, 256 x 1024 108 -> 108, 256 x 1536 (384) 133 -> 152; bf16: 192 x 576 75 -> 69, 256 x 1024 88 -> 81
+    // round (two, where Q has 64 rows).  Five steps, two launches -> one, two pieces: 64 x 1728 88 -> 72 us, 64 x 8192 116 -> 102, 128 x 2048 88 -> 80, 192 x 576 77 -> 70,
+    // 256 x 1024 86 -> 81; beyond that 128 x 6144 (768 workgroups) 115 -> 130, 256 x 1536 (384) 109 -> 117; three pieces: 192 x 576 95 -> 87, 256 x 1024 108 -> 108
     bool joined(int cus) const { return !whole && most_mb <= NS_JOINED_ROWS && work[APPLY].tiles[FINE] <= (most_mb <= 2 ? 2 : 1) * cus; }
     size_t bytes(int P, int cus) const
     {
         if (whole) return 256;               // (none is used)
-        return squares_bytes() + operands + partial_bytes(choose(P, GRAM, work[GRAM], cus), work[GRAM]);
+        return squares_bytes() + operands_bytes(P) + partial_bytes(choose(P, GRAM, work[GRAM], cus), work[GRAM]);
     }
 };
 

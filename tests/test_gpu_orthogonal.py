@@ -95,6 +95,57 @@ def test_orthogonalise_large(shape, dtype):
     assert torch.equal(got, again)
 
 
+# a polynomial that takes singular values to 4.9: beyond what two fp16 pieces hold
+FAR = (12.5, -12.0, 0.5)
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("shape", SHAPES + LARGE)
+def test_values_beyond_fp16(shape, dtype):
+    """Two steps.  Singular values are at most 1, then m = 4.95; the polynomial's slope is at most l(1) = 51, then l(m): an error u |X| of the first X, 51 u of the second and
+    4.95 u of the result's factors come to at most 3 l(1) l(m) u in the Frobenius norm, times |X| = 1."""
+    gen = torch.Generator(device="cuda").manual_seed(case_seed(shape, 5))
+    g = torch.randn(shape, device="cuda", generator=gen).to(DTYPES[dtype])
+    got, = run([g], steps=2, coefficients=FAR)
+    a, b, c = FAR
+    x = g.double().t() if shape[0] > shape[1] else g.double()
+    x = x / (x.norm() + EPS)
+    for _ in range(2):
+        p = x @ x.t()
+        x = a * x + (b * p + c * (p @ p)) @ x
+    ref = x.t() if shape[0] > shape[1] else x
+    slope = lambda s: a - 3 * b * s ** 2 + 5 * c * s ** 4
+    tol = 3 * slope(1.0) * slope(4.95) * 2.0 ** -23 + (2.0 ** -8 * ref.norm().item() if dtype == "bf16" else 0)
+    assert note("|error|", (got.double() - ref).norm().item() / tol, 1.0)
+
+
+def test_muon_step_beyond_fp16():
+    rng = np.random.default_rng(8)
+    for rows, cols in ((20, 300), (70, 90), (100, 700)):
+        w, g, m = (rng.standard_normal((rows, cols)).astype(np.float32) for _ in range(3))
+        tw, tg, tm = on_gpu(w), on_gpu(g), on_gpu(m)
+        params = B.muon_params([(tw, tg, tm)])
+        B.muon_step(params, scratch(B.muon_step_workspace_bytes(params)), 0.5, momentum=0.5, weight_decay=0.0, steps=1, coefficients=FAR, eps=0.0)
+        torch.cuda.synchronize()
+        m64 = 0.5 * m.astype(np.float64) + g
+        o = newton_schulz(g + 0.5 * m64, 1, FAR, 0.0)
+        ref = w - 0.5 * np.sqrt(max(1.0, rows / cols)) * o
+        # one step: 2 l(1) u |X|, and the weights' own rounding
+        assert note("weights", np.linalg.norm(array(tw) - ref) / (0.5 * 2 * 51 * 2.0 ** -23 + 2.0 ** -23 * np.linalg.norm(ref)), 1.0)
+
+
+@pytest.mark.parametrize("shape", ((20, 30), (64, 100), (70, 90), (100, 3000), (300, 900)))
+@pytest.mark.parametrize("below", (1, 3, 6, 10, 14, 20, 40))
+def test_norms_below_eps(shape, below):
+    """|G| = 2^-below eps: X starts as small, and small values are kept to the same relative precision as others.  An error u |X| of a matrix X grows as X does, at most
+    a-fold in a step: |error| <= 6 a^5 u |X|, |X| = 2^-below at the start."""
+    g = gradient(np.random.default_rng(case_seed(shape, below)), *shape)
+    g = (g / np.linalg.norm(g.astype(np.float64)) * 2.0 ** -10).astype(np.float32)
+    got, = run([on_gpu(g)], eps=2.0 ** (below - 10))
+    ref = newton_schulz(g.astype(np.float64), eps=2.0 ** (below - 10))
+    assert note("|error|", np.linalg.norm(array(got) - ref) / (6 * COEFFICIENTS[0] ** 5 * 2.0 ** -23 * 2.0 ** -below), 1.0)
+
+
 @pytest.mark.parametrize("dtype", ("f32", "bf16"))
 @pytest.mark.parametrize("shape", SHAPES)
 def test_orthogonalise(shape, dtype):

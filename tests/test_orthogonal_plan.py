@@ -15,12 +15,20 @@ int main()
 {
     int cus, pieces, n;
     while (scanf("%d %d %d", &cus, &pieces, &n) == 3) {
+        if (cus == 0) {                          // (n steps of a polynomial)
+            double a, b, c;
+            int growth;
+            if (scanf("%lf %lf %lf", &a, &b, &c) != 3) return 1;
+            const bool small = dr::stays_small(n, a, b, c, &growth);
+            printf("%d %d\n", small, growth);
+            continue;
+        }
         dr::Group g;
         g.start();
         for (int i = 0; i < n; ++i) {
             int rows, cols;
             if (scanf("%d %d", &rows, &cols) != 2) return 1;
-            g.add(rows, cols, pieces);
+            g.add(rows, cols);
         }
         printf("%d %d %zu", g.whole, g.joined(cus), g.bytes(pieces, cus));
         for (int w = 0; w < dr::PRODUCTS; ++w) {
@@ -42,7 +50,8 @@ def ask(tmp_path_factory):
 
     def ask(cases):
         """cases: (compute units, pieces, shapes)"""
-        text = "\n".join("%d %d %d " % (cus, p, len(s)) + " ".join("%d %d" % v for v in s) for cus, p, s in cases)
+        line = lambda cus, p, s: "%d %d %d " % (cus, p, len(s)) + " ".join("%d %d" % v for v in s)
+        text = "\n".join(v if isinstance(v, str) else line(*v) for v in cases)
         out = subprocess.run([str(d / "plan")], input=text, capture_output=True, text=True, check=True, timeout=60).stdout.splitlines()
         assert len(out) == len(cases)
         return [[int(v) for v in line.split()] for line in out]
@@ -71,7 +80,7 @@ def check(case, plan):
         if splits > 1:
             assert w == 0 and kernel < 2 and tiles * splits <= cus and splits * WAVES[kernel] * AHEAD[kernel] <= longest, case
     if not whole:
-        squares = -(-8 * sum(square(s) for s in shapes) // 1024) * 1024
+        squares = -(-(8 * sum(square(s) for s in shapes) + 256) // 1024) * 1024
         kernel, splits, tiles, _ = products[:4]
         assert need == squares + operands + (tiles * splits * SIDE[kernel] ** 2 * 4096 if splits > 1 else 0), case
     return joined, products
@@ -98,3 +107,23 @@ def test_the_gpu_tests_reach_every_kernel(ask):
                 shared |= {products[0]} if products[1] > 1 else set()
         assert whole and together and seen == {(k, w) for k in range(5) for w in (False, True)}, (pieces, sorted(seen))
         assert shared == {0, 1}, (pieces, shared)
+
+
+def test_which_polynomials_stay_in_range(ask):
+    """... against the largest values on a fine grid: fp16 pieces only where X, A and Q stay below 65504 over their scales, and the growth of a step is not underestimated."""
+    import numpy as np
+    rng = random.Random(4)
+    cases = [(5, 3.4445, -4.7750, 2.0315), (5, 1.5, -0.5, 0.0), (64, 15 / 8, -10 / 8, 3 / 8), (1, 13.0, 0.0, 0.0), (3, 0.0, 0.0, 0.0), (2, 12.5, -12.0, 0.5), (4, 2.0, 0.0, 0.0),
+             (2, float("nan"), 0.0, 0.0), (1, 1.0, float("inf"), 0.0)]
+    cases += [(rng.randint(1, 8), rng.uniform(-6, 6), rng.uniform(-8, 8), rng.choice((0.0, rng.uniform(-4, 4)))) for _ in range(400)]
+    answers = ask(["0 0 %d %r %r %r" % v for v in cases])
+    assert answers[0] == [1, 2] and answers[1][0] and answers[2][0] and not any(answers[i][0] for i in (3, 5, 7, 8)) and 30 < sum(v[0] for v in answers[9:]) < 370
+    for (steps, a, b, c), (small, growth) in zip(cases, answers):
+        if not small:
+            continue
+        most = 1.0
+        for _ in range(steps):
+            s = np.linspace(0, most, 4001)
+            q = np.abs(a + b * s ** 2 + c * s ** 4)
+            assert most * 16384 < 65504 * 0.8 and most ** 2 * 4096 < 65504 * 0.8 and q.max() * 4096 < 65504 * 0.8 and q.max() <= 2.0 ** growth, (steps, a, b, c)
+            most = (s * q).max()
