@@ -382,6 +382,8 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[P], const u32x4 (&b)[P
 
 // A product of small matrices: W waves share a tile of T x T blocks, every wave a W-th of the contraction.  Operands go straight to registers, some k-blocks of them
 // while as many are multiplied: what such a product waits for is its first operands.  splits > 1: as many workgroups share a tile, and leave sums for sum_kernel.
+// 32 x 32 tiles: four k-blocks a wave ahead.  64 x 64: eight waves with one (four waves with two: five steps of 1201 x 500 127 us for 124, of 1024 x 1024 208 for 201, a step
+// of GoogLeNet's filters 487 for 475; 1024 x 4096 444 for 451).
 template <typename E, int P, int WHAT, int T, int W, bool MUON, int N>
 __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Jobs<N> j, int nth, int last, int splits)
 {
@@ -1146,7 +1148,7 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
             hipLaunchKernelGGL((tile_kernel<R, P, WHAT, 2, 2, T / 2, T / 2, decltype(depth)::value, decltype(apart)::value, END, N>), dim3(tiles), dim3(256), 0, st, c, j, nth, last);
         };
         if (choice.kernel == FINE) direct(integral_constant<int, 1>{}, integral_constant<int, 8>{});
-        else if (choice.kernel == DIRECT) direct(integral_constant<int, 2>{}, integral_constant<int, 4>{});
+        else if (choice.kernel == DIRECT) direct(integral_constant<int, 2>{}, integral_constant<int, 8>{});
         else if (choice.kernel == TILE4) tile(integral_constant<int, 4>{}, integral_constant<int, 2>{}, std::bool_constant<P == 3>{});
         else if (choice.kernel == TILE6) tile(integral_constant<int, 6>{}, integral_constant<int, 2>{}, std::false_type{});
         else tile(integral_constant<int, 8>{}, integral_constant<int, P == 3 ? 1 : 2>{}, std::false_type{});      // (registers: three pieces two deep 658 us for 590)

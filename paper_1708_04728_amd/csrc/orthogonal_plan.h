@@ -64,7 +64,7 @@ constexpr double NS_MOST_BLOCKS = 8388607;
 
 // Kernels for a product, by the blocks of a tile's side; k-blocks that a wave of the first two has in flight, and their waves
 enum { FINE, DIRECT, TILE4, TILE6, TILE8, KERNELS };
-constexpr int SIDE[KERNELS] = {1, 2, 4, 6, 8}, AHEAD[] = {4, 2}, WAVES[] = {8, 4};
+constexpr int SIDE[KERNELS] = {1, 2, 4, 6, 8}, AHEAD[] = {4, 1}, WAVES[] = {8, 8};
 
 inline int tiles_of(int what, int mb, int nb, int T)
 {
@@ -114,7 +114,7 @@ inline Choice choose(int P, int what, const Work& w, int cus)
         if (k == 0 || t < least) { least = t; best = Choice{k, 1}; }
     }
     if (what != GRAM) return best;
-    // few tiles of long rows: up to a workgroup per compute unit, with eight waves' (four waves') k-blocks in flight at once at least; the sums take a launch of 4 us
+    // few tiles of long rows: up to a workgroup per compute unit, with as many k-blocks for each as its waves have in flight at least; the sums take a launch of 4 us
     for (int k = FINE; k <= DIRECT; ++k) {
         const int splits = std::min(cus / std::max(w.tiles[k], 1), w.longest / (WAVES[k] * AHEAD[k]));
         if (splits < 2) continue;

@@ -39,7 +39,7 @@ int main()
     }
 }
 """
-SIDE, WAVES, AHEAD = (1, 2, 4, 6, 8), (8, 4), (4, 2)
+SIDE, WAVES, AHEAD = (1, 2, 4, 6, 8), (8, 8), (4, 1)
 
 
 @pytest.fixture(scope="module")
