@@ -108,12 +108,12 @@ struct Scales {
     }
     __device__ __forceinline__ float result_of(float v) const { return P == 2 ? ldexpf(v * (FROM_APPLY<P> * TO_RESULT<P>), -down) : v; }
 };
-// 2^shift times a norm of `norm` after the division is below 1; from 2^-200 on nothing of it is left in fp32 either way
+// 2^shift times a norm of `norm` after the division is from 1/2 to 1
 __device__ __forceinline__ int shift_of(double norm)
 {
     int exponent = 0;
     if (norm > 0.0 && norm < 0.5) frexp(norm, &exponent);
-    return min(-exponent, 200);
+    return -exponent;
 }
 
 // Operands of a matrix: X, X^T twice (a product reads one and writes the other), A, Q
@@ -143,7 +143,8 @@ __device__ __forceinline__ double sum256(double v, double* red)
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// Momentum (descent step), and the sums of the squares of U's elements, in double: a square of 1e20 or 1e-30 is no fp32 number
+// Momentum (descent step), and the sums of the squares of U's elements, in double: a square of 1e20 or 1e-30 is no fp32 number.  HBM bounds it: the step's 7.0 million
+// parameters of GoogLeNet 15.6 us, 5.4 TB/s; small ones a launch of 3 to 6 us.  (2048 elements a workgroup for 4096: 0.5 to 1 % of a single matrix' time less, 0.7 % of that list's more.)
 template <typename T, bool MUON, int N>
 __global__ __launch_bounds__(256) void squares_kernel(const Call c, const Jobs<N> j)
 {
@@ -244,7 +245,8 @@ __device__ __forceinline__ void put8(const float (&v)[8], unsigned char* block, 
     for (int e = 0; e < P; ++e) *reinterpret_cast<u32x4*>(block + (kb * P + e) * BLOCK + (threadIdx.x & 63) * 16) = p[e];
 }
 
-// X = U / (|U| + eps) in both orders, cut into pieces: a wave per 32 x 32 block
+// X = U / (|U| + eps) in both orders, cut into pieces: a wave per 32 x 32 block, through LDS, so that both are stored as whole KiB.  HBM bounds it: GoogLeNet's parameters
+// 112 MB in 21.6 us, 5.2 TB/s; small ones a launch of 5 us.
 template <typename T, int P, bool MUON, int N>
 __global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs<N> j)
 {
@@ -382,6 +384,7 @@ __device__ __forceinline__ void multiply(const u32x4 (&a)[P], const u32x4 (&b)[P
 
 // A product of small matrices: W waves share a tile of T x T blocks, every wave a W-th of the contraction.  Operands go straight to registers, some k-blocks of them
 // while as many are multiplied: what such a product waits for is its first operands.  splits > 1: as many workgroups share a tile, and leave sums for sum_kernel.
+// 4 to 5 us for matrices of one round of short contractions; Q X of 1201 x 500 10, GoogLeNet's list 27 for A and 20 for Q, by what a compute unit reads from L2 (64 bytes a cycle).
 // 32 x 32 tiles: four k-blocks a wave ahead.  64 x 64: eight waves with one (four waves with two: five steps of 1201 x 500 127 us for 124, of 1024 x 1024 208 for 201, a step
 // of GoogLeNet's filters 487 for 475; 1024 x 4096 444 for 451).
 template <typename E, int P, int WHAT, int T, int W, bool MUON, int N>
@@ -481,12 +484,6 @@ __global__ __launch_bounds__(W * 64) void product_kernel(const Call c, const Job
         if (i < lrows && k < rrows && (WHAT == APPLY || i >= k)) finish_task<P, WHAT>(c, m, op, sums[0][blk], i, k, by, turn, t & 3);
     }
 }
-
-// A product of larger matrices: WM x WN waves share a tile, TM x TN blocks of 32 x 32 each.  A stage is one k-block (16 k) of the tile's operands in LDS; of three stages
-// one is multiplied, one is complete, one is written, from registers that were loaded DEPTH iterations before, with a barrier an iteration.  A wave keeps one k-block of
-// its operands in registers.  The products of pieces come in an order in which every piece of the next k-block is read between the last product that needs the present one
-// and the first that needs it; reads, writes and loads are issued one by one between matrix instructions, which cover them: one wave per SIMD keeps its unit busy.
-template <int P, int BM, int BN> constexpr int tile_lds() { return 3 * (BM + BN) * P * BLOCK; }
 
 __device__ __forceinline__ void lds_barrier()        // orders LDS traffic only
 {
@@ -611,7 +608,7 @@ __global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Job
     else if (wave < 4) finish_task<P, APPLY>(c, m, op, sums[0], bi, bj, by, turn, wave);
 }
 
-// Adds the sums that the workgroups of a tile have left, in their order
+// Adds the sums that the workgroups of a tile have left, in their order: a launch more, 4 us, for contractions that would keep few compute units busy for longer
 template <typename E, int P, int WHAT, int T, bool MUON, int N>
 __global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j, int nth, int last, int splits)
 {
@@ -644,6 +641,13 @@ __device__ __forceinline__ void each_of(F f, std::integer_sequence<int, I...>) {
 template <int N, class F>
 __device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequence<int, N>{}); }
 
+// A product of larger matrices: WM x WN waves share a tile, TM x TN blocks of 32 x 32 each.  A stage is one k-block (16 k) of the tile's operands in LDS; of three stages
+// one is multiplied, one is complete, one is written, from registers that were loaded DEPTH iterations before, with a barrier an iteration.  A wave keeps one k-block of
+// its operands in registers.  The products of pieces come in an order in which every piece of the next k-block is read between the last product that needs the present one
+// and the first that needs it; reads, writes and loads are issued one by one between matrix instructions, which cover them: one wave per SIMD keeps its unit busy.
+// APART: sums of products with lower pieces on their own, where registers allow it.  The matrix cores' power bounds it: 4096 x 4096 on two pieces takes 193 us for A and 206 for Q
+// (1.1 PFLOP/s of products in 192 x 192 tiles) and 327 for Q X (1.26 in 256 x 256), three pieces 310, 325 and 540, and those with all operands zero 0.68 of that.
+template <int P, int BM, int BN> constexpr int tile_lds() { return 3 * (BM + BN) * P * BLOCK; }
 template <typename E, int P, int WHAT, int WM, int WN, int TM, int TN, int DEPTH, bool APART, bool MUON, int N>
 __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const Jobs<N> j, int nth, int last)
 {
