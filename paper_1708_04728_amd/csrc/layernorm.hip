@@ -43,7 +43,8 @@ __device__ __forceinline__ float block_sum(float v, float* red)
     return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// ---- any tensor: a workgroup per pixel, its channels read once for each sum
+// ---- any tensor: a workgroup per pixel, its channels read once for each sum.  For rows beyond 4096 vectors of 16 bytes (1024 x 32768 fp32 132 us, 2.0 TB/s), and planes so large that 32
+// bits do not address 64 pixels of an image (8192 channels of 301 x 300 fp32 48 ms: 4 bytes of every 64 that it fetches)
 template <typename T>
 __global__ __launch_bounds__(256) void norm_any_kernel(const Pixels px, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta,
                                                        float eps, int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(256) void norm_vectors_any_kernel(const Pixels px, 
     }
 }
 
-// dgamma and dbeta from the partial sums of `ranges` ranges of pixels, in a fixed order, in double
+// dgamma and dbeta from the partial sums of `ranges` ranges of pixels, in a fixed order, in double: 4 us, a launch
 __global__ __launch_bounds__(1024) void norm_vectors_sum_kernel(const float* __restrict__ partial, int ranges, int C, float* __restrict__ dgamma, float* __restrict__ dbeta)
 {
     __shared__ double red[64][17];
@@ -251,6 +252,8 @@ struct Place {
     }
 };
 
+// HBM bounds it: each element once.  192 channels of 56 x 56 x 128 bf16 56 us, 5.5 TB/s (part of it stays in the memory-side cache), fp32 119, 5.2; 333 of 56 x 56 x 64 fp32, whose rows start
+// anywhere, 111, 4.8; rows of 8192 fp32 5.9.  Small maps take a launch: 7.2 us of 14.7 MB.
 template <typename T, int G, int NV, int THREADS, bool RAGGED>
 __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps,
                                                             int relu, T* y, float* __restrict__ mean_out, float* __restrict__ rstd_out)
@@ -321,7 +324,8 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, 
     }
 }
 
-// ... and the gradient: every lane adds its columns of dgamma and dbeta over the workgroup's rows; partial[workgroup][2][C]
+// ... and the gradient: every lane adds its columns of dgamma and dbeta over the workgroup's rows; partial[workgroup][2][C].  192 channels of 56 x 56 x 128 bf16 102 us with the sum behind it,
+// 4.5 TB/s, fp32 182, 5.1; rows of 4096 bf16 47, 4.3; 14.9 MB 13.7, two launches
 template <typename T, int G, int NV, int THREADS, bool RAGGED>
 __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, int C, const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
                                                                  const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
@@ -420,7 +424,8 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
     for (int i = threadIdx.x; i < 2 * C; i += THREADS) partial[(size_t)blockIdx.x * 2 * C + i] = columns[i];
 }
 
-// ---- channels last, rows shorter than 16 bytes: a lane has a whole row
+// ---- channels last, rows shorter than 16 bytes: a lane has a whole row.  3 channels of 16.8 million pixels fp32 132 us, 3.1 TB/s (the gradient 188, 3.2); 7 of 8.4 million
+// in bf16 137 (159): element by element, bound by instructions
 constexpr int NARROW = 8;
 template <typename T>
 __global__ __launch_bounds__(256) void norm_narrow_kernel(size_t rows, int C, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta, float eps, int relu, T* y,
@@ -502,7 +507,8 @@ __global__ __launch_bounds__(256) void norm_grad_narrow_kernel(size_t rows, int 
 
 // ---- channel planes: LP pixels of any images a workgroup, a lane for each in 64 / LP channels at a time; its waves (16 at most) share the channels, NC of them at most in a
 // lane's registers.  An element's address is a plane's, the same for the wave, and the lane's 32-bit distance from it: with 64-bit addresses of their own the loads wait for
-// arithmetic (the gradient of 192 channels on 28 x 28 x 32 pixels fp32 22.8 us for 17.2).
+// arithmetic (the gradient of 192 channels on 28 x 28 x 32 pixels fp32 22.8 us for 17.2).  HBM bounds them:
+// 192 channels of 56 x 56 x 64 fp32 62 us, 5.0 TB/s, the gradient 105, 4.4; bf16, whose planes are 128 bytes of 64 pixels, 3.3 and 3.8; 28 x 28 x 32 fp32 11.3 and 19.4, a round of workgroups.
 constexpr int PLANES_WAVES = 16;
 template <typename T, int LP>
 struct Planes {
@@ -692,7 +698,8 @@ __global__ __launch_bounds__(PLANES_WAVES * 64) void norm_grad_planes_kernel(con
     }
 }
 
-// ... of more channels than registers hold: read again for each use (from the caches), CHUNK channels of a lane at a time, by 16 waves
+// ... of more channels than registers hold: read again for each use (from the caches), CHUNK channels of a lane at a time, by 16 waves: 2048 of 28 x 28 x 32 fp32
+// 183 us, 3.3 TB/s of three passes, the gradient 232, 4.4 of five
 constexpr int CHUNK = 16;
 template <typename T, int LP>
 __global__ __launch_bounds__(PLANES_WAVES * 64) void norm_long_planes_kernel(const Pixels px, const T* x, const float* __restrict__ gamma, const float* __restrict__ beta,
@@ -846,18 +853,20 @@ void with_lanes(int nvec, int most, size_t rows, F f)
 }
 
 // f(LP, NC): pixels of a workgroup, channels of a lane; NC = 0: more channels than registers hold (`most` of a lane).  64 pixels, a whole 256 bytes of a plane, but where they
-// make fewer workgroups than half of the compute units: 16 (832 channels of 7 x 7 x 128 fp32 33.5 us with 64, 22.8 with 16; 192 of 28 x 28 x 32 11.2 and 14.2 with 32).
+// make fewer workgroups than half of the compute units: 16 (832 channels of 7 x 7 x 128 fp32 33.5 us with 64, 22.8 with 16; 192 of 28 x 28 x 32 11.2 and 14.2 with 32),
+// and where 16 have up to `once` channels in registers which 64 have not (forward: 832 channels of 14 x 14 x 128 90.8 us read twice, 81.1 once; 1024 of 28 x 28 x 64 183 and 137;
+// the gradient 109 and 133, 212 and 224; 2048 of 28 x 28 x 32, 32 channels of a lane, forward 183 and 189).
 template <class F>
-void with_planes(const Pixels& px, int most, F f)
+void with_planes(const Pixels& px, int most, int once, F f)
 {
     auto with_nc = [&](auto lp) {
         constexpr int LP = decltype(lp)::value, GROUPS = PLANES_WAVES * (64 / LP);      // lanes of a pixel at most
         if (px.C <= 8 * GROUPS / 2) f(lp, IC<8>{});
         else if (px.C <= 16 * GROUPS) f(lp, IC<16>{});
-        else if (px.C <= std::min(most, 32) * GROUPS) f(lp, IC<32>{});
+        else if (px.C <= most * GROUPS) f(lp, IC<32>{});
         else f(lp, IC<0>{});
     };
-    if (px.count >= 32 * (size_t)device_cus()) with_nc(IC<64>{});
+    if (px.count >= 32 * (size_t)device_cus() && (px.C <= most * PLANES_WAVES || px.C > once)) with_nc(IC<64>{});
     else with_nc(IC<16>{});
 }
 constexpr int COLUMNS_MOST = 8192;      // channels whose sums fit LDS (64 KB)
@@ -876,7 +885,7 @@ int norm_fwd(const dr_tensor& d, const T* x, const float* gamma, const float* be
         else hipLaunchKernelGGL((norm_rows_kernel<T, G, NV, TH, true>), dim3(grid), dim3(TH), 0, st, px.count, C, x, gamma, beta, eps, relu, y, mean, rstd);
     };
     if (px.planes && planes_near(px, sizeof(T))) {
-        with_planes(px, 32, [&](auto lp, auto nc) {
+        with_planes(px, 32, 16 * 4 * PLANES_WAVES, [&](auto lp, auto nc) {
             constexpr int LP = decltype(lp)::value, NC = decltype(nc)::value, EACH = NC * (64 / LP);
             const dim3 grid((unsigned)((px.count + LP - 1) / LP));
             if constexpr (NC == 0) hipLaunchKernelGGL((norm_long_planes_kernel<T, LP>), grid, dim3(PLANES_WAVES * 64), 0, st, px, x, gamma, beta, eps, relu, y, mean, rstd);
@@ -915,7 +924,7 @@ int norm_bwd(const dr_tensor& d, const T* dy, const T* x, const float* gamma, co
         };
         if (px.planes) {
             if (planes_near(px, sizeof(T)) && C <= COLUMNS_MOST)
-                with_planes(px, px.count >= 32 * (size_t)device_cus() ? 32 : 16, [&](auto lp, auto nc) {
+                with_planes(px, px.count >= 32 * (size_t)device_cus() ? 32 : 16, 0, [&](auto lp, auto nc) {
                     constexpr int LP = decltype(lp)::value, NC = decltype(nc)::value, EACH = NC * (64 / LP);
                     ranges = even_blocks((px.count + LP - 1) / LP, most);
                     if constexpr (NC == 0)

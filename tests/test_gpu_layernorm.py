@@ -103,6 +103,7 @@ SHAPES = [
     (1, 1, 1, 1), (5, 1, 3, 3), (1, 3, 7, 9), (2, 7, 5, 5), (3, 8, 1, 1), (130, 16, 1, 1), (1, 24, 63, 1), (2, 64, 13, 5), (3, 65, 8, 8), (1, 96, 1, 129),
     (2, 192, 14, 14), (7, 333, 3, 5), (3, 509, 5, 7), (1, 512, 8, 8), (1, 1000, 1, 1), (4, 1024, 3, 3), (300, 1024, 1, 1), (2, 1100, 7, 3), (3, 2048, 2, 2), (5, 2056, 1, 1),
     (2, 4096, 1, 3), (1, 5001, 2, 2), (2, 8192, 1, 2), (1, 20000, 1, 2), (1, 70001, 1, 1), (65, 192, 7, 7), (9, 12, 31, 33),
+    (11, 700, 28, 28),
 ]
 
 
