@@ -247,7 +247,7 @@ _ALIKE = "tensors of one call share shape, dtype and order"
 
 
 def _alike(x, *others):
-    """dr_tensor of x, then the pointers of x and of others like it (None: NULL)."""
+    """dr_tensor of x, its channels and pixels, then the pointers of x and of others like it (None: NULL)."""
     if isinstance(x, NHWC):
         x = x.t
         n, h, w, c = shape = x.shape
@@ -259,7 +259,8 @@ def _alike(x, *others):
     dtype = x.dtype
     if not x.is_contiguous():
         raise ValueError("tensor must be contiguous")
-    out = [dr_tensor(n, c, h, w, _dtype_code(x), layout), x.data_ptr()]
+    code = _DTYPES.get(dtype)
+    out = [dr_tensor(n, c, h, w, _dtype_code(x) if code is None else code, layout), c, n * h * w, x.data_ptr()]
     for t in others:
         if t is None:
             out.append(None)
@@ -510,9 +511,9 @@ def sgd_step(w, dw, lr, stream=None):
 
 def layernorm_fwd(x, gamma, beta, eps, relu, y, mean=None, rstd=None, stream=None):
     """y = layer normalisation of x over its channels (then ReLU if relu); mean, rstd: fp32 tensors of n * h * w entries for layernorm_bwd, or None."""
-    d, px, py = _alike(x, y)
-    g, b = _vectors(d.c, gamma, beta)
-    m, r = _vectors(d.n * d.h * d.w, mean, rstd) if mean is not None or rstd is not None else (None, None)
+    d, c, pixels, px, py = _alike(x, y)
+    g, b = _vectors(c, gamma, beta)
+    m, r = _vectors(pixels, mean, rstd) if mean is not None or rstd is not None else (None, None)
     rc = lib().dr_layernorm_fwd(d, px, g, b, eps, int(relu), py, m, r, _stream(stream))
     if rc:
         _check(rc)
@@ -527,9 +528,9 @@ def layernorm_bwd_workspace_bytes(x):
 
 def layernorm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, stream=None):
     """dx, dgamma, dbeta (each may be None) from dy and the forward pass's x, mean and rstd."""
-    d, px, pdy, pdx = _alike(x, dy, dx)
-    g, dg, db = _vectors(d.c, gamma, dgamma, dbeta)
-    m, r = _vectors(d.n * d.h * d.w, mean, rstd)
+    d, c, pixels, px, pdy, pdx = _alike(x, dy, dx)
+    g, dg, db = _vectors(c, gamma, dgamma, dbeta)
+    m, r = _vectors(pixels, mean, rstd)
     _check(lib().dr_layernorm_bwd(d, pdy, px, g, m, r, pdx, dg, db, _ptr(ws), _nbytes(ws), _stream(stream)))
     return dx, dgamma, dbeta
 
