@@ -134,6 +134,27 @@ def test_muon_step_beyond_fp16():
         assert note("weights", np.linalg.norm(array(tw) - ref) / (0.5 * 2 * 51 * 2.0 ** -23 + 2.0 ** -23 * np.linalg.norm(ref)), 1.0)
 
 
+@pytest.mark.parametrize("shape", ((40, 60), (64, 147), (192, 576), (500, 700)))
+@pytest.mark.parametrize("kind", ("rows of all sizes", "elements of all sizes", "three directions", "one element"))
+def test_values_far_apart(shape, kind):
+    """Rows or elements eight decades apart, a matrix of rank three, a single element: what is small is kept well enough for the bound on the whole."""
+    rng = np.random.default_rng(case_seed((shape, kind)))
+    g = rng.standard_normal(shape)
+    if kind == "rows of all sizes":
+        g *= np.logspace(0, -8, shape[0])[:, None]
+    elif kind == "elements of all sizes":
+        g *= 10 ** (-8 * rng.random(shape))
+    elif kind == "three directions":
+        g = g[:, :3] @ rng.standard_normal((3, shape[1]))
+    else:
+        g[:] = 0
+        g[shape[0] // 2, shape[1] // 3] = 7
+    g = g.astype(np.float32)
+    got, = run([on_gpu(g)])
+    ref = newton_schulz(g.astype(np.float64))
+    assert note("|error|", np.linalg.norm(array(got) - ref) / bound(ref, "f32"), 1.0)
+
+
 @pytest.mark.parametrize("shape", ((20, 30), (64, 100), (70, 90), (100, 3000), (300, 900)))
 @pytest.mark.parametrize("below", (1, 3, 6, 10, 14, 20, 40))
 def test_norms_below_eps(shape, below):
