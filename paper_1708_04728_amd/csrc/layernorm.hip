@@ -324,15 +324,15 @@ __global__ __launch_bounds__(THREADS) void norm_rows_kernel(size_t rows, int C, 
     }
 }
 
-// ... and the gradient: every lane adds its columns of dgamma and dbeta over the workgroup's rows; partial[workgroup][2][C].  192 channels of 56 x 56 x 128 bf16 102 us with the sum behind it,
-// 4.5 TB/s, fp32 182, 5.1; rows of 4096 bf16 47, 4.3; 14.9 MB 13.7, two launches
+// ... and the gradient: every lane adds its columns of dgamma and dbeta over the workgroup's rows; partial[workgroup][2][C].  192 channels of 56 x 56 x 128 bf16 95 us with the sum behind it,
+// 4.9 TB/s; rows of 4096 bf16 46, 4.4; 14.9 MB 11.5, 6.3 in this launch (9.6 where the waves added their columns to one array in turn)
 template <typename T, int G, int NV, int THREADS, bool RAGGED>
 __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, int C, const T* dy, const T* x, const float* __restrict__ gamma, const float* __restrict__ mean,
                                                                  const float* __restrict__ rstd, T* dx, float* __restrict__ partial)
 {
     constexpr int VN = Store<T>::VN, GROUPS = THREADS / G, IN_WAVE = G < 64 ? 64 / G : 1, TURNS = GROUPS / IN_WAVE;
     __shared__ float red[2][THREADS / 64][2];
-    extern __shared__ float columns[];                 // [2][C]
+    extern __shared__ float columns[];                 // [TURNS][2][C]
     int turn = 0;
     const int lane = threadIdx.x % G, group = threadIdx.x / G, nvec = (C + VN - 1) / VN;
     uint4 nx[NV], nd[NV];
@@ -395,7 +395,7 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
         }
     }
     if (!partial) return;
-    // the groups of a wave, then the waves in turn
+    // the groups of a wave, each wave's sums (those of the waves that share a row) on their own in LDS, then all of a column's
 #pragma unroll
     for (int k = G; k < 64; k *= 2)
 #pragma unroll
@@ -405,23 +405,26 @@ __global__ __launch_bounds__(THREADS) void norm_grad_rows_kernel(size_t rows, in
                 dg[j][e] += __shfl_xor(dg[j][e], k, 64);
                 db[j][e] += __shfl_xor(db[j][e], k, 64);
             }
-    for (int t = 0; t < TURNS; ++t) {
-        if (group / IN_WAVE == t && group % IN_WAVE == 0) {
+    if (group % IN_WAVE == 0) {
+        float* const mine = columns + (size_t)(group / IN_WAVE) * 2 * C;
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
-                if (lane + j * G < nvec) {
+        for (int j = 0; j < NV; ++j)
+            if (lane + j * G < nvec) {
 #pragma unroll
-                    for (int e = 0; e < VN; ++e) {
-                        if (RAGGED && e < at(j).skip) continue;
-                        const int c = at(j).first + e;
-                        columns[c] = t ? columns[c] + dg[j][e] : dg[j][e];
-                        columns[C + c] = t ? columns[C + c] + db[j][e] : db[j][e];
-                    }
+                for (int e = 0; e < VN; ++e) {
+                    if (RAGGED && e < at(j).skip) continue;
+                    mine[at(j).first + e] = dg[j][e];
+                    mine[C + at(j).first + e] = db[j][e];
                 }
-        }
-        __syncthreads();
+            }
     }
-    for (int i = threadIdx.x; i < 2 * C; i += THREADS) partial[(size_t)blockIdx.x * 2 * C + i] = columns[i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * C; i += THREADS) {
+        float s = columns[i];
+#pragma unroll
+        for (int t = 1; t < TURNS; ++t) s += columns[t * 2 * C + i];
+        partial[(size_t)blockIdx.x * 2 * C + i] = s;
+    }
 }
 
 // ---- channels last, rows shorter than 16 bytes: a lane has a whole row.  3 channels of 16.8 million pixels fp32 132 us, 3.1 TB/s (the gradient 188, 3.2); 7 of 8.4 million
@@ -919,8 +922,9 @@ int norm_bwd(const dr_tensor& d, const T* dy, const T* x, const float* gamma, co
         auto rows = [&](auto g, auto nv, auto threads) {
             constexpr int G = decltype(g)::value, NV = decltype(nv)::value, TH = decltype(threads)::value;
             ranges = (int)blocks_for(px.count, TH / G, std::min(most, device_cus() * (TH > 256 ? 1 : 2)));
-            if (C % VN == 0) hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH, false>), dim3(ranges), dim3(TH), 2 * C * sizeof(float), st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
-            else hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH, true>), dim3(ranges), dim3(TH), 2 * C * sizeof(float), st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
+            const size_t columns = (size_t)(G < 64 ? TH / 64 : TH / G) * 2 * C * sizeof(float);      // (64 KB at most)
+            if (C % VN == 0) hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH, false>), dim3(ranges), dim3(TH), columns, st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
+            else hipLaunchKernelGGL((norm_grad_rows_kernel<T, G, NV, TH, true>), dim3(ranges), dim3(TH), columns, st, px.count, C, dy, x, gamma, mean, rstd, dx, partial);
         };
         if (px.planes) {
             if (planes_near(px, sizeof(T)) && C <= COLUMNS_MOST)
