@@ -608,21 +608,20 @@ __global__ __launch_bounds__(512) void poly_apply_kernel(const Call c, const Job
     else if (wave < 4) finish_task<P, APPLY>(c, m, op, sums[0], bi, bj, by, turn, wave);
 }
 
-// Adds the sums that the workgroups of a tile have left, in their order: a launch more, 4 us, for contractions that would keep few compute units busy for longer
-template <typename E, int P, int WHAT, int T, bool MUON, int N>
-__global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j, int nth, int last, int splits)
+// Adds the sums that the workgroups of a tile of A have left, in their order: a launch more, 4 us, for contractions that would keep few compute units busy for longer
+template <int P, int T, int N>
+__global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j, int nth, int splits)
 {
     __shared__ __attribute__((aligned(16))) float tile[32 * PITCH];
     const int unit = (int)blockIdx.x / (T * T), blk = (int)blockIdx.x - unit * (T * T);
     const Mat m = find_matrix(j, unit);
     const Operands<P> op(c, j, m);
-    const int turn = nth & 1;
     const Scales<P> by(c, P == 2 ? c.shifts[m.k] : 0, nth);
     int bi, bj;
-    tile_blocks<WHAT, T>(m, unit - m.first, bi, bj);
+    tile_blocks<GRAM, T>(m, unit - m.first, bi, bj);
     bi += blk / T;
     bj += blk % T;
-    if (bi >= m.mb || bj >= (WHAT == APPLY ? m.nb : m.mb) || (WHAT != APPLY && bi < bj)) return;
+    if (bi >= m.mb || bj >= m.mb || bi < bj) return;
     const float* const from = c.partial + ((size_t)unit * splits * (T * T) + blk) * 1024;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     for (int k = 0; k < splits; ++k)
@@ -631,8 +630,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const Call c, const Jobs<N> j,
 #pragma unroll
     for (int n = 0; n < 4; ++n) tile[(n * 8 + (threadIdx.x >> 5)) * PITCH + (threadIdx.x & 31)] = s[n];
     __syncthreads();
-    if (WHAT == APPLY && last) finish_result<E, P, MUON, N>(c, j, m, tile, bi, bj, by, threadIdx.x >> 5, 8);
-    else finish_task<P, WHAT>(c, m, op, tile, bi, bj, by, turn, threadIdx.x >> 6);
+    finish_task<P, GRAM>(c, m, op, tile, bi, bj, by, nth & 1, threadIdx.x >> 6);
 }
 
 // f(0), ..., f(N - 1), as constants
@@ -790,15 +788,13 @@ __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const 
             // register v holds row 8 (v / 4) + 4 half + v % 4 of column lane % 32
 #pragma unroll
             for (int v = 0; v < 16; ++v) tile[(8 * (v >> 2) + 4 * half + (v & 3)) * PITCH + l32] = APART ? acc[i][k][v] + small[APART ? i : 0][APART ? k : 0][v] : acc[i][k][v];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-            __builtin_amdgcn_wave_barrier();
+            wave_lds();
             if (WHAT == APPLY && last) finish_result<E, P, MUON, N>(c, j, m, tile, ri, rk, by, half, 2);
             else {
 #pragma unroll 1
                 for (int t = 0; t < 4; ++t) finish_task<P, WHAT>(c, m, op, tile, ri, rk, by, turn, t);
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
-            __builtin_amdgcn_wave_barrier();
+            wave_lds();
         }
 }
 
@@ -1144,7 +1140,7 @@ int run_group(const Group& group, Call c, Jobs<N>& j, int steps, void* ws, hipSt
             constexpr int T = decltype(side)::value, W = decltype(waves)::value;
             hipLaunchKernelGGL((product_kernel<R, P, WHAT, T, W, END, N>), dim3(tiles * choice.splits), dim3(W * 64), 0, st, c, j, nth, last, choice.splits);
             if constexpr (WHAT == GRAM) {
-                if (choice.splits > 1) hipLaunchKernelGGL((sum_kernel<R, P, WHAT, T, END, N>), dim3(tiles * T * T), dim3(256), 0, st, c, j, nth, last, choice.splits);
+                if (choice.splits > 1) hipLaunchKernelGGL((sum_kernel<P, T, N>), dim3(tiles * T * T), dim3(256), 0, st, c, j, nth, choice.splits);
             }
         };
         auto tile = [&](auto side, auto depth, auto apart) {
