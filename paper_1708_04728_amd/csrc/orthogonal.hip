@@ -108,6 +108,8 @@ struct Scales {
     }
     __device__ __forceinline__ float result_of(float v) const { return P == 2 ? ldexpf(v * (FROM_APPLY<P> * TO_RESULT<P>), -down) : v; }
 };
+// (0 where |U| + eps is: a matrix of zeros stays zero with eps = 0 too)
+__device__ __forceinline__ double one_over(double v) { return v == 0.0 ? 0.0 : 1.0 / v; }
 // 2^shift times a norm of `norm` after the division is from 1/2 to 1
 __device__ __forceinline__ int shift_of(double norm)
 {
@@ -273,7 +275,7 @@ __global__ __launch_bounds__(256) void cut_kernel(const Call c, const Jobs<N> j)
     }
     double s = 0.0;
     for (int i = threadIdx.x; i < squares_of(m.rows, m.cols); i += 256) s += c.squares[j.squares[m.k] + i];
-    const double norm = sqrt(sum256(s, red)), inv = 1.0 / (norm + (double)c.eps);
+    const double norm = sqrt(sum256(s, red)), inv = one_over(norm + (double)c.eps);
     double scale = inv;
     if constexpr (P == 2) {
         const int shift = shift_of(norm * inv);
@@ -866,7 +868,7 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
     for (int d = 32; d >= 1; d >>= 1) s += __shfl_xor(s, d, 64);
     if (lane == 0) red[wave] = s;
     __syncthreads();
-    const double norm = sqrt(((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]))), inv = 1.0 / (norm + (double)c.eps);
+    const double norm = sqrt(((red[0] + red[1]) + (red[2] + red[3])) + ((red[4] + red[5]) + (red[6] + red[7]))), inv = one_over(norm + (double)c.eps);
     const int shift = P == 2 ? shift_of(norm * inv) : 0;
     // (inv as factor 2^exponent: inv itself may be no fp32 number, and a product in double is four times the work)
     int exponent;
