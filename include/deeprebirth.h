@@ -249,10 +249,11 @@ int dr_layernorm_bwd(const dr_tensor* d, const void* dy, const void* x, const fl
  *   X = G / (|G|_F + eps), on the transpose where G has more rows than columns;
  *   `steps` times:  A = X X^T,  X = a X + (b A + c A A) X.
  * count matrices of dtype (DR_F32 or DR_BF16), dense, row by row; ms, g, o: host arrays of count shapes / device
- * pointers (o[i] == g[i] is allowed).  Elements of X, A and their polynomial are held to 2^-23 of their values, or 2^-37 of
- * the norm that X starts with where that is more, and sums in fp32, whatever the matrix units multiply.  A matrix of zeros stays zero; one that holds an infinity or a NaN
- * becomes NaN and touches no other.  1 <= steps <= DR_MAX_NS_STEPS, eps >= 0.  A matrix has at most 2^31-1 elements, a
- * list less than 2^23 blocks of 32 x 32 (matrices padded to them).  ws: device scratch of at least
+ * pointers (o[i] == g[i] is allowed).  Elements of X, A and their polynomial are held to 2^-23 of their values, or 2^-33 of
+ * what the norm of X can be at that step where that is more (rows or directions of G that far below its norm may be lost),
+ * and sums in fp32, whatever the matrix units multiply.  A matrix of zeros stays zero, with eps = 0 too; one that holds an
+ * infinity or a NaN becomes NaN and touches no other.  1 <= steps <= DR_MAX_NS_STEPS, eps >= 0.  A matrix has at most 2^31-1
+ * elements, a list less than 2^23 blocks of 32 x 32 (matrices padded to them).  ws: device scratch of at least
  * dr_orthogonalise_workspace_bytes, 256-byte aligned. */
 #define DR_MAX_NS_STEPS 64
 typedef struct { int rows, cols; } dr_matrix;

@@ -67,8 +67,9 @@ struct Jobs {
 
 struct Call {
     double* squares;
-    int* shifts;                             // of the matrices (pieces of fp16): X is held multiplied by 2^held_at(shift, growth, step)
+    int* shifts;                             // of the matrices (pieces of fp16): X is held multiplied by 2^held_at(shift, growth, spare, step)
     int growth;
+    float spare;
     float* partial;                          // sums of workgroups that share a tile
     unsigned char* ws;
     float a, b, c, eps;                      // a times, c by the scale of A and Q: Q's scale times (a I + b A + c A A) of A's sums
@@ -99,7 +100,7 @@ struct Scales {
     int down;                                // the result, times 2^-down
     __device__ __forceinline__ Scales(const Call& call, int shift, int step)
     {
-        const int now = P == 2 ? held_at(shift, call.growth, step) : 0, next = P == 2 ? held_at(shift, call.growth, step + 1) : 0;
+        const int now = P == 2 ? held_at(shift, call.growth, call.spare, step) : 0, next = P == 2 ? held_at(shift, call.growth, call.spare, step + 1) : 0;
         gram = FROM_GRAM<P>;
         b = P == 2 ? ldexpf(call.b, -2 * now) : call.b;
         c = P == 2 ? ldexpf(call.c, -4 * now) : call.c;
@@ -1040,7 +1041,7 @@ __global__ __launch_bounds__(512) void whole_kernel(const Call c, const Jobs<N> 
     };
     if (mb == 1) iterate(std::integral_constant<int, 1>{});
     else iterate(std::integral_constant<int, 2>{});
-    const int held = held_at(shift, c.growth, steps);
+    const int held = held_at(shift, c.growth, c.spare, steps);
     auto result_of = [&](float v) __attribute__((always_inline)) { return P == 2 ? ldexpf(v * TO_RESULT<P>, -held) : v; };
     elements([&](int i, const int (&at)[AT_ONCE]) {
         float w[AT_ONCE];
@@ -1201,7 +1202,7 @@ int run_list(Call c, int count, const dr_newton_schulz& ns, void* ws, hipStream_
         c.a = ns.a * A_SCALE<P>; c.c = ns.c / A_SCALE<P>;
         return count == 1 ? run_jobs<E, P, MUON, 1>(c, count, ns.steps, ws, st, fill) : run_jobs<E, P, MUON, JOBS>(c, count, ns.steps, ws, st, fill);
     };
-    return stays_small(ns.steps, ns.a, ns.b, ns.c, &c.growth) ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 3>{});
+    return stays_small(ns.steps, ns.a, ns.b, ns.c, &c.growth, &c.spare) ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 3>{});
 }
 
 }  // namespace

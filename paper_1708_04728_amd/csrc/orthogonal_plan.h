@@ -21,12 +21,14 @@ constexpr int squares_of(int rows, int cols)
 
 // Scales of the fp16 pieces of X and of A and Q, and whether those suffice: no element of X, A = X X^T or Q = a I + b A + c A A may pass 65504 by far.  Elements are at
 // most the largest singular value, 1 at the start (|X|_F <= 1), which each step takes to at most the largest |a s + b s^3 + c s^5| of s up to it; that of Q is at most the
-// largest |a + b t + c t^2| of t = s^2.  Beyond 3, 9 and 12 (a quarter left for roundings) the pieces are of bf16, three of them.  growth: log2 of what a step multiplies
-// a singular value by, at most.
+// largest |a + b t + c t^2| of t = s^2.  Beyond 3, 9 and 12 (a quarter left for roundings) the pieces are of bf16, three of them.
+// growth, spare: a step multiplies a singular value by 2^(growth - spare) at most; growth is whole, spare below one of it, or what a polynomial below one takes away.
+// Small values grow by |a|: where that is so much less that the steps together would take more than two bits from what X's scale leaves them, or where Q is so small
+// itself that fp16's lower pieces end above its 2^-33, bf16 as well.
 constexpr float NS_X_SCALE = 16384.f, NS_A_SCALE = 4096.f;
-inline bool stays_small(int steps, double a, double b, double c, int* growth)
+inline bool stays_small(int steps, double a, double b, double c, int* growth, float* spare = nullptr)
 {
-    double most = 1.0;
+    double most = 1.0, fastest = 0.0;
     *growth = 0;
     for (int i = 0; i < steps; ++i) {
         const double end = most * most;
@@ -43,15 +45,22 @@ inline bool stays_small(int steps, double a, double b, double c, int* growth)
             if (d >= 0) { look((-3 * b + sqrt(d)) / (10 * c)); look((-3 * b - sqrt(d)) / (10 * c)); }
         } else if (b != 0) look(-a / (3 * b));
         if (!(x <= 3 && q <= 12)) return false;
-        while (q * 1.001 > (1 << *growth)) ++*growth;
+        fastest = std::max(fastest, q * 1.001);
         most = x * 1.001;                                            // (roundings)
     }
+    if (!(fabs(a) >= 1.0 / 16 && steps * log2(fastest / fabs(a)) <= 2.0)) return false;
+    while (fastest > (1 << *growth)) ++*growth;
+    if (spare) *spare = (float)(*growth - log2(fastest));
     return true;
 }
 
 // A matrix whose norm is far below eps starts from an X as small, which fp16 does not hold: it is held multiplied by 2^shift, at step k by 2^(what is left), as much less as
-// the steps before may have multiplied it by
-constexpr int held_at(int shift, int growth, int step) { return shift > growth * step ? shift - growth * step : 0; }
+// the steps before may have multiplied it by (in whole bits of all of them together: of each by itself, forty steps of a polynomial near one would take forty bits)
+constexpr int held_at(int shift, int growth, float spare, int step)
+{
+    const int left = shift - growth * step + (int)(spare * (float)step);
+    return left > 0 ? left : 0;
+}
 
 // matrices that fit the LDS of one workgroup: blocks of 32 of the short and of the long side
 constexpr bool whole_fits(int mb, int nb) { return mb == 1 ? nb <= 28 : mb == 2 && nb <= 11; }

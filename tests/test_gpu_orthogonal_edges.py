@@ -3,8 +3,8 @@ import numpy as np
 import pytest
 
 from paper_1708_04728_amd import binding as B
-from test_gpu_orthogonal import DTYPES, array, gradient, on_gpu, run, scratch
-from util import case_seed
+from test_gpu_orthogonal import COEFFICIENTS, DTYPES, array, gradient, newton_schulz, on_gpu, run, scratch
+from util import case_seed, note
 
 pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
@@ -37,3 +37,18 @@ def test_a_layer_without_gradient_keeps_its_weights(shapes):
     torch.cuda.synchronize()
     for before, after, momentum in zip(start, w, m):
         assert not momentum.any() and np.array_equal(array(after), array(before * 0.875))
+
+
+@pytest.mark.parametrize("shape", ((20, 30), (64, 100), (100, 300), (300, 900)))
+@pytest.mark.parametrize("coefficients,steps,below", (((1.0, 0.0, 0.0), 41, 40), ((1.1, -0.1, 0.0), 40, 40), ((1.5, -0.5, 0.0), 40, 60), (COEFFICIENTS, 30, 100), ((0.5, 0.0, 0.0), 40, 0),
+                                                      ((0.5, 0.0, 0.0), 40, 20), ((0.5, 1.5, -1.0), 40, 40)))
+def test_many_steps_on_small_norms(shape, coefficients, steps, below):
+    """|G| = 2^-below eps (0: no eps).  Every X stays far below one, or far below the one before it, so that each step multiplies it by a and nothing else: an error u |X| in
+    each of the steps + 1 matrices X, and one u in each of the a, come to at most (2 steps + 1) |a|^steps u 2^-below at the end."""
+    coefficients = tuple(float(np.float32(v)) for v in coefficients)
+    g = gradient(np.random.default_rng(case_seed((shape, steps), below)), *shape)
+    g = (g / np.linalg.norm(g.astype(np.float64)) * 2.0 ** -10).astype(np.float32)
+    eps = 2.0 ** (below - 10) if below else 0.0
+    got, = run([on_gpu(g)], steps=steps, coefficients=coefficients, eps=eps)
+    ref = newton_schulz(g.astype(np.float64), steps, coefficients, eps)
+    assert note("|error|", np.linalg.norm(array(got) - ref) / ((2 * steps + 1) * abs(coefficients[0]) ** steps * 2.0 ** -23 * 2.0 ** -below), 1.0)
