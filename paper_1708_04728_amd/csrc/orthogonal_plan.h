@@ -42,7 +42,8 @@ inline bool stays_small(int steps, double a, double b, double c, int* growth, fl
         if (c != 0) {
             look(-b / (2 * c));                                      // where the derivative of Q's is zero
             const double d = 9 * b * b - 20 * a * c;                 // ... of X's: a + 3 b t + 5 c t^2 = 0
-            if (d >= 0) { look((-3 * b + sqrt(d)) / (10 * c)); look((-3 * b - sqrt(d)) / (10 * c)); }
+            const double far = -3 * b - copysign(sqrt(d), b);        // (a sum without cancellation: c may be nearly nothing beside b)
+            if (d >= 0) { look(far / (10 * c)); if (far != 0) look(2 * a / far); }
         } else if (b != 0) look(-a / (3 * b));
         if (!(x <= 3 && q <= 12)) return false;
         fastest = std::max(fastest, q * 1.001);

@@ -79,3 +79,12 @@ def test_small_values_keep_their_bits(ask):
 def test_polynomials_that_are_small_themselves_take_three_pieces(ask):
     """Q is held multiplied by 2^12: below 2^-4 of one it would keep fewer than 33 bits below its largest value."""
     assert ask([(5, 0.01, 0.0, 0.0, 0), (1, 1e-6, 1e-7, 0.0, 0), (1, 0.0, 0.0, 0.0, 0), (1, 0.0, 1.0, 0.0, 0)]) == [None] * 4
+
+
+def test_the_largest_value_of_nearly_cubic_polynomials(ask):
+    """A coefficient c that is nearly nothing beside b: where X is largest, between 0 and 1, is found all the same."""
+    cases = [(1, sign * a, -sign * a, sign * c, 0) for a in (8.0, 11.0, 12.0) for sign in (1, -1) for c in (0.0, 1e-9, -1e-9, 1e-13, 1e-15, -1e-15, 1e-17, -1e-17, 1e-25, -1e-38)]
+    for (steps, a, b, c, _), held in zip(cases, ask(cases)):
+        s = np.linspace(0, 1, 20001)
+        most = (s * np.abs(a + b * s ** 2 + c * s ** 4)).max()
+        assert (held is None) == (most > 3), (a, b, c, most)
