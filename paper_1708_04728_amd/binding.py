@@ -246,6 +246,15 @@ def _ptrs(ts, n=1):
 _ALIKE = "tensors of one call share shape, dtype and order"
 
 
+def _rows_or_maps(shape):
+    """Dimensions of a (rows, c) or an (n, c, h, w) tensor."""
+    if len(shape) == 4:
+        return shape
+    if len(shape) == 2:
+        return shape[0], shape[1], 1, 1
+    raise ValueError("layer normalisation takes (rows, channels), (n, channels, h, w) or NHWC tensors")
+
+
 def _alike(x, *others):
     """dr_tensor of x, its channels and pixels, then the pointers of x and of others like it (None: NULL)."""
     if isinstance(x, NHWC):
@@ -254,7 +263,7 @@ def _alike(x, *others):
         layout, kind = DR_NHWC, NHWC
     else:
         shape = x.shape
-        n, c, h, w = shape if len(shape) == 4 else (tuple(shape) + (1, 1, 1, 1))[:4]
+        n, c, h, w = _rows_or_maps(shape)
         layout, kind = DR_NCHW, None
     dtype = x.dtype
     if not x.is_contiguous():
@@ -510,7 +519,8 @@ def sgd_step(w, dw, lr, stream=None):
 
 
 def layernorm_fwd(x, gamma, beta, eps, relu, y, mean=None, rstd=None, stream=None):
-    """y = layer normalisation of x over its channels (then ReLU if relu); mean, rstd: fp32 tensors of n * h * w entries for layernorm_bwd, or None."""
+    """y = layer normalisation of x, (rows, c), (n, c, h, w) or NHWC, over its channels (then ReLU if relu); mean, rstd: fp32 tensors of n * h * w entries for
+    layernorm_bwd, or None."""
     d, c, pixels, px, py = _alike(x, y)
     g, b = _vectors(c, gamma, beta)
     m, r = _vectors(pixels, mean, rstd) if mean is not None or rstd is not None else (None, None)
@@ -522,7 +532,7 @@ def layernorm_fwd(x, gamma, beta, eps, relu, y, mean=None, rstd=None, stream=Non
 
 def layernorm_bwd_workspace_bytes(x):
     n = C.c_size_t(0)
-    _check(lib().dr_layernorm_bwd_workspace_bytes(desc(x), C.byref(n)))
+    _check(lib().dr_layernorm_bwd_workspace_bytes(_alike(x)[0], C.byref(n)))
     return n.value
 
 
