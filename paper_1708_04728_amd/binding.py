@@ -243,6 +243,10 @@ def _ptrs(ts, n=1):
     return pack(*v)
 
 
+# checked here: ctypes would hand the library what 32 bits leave of a dimension
+_MOST_ELEMENTS = 2 ** 31 - 1
+_TOO_MANY = "tensor has more than 2^31-1 elements"
+
 _ALIKE = "tensors of one call share shape, dtype and order"
 
 
@@ -268,8 +272,11 @@ def _alike(x, *others):
     dtype = x.dtype
     if not x.is_contiguous():
         raise ValueError("tensor must be contiguous")
+    pixels = n * h * w
+    if pixels * c > _MOST_ELEMENTS:
+        raise ValueError(_TOO_MANY)
     code = _DTYPES.get(dtype)
-    out = [dr_tensor(n, c, h, w, _dtype_code(x) if code is None else code, layout), c, n * h * w, x.data_ptr()]
+    out = [dr_tensor(n, c, h, w, _dtype_code(x) if code is None else code, layout), c, pixels, x.data_ptr()]
     for t in others:
         if t is None:
             out.append(None)
@@ -555,8 +562,10 @@ def _matrix_dims(t):
         raise ValueError("a matrix or a filter tensor is at least 2-d")
     if not t.is_contiguous():
         raise ValueError("tensor must be contiguous")
-    rows = t.shape[0]
-    return rows, (t.numel() // rows if rows else 0)
+    rows, elements = t.shape[0], t.numel()
+    if elements > _MOST_ELEMENTS:
+        raise ValueError(_TOO_MANY)
+    return (rows, elements // rows) if elements else (0, 0)
 
 
 def _matrices(gs):
