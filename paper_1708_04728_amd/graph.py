@@ -202,5 +202,6 @@ def flat_params(params, dtype="f32", device="cuda", pack=False):
                 w = B.pack_filters(w)
             out += [w, to_device(q["b"], "f32", device)]
         else:
-            out += [to_device(q[k], "f32", device) for k in ("gamma", "beta", "mean", "var") if k in q]
+            names = ("gamma", "beta", "mean", "var") if "mean" in q or "var" in q else ("gamma", "beta")
+            out += [to_device(q[k], "f32", device) for k in names]
     return out
