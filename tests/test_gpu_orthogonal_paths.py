@@ -1,0 +1,120 @@
+"""Newton-Schulz orthogonalisation and the descent step on it where the kernels of large matrices and of long lists run, against the formulas in 64 bits (products of torch on the
+GPU); tests/test_orthogonal_reach.py counts which kernels these sizes reach.
+
+Tolerance.  X, A, Q and their products are kept to a relative u = 2^-23, whatever the type of the matrix.  A step multiplies an error in X by at most the largest slope l of
+the polynomial, and |X|_F likewise: over the steps the errors of the steps + 1 matrices X come to at most (steps + 1) l_1 l_2 ... u in the Frobenius norm.  Rounding to bf16 then moves
+an element by up to 2^-8 of it (8 significant bits), which is taken off element by element before the norm."""
+import numpy as np
+import pytest
+
+from paper_1708_04728_amd import binding as B
+from test_gpu_orthogonal import COEFFICIENTS, DTYPES, EPS, FAR, LARGE, run, scratch
+from util import case_seed, note
+
+pytestmark = pytest.mark.gpu
+torch = pytest.importorskip("torch")
+
+U = 2.0 ** -23
+# steps, coefficients, product of the steps' largest slopes: the published polynomial's slope is a at zero and largest there; FAR takes 1 to 4.95
+POLYNOMIALS = {"two pieces": (5, COEFFICIENTS, COEFFICIENTS[0] ** 5), "three pieces": (2, FAR, (12.5 + 36 + 2.5) * (12.5 + 36 * 4.95 ** 2 + 2.5 * 4.95 ** 4))}
+
+SINGLES = LARGE + [(700, 1300), (1501, 1500), (2700, 200), (64, 20000), (5000, 1100), (300, 900), (290, 451), (192, 576)]
+LISTS = {
+    "one workgroup for each of them": [(64, 147), (33, 31), (300, 20), (1, 1)],
+    "few rows": [(192, 576), (64, 147), (100, 700)],
+    "few rows of one long matrix": [(20, 30), (50, 18000)],
+    "a long contraction": [(2700, 200), (100, 100), (33, 40)],
+    "a longer one": [(20, 30), (500, 6000), (64, 64)],
+    "unlike each other": [(700, 1300), (64, 147), (1300, 700), (0, 5), (901, 900)],
+    "wide and tall": [(300, 700), (310, 690), (256, 2400), (600, 300), (20, 30)],
+    "large": [(1500, 1501), (1301, 1700), (17, 33)],
+    "larger": [(2700, 2600), (100, 700), (1500, 1501)],
+    "largest": [(4100, 4200), (300, 300)],
+    "two of the largest": [(3000, 3100), (3001, 2900)],
+    "more than a table's worth": [(10 + 7 * i % 150, 8 + 11 * i % 140) for i in range(66)] + [(400, 500), (90, 1000)],
+}
+
+
+def product_gradient(gen, rows, cols):
+    """A filter gradient: gradients behind a ReLU times features behind a ReLU, summed over pixels."""
+    pixels = 2 * min(rows, cols) + 64
+    dz = torch.randn((rows, pixels), device="cuda", generator=gen)
+    return (dz * (torch.rand((rows, pixels), device="cuda", generator=gen) < 0.6)) @ torch.randn((pixels, cols), device="cuda", generator=gen).abs()
+
+
+def newton_schulz64(u, steps, coefficients, eps=EPS):
+    a, b, c = coefficients
+    tall = u.shape[0] > u.shape[1]
+    x = u.double().t().contiguous() if tall else u.double()
+    x = x / (x.norm() + eps)
+    for _ in range(steps):
+        p = x @ x.t()
+        x = a * x + (b * p + c * (p @ p)) @ x
+    return x.t() if tall else x
+
+
+def check(got, g, dtype, polynomial, what=""):
+    steps, coefficients, slopes = POLYNOMIALS[polynomial]
+    ref = newton_schulz64(g, steps, coefficients)
+    off = (got.double() - ref).abs()
+    if dtype == "bf16":
+        off = (off - 2.0 ** -8 * ref.abs()).clamp(min=0)
+    return note("|error| " + what, off.norm().item() / ((steps + 1) * slopes * U), 1.0)
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("polynomial", POLYNOMIALS)
+@pytest.mark.parametrize("shape", SINGLES)
+def test_single_matrices(shape, polynomial, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(case_seed(shape, 11))
+    g = product_gradient(gen, *shape).to(DTYPES[dtype])
+    steps, coefficients, _ = POLYNOMIALS[polynomial]
+    got, = run([g], steps=steps, coefficients=coefficients)
+    assert check(got, g, dtype, polynomial)
+
+
+@pytest.mark.parametrize("dtype", ("f32", "bf16"))
+@pytest.mark.parametrize("polynomial", POLYNOMIALS)
+@pytest.mark.parametrize("name", LISTS)
+def test_lists_of_matrices(name, polynomial, dtype):
+    gen = torch.Generator(device="cuda").manual_seed(case_seed(name, 12))
+    gs = [product_gradient(gen, *s).to(DTYPES[dtype]) if min(s) else torch.zeros(s, dtype=DTYPES[dtype], device="cuda") for s in LISTS[name]]
+    steps, coefficients, _ = POLYNOMIALS[polynomial]
+    got = run(gs, steps=steps, coefficients=coefficients)
+    for o, g in zip(got, gs):
+        if g.numel():
+            assert check(o, g, dtype, polynomial, "%dx%d" % tuple(g.shape))
+    # the same bits again, in place
+    B.orthogonalise(gs, gs, scratch(B.orthogonalise_workspace_bytes(gs), 0), steps=steps, coefficients=coefficients)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, gs))
+
+
+@pytest.mark.parametrize("polynomial", POLYNOMIALS)
+@pytest.mark.parametrize("shapes", [[s] for s in SINGLES] + list(LISTS.values()), ids=["%dx%d" % s for s in SINGLES] + list(LISTS))
+def test_descent_steps(shapes, polynomial):
+    gen = torch.Generator(device="cuda").manual_seed(case_seed(shapes, 13))
+    steps, coefficients, slopes = POLYNOMIALS[polynomial]
+    lr, mu, decay = (float(np.float32(v)) for v in (0.3, 0.9, 0.1))
+    make = lambda s, f: f() if min(s) else torch.zeros(s, device="cuda")
+    w = [make(s, lambda: torch.randn(s, device="cuda", generator=gen) * (2.0 / s[1]) ** 0.5) for s in shapes]
+    g, m = ([make(s, lambda: product_gradient(gen, *s)) for s in shapes] for _ in range(2))
+    before = [tuple(t.double() for t in v) for v in zip(w, g, m)]
+    params = B.muon_params(list(zip(w, g, m)))
+    B.muon_step(params, scratch(B.muon_step_workspace_bytes(params)), lr, momentum=mu, weight_decay=decay, steps=steps, coefficients=coefficients)
+    torch.cuda.synchronize()
+    for s, (w0, g0, m0), got_w, got_g, got_m in zip(shapes, before, w, g, m):
+        if not min(s):
+            continue
+        m1 = mu * m0 + g0
+        u1 = g0 + mu * m1
+        move = lr * max(1.0, s[0] / s[1]) ** 0.5
+        w1 = (1 - lr * decay) * w0 - move * newton_schulz64(u1, steps, coefficients)
+        what = "%dx%d" % s
+        assert torch.equal(got_g.double(), g0)
+        # momentum: a product and a sum in fp32; U: the same again
+        assert note("momentum " + what, ((got_m.double() - m1).abs() / (U * ((mu * m0).abs() + g0.abs()) + 1e-30)).max().item(), 1.0)
+        # weights: two products and a sum in fp32; the direction, from a U that is off by 2^-22 of its terms
+        off_u = 2.0 ** -22 * ((g0.norm() + (mu * m0).norm()) / u1.norm()).item()
+        slack = 2.0 ** -22 * (w0.abs() + w1.abs()).norm().item() + move * slopes * ((steps + 1) * U + off_u)
+        assert note("weights " + what, (got_w.double() - w1).norm().item() / slack, 1.0)
