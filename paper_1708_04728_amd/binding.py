@@ -83,7 +83,7 @@ class dr_matrix(C.Structure):
 
 
 class dr_newton_schulz(C.Structure):
-    _fields_ = [("steps", C.c_int)] + [(f, C.c_float) for f in ("a", "b", "c", "eps")]
+    _fields_ = [("steps", C.c_int)] + [(f, C.c_float) for f in ("a", "b", "c", "eps")] + [("all_bits", C.c_int)]
 
 
 class dr_muon_param(C.Structure):
@@ -581,12 +581,14 @@ def orthogonalise_workspace_bytes(gs):
     return n.value
 
 
-def orthogonalise(gs, os, ws, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, stream=None):
-    """os[i] = the matrix gs[i] with its singular values moved to near one; lists of device tensors (filters: k x everything else)."""
+def orthogonalise(gs, os, ws, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, stream=None, all_bits=False):
+    """os[i] = the matrix gs[i] with its singular values moved to near one; lists of device tensors (filters: k x everything else).  all_bits: what lies more than
+    2^33 below a matrix' norm is kept too."""
     ms, dtype = _matrices(gs)
     if [(o.shape, o.dtype) for o in os] != [(g.shape, g.dtype) for g in gs] or not all(o.is_contiguous() for o in os):
         raise ValueError("outputs have the inputs' shapes and dtype and are contiguous")
-    _check(lib().dr_orthogonalise(len(gs), ms, dtype, _ptrs(gs), _ptrs(os), dr_newton_schulz(steps, *coefficients, eps), _ptr(ws), _nbytes(ws), _stream(stream)))
+    _check(lib().dr_orthogonalise(len(gs), ms, dtype, _ptrs(gs), _ptrs(os), dr_newton_schulz(steps, *coefficients, eps, int(all_bits)), _ptr(ws), _nbytes(ws),
+                                _stream(stream)))
     return os
 
 
@@ -615,10 +617,11 @@ def muon_step_workspace_bytes(params):
     return n.value
 
 
-def muon_step(params, ws, lr, momentum=0.95, weight_decay=0.0, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, stream=None):
-    """One descent step on orthogonalised momentum for every (w, dw, momentum) of muon_params."""
-    _check(lib().dr_muon_step(len(params.array), params.array, dr_muon(lr, momentum, weight_decay, dr_newton_schulz(steps, *coefficients, eps)), _ptr(ws), _nbytes(ws),
-                              _stream(stream)))
+def muon_step(params, ws, lr, momentum=0.95, weight_decay=0.0, steps=5, coefficients=NEWTON_SCHULZ, eps=1e-7, stream=None,
+              all_bits=False):
+    """One descent step on orthogonalised momentum for every (w, dw, momentum) of muon_params.  all_bits: as in orthogonalise."""
+    _check(lib().dr_muon_step(len(params.array), params.array, dr_muon(lr, momentum, weight_decay, dr_newton_schulz(steps, *coefficients, eps, int(all_bits))), _ptr(ws),
+                              _nbytes(ws), _stream(stream)))
     return params
 
 

@@ -8,7 +8,7 @@
 // in bf16, and 1e-6 to 1e-5 in fp32.  So matrices are held as two fp16 pieces whose sum is the value to 2^-23 (11 bits each, the lower one with a sign of its own), at
 // scales that keep them in fp16's range, and multiplied on the matrix cores: three products of pieces, with sums in fp32, for each product; the fourth, of the lower
 // pieces, is 2^-24 of it.  They end where fp32 ends (4096 x 4096: 3.5e-6 off, in fp32 4.3e-6) in half the time of three bf16 pieces, whose six products hold all of fp32's bits
-// and all of its range: polynomials whose values could pass fp16's take those (f32_pieces.h).  Results in bf16 go the same way: 16 bits would do, and two fp16 pieces cost no more.
+// and all of its range: polynomials whose values could pass fp16's take those (f32_pieces.h), and so do callers who ask for all bits.  Results in bf16 go the same way: 16 bits would do, and two fp16 pieces cost no more.
 //
 // A and A A are symmetric: only blocks on and below the diagonal are computed, and stored on both sides.
 //
@@ -1202,7 +1202,7 @@ int run_list(Call c, int count, const dr_newton_schulz& ns, void* ws, hipStream_
         c.a = ns.a * A_SCALE<P>; c.c = ns.c / A_SCALE<P>;
         return count == 1 ? run_jobs<E, P, MUON, 1>(c, count, ns.steps, ws, st, fill) : run_jobs<E, P, MUON, JOBS>(c, count, ns.steps, ws, st, fill);
     };
-    return stays_small(ns.steps, ns.a, ns.b, ns.c, &c.growth, &c.spare) ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 3>{});
+    return !ns.all_bits && stays_small(ns.steps, ns.a, ns.b, ns.c, &c.growth, &c.spare) ? run(std::integral_constant<int, 2>{}) : run(std::integral_constant<int, 3>{});
 }
 
 }  // namespace

@@ -52,3 +52,53 @@ def test_many_steps_on_small_norms(shape, coefficients, steps, below):
     got, = run([on_gpu(g)], steps=steps, coefficients=coefficients, eps=eps)
     ref = newton_schulz(g.astype(np.float64), steps, coefficients, eps)
     assert note("|error|", np.linalg.norm(array(got) - ref) / ((2 * steps + 1) * abs(coefficients[0]) ** steps * 2.0 ** -23 * 2.0 ** -below), 1.0)
+
+
+def directions(shape):
+    """A matrix with one element a row (a column, where it is tall): singular values from 1 to 10^-28, 28 decades in all."""
+    m = min(shape)
+    g = np.zeros(shape, dtype=np.float32)
+    i = np.arange(m)
+    g[(i, (7 * i + 3) % shape[1]) if m == shape[0] else ((7 * i + 3) % shape[0], i)] = 10.0 ** np.linspace(0, -28, m)
+    return g
+
+
+def off_by(got, g, all_bits):
+    """Largest ratio of an element's error to its bound.  Elements do not meet: each is s -> s (a + b s^2 + c s^4) five times.  Rounding X, Q and their product, five times, and X and
+    the norm at the start come to at most 17 u s, which grows at most a-fold in a step; without all bits what is held is off by as much as 2^-33 of the largest instead, where that is more."""
+    s = g.astype(np.float64) / (np.linalg.norm(g.astype(np.float64)) + float(np.float32(1e-7)))
+    ref, (a, b, c) = s.copy(), COEFFICIENTS
+    for _ in range(5):
+        ref = ref * (a + b * ref ** 2 + c * ref ** 4)
+    tol = 17 * a ** 5 * (2.0 ** -23 * s + (0 if all_bits else 2.0 ** -33 * (s > 0)))
+    assert not got[s == 0].any()
+    return (np.abs(got - ref)[s > 0] / tol[s > 0]).max()
+
+
+@pytest.mark.parametrize("all_bits", (False, True))
+@pytest.mark.parametrize("shape", ((2, 2), (40, 61), (64, 150), (61, 40), (192, 577), (290, 451), (700, 1300), (1501, 1500), (2700, 2600)))
+def test_singular_values_far_apart(shape, all_bits):
+    g = directions(shape)
+    got, = run([on_gpu(g)], all_bits=all_bits)
+    assert note("|error|", off_by(array(got), g, all_bits), 1.0)
+    # in a list
+    got = run([on_gpu(g), on_gpu(g[:1])], all_bits=all_bits)
+    assert note("|error|", max(off_by(array(got[0]), g, all_bits), off_by(array(got[1]), g[:1], all_bits)), 1.0)
+
+
+@pytest.mark.parametrize("shape", ((40, 61), (192, 577), (700, 1301)))
+def test_a_step_on_singular_values_far_apart(shape):
+    """From weights of zero without momentum and decay, a step of one: minus the orthogonalised gradient."""
+    g = directions(shape)
+    w, m = (torch.zeros(shape, device="cuda") for _ in range(2))
+    params = B.muon_params([(w, on_gpu(g), m)])
+    B.muon_step(params, scratch(B.muon_step_workspace_bytes(params)), 1.0, momentum=0.0, weight_decay=0.0, all_bits=True)
+    torch.cuda.synchronize()
+    assert note("|error|", off_by(-array(w), g, True), 1.0)
+
+
+def test_all_bits_of_bf16_matrices():
+    g = torch.from_numpy(directions((64, 150))).bfloat16().cuda()
+    got, = run([g], all_bits=True)
+    wide, = run([g.float()], all_bits=True)
+    assert torch.equal(got, wide.bfloat16())

@@ -15,8 +15,9 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 U = 2.0 ** -23
-# steps, coefficients, product of the steps' largest slopes: the published polynomial's slope is a at zero and largest there; FAR takes 1 to 4.95
-POLYNOMIALS = {"two pieces": (5, COEFFICIENTS, COEFFICIENTS[0] ** 5), "three pieces": (2, FAR, (12.5 + 36 + 2.5) * (12.5 + 36 * 4.95 ** 2 + 2.5 * 4.95 ** 4))}
+# what a call asks for, and the product of the steps' largest slopes: the published polynomial's slope is a at zero and largest there; FAR takes 1 to 4.95
+POLYNOMIALS = {"two pieces": (dict(steps=5, coefficients=COEFFICIENTS), COEFFICIENTS[0] ** 5), "all bits": (dict(steps=5, coefficients=COEFFICIENTS, all_bits=True), COEFFICIENTS[0] ** 5),
+               "three pieces": (dict(steps=2, coefficients=FAR), (12.5 + 36 + 2.5) * (12.5 + 36 * 4.95 ** 2 + 2.5 * 4.95 ** 4))}
 
 SINGLES = LARGE + [(700, 1300), (1501, 1500), (2700, 200), (64, 20000), (5000, 1100), (300, 900), (290, 451), (192, 576)]
 LISTS = {
@@ -42,7 +43,7 @@ def product_gradient(gen, rows, cols):
     return (dz * (torch.rand((rows, pixels), device="cuda", generator=gen) < 0.6)) @ torch.randn((pixels, cols), device="cuda", generator=gen).abs()
 
 
-def newton_schulz64(u, steps, coefficients, eps=EPS):
+def newton_schulz64(u, steps, coefficients, eps=EPS, all_bits=None):
     a, b, c = coefficients
     tall = u.shape[0] > u.shape[1]
     x = u.double().t().contiguous() if tall else u.double()
@@ -54,12 +55,12 @@ def newton_schulz64(u, steps, coefficients, eps=EPS):
 
 
 def check(got, g, dtype, polynomial, what=""):
-    steps, coefficients, slopes = POLYNOMIALS[polynomial]
-    ref = newton_schulz64(g, steps, coefficients)
+    asked, slopes = POLYNOMIALS[polynomial]
+    ref = newton_schulz64(g, **asked)
     off = (got.double() - ref).abs()
     if dtype == "bf16":
         off = (off - 2.0 ** -8 * ref.abs()).clamp(min=0)
-    return note("|error| " + what, off.norm().item() / ((steps + 1) * slopes * U), 1.0)
+    return note("|error| " + what, off.norm().item() / ((asked["steps"] + 1) * slopes * U), 1.0)
 
 
 @pytest.mark.parametrize("dtype", ("f32", "bf16"))
@@ -68,8 +69,7 @@ def check(got, g, dtype, polynomial, what=""):
 def test_single_matrices(shape, polynomial, dtype):
     gen = torch.Generator(device="cuda").manual_seed(case_seed(shape, 11))
     g = product_gradient(gen, *shape).to(DTYPES[dtype])
-    steps, coefficients, _ = POLYNOMIALS[polynomial]
-    got, = run([g], steps=steps, coefficients=coefficients)
+    got, = run([g], **POLYNOMIALS[polynomial][0])
     assert check(got, g, dtype, polynomial)
 
 
@@ -79,13 +79,12 @@ def test_single_matrices(shape, polynomial, dtype):
 def test_lists_of_matrices(name, polynomial, dtype):
     gen = torch.Generator(device="cuda").manual_seed(case_seed(name, 12))
     gs = [product_gradient(gen, *s).to(DTYPES[dtype]) if min(s) else torch.zeros(s, dtype=DTYPES[dtype], device="cuda") for s in LISTS[name]]
-    steps, coefficients, _ = POLYNOMIALS[polynomial]
-    got = run(gs, steps=steps, coefficients=coefficients)
+    got = run(gs, **POLYNOMIALS[polynomial][0])
     for o, g in zip(got, gs):
         if g.numel():
             assert check(o, g, dtype, polynomial, "%dx%d" % tuple(g.shape))
     # the same bits again, in place
-    B.orthogonalise(gs, gs, scratch(B.orthogonalise_workspace_bytes(gs), 0), steps=steps, coefficients=coefficients)
+    B.orthogonalise(gs, gs, scratch(B.orthogonalise_workspace_bytes(gs), 0), **POLYNOMIALS[polynomial][0])
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, gs))
 
@@ -94,14 +93,14 @@ def test_lists_of_matrices(name, polynomial, dtype):
 @pytest.mark.parametrize("shapes", [[s] for s in SINGLES] + list(LISTS.values()), ids=["%dx%d" % s for s in SINGLES] + list(LISTS))
 def test_descent_steps(shapes, polynomial):
     gen = torch.Generator(device="cuda").manual_seed(case_seed(shapes, 13))
-    steps, coefficients, slopes = POLYNOMIALS[polynomial]
+    asked, slopes = POLYNOMIALS[polynomial]
     lr, mu, decay = (float(np.float32(v)) for v in (0.3, 0.9, 0.1))
     make = lambda s, f: f() if min(s) else torch.zeros(s, device="cuda")
     w = [make(s, lambda: torch.randn(s, device="cuda", generator=gen) * (2.0 / s[1]) ** 0.5) for s in shapes]
     g, m = ([make(s, lambda: product_gradient(gen, *s)) for s in shapes] for _ in range(2))
     before = [tuple(t.double() for t in v) for v in zip(w, g, m)]
     params = B.muon_params(list(zip(w, g, m)))
-    B.muon_step(params, scratch(B.muon_step_workspace_bytes(params)), lr, momentum=mu, weight_decay=decay, steps=steps, coefficients=coefficients)
+    B.muon_step(params, scratch(B.muon_step_workspace_bytes(params)), lr, momentum=mu, weight_decay=decay, **asked)
     torch.cuda.synchronize()
     for s, (w0, g0, m0), got_w, got_g, got_m in zip(shapes, before, w, g, m):
         if not min(s):
@@ -109,12 +108,12 @@ def test_descent_steps(shapes, polynomial):
         m1 = mu * m0 + g0
         u1 = g0 + mu * m1
         move = lr * max(1.0, s[0] / s[1]) ** 0.5
-        w1 = (1 - lr * decay) * w0 - move * newton_schulz64(u1, steps, coefficients)
+        w1 = (1 - lr * decay) * w0 - move * newton_schulz64(u1, **asked)
         what = "%dx%d" % s
         assert torch.equal(got_g.double(), g0)
         # momentum: a product and a sum in fp32; U: the same again
         assert note("momentum " + what, ((got_m.double() - m1).abs() / (U * ((mu * m0).abs() + g0.abs()) + 1e-30)).max().item(), 1.0)
         # weights: two products and a sum in fp32; the direction, from a U that is off by 2^-22 of its terms
         off_u = 2.0 ** -22 * ((g0.norm() + (mu * m0).norm()) / u1.norm()).item()
-        slack = 2.0 ** -22 * (w0.abs() + w1.abs()).norm().item() + move * slopes * ((steps + 1) * U + off_u)
+        slack = 2.0 ** -22 * (w0.abs() + w1.abs()).norm().item() + move * slopes * ((asked["steps"] + 1) * U + off_u)
         assert note("weights " + what, (got_w.double() - w1).norm().item() / slack, 1.0)
