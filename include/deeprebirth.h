@@ -252,7 +252,7 @@ int dr_layernorm_bwd(const dr_tensor* d, const void* dy, const void* x, const fl
  * pointers (o[i] == g[i] is allowed).  Elements of X, A and their polynomial are held to 2^-23 of their values, or 2^-33 of
  * what the norm of X can be at that step where that is more (rows or directions of G that far below its norm may be lost),
  * and sums in fp32, whatever the matrix units multiply.  all_bits != 0: to 2^-23 of their values from 2^-100 on, whatever
- * the norm, in 1.1 to 1.7 times the time.  A matrix of zeros stays zero, with eps = 0 too; one that holds an
+ * the norm, in 1.2 to 1.7 times the time.  A matrix of zeros stays zero, with eps = 0 too; one that holds an
  * infinity or a NaN becomes NaN and touches no other.  1 <= steps <= DR_MAX_NS_STEPS, eps >= 0.  A matrix has at most 2^31-1
  * elements, a list less than 2^23 blocks of 32 x 32 (matrices padded to them).  ws: device scratch of at least
  * dr_orthogonalise_workspace_bytes, 256-byte aligned (enough for any polynomial and either precision). */

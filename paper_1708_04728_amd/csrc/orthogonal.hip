@@ -646,8 +646,9 @@ __device__ __forceinline__ void each(F f) { each_of(f, std::make_integer_sequenc
 // one is multiplied, one is complete, one is written, from registers that were loaded DEPTH iterations before, with a barrier an iteration.  A wave keeps one k-block of
 // its operands in registers.  The products of pieces come in an order in which every piece of the next k-block is read between the last product that needs the present one
 // and the first that needs it; reads, writes and loads are issued one by one between matrix instructions, which cover them: one wave per SIMD keeps its unit busy.
-// APART: sums of products with lower pieces on their own, where registers allow it.  The matrix cores' power bounds it: 4096 x 4096 on two pieces takes 193 us for A and 206 for Q
-// (1.1 PFLOP/s of products in 192 x 192 tiles) and 327 for Q X (1.26 in 256 x 256), three pieces 310, 325 and 540, and those with all operands zero 0.68 of that.
+// APART: sums of products with lower pieces on their own, where registers allow it; elsewhere a sum is rounded three (six) times a k-block instead of once, by 2^-24 of it each time.
+// The matrix cores' power seems to bound it: 4096 x 4096 on two pieces takes 193 us for A and 206 for Q (1.1 PFLOP/s of products in 192 x 192 tiles) and 327 for Q X (1.26 in
+// 256 x 256), three pieces 310, 325 and 540; of a matrix of zeros five steps take 2.41 ms for 3.73, on three pieces 4.35 for 6.22.
 template <int P, int BM, int BN> constexpr int tile_lds() { return 3 * (BM + BN) * P * BLOCK; }
 template <typename E, int P, int WHAT, int WM, int WN, int TM, int TN, int DEPTH, bool APART, bool MUON, int N>
 __global__ __launch_bounds__(WM * WN * 64) void tile_kernel(const Call c, const Jobs<N> j, int nth, int last)
