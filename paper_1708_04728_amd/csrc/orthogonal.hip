@@ -7,7 +7,7 @@
 // small singular values by a = 3.4 in every step, and with them what roundings of X leave there: 64 to 512 rows of a filter's gradient end 1e-2 off with X, A and Q
 // in bf16, and 1e-6 to 1e-5 in fp32.  So matrices are held as two fp16 pieces whose sum is the value to 2^-23 (11 bits each, the lower one with a sign of its own), at
 // scales that keep them in fp16's range, and multiplied on the matrix cores: three products of pieces, with sums in fp32, for each product; the fourth, of the lower
-// pieces, is 2^-24 of it.  They end where fp32 ends (4096 x 4096: 3.5e-6 off, in fp32 4.3e-6) in half the time of three bf16 pieces, whose six products hold all of fp32's bits
+// pieces, is 2^-24 of it.  They end where fp32 ends (4096 x 4096: 3.5e-6 off, in fp32 4.3e-6) in 0.6 of the time of three bf16 pieces, whose six products hold all of fp32's bits
 // and all of its range: polynomials whose values could pass fp16's take those (f32_pieces.h), and so do callers who ask for all bits.  Results in bf16 go the same way: 16 bits would do, and two fp16 pieces cost no more.
 //
 // A and A A are symmetric: only blocks on and below the diagonal are computed, and stored on both sides.
