@@ -273,6 +273,57 @@ typedef struct { float lr, momentum, weight_decay; dr_newton_schulz ns; } dr_muo
 int dr_muon_step_workspace_bytes(int count, const dr_muon_param* params, size_t* bytes);
 int dr_muon_step(int count, const dr_muon_param* params, const dr_muon* opt, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- adapting a network's classifier -------------------------------------------------------------------------------
+ * Dropout in front of the classifier (one of the paper's non-tensor layers; Srivastava et al. 2014), low-rank adapters of
+ * many tasks beside one shared projection (Hu et al. 2021), and the softmax loss.  Learning an adapter: dr_dropout_fwd or
+ * the adapters' own dropout, dr_adapter_fwd, dr_softmax_loss_grad, dr_adapter_bwd, dr_sgd_step.
+ *
+ * Dropout with probability p: y_i = x_i 65536 / (65536 - T) where d_i >= T, else 0, with T = round(65536 p) and d_i the half
+ * i % 8 (low half of the first word first) of Philox4x32-10 (Salmon et al. 2011) of the counter (i / 8, offset + *step), two
+ * 64-bit numbers, under the 64-bit key `seed`; i counts elements in memory order.  The mask is not stored: the gradient is
+ * the same call on dy.  step: a device number (NULL: 0), read when the kernel runs, so that a recorded graph draws
+ * new masks when the caller changes it.  Calls that shall draw apart differ in seed or offset.  0 <= p <= 1.  x == y is allowed. */
+typedef struct { float p; unsigned long long seed, offset; const unsigned long long* step; } dr_dropout;
+int dr_dropout_fwd(const dr_tensor* d, const void* x, const dr_dropout* drop, void* y, void* stream);
+
+/* Softmax loss of the rows of an {n, c, 1, 1} tensor z of logits, fp32 or bf16, and dL/dz: with the label t of a row
+ *   l = log sum exp z - (1 - smoothing) z_t - smoothing / c sum z,
+ *   dz_j = g (exp(z_j) / sum exp z - (1 - smoothing) [j = t] - smoothing / c).
+ * mean != 0: L = sum l / N and g = 1 / N over the N rows that have a label; else L = sum l, g = 1.  A label outside
+ * 0 .. c - 1 is none: the row's l and dz are 0 whatever its logits (N = 0: L = 0).  Logits of -inf have probability 0; a row with
+ * a label that holds a NaN, +inf or nothing but -inf becomes NaN.  labels: n device ints.  dz (may be NULL, may be z), loss: one device
+ * float (may be NULL), row_loss: n device floats, the l (may be NULL).  0 <= smoothing <= 1.  ws: device scratch of at least
+ * dr_softmax_loss_workspace_bytes, 256-byte aligned.  Sums are added in a fixed order. */
+int dr_softmax_loss_workspace_bytes(const dr_tensor* d, size_t* bytes);
+int dr_softmax_loss_grad(const dr_tensor* d, const void* z, const int* labels, float smoothing, int mean, void* dz, float* loss, float* row_loss, void* ws,
+                         size_t ws_bytes, void* stream);
+
+/* A projection (an inner product, or a 1x1 convolution at every pixel) of c_in channels to c_out that is shared, with `count`
+ * adapters of rank `rank` beside it.  For every pixel x of image i, with its adapter a = ids[i]:
+ *   inner = scales_a A_a drop(x),   y = W x + bias + B_a inner.
+ * An id outside 0 .. count - 1 is none: y = W x + bias, inner = 0.  x, y: channels-last tensors (any order where the map is
+ * 1x1), fp32 or bf16; W: c_out x c_in, A: count x rank x c_in, B: count x c_out x rank, dense, of the same type.  bias, scales: fp32,
+ * c_out and count entries (NULL: zeros, ones).  ids: one device int per image of x.  drop (NULL or p = 0: none): dropout of x in
+ * front of A only.  inner: fp32, rank values per pixel, that the gradient reads (NULL: not stored).  Sums, inner among them, are held in
+ * fp32.  1 <= rank <= DR_MAX_ADAPTER_RANK, 0 <= count <= DR_MAX_ADAPTERS (0: A, B and ids may be NULL).  Tensors do not overlap.
+ * ws: device scratch of at least dr_adapter_fwd_workspace_bytes, 256-byte aligned. */
+#define DR_MAX_ADAPTER_RANK 128
+#define DR_MAX_ADAPTERS 16384
+typedef struct { int count, rank, c_in, c_out; } dr_adapters;
+int dr_adapter_fwd_workspace_bytes(const dr_tensor* xd, const dr_adapters* ad, size_t* bytes);
+int dr_adapter_fwd(const dr_tensor* xd, const void* x, const dr_adapters* ad, const void* w, const float* bias, const void* a, const void* b, const float* scales,
+                   const int* ids, const dr_dropout* drop, const dr_tensor* yd, void* y, float* inner, void* ws, size_t ws_bytes, void* stream);
+
+/* Its gradient from dy = dL/dy, with the forward pass's x, inner, ids and dropout: with u = scales_a B_a^T dy
+ *   dx = W^T dy + drop'(A_a^T u),   dA_a = sum u drop(x)^T,   dB_a = sum dy inner^T   over the pixels of adapter a
+ * (zeros for an adapter without pixels).  W and bias are shared and fixed.  dx has x's type, da and db are fp32 in the order of A and
+ * B; each of the three may be NULL (not computed; db NULL: inner may be NULL).  Sums are added in a fixed order.  ws as above, of
+ * at least dr_adapter_bwd_workspace_bytes. */
+int dr_adapter_bwd_workspace_bytes(const dr_tensor* xd, const dr_adapters* ad, size_t* bytes);
+int dr_adapter_bwd(const dr_tensor* yd, const void* dy, const dr_tensor* xd, const void* x, const dr_adapters* ad, const void* w, const void* a, const void* b,
+                   const float* scales, const int* ids, const dr_dropout* drop, const float* inner, void* dx, float* da, float* db, void* ws, size_t ws_bytes,
+                   void* stream);
+
 /* ---- inception module (Sec. 3.2, Fig. 4) ---------------------------------------------------- */
 
 #define DR_MAX_STEPS 4

@@ -4,5 +4,6 @@
 ``graph``    - layer lists -> library descriptors / device parameters
 ``slim``     - streamline and branch slimming as transforms on layer lists
 ``fit``      - learning a slim layer with a normalisation of its own
+``adapt``    - adapting a network's classifier to many tasks (dropout, low-rank adapters, softmax loss)
 ``build``    - compiles the library for gfx950
 """

@@ -94,6 +94,14 @@ class dr_muon(C.Structure):
     _fields_ = [(f, C.c_float) for f in ("lr", "momentum", "weight_decay")] + [("ns", dr_newton_schulz)]
 
 
+class dr_dropout(C.Structure):
+    _fields_ = [("p", C.c_float), ("seed", C.c_ulonglong), ("offset", C.c_ulonglong), ("step", C.c_void_p)]
+
+
+class dr_adapters(C.Structure):
+    _fields_ = [(f, C.c_int) for f in ("count", "rank", "c_in", "c_out")]
+
+
 class DeepRebirthError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__("deeprebirth error %d: %s" % (code, msg))
@@ -138,6 +146,13 @@ _SIGNATURES = {
     "dr_orthogonalise": ([_i, _P(dr_matrix), _i, _vp, _vp, _P(dr_newton_schulz), _vp, _z, _vp], _i),
     "dr_muon_step_workspace_bytes": ([_i, _P(dr_muon_param), _P(_z)], _i),
     "dr_muon_step": ([_i, _P(dr_muon_param), _P(dr_muon), _vp, _z, _vp], _i),
+    "dr_dropout_fwd": ([_P(dr_tensor), _vp, _P(dr_dropout), _vp, _vp], _i),
+    "dr_softmax_loss_workspace_bytes": ([_P(dr_tensor), _P(_z)], _i),
+    "dr_softmax_loss_grad": ([_P(dr_tensor), _vp, _vp, _f, _i, _vp, _vp, _vp, _vp, _z, _vp], _i),
+    "dr_adapter_fwd_workspace_bytes": ([_P(dr_tensor), _P(dr_adapters), _P(_z)], _i),
+    "dr_adapter_fwd": ([_P(dr_tensor), _vp, _P(dr_adapters), _vp, _vp, _vp, _vp, _vp, _vp, _P(dr_dropout), _P(dr_tensor), _vp, _vp, _vp, _z, _vp], _i),
+    "dr_adapter_bwd_workspace_bytes": ([_P(dr_tensor), _P(dr_adapters), _P(_z)], _i),
+    "dr_adapter_bwd": ([_P(dr_tensor), _vp, _P(dr_tensor), _vp, _P(dr_adapters), _vp, _vp, _vp, _vp, _vp, _P(dr_dropout), _vp, _vp, _vp, _vp, _vp, _z, _vp], _i),
     "dr_inception_workspace_bytes": ([_P(dr_tensor), _P(dr_inception), _P(_z)], _i),
     "dr_inception_fwd": ([_P(dr_tensor), _vp, _P(dr_inception), _vp, _vp, _P(dr_tensor), _vp, _vp, _z, _vp], _i),
     "dr_net_create": ([_P(dr_layer_desc), _i, _P(_vp)], _i),
@@ -623,6 +638,171 @@ def muon_step(params, ws, lr, momentum=0.95, weight_decay=0.0, steps=5, coeffici
     _check(lib().dr_muon_step(len(params.array), params.array, dr_muon(lr, momentum, weight_decay, dr_newton_schulz(steps, *coefficients, eps, int(all_bits))), _ptr(ws),
                               _nbytes(ws), _stream(stream)))
     return params
+
+
+def _on_device(*ts):
+    """Refuses tensors that are not on the current device (None: nothing is passed)."""
+    current = -1
+    for t in ts:
+        if t is None:
+            continue
+        if isinstance(t, NHWC):
+            t = t.t
+        if not t.is_cuda:
+            raise ValueError("tensors of a call lie on the current device")
+        if current < 0:
+            current = torch.cuda.current_device() if _device is None else _device()
+        if t.get_device() != current:
+            raise ValueError("tensors of a call lie on the current device")
+
+
+def dropout_desc(p, seed, offset=0, step=None):
+    """Dropout with probability p; draws differ by seed and offset (64-bit numbers).  step: a device int64 tensor of one number added to offset when the kernel runs, or
+    None; the caller keeps it alive."""
+    if step is not None and (step.dtype != torch.int64 or step.numel() != 1 or not step.is_cuda):
+        raise ValueError("step is a device int64 tensor of one number")
+    if not (0 <= seed < 2 ** 64 and 0 <= offset < 2 ** 64):
+        raise ValueError("seed and offset are 64-bit numbers")
+    d = dr_dropout(p, seed, offset, None if step is None else step.data_ptr())
+    d.keep = step
+    return d
+
+
+def dropout_fwd(x, drop, y, stream=None):
+    """y = x with elements dropped as dropout_desc says, the others scaled; of dy for the gradient.  Any contiguous tensors of one shape; y may be x."""
+    tx, ty = (t.t if isinstance(t, NHWC) else t for t in (x, y))
+    if isinstance(x, NHWC) is not isinstance(y, NHWC) or tx.dtype is not ty.dtype or tx.shape != ty.shape:
+        raise ValueError(_ALIKE)
+    if not (tx.is_contiguous() and ty.is_contiguous()):
+        raise ValueError("tensor must be contiguous")
+    count = tx.numel()
+    if count > _MOST_ELEMENTS:
+        raise ValueError(_TOO_MANY)
+    _on_device(tx, ty)
+    _check(lib().dr_dropout_fwd(dr_tensor(1, count, 1, 1, _dtype_code(tx), DR_NCHW), tx.data_ptr(), drop, ty.data_ptr(), _stream(stream)))
+    return y
+
+
+def _logits(z):
+    """dr_tensor of a contiguous (rows, classes) tensor."""
+    if isinstance(z, NHWC) or z.dim() != 2:
+        raise ValueError("logits are (rows, classes)")
+    if not z.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    n, c = z.shape
+    if n * c > _MOST_ELEMENTS:
+        raise ValueError(_TOO_MANY)
+    return dr_tensor(n, c, 1, 1, _dtype_code(z), DR_NCHW)
+
+
+def _ints(t, n, what):
+    if t.dtype is not torch.int32:
+        raise TypeError("%s are int32" % what)
+    if t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s: a contiguous tensor of %d entries" % (what, n))
+    return t.data_ptr()
+
+
+def softmax_loss_workspace_bytes(z):
+    n = C.c_size_t(0)
+    _check(lib().dr_softmax_loss_workspace_bytes(_logits(z), C.byref(n)))
+    return n.value
+
+
+def softmax_loss_grad(z, labels, dz, loss, ws, smoothing=0.0, mean=True, row_loss=None, stream=None):
+    """loss[0] = softmax loss of logits z (rows, classes) for int32 labels, dz = its gradient (like z; may be z, may be None); mean: over the rows whose label is one of the
+    classes, else their sum.  row_loss: fp32, a value per row, or None."""
+    d = _logits(z)
+    if dz is not None and (isinstance(dz, NHWC) or dz.dtype is not z.dtype or dz.shape != z.shape or not dz.is_contiguous()):
+        raise ValueError("the gradient has the logits' shape and dtype and is contiguous")
+    for t, n in ((loss, 1), (row_loss, d.n)):
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("losses are contiguous fp32 tensors: one entry, and one per row")
+    _on_device(z, labels, dz, loss, row_loss, ws)
+    _check(lib().dr_softmax_loss_grad(d, z.data_ptr(), _ints(labels, d.n, "labels"), smoothing, int(mean), _ptr(dz), _ptr(loss), _ptr(row_loss), _ptr(ws), _nbytes(ws),
+                                      _stream(stream)))
+    return dz
+
+
+def _adapted(x, a, b):
+    """dr_tensor of x, a (rows, channels) or NHWC tensor, and dr_adapters of the adapters a (count, rank, c_in), b (count, c_out, rank)."""
+    if isinstance(x, NHWC):
+        n, h, w, c = x.t.shape
+        t, layout = x.t, DR_NHWC
+    elif x.dim() == 2:
+        (n, c), h, w = x.shape, 1, 1
+        t, layout = x, DR_NCHW
+    else:
+        raise ValueError("adapters take (rows, channels) or NHWC tensors")
+    if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
+        raise ValueError("adapters are (count, rank, c_in) and (count, c_out, rank)")
+    if a.dtype is not t.dtype or b.dtype is not t.dtype:
+        raise TypeError("input, projection and adapters share a dtype")
+    if not (t.is_contiguous() and a.is_contiguous() and b.is_contiguous()):
+        raise ValueError("tensor must be contiguous")
+    if max(t.numel(), a.numel(), b.numel()) > _MOST_ELEMENTS:
+        raise ValueError(_TOO_MANY)
+    count, rank, cin = a.shape
+    return dr_tensor(n, c, h, w, _dtype_code(t), layout), dr_adapters(count, rank, cin, b.shape[1])
+
+
+def _projected(xd, ad, x, y, w):
+    """dr_tensor of the projection's output y; checks w."""
+    if w is not None and (w.dtype is not x.dtype or tuple(w.shape) not in ((ad.c_out, ad.c_in), (ad.c_out, ad.c_in, 1, 1)) or not w.is_contiguous()):
+        raise ValueError("the projection is a contiguous (c_out, c_in) tensor of the input's dtype")
+    t = y.t if isinstance(y, NHWC) else y
+    if isinstance(y, NHWC) is not (xd.layout == DR_NHWC) or t.dtype is not x.dtype or tuple(t.shape) != ((xd.n, xd.h, xd.w, ad.c_out) if xd.layout == DR_NHWC else (xd.n, ad.c_out)):
+        raise ValueError("the output has the input's pixels, order and dtype and c_out channels")
+    if not t.is_contiguous():
+        raise ValueError("tensor must be contiguous")
+    if t.numel() > _MOST_ELEMENTS:
+        raise ValueError(_TOO_MANY)
+    return dr_tensor(xd.n, ad.c_out, xd.h, xd.w, xd.dtype, xd.layout)
+
+
+def adapter_fwd_workspace_bytes(x, a, b):
+    n = C.c_size_t(0)
+    _check(lib().dr_adapter_fwd_workspace_bytes(*_adapted(x, a, b), C.byref(n)))
+    return n.value
+
+
+def adapter_fwd(x, w, bias, a, b, ids, y, ws, scales=None, drop=None, inner=None, stream=None):
+    """y = projection w (c_out, c_in) of x plus bias plus the adapter b[ids] a[ids] of every image (or row) of x; an id outside the adapters adds nothing.  x: (rows, c_in) or
+    NHWC; ids: int32, one per row or image; scales: fp32 per adapter; drop: dropout_desc(...) of what the adapters read; inner: fp32, rank values per pixel, for adapter_bwd."""
+    xd, ad = _adapted(x, a, b)
+    yd = _projected(xd, ad, x, y, w)
+    if w is None:
+        raise ValueError("no projection")
+    for t, n in ((bias, ad.c_out), (scales, ad.count), (inner, xd.n * xd.h * xd.w * ad.rank)):
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("bias, scales and inner are contiguous fp32 tensors: entries per output channel, per adapter, and rank entries per pixel")
+    _on_device(x, w, bias, a, b, ids, y, ws, scales, inner)
+    _check(lib().dr_adapter_fwd(xd, _ptr(x), ad, w.data_ptr(), _ptr(bias), a.data_ptr(), b.data_ptr(), _ptr(scales), _ints(ids, xd.n, "ids"), drop, yd, _ptr(y), _ptr(inner),
+                                _ptr(ws), _nbytes(ws), _stream(stream)))
+    return y
+
+
+def adapter_bwd_workspace_bytes(x, a, b):
+    n = C.c_size_t(0)
+    _check(lib().dr_adapter_bwd_workspace_bytes(*_adapted(x, a, b), C.byref(n)))
+    return n.value
+
+
+def adapter_bwd(dy, x, w, a, b, ids, inner, dx, da, db, ws, scales=None, drop=None, stream=None):
+    """dx (like x), da, db (fp32, like a and b; each of the three may be None) from dy and the forward pass's x, ids, inner and dropout."""
+    xd, ad = _adapted(x, a, b)
+    yd = _projected(xd, ad, x, dy, w)
+    if dx is not None:
+        t, u = (v.t if isinstance(v, NHWC) else v for v in (x, dx))
+        if isinstance(x, NHWC) is not isinstance(dx, NHWC) or t.dtype is not u.dtype or t.shape != u.shape or not u.is_contiguous():
+            raise ValueError("dx has the input's shape, order and dtype and is contiguous")
+    for t, n in ((scales, ad.count), (inner, xd.n * xd.h * xd.w * ad.rank), (da, a.numel()), (db, b.numel())):
+        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
+            raise ValueError("scales, inner, da and db are contiguous fp32 tensors: entries per adapter, rank entries per pixel, and the adapters' shapes")
+    _on_device(dy, x, w, a, b, ids, inner, dx, da, db, ws, scales)
+    _check(lib().dr_adapter_bwd(yd, _ptr(dy), xd, _ptr(x), ad, _ptr(w), a.data_ptr(), b.data_ptr(), _ptr(scales), _ints(ids, xd.n, "ids"), drop, _ptr(inner), _ptr(dx), _ptr(da),
+                                _ptr(db), _ptr(ws), _nbytes(ws), _stream(stream)))
+    return dx, da, db
 
 
 def trace_begin(label_filter="", conv_k=0, conv_c=0, conv_r=0, capacity=4096):

@@ -1,0 +1,503 @@
+// Low-rank adapters of many requests beside one shared projection (dr_adapter_fwd) and their gradient (dr_adapter_bwd).  Rows are the pixels of channels-last images, and
+// every image names its adapter a:
+//
+//   forward    t = s_a A_a drop(x),  y = W x + b + B_a t
+//   gradient   u = s_a B_a^T dy,  dx = W^T dy + drop'(A_a^T u),  dA_a = sum u drop(x)^T,  dB_a = sum dy t^T  over the rows of adapter a
+//
+// Both are a narrow product (t, u: rows x rank), a wide one whose contraction runs over the projection and then over the rank, and for the gradient two sums over the rows
+// of each adapter.  Rows are visited in the order of their adapters, so that few tiles hold rows of several; such a tile takes its adapters one after the other.
+// t and u are held in fp32 and enter bf16 products as two pieces each (16 bits of their values): with one piece the adapter's part of y would be rounded twice.
+#include <algorithm>
+
+#include "dr_internal.h"
+#include "philox.h"
+#include "rows8.h"
+
+namespace dr {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Eight elements of an operand's row, as the matrix instructions take them.  A lane of group g = lane / 16 holds elements 8 g .. 8 g + 7 of a slice of 32: one
+// instruction in bf16, eight in fp32 (the j-th of them multiplies the j-th elements of the four groups).
+template <typename T> struct Operand;
+template <> struct Operand<uint16_t> {
+    u32x4 v;
+    __device__ __forceinline__ void load(const uint16_t* p, int n)      // n: elements that exist
+    {
+        if (n >= 8) v = *reinterpret_cast<const u32x4_any*>(p);
+        else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = (2 * i < n ? p[2 * i] : 0u) | (2 * i + 1 < n ? (unsigned)p[2 * i + 1] << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ void keep(int j, bool yes)
+    {
+        if (!yes) v[j >> 1] &= j & 1 ? 0xFFFFu : 0xFFFF0000u;
+    }
+};
+template <> struct Operand<float> {
+    f32x4 v[2];
+    __device__ __forceinline__ void load(const float* p, int n)
+    {
+        if (n >= 8) {
+            v[0] = *reinterpret_cast<const f32x4_any*>(p);
+            v[1] = *reinterpret_cast<const f32x4_any*>(p + 4);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = i < n ? p[i] : 0.f;
+        }
+    }
+    __device__ __forceinline__ void keep(int j, bool yes)
+    {
+        if (!yes) v[j >> 2][j & 3] = 0.f;
+    }
+};
+__device__ __forceinline__ f32x4 mfma(const Operand<uint16_t>& a, const Operand<uint16_t>& b, f32x4 c) { return mfma(a.v, b.v, c); }
+__device__ __forceinline__ f32x4 mfma(const Operand<float>& a, const Operand<float>& b, f32x4 c)
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i >> 2][i & 3], b.v[i >> 2][i & 3], c, 0, 0, 0);
+    return c;
+}
+
+// Which of the eight elements from `first` on dropout keeps: sets the others to zero (what is kept is scaled where the sums are, exactly)
+template <typename T>
+__device__ __forceinline__ void mask8(const Drop& d, uint64_t place, uint64_t first, Operand<T>& v)
+{
+    float one[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+    drop8_from(d, place, first, one);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v.keep(j, one[j] != 0.f);
+}
+// ... and of a single one
+__device__ __forceinline__ bool kept(const Drop& d, uint64_t place, uint64_t at)
+{
+    uint32_t r[4];
+    philox(d.seed, at >> 3, place, r);
+    const unsigned j = (unsigned)at & 7, w = j & 4 ? (j & 2 ? r[3] : r[2]) : (j & 2 ? r[1] : r[0]);
+    return (j & 1 ? w >> 16 : w & 0xFFFFu) >= d.border;
+}
+
+// Which row is at a position, and its adapter.  Positions walk the images in `order` (NULL: as they come).
+struct Rows {
+    int count, hw;               // rows; pixels of an image
+    int adapters, rank;
+    const int* ids;              // of every image
+    const int* order;
+    const int* starts;           // adapter a's images are order[starts[a]] .. order[starts[a + 1] - 1] (read by the sums over rows)
+    const float* scales;
+    __device__ __forceinline__ int row(int p, int* id) const
+    {
+        const int slot = p / hw, img = order ? order[slot] : slot, a = ids[img];
+        *id = (unsigned)a < (unsigned)adapters ? a : -1;
+        return img * hw + (p - slot * hw);
+    }
+};
+
+// ---- order of the images by adapter ---------------------------------------------------------------------------------------------------------
+// Workgroup a writes the images of adapter a (the last one those without) in the order in which they come: first how many belong before them, then which they are.
+__global__ __launch_bounds__(1024) void order_kernel(const int* __restrict__ ids, int n, int adapters, int* __restrict__ order, int* __restrict__ starts)
+{
+    __shared__ int red[16];
+    const int a = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    auto key = [&](int i) { const int id = ids[i]; return (unsigned)id < (unsigned)adapters ? id : adapters; };
+    int before = 0;
+    for (int i = threadIdx.x; i < n; i += 1024) before += key(i) < a;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) before += __shfl_xor(before, d, 64);
+    if (lane == 0) red[wave] = before;
+    __syncthreads();
+    int base = 0;
+    for (int w = 0; w < 16; ++w) base += red[w];
+    if (threadIdx.x == 0) starts[a] = base;
+    if (a == adapters && threadIdx.x == 0) starts[a + 1] = n;
+    for (int i0 = 0; i0 < n; i0 += 1024) {
+        const int i = i0 + threadIdx.x;
+        const bool mine = i < n && key(i) == a;
+        const unsigned long long set = __ballot(mine);
+        __syncthreads();
+        if (lane == 0) red[wave] = __popcll(set);
+        __syncthreads();
+        int at = base;
+        for (int w = 0; w < 16; ++w) {
+            at += w < wave ? red[w] : 0;
+            base += red[w];
+        }
+        if (mine) order[at + __popcll(set & ((1ull << lane) - 1))] = i;
+    }
+}
+
+// ---- a narrow product: out[row][r] = s_a sum_k v[row][k] M_a[r][k] -----------------------------------------------------------------------------
+// A workgroup takes 16 rows and the adapters among them, every `slots`-th from its own on; its waves share the contraction in slices of 32 and add up in LDS.
+template <typename T, int RB, int NW>
+__global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
+{
+    __shared__ int row_of[16], id_of[16];
+    __shared__ float red[NW][RB * 16][17];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+    if (threadIdx.x < 16) {
+        const int p = blockIdx.x * 16 + threadIdx.x;
+        int id = -2, row = -1;
+        if (p < q.count) row = q.row(p, &id);
+        row_of[threadIdx.x] = row;
+        id_of[threadIdx.x] = id;
+    }
+    __syncthreads();
+    if (blockIdx.y == 0)
+        for (int i = threadIdx.x; i < 16 * q.rank; i += NW * 64)
+            if (id_of[i / q.rank] == -1) out[(size_t)row_of[i / q.rank] * q.rank + i % q.rank] = 0.f;
+    const uint64_t place = drop.border ? drop_place(drop) : 0;
+    const int row = row_of[l16];
+    const T* vr = v + (size_t)max(row, 0) * K;
+    for (int a = -1, turn = 0;; ++turn) {
+        int next = 0x7FFFFFFF;
+        for (int i = 0; i < 16; ++i) next = id_of[i] > a ? min(next, id_of[i]) : next;
+        if (next == 0x7FFFFFFF) break;
+        a = next;
+        if (turn % gridDim.y != blockIdx.y) continue;
+        f32x4 acc[RB] = {};
+        for (int k = wave * 32 + g * 8; k - g * 8 < K; k += NW * 32) {
+            Operand<T> x, w;
+            x.load(vr + k, row >= 0 ? K - k : 0);
+            if (drop.border) mask8(drop, place, (uint64_t)((size_t)max(row, 0) * K + k), x);
+#pragma unroll
+            for (int b = 0; b < RB; ++b) {
+                const int r = b * 16 + l16;
+                w.load(m + ((size_t)a * q.rank + min(r, q.rank - 1)) * K + k, r < q.rank ? K - k : 0);
+                acc[b] = mfma(w, x, acc[b]);
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[wave][b * 16 + g * 4 + i][l16] = acc[b][i];
+        __syncthreads();
+        const float scale = (q.scales ? q.scales[a] : 1.f) * (drop.border ? drop.scale : 1.f);
+        for (int i = threadIdx.x; i < 16 * q.rank; i += NW * 64) {
+            const int n = i / q.rank, r = i - n * q.rank;
+            if (id_of[n] != a) continue;
+            float s = red[0][r][n];
+#pragma unroll
+            for (int w = 1; w < NW; ++w) s += red[w][r][n];
+            out[(size_t)row_of[n] * q.rank + r] = s * scale;
+        }
+    }
+}
+
+// ---- the wide product: y[row][o] = sum_k W[o][k] x[row][k] + bias[o] + drop'(sum_r B_a[o][r] t[row][r]) ---------------------------------------------
+// A workgroup owns 64 outputs of 64 rows, a wave 32 x 32 of them; operands straight from memory.
+template <typename T>
+__global__ __launch_bounds__(256) void wide_kernel(const Rows q, const T* __restrict__ x, int K, const T* __restrict__ w, const float* __restrict__ bias,
+                                                   const float* __restrict__ t, const T* __restrict__ b, int N, const Drop drop, T* __restrict__ y)
+{
+    __shared__ int row_of[64], id_of[64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+    if (threadIdx.x < 64) {
+        const int p = blockIdx.x * 64 + threadIdx.x;
+        int id = -2, row = -1;
+        if (p < q.count) row = q.row(p, &id);
+        row_of[threadIdx.x] = row;
+        id_of[threadIdx.x] = id;
+    }
+    __syncthreads();
+    const int first = (wave >> 1) * 32, o0 = blockIdx.y * 64 + (wave & 1) * 32;
+    int row[2], id[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        row[j] = row_of[first + j * 16 + l16];
+        id[j] = id_of[first + j * 16 + l16];
+    }
+    const uint64_t place = drop.border ? drop_place(drop) : 0;
+    f32x4 acc[2][2] = {};
+    for (int a = -1;;) {
+        int next = 0x7FFFFFFF;
+        for (int i = 0; i < 32; ++i) next = id_of[first + i] > a ? min(next, id_of[first + i]) : next;
+        if (next == 0x7FFFFFFF) break;
+        a = next;
+        f32x4 part[2][2] = {};               // of its own: rows of other adapters must not meet this one's numbers, not even times zero
+        constexpr int STEP = sizeof(T) == 2 ? 16 : 32;        // bf16: groups 0 and 1 hold the upper pieces of t, 2 and 3 the lower ones
+        for (int r0 = 0; r0 < q.rank; r0 += STEP) {
+            const int r = r0 + (sizeof(T) == 2 ? (g & 1) : g) * 8;
+            Operand<T> ob[2], ot[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int o = o0 + i * 16 + l16;
+                ob[i].load(b + ((size_t)a * N + min(o, N - 1)) * q.rank + r, o < N ? q.rank - r : 0);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float e[8];
+                load8(t + (size_t)max(row[j], 0) * q.rank + r, id[j] == a ? q.rank - r : 0, 0.f, e);
+                if constexpr (sizeof(T) == 2) {
+                    ot[j].v = pack8(e);
+                    if (g >= 2) {
+                        float high[8];
+                        unpack8(ot[j].v, high);
+#pragma unroll
+                        for (int c = 0; c < 8; ++c) e[c] -= high[c];
+                        ot[j].v = pack8(e);
+                    }
+                } else {
+                    ot[j].v[0] = f32x4{e[0], e[1], e[2], e[3]};
+                    ot[j].v[1] = f32x4{e[4], e[5], e[6], e[7]};
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) part[i][j] = mfma(ob[i], ot[j], part[i][j]);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = part[i][j][e];
+                    if (drop.border) v = kept(drop, place, (uint64_t)((size_t)max(row[j], 0) * N + o0 + i * 16 + g * 4 + e)) ? v * drop.scale : 0.f;
+                    acc[i][j][e] = id[j] == a ? v : acc[i][j][e];
+                }
+    }
+    for (int k = g * 8; k - g * 8 < K; k += 32) {
+        Operand<T> ow[2], ox[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int o = o0 + i * 16 + l16;
+            ow[i].load(w + (size_t)min(o, N - 1) * K + k, o < N ? K - k : 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) ox[j].load(x + (size_t)max(row[j], 0) * K + k, row[j] >= 0 ? K - k : 0);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = mfma(ow[i], ox[j], acc[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int o = o0 + i * 16 + g * 4 + e;
+                if (row[j] >= 0 && o < N) Store<T>::st(y + (size_t)row[j] * N + o, acc[i][j][e] + (bias ? bias[o] : 0.f));
+            }
+}
+
+// ---- transposed copies: src[batch][R][C] -> dst[batch][C][R] --------------------------------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ src, T* __restrict__ dst, int R, int C, int tiles_r, int tiles_c)
+{
+    __shared__ T tile[32][33];
+    const int b = blockIdx.x / (tiles_r * tiles_c), i = blockIdx.x - b * (tiles_r * tiles_c), r0 = i / tiles_c * 32, c0 = (i - i / tiles_c * tiles_c) * 32;
+    const int l = threadIdx.x & 31, h = threadIdx.x >> 5;
+    for (int k = h; k < 32; k += 8)
+        if (r0 + k < R && c0 + l < C) tile[k][l] = src[((size_t)b * R + r0 + k) * C + c0 + l];
+    __syncthreads();
+    for (int k = h; k < 32; k += 8)
+        if (c0 + k < C && r0 + l < R) dst[((size_t)b * C + c0 + k) * R + r0 + l] = tile[l][k];
+}
+
+// ---- sums over the rows of an adapter: out[a][r][c] (or [a][c][r]) = sum f[row][r] drop(v[row][c]) ---------------------------------------------------
+// A workgroup adds a share of adapter a's rows for 64 columns and 16 of the rank, its four waves every fourth row each; partial sums of several shares are added after.
+struct Sums {
+    int C, splits;
+    int ranks_last;              // out[a][c][r]
+    float* out;                  // [split][adapters][..]
+};
+template <typename T>
+__global__ __launch_bounds__(256) void rows_kernel(const Rows q, const Sums s, const T* __restrict__ v, const float* __restrict__ f, const Drop drop)
+{
+    __shared__ float red[4][16][65];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
+    const int a = blockIdx.y / s.splits, split = blockIdx.y - a * s.splits, r0 = blockIdx.z * 16;
+    const long long begin = (long long)q.starts[a] * q.hw, all = (long long)q.starts[a + 1] * q.hw - begin;
+    const int lo = (int)(begin + all * split / s.splits), hi = (int)(begin + all * (split + 1) / s.splits);
+    const uint64_t place = drop.border ? drop_place(drop) : 0;
+    float acc[16] = {};
+    for (int p = lo + wave; p < hi; p += 4) {
+        int id;
+        const int row = q.row(p, &id);
+        float e = c < s.C ? Store<T>::ld(v + (size_t)row * s.C + c) : 0.f;
+        if (drop.border && !kept(drop, place, (uint64_t)((size_t)row * s.C + c))) e = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[i] = __builtin_fmaf(r0 + i < q.rank ? f[(size_t)row * q.rank + r0 + i] : 0.f, e, acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) red[wave][i][lane] = acc[i];
+    __syncthreads();
+    const float scale = drop.border ? drop.scale : 1.f;
+    for (int i = threadIdx.x; i < 1024; i += 256) {
+        const int r = r0 + (s.ranks_last ? i & 15 : i >> 6), l = s.ranks_last ? i >> 4 : i & 63, cc = blockIdx.x * 64 + l;
+        if (r >= q.rank || cc >= s.C) continue;
+        const float sum = ((red[0][r - r0][l] + red[1][r - r0][l]) + (red[2][r - r0][l] + red[3][r - r0][l])) * scale;
+        float* out = s.out + ((size_t)split * q.adapters + a) * q.rank * s.C;
+        out[s.ranks_last ? (size_t)cc * q.rank + r : (size_t)r * s.C + cc] = sum;
+    }
+}
+__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ partial, int splits, size_t count, float* __restrict__ out)
+{
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= count) return;
+    float s = partial[i];
+    for (int k = 1; k < splits; ++k) s += partial[(size_t)k * count + i];
+    out[i] = s;
+}
+
+// ---- host ---------------------------------------------------------------------------------------------------------------------------------------
+constexpr int NARROW_WAVES = 8;
+
+template <typename T>
+void narrow(const Rows& q, const void* v, int K, const void* m, const Drop& drop, float* out, hipStream_t st)
+{
+    if (!q.count) return;
+    const int tiles = (q.count + 15) / 16, slots = tiles < 256 ? std::min({16, q.adapters, (256 + tiles - 1) / tiles}) : 1;
+    const dim3 grid(tiles, std::max(slots, 1)), block(NARROW_WAVES * 64);
+    if (q.rank <= 16) hipLaunchKernelGGL((narrow_kernel<T, 1, NARROW_WAVES>), grid, block, 0, st, q, (const T*)v, K, (const T*)m, drop, out);
+    else if (q.rank <= 32) hipLaunchKernelGGL((narrow_kernel<T, 2, NARROW_WAVES>), grid, block, 0, st, q, (const T*)v, K, (const T*)m, drop, out);
+    else if (q.rank <= 64) hipLaunchKernelGGL((narrow_kernel<T, 4, NARROW_WAVES>), grid, block, 0, st, q, (const T*)v, K, (const T*)m, drop, out);
+    else hipLaunchKernelGGL((narrow_kernel<T, 8, 4>), grid, dim3(256), 0, st, q, (const T*)v, K, (const T*)m, drop, out);
+}
+
+template <typename T>
+void wide(const Rows& q, const void* x, int K, const void* w, const float* bias, const float* t, const void* b, int N, const Drop& drop, void* y, hipStream_t st)
+{
+    if (!q.count) return;
+    hipLaunchKernelGGL((wide_kernel<T>), dim3((q.count + 63) / 64, (N + 63) / 64), dim3(256), 0, st, q, (const T*)x, K, (const T*)w, bias, t, (const T*)b, N, drop, (T*)y);
+}
+
+template <typename T>
+void transpose(const void* src, void* dst, int batch, int R, int C, hipStream_t st)
+{
+    const int tr = (R + 31) / 32, tc = (C + 31) / 32;
+    if (batch) hipLaunchKernelGGL((transpose_kernel<T>), dim3((unsigned)batch * tr * tc), dim3(256), 0, st, (const T*)src, (T*)dst, R, C, tr, tc);
+}
+
+// shares of an adapter's rows that workgroups of their own add: enough for four workgroups on every compute unit, of 64 rows and more if adapters have rows alike
+int splits_of(int rows, int adapters, int columns, int rank)
+{
+    const long long groups = (long long)adapters * ((columns + 63) / 64) * ((rank + 15) / 16);
+    const int per = adapters ? rows / adapters : 0;
+    return (int)std::max<long long>(1, std::min<long long>({(1024 + groups - 1) / std::max(groups, 1ll), (long long)per / 64, 64ll}));
+}
+
+template <typename T>
+void sum_rows(const Rows& q, const void* v, const float* f, int C, const Drop& drop, int ranks_last, float* out, float* partial, hipStream_t st)
+{
+    Sums s;
+    s.C = C; s.ranks_last = ranks_last;
+    s.splits = splits_of(q.count, q.adapters, C, q.rank);
+    s.out = s.splits > 1 ? partial : out;
+    hipLaunchKernelGGL((rows_kernel<T>), dim3((C + 63) / 64, q.adapters * s.splits, (q.rank + 15) / 16), dim3(256), 0, st, q, s, (const T*)v, f, drop);
+    if (s.splits > 1) {
+        const size_t count = (size_t)q.adapters * q.rank * C;
+        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, partial, s.splits, count, out);
+    }
+}
+
+struct Scratch {                 // places in the workspace
+    size_t order, starts, inner, wt, at, bt, partial, bytes;
+};
+Scratch scratch_of(const AdapterShape& p, bool backward)
+{
+    Scratch s = {};
+    size_t at = 0;
+    auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
+    const size_t el = elem_size(p.dtype), factors = (size_t)p.adapters * p.rank;
+    s.order = take((size_t)p.images * 4);
+    s.starts = take(((size_t)p.adapters + 2) * 4);
+    s.inner = take((size_t)p.images * p.hw * p.rank * 4);
+    if (backward) {
+        s.wt = take((size_t)p.in * p.out * el);
+        s.at = take(factors * p.in * el);
+        s.bt = take(factors * p.out * el);
+        const int rows = p.images * p.hw;
+        s.partial = take(factors * std::max((size_t)p.in * splits_of(rows, p.adapters, p.in, p.rank), (size_t)p.out * splits_of(rows, p.adapters, p.out, p.rank)) * 4);
+    }
+    s.bytes = at;
+    return s;
+}
+
+Rows rows_of(const AdapterShape& p, const AdapterArgs& g, char* ws, const Scratch& s, bool sorted)
+{
+    Rows q;
+    q.count = p.images * p.hw; q.hw = p.hw; q.adapters = p.adapters; q.rank = p.rank;
+    q.ids = g.ids; q.scales = g.scales;
+    q.order = sorted ? (const int*)(ws + s.order) : nullptr;
+    q.starts = (const int*)(ws + s.starts);
+    return q;
+}
+
+void put_in_order(const AdapterShape& p, const AdapterArgs& g, char* ws, const Scratch& s, hipStream_t st)
+{
+    hipLaunchKernelGGL(order_kernel, dim3(p.adapters + 1), dim3(1024), 0, st, g.ids, p.images, p.adapters, (int*)(ws + s.order), (int*)(ws + s.starts));
+}
+
+template <typename T>
+void forward(const AdapterShape& p, const AdapterArgs& g, const void* x, void* y, float* inner, const Drop& drop, char* ws, hipStream_t st)
+{
+    const Scratch s = scratch_of(p, false);
+    const bool sorted = p.images > 64 && p.hw < 64 && p.adapters > 1;      // few images, or images as long as a tile: as they come
+    if (sorted) put_in_order(p, g, ws, s, st);
+    const Rows q = rows_of(p, g, ws, s, sorted);
+    float* t = inner ? inner : (float*)(ws + s.inner);
+    if (p.adapters || inner) narrow<T>(q, x, p.in, g.a, drop, t, st);
+    wide<T>(q, x, p.in, g.w, g.bias, t, g.b, p.out, make_drop(0.f, 0, 0, nullptr), y, st);
+}
+
+template <typename T>
+void backward(const AdapterShape& p, const AdapterArgs& g, const void* dy, const void* x, const float* inner, void* dx, float* da, float* db, const Drop& drop, char* ws,
+              hipStream_t st)
+{
+    const Scratch s = scratch_of(p, true);
+    const Drop none = make_drop(0.f, 0, 0, nullptr);
+    put_in_order(p, g, ws, s, st);
+    const Rows q = rows_of(p, g, ws, s, true);
+    float* u = (float*)(ws + s.inner);
+    if (p.adapters && (dx || da)) {
+        transpose<T>(g.b, ws + s.bt, p.adapters, p.out, p.rank, st);
+        narrow<T>(q, dy, p.out, ws + s.bt, none, u, st);
+    }
+    if (dx) {
+        transpose<T>(g.w, ws + s.wt, 1, p.out, p.in, st);
+        transpose<T>(g.a, ws + s.at, p.adapters, p.rank, p.in, st);
+        wide<T>(q, dy, p.out, ws + s.wt, nullptr, u, ws + s.at, p.in, drop, dx, st);
+    }
+    if (p.adapters && da) sum_rows<T>(q, x, u, p.in, drop, 0, da, (float*)(ws + s.partial), st);
+    if (p.adapters && db) sum_rows<T>(q, dy, inner, p.out, none, 1, db, (float*)(ws + s.partial), st);
+}
+
+long long product_bytes(const AdapterShape& p, bool backward)
+{
+    const size_t rows = (size_t)p.images * p.hw;
+    return (long long)((rows * (p.in * (backward ? 2 : 1) + p.out) + (size_t)p.in * p.out + (size_t)p.adapters * p.rank * (p.in + p.out)) * elem_size(p.dtype));
+}
+
+}  // namespace
+
+size_t adapter_workspace_bytes(const AdapterShape& p, bool backward) { return scratch_of(p, backward).bytes; }
+
+int launch_adapter_fwd(const AdapterShape& p, const AdapterArgs& g, const void* x, void* y, float* inner, const Drop& drop, void* ws, hipStream_t st)
+{
+    TraceScope trace("adapter", nullptr, (long long)p.images * p.hw, st, product_bytes(p, false));
+    if (p.dtype == DR_BF16) forward<uint16_t>(p, g, x, y, inner, drop, (char*)ws, st);
+    else forward<float>(p, g, x, y, inner, drop, (char*)ws, st);
+    return check_launch("adapter");
+}
+
+int launch_adapter_bwd(const AdapterShape& p, const AdapterArgs& g, const void* dy, const void* x, const float* inner, void* dx, float* da, float* db, const Drop& drop,
+                       void* ws, hipStream_t st)
+{
+    TraceScope trace("adapter_bwd", nullptr, (long long)p.images * p.hw, st, product_bytes(p, true));
+    if (p.dtype == DR_BF16) backward<uint16_t>(p, g, dy, x, inner, dx, da, db, drop, (char*)ws, st);
+    else backward<float>(p, g, dy, x, inner, dx, da, db, drop, (char*)ws, st);
+    return check_launch("adapter_bwd");
+}
+
+}  // namespace dr

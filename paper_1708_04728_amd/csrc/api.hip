@@ -14,6 +14,7 @@
 #include "dr_internal.h"
 #include "inception_levels.h"
 #include "orthogonal_plan.h"
+#include "philox.h"
 
 namespace dr {
 
@@ -1571,6 +1572,136 @@ int dr_layernorm_bwd(const dr_tensor* d, const void* dy, const void* x, const fl
     if (tensor_elems(*d) && (!dy || !x || !mean || !rstd)) return fail(DR_ERR_NULL, "%s: dy, x, mean or rstd is NULL", who);
     if (tensor_elems(*d) && dx == x) return fail(DR_ERR_UNSUPPORTED, "%s: dx must not be x", who);
     return launch_layernorm_bwd(*d, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, ws, (hipStream_t)stream);
+}
+
+static int check_dropout(const char* who, const dr_dropout* d, Drop* out)
+{
+    *out = make_drop(0.f, 0, 0, nullptr);
+    if (!d) return DR_OK;
+    if (!(d->p >= 0.f && d->p <= 1.f)) return fail(DR_ERR_SHAPE, "%s: a dropout probability must lie in 0..1", who);
+    *out = make_drop(d->p, d->seed, d->offset, (const uint64_t*)d->step);
+    return DR_OK;
+}
+
+int dr_dropout_fwd(const dr_tensor* d, const void* x, const dr_dropout* drop, void* y, void* stream)
+{
+    const char* who = "dr_dropout_fwd";
+    DR_TRY(check_tensor(who, "d", d));
+    if (!drop) return fail(DR_ERR_NULL, "%s: drop is NULL", who);
+    Drop p;
+    DR_TRY(check_dropout(who, drop, &p));
+    if (tensor_elems(*d) == 0) return DR_OK;
+    if (!x || !y) return fail(DR_ERR_NULL, "%s: x or y is NULL", who);
+    return launch_dropout(d->dtype, x, p, y, tensor_elems(*d), (hipStream_t)stream);
+}
+
+static int check_logits(const char* who, const dr_tensor* d)
+{
+    DR_TRY(check_tensor(who, "d", d));
+    if (d->h != 1 || d->w != 1) return fail(DR_ERR_SHAPE, "%s: logits must be {n, c, 1, 1}", who);
+    if (d->c < 1) return fail(DR_ERR_SHAPE, "%s: no classes", who);
+    return DR_OK;
+}
+
+int dr_softmax_loss_workspace_bytes(const dr_tensor* d, size_t* bytes)
+{
+    const char* who = "dr_softmax_loss_workspace_bytes";
+    DR_TRY(check_logits(who, d));
+    if (!bytes) return fail(DR_ERR_NULL, "%s: bytes is NULL", who);
+    *bytes = softmax_loss_workspace_bytes(d->n);
+    return DR_OK;
+}
+
+int dr_softmax_loss_grad(const dr_tensor* d, const void* z, const int* labels, float smoothing, int mean, void* dz, float* loss, float* row_loss, void* ws,
+                         size_t ws_bytes, void* stream)
+{
+    const char* who = "dr_softmax_loss_grad";
+    DR_TRY(check_logits(who, d));
+    if (!(smoothing >= 0.f && smoothing <= 1.f)) return fail(DR_ERR_SHAPE, "%s: smoothing must lie in 0..1", who);
+    if (d->n && (!z || !labels)) return fail(DR_ERR_NULL, "%s: z or labels is NULL", who);
+    DR_TRY(check_scratch(who, ws, ws_bytes, softmax_loss_workspace_bytes(d->n)));
+    return launch_softmax_loss_grad(d->dtype, d->n, d->c, z, labels, smoothing, mean, dz, loss, row_loss, ws, (hipStream_t)stream);
+}
+
+static int check_adapters(const char* who, const dr_tensor* xd, const dr_adapters* ad, AdapterShape* p)
+{
+    DR_TRY(check_tensor(who, "xd", xd));
+    if (!ad) return fail(DR_ERR_NULL, "%s: adapter descriptor is NULL", who);
+    if (ad->c_in < 1 || ad->c_out < 1) return fail(DR_ERR_SHAPE, "%s: a projection of %d channels to %d", who, ad->c_in, ad->c_out);
+    if (ad->rank < 1 || ad->rank > DR_MAX_ADAPTER_RANK) return fail(DR_ERR_UNSUPPORTED, "%s: rank %d (1..%d supported)", who, ad->rank, DR_MAX_ADAPTER_RANK);
+    if (ad->count < 0 || ad->count > DR_MAX_ADAPTERS) return fail(DR_ERR_UNSUPPORTED, "%s: %d adapters (0..%d supported)", who, ad->count, DR_MAX_ADAPTERS);
+    if (xd->c != ad->c_in) return fail(DR_ERR_SHAPE, "%s: input has %d channels, the projection expects %d", who, xd->c, ad->c_in);
+    if (xd->layout == DR_NCHW && (double)xd->h * xd->w > 1) return fail(DR_ERR_UNSUPPORTED, "%s: maps must be channels-last", who);
+    const double pixels = (double)xd->n * xd->h * xd->w, most = std::max(ad->c_in, ad->c_out), factors = (double)ad->count * ad->rank;
+    if (pixels * std::max(most, (double)ad->rank) >= 2147483648.0 || (double)ad->c_in * ad->c_out >= 2147483648.0 || factors * most >= 2147483648.0)
+        return fail(DR_ERR_UNSUPPORTED, "%s: a tensor of more than 2^31-1 elements", who);
+    p->images = pixels > 0 ? xd->n : 0;
+    p->hw = pixels > 0 ? xd->h * xd->w : 1;
+    p->in = ad->c_in; p->out = ad->c_out; p->adapters = ad->count; p->rank = ad->rank; p->dtype = xd->dtype;
+    return DR_OK;
+}
+static int check_projected(const char* who, const dr_tensor* xd, const dr_adapters* ad, const dr_tensor* yd)
+{
+    DR_TRY(check_tensor(who, "yd", yd));
+    if (yd->n != xd->n || yd->c != ad->c_out || yd->h != xd->h || yd->w != xd->w) return fail(DR_ERR_SHAPE, "%s: output must be {%d, %d, %d, %d}", who, xd->n, ad->c_out, xd->h, xd->w);
+    if (yd->dtype != xd->dtype) return fail(DR_ERR_UNSUPPORTED, "%s: input and output dtypes differ", who);
+    if (yd->layout == DR_NCHW && (double)yd->h * yd->w > 1) return fail(DR_ERR_UNSUPPORTED, "%s: maps must be channels-last", who);
+    return DR_OK;
+}
+
+static int adapter_bytes(const char* who, const dr_tensor* xd, const dr_adapters* ad, size_t* bytes, bool backward)
+{
+    AdapterShape p;
+    DR_TRY(check_adapters(who, xd, ad, &p));
+    if (!bytes) return fail(DR_ERR_NULL, "%s: bytes is NULL", who);
+    *bytes = adapter_workspace_bytes(p, backward);
+    return DR_OK;
+}
+int dr_adapter_fwd_workspace_bytes(const dr_tensor* xd, const dr_adapters* ad, size_t* bytes)
+{
+    return adapter_bytes("dr_adapter_fwd_workspace_bytes", xd, ad, bytes, false);
+}
+int dr_adapter_bwd_workspace_bytes(const dr_tensor* xd, const dr_adapters* ad, size_t* bytes)
+{
+    return adapter_bytes("dr_adapter_bwd_workspace_bytes", xd, ad, bytes, true);
+}
+
+int dr_adapter_fwd(const dr_tensor* xd, const void* x, const dr_adapters* ad, const void* w, const float* bias, const void* a, const void* b, const float* scales,
+                   const int* ids, const dr_dropout* drop, const dr_tensor* yd, void* y, float* inner, void* ws, size_t ws_bytes, void* stream)
+{
+    const char* who = "dr_adapter_fwd";
+    AdapterShape p;
+    DR_TRY(check_adapters(who, xd, ad, &p));
+    DR_TRY(check_projected(who, xd, ad, yd));
+    Drop d;
+    DR_TRY(check_dropout(who, drop, &d));
+    DR_TRY(check_scratch(who, ws, ws_bytes, adapter_workspace_bytes(p, false)));
+    if (p.images == 0) return DR_OK;
+    if (!x || !w || !y) return fail(DR_ERR_NULL, "%s: x, w or y is NULL", who);
+    if (p.adapters && (!a || !b || !ids)) return fail(DR_ERR_NULL, "%s: a, b or ids is NULL", who);
+    if (x == y) return fail(DR_ERR_UNSUPPORTED, "%s: y must not be x", who);
+    const AdapterArgs g = {w, bias, a, b, scales, ids};
+    return launch_adapter_fwd(p, g, x, y, inner, d, ws, (hipStream_t)stream);
+}
+
+int dr_adapter_bwd(const dr_tensor* yd, const void* dy, const dr_tensor* xd, const void* x, const dr_adapters* ad, const void* w, const void* a, const void* b,
+                   const float* scales, const int* ids, const dr_dropout* drop, const float* inner, void* dx, float* da, float* db, void* ws, size_t ws_bytes,
+                   void* stream)
+{
+    const char* who = "dr_adapter_bwd";
+    AdapterShape p;
+    DR_TRY(check_adapters(who, xd, ad, &p));
+    DR_TRY(check_projected(who, xd, ad, yd));
+    Drop d;
+    DR_TRY(check_dropout(who, drop, &d));
+    DR_TRY(check_scratch(who, ws, ws_bytes, adapter_workspace_bytes(p, true)));
+    if (p.images && ((dx || da || db) && !dy)) return fail(DR_ERR_NULL, "%s: dy is NULL", who);
+    if (p.images && dx && !w) return fail(DR_ERR_NULL, "%s: w is NULL", who);
+    if (p.images && p.adapters && (((dx || da) && !b) || (dx && !a) || (da && !x) || (db && !inner) || !ids))
+        return fail(DR_ERR_NULL, "%s: x, a, b, inner or ids is NULL", who);
+    if (dx && (dx == dy || dx == x)) return fail(DR_ERR_UNSUPPORTED, "%s: dx must be neither dy nor x", who);
+    const AdapterArgs g = {w, nullptr, a, b, scales, ids};
+    return launch_adapter_bwd(p, g, dy, x, inner, dx, da, db, d, ws, (hipStream_t)stream);
 }
 
 // blocks: of the list's matrices so far, padded

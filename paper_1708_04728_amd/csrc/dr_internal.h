@@ -208,6 +208,25 @@ int launch_orthogonalise(int count, const dr_matrix* ms, int dtype, const void* 
 size_t muon_step_workspace_bytes(int count, const dr_muon_param* ps);
 int launch_muon_step(int count, const dr_muon_param* ps, const dr_muon& opt, void* ws, hipStream_t st);
 
+// dropout.hip, softmax_loss.hip, adapter.hip: adapting a network's classifier
+struct Drop;
+int launch_dropout(int dtype, const void* x, const Drop& drop, void* y, size_t count, hipStream_t st);
+size_t softmax_loss_workspace_bytes(int rows);
+int launch_softmax_loss_grad(int dtype, int rows, int classes, const void* z, const int* labels, float smoothing, int mean, void* dz, float* loss, float* row_loss,
+                             void* ws, hipStream_t st);
+struct AdapterShape { int images, hw, in, out, adapters, rank, dtype; };
+struct AdapterArgs {
+    const void* w;               // [out][in]
+    const float* bias;           // may be NULL (forward)
+    const void *a, *b;           // [adapters][rank][in], [adapters][out][rank]
+    const float* scales;         // may be NULL
+    const int* ids;              // [images]
+};
+size_t adapter_workspace_bytes(const AdapterShape& p, bool backward);
+int launch_adapter_fwd(const AdapterShape& p, const AdapterArgs& g, const void* x, void* y, float* inner, const Drop& drop, void* ws, hipStream_t st);
+int launch_adapter_bwd(const AdapterShape& p, const AdapterArgs& g, const void* dy, const void* x, const float* inner, void* dx, float* da, float* db, const Drop& drop,
+                       void* ws, hipStream_t st);
+
 // pointwise.hip
 int launch_pack_filters(int dtype, const void* w_kcrs, void* w_krsc, int K, int C, int RS, hipStream_t st);
 int launch_relu(int dtype, const void* x, void* y, size_t count, hipStream_t st);
