@@ -192,102 +192,218 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
 }
 
 // ---- the wide product: y[row][o] = sum_k W[o][k] x[row][k] + bias[o] + drop'(sum_r B_a[o][r] t[row][r]) ---------------------------------------------
-// A workgroup owns 64 outputs of 64 rows, a wave 32 x 32 of them; operands straight from memory.
-template <typename T>
-__global__ __launch_bounds__(256) void wide_kernel(const Rows q, const T* __restrict__ x, int K, const T* __restrict__ w, const float* __restrict__ bias,
-                                                   const float* __restrict__ t, const T* __restrict__ b, int N, const Drop drop, T* __restrict__ y)
+// A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  128 bytes of every row of W and x are a stage: loaded
+// into registers while the stage before is multiplied, then written to the other half of LDS, 16-byte pieces in the order piece ^ (row & 7), so that neither the writes (a
+// row's eight pieces together) nor the reads (one piece of 32 rows) meet in a bank.
+template <typename T> struct Wide {
+    Rows q;
+    const T *x, *w, *b;
+    const float *bias, *t;
+    int K, N;
+    Drop drop;
+    T* y;
+    int tiles_n, tiles;          // tiles of rows; all tiles
+};
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+// one 16-byte piece of each operand: a lane of half h = lane / 32 holds piece 2 s + h
+template <typename T> __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c);
+template <> __device__ __forceinline__ f32x16 mfma32<uint16_t>(u32x4 a, u32x4 b, f32x16 c)
 {
-    __shared__ int row_of[64], id_of[64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-    if (threadIdx.x < 64) {
-        const int p = blockIdx.x * 64 + threadIdx.x;
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ f32x16 mfma32<float>(u32x4 a, u32x4 b, f32x16 c)
+{
+    const f32x4 p = __builtin_bit_cast(f32x4, a), q = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(p[i], q[i], c, 0, 0, 0);
+    return c;
+}
+
+// 16 bytes of a row, of which `n` elements exist (zeros behind them)
+__device__ __forceinline__ u32x4 piece(const char* p) { return *reinterpret_cast<const u32x4_any*>(p); }
+template <typename T>
+__device__ __forceinline__ u32x4 piece(const char* p, int n)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (n >= E) return piece(p);
+    u32x4 v = {0, 0, 0, 0};
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) v[i >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) v[i] = reinterpret_cast<const unsigned*>(p)[i];
+    }
+    return v;
+}
+
+// The tiles that the 8 dies' workgroups (dealt out in turn) see are neighbours: die d takes the d-th run of the list, which goes down runs of 8 tiles of rows.
+__device__ __forceinline__ void tile_of(int block, int tiles, int tiles_n, int* m, int* n)
+{
+    const int die = block & 7, per = tiles >> 3, odd = tiles & 7, i = die * per + min(die, odd) + (block >> 3);
+    const int tiles_m = tiles / tiles_n, run = i / (8 * tiles_m), wide = min(8, tiles_n - run * 8), j = i - run * 8 * tiles_m;
+    *m = j / wide;
+    *n = run * 8 + (j - *m * wide);
+}
+
+template <typename T, int WM, int WN, int MB, int NB>
+__global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
+{
+    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * 8 / THREADS, E = 16 / sizeof(T), STAGE_K = 8 * E;
+    __shared__ __attribute__((aligned(128))) unsigned char lds[2][(TM + TN) * 128];
+    __shared__ int row_of[TN], id_of[TN];
+    const Rows& q = p.q;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
+    int tm, tn;
+    tile_of(blockIdx.x, p.tiles, p.tiles_n, &tm, &tn);
+    const int o0 = tm * TM, p0 = tn * TN;
+    for (int i = threadIdx.x; i < TN; i += THREADS) {
         int id = -2, row = -1;
-        if (p < q.count) row = q.row(p, &id);
-        row_of[threadIdx.x] = row;
-        id_of[threadIdx.x] = id;
+        if (p0 + i < q.count) row = q.row(p0 + i, &id);
+        row_of[i] = row;
+        id_of[i] = id;
     }
     __syncthreads();
-    const int first = (wave >> 1) * 32, o0 = blockIdx.y * 64 + (wave & 1) * 32;
-    int row[2], id[2];
+
+    // this thread's pieces of a stage: row and piece are the same in every stage.  Rows that do not exist repeat one that does: what comes of them is not stored
+    unsigned from[PIECES];
+    int at[PIECES];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        row[j] = row_of[first + j * 16 + l16];
-        id[j] = id_of[first + j * 16 + l16];
+    for (int i = 0; i < PIECES; ++i) {
+        const int e = threadIdx.x + i * THREADS, r = e >> 3, c = e & 7;
+        const int row = r < TM ? min(o0 + r, p.N - 1) : max(row_of[r - TM], 0);
+        from[i] = (unsigned)((size_t)row * p.K * sizeof(T)) + c * 16;
+        at[i] = r * 128 + ((c ^ (r & 7)) << 4);
     }
-    const uint64_t place = drop.border ? drop_place(drop) : 0;
-    f32x4 acc[2][2] = {};
+    const int stages = (p.K + STAGE_K - 1) / STAGE_K, whole = p.K / STAGE_K;
+    u32x4 held[PIECES];
+    auto fetch = [&](int s) {
+        const char *w = (const char*)p.w + (size_t)s * 128, *x = (const char*)p.x + (size_t)s * 128;
+        if (s < whole) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) held[i] = piece((i < PIECES * TM / (TM + TN) ? w : x) + from[i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) held[i] = piece<T>((i < PIECES * TM / (TM + TN) ? w : x) + from[i], p.K - s * STAGE_K - (int)((threadIdx.x + i * THREADS) & 7) * E);
+        }
+    };
+    auto put = [&](unsigned char* to) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) *reinterpret_cast<u32x4*>(to + at[i]) = held[i];
+    };
+    f32x16 acc[MB][NB] = {};
+    const int rd_m = (wm * MB * 32 + l32) * 128, rd_n = (TM + wn * NB * 32 + l32) * 128;
+    fetch(0);
+    put(lds[0]);
+    __syncthreads();
+    for (int s = 0; s < stages; ++s) {
+        if (s + 1 < stages) fetch(s + 1);
+        const unsigned char* buf = lds[s & 1];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int c = ((2 * k + h) ^ (l32 & 7)) << 4;
+            u32x4 a[MB], b[NB];
+#pragma unroll
+            for (int i = 0; i < MB; ++i) a[i] = *reinterpret_cast<const u32x4*>(buf + rd_m + i * 4096 + c);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) b[j] = *reinterpret_cast<const u32x4*>(buf + rd_n + j * 4096 + c);
+#pragma unroll
+            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = mfma32<T>(a[i], b[j], acc[i][j]);
+        }
+        if (s + 1 < stages) put(lds[(s + 1) & 1]);
+        __syncthreads();
+    }
+
+    // the adapters of this wave's rows, one after the other
+    int row[NB], id[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+        row[j] = row_of[(wn * NB + j) * 32 + l32];
+        id[j] = id_of[(wn * NB + j) * 32 + l32];
+    }
+    const int ow = o0 + wm * MB * 32;
+    const uint64_t place = p.drop.border ? drop_place(p.drop) : 0;
+    const float scale = p.drop.border ? p.drop.scale : 1.f;
     for (int a = -1;;) {
         int next = 0x7FFFFFFF;
-        for (int i = 0; i < 32; ++i) next = id_of[first + i] > a ? min(next, id_of[first + i]) : next;
+#pragma unroll
+        for (int j = 0; j < NB; ++j) next = id[j] > a ? min(next, id[j]) : next;
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) next = min(next, __shfl_xor(next, d, 64));
+        next = __builtin_amdgcn_readfirstlane(next);
         if (next == 0x7FFFFFFF) break;
         a = next;
-        f32x4 part[2][2] = {};               // of its own: rows of other adapters must not meet this one's numbers, not even times zero
-        constexpr int STEP = sizeof(T) == 2 ? 16 : 32;        // bf16: groups 0 and 1 hold the upper pieces of t, 2 and 3 the lower ones
+        constexpr int STEP = 2 * E;
         for (int r0 = 0; r0 < q.rank; r0 += STEP) {
-            const int r = r0 + (sizeof(T) == 2 ? (g & 1) : g) * 8;
-            Operand<T> ob[2], ot[2];
+            const int r = r0 + h * E;
+            u32x4 high[NB], low[NB];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int o = o0 + i * 16 + l16;
-                ob[i].load(b + ((size_t)a * N + min(o, N - 1)) * q.rank + r, o < N ? q.rank - r : 0);
-            }
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < NB; ++j) {
                 float e[8];
-                load8(t + (size_t)max(row[j], 0) * q.rank + r, id[j] == a ? q.rank - r : 0, 0.f, e);
+                load8(p.t + (size_t)max(row[j], 0) * q.rank + r, id[j] == a ? min(q.rank - r, E) : 0, 0.f, e);
                 if constexpr (sizeof(T) == 2) {
-                    ot[j].v = pack8(e);
-                    if (g >= 2) {
-                        float high[8];
-                        unpack8(ot[j].v, high);
+                    float up[8];
+                    high[j] = pack8(e);
+                    unpack8(high[j], up);
 #pragma unroll
-                        for (int c = 0; c < 8; ++c) e[c] -= high[c];
-                        ot[j].v = pack8(e);
+                    for (int c = 0; c < 8; ++c) e[c] -= up[c];
+                    low[j] = pack8(e);
+                } else high[j] = __builtin_bit_cast(u32x4, f32x4{e[0], e[1], e[2], e[3]});
+            }
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                const int o = min(ow + i * 32 + l32, p.N - 1);
+                const u32x4 v = piece<T>((const char*)(p.b + ((size_t)a * p.N + o) * q.rank + r), q.rank - r);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    // this lane's row of the block: outputs 16 h .. 16 h + 15, the others from the lane that holds the same row
+                    unsigned keep = 0xFFFFFFFFu;
+                    if (p.drop.border) {
+                        const unsigned own = kept16(p.drop, place, (uint64_t)((size_t)max(row[j], 0) * p.N + ow + i * 32 + h * 16)), other = __shfl_xor(own, 32, 64);
+                        keep = h ? own << 16 | other : other << 16 | own;
+                        keep >>= h * 4;
                     }
-                } else {
-                    ot[j].v[0] = f32x4{e[0], e[1], e[2], e[3]};
-                    ot[j].v[1] = f32x4{e[4], e[5], e[6], e[7]};
+                    f32x16 part = {};          // of its own: rows of other adapters must not meet this one's numbers, not even times zero
+                    part = mfma32<T>(v, high[j], part);
+                    if constexpr (sizeof(T) == 2) part = mfma32<T>(v, low[j], part);
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const bool mine = id[j] == a && (keep >> ((e >> 2) * 8 + (e & 3)) & 1);
+                        acc[i][j][e] += mine ? part[e] * scale : 0.f;
+                    }
                 }
             }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) part[i][j] = mfma(ob[i], ot[j], part[i][j]);
         }
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = part[i][j][e];
-                    if (drop.border) v = kept(drop, place, (uint64_t)((size_t)max(row[j], 0) * N + o0 + i * 16 + g * 4 + e)) ? v * drop.scale : 0.f;
-                    acc[i][j][e] = id[j] == a ? v : acc[i][j][e];
-                }
-    }
-    for (int k = g * 8; k - g * 8 < K; k += 32) {
-        Operand<T> ow[2], ox[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const int o = o0 + i * 16 + l16;
-            ow[i].load(w + (size_t)min(o, N - 1) * K + k, o < N ? K - k : 0);
-        }
-#pragma unroll
-        for (int j = 0; j < 2; ++j) ox[j].load(x + (size_t)max(row[j], 0) * K + k, row[j] >= 0 ? K - k : 0);
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) acc[i][j] = mfma(ow[i], ox[j], acc[i][j]);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int e = 0; e < 4; ++e) {
+            const int o = ow + i * 32 + e * 8 + h * 4;
+            float add[4] = {};
+            if (p.bias) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int o = o0 + i * 16 + g * 4 + e;
-                if (row[j] >= 0 && o < N) Store<T>::st(y + (size_t)row[j] * N + o, acc[i][j][e] + (bias ? bias[o] : 0.f));
+                for (int c = 0; c < 4; ++c) add[c] = p.bias[min(o + c, p.N - 1)];
             }
+#pragma unroll
+            for (int j = 0; j < NB; ++j) {
+                if (row[j] < 0) continue;
+                T* to = p.y + (size_t)row[j] * p.N + o;
+                float v[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = acc[i][j][e * 4 + c] + add[c];
+                if (o + 4 <= p.N) store4(to, v);
+                else
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        if (o + c < p.N) Store<T>::st(to + c, v[c]);
+            }
+        }
 }
 
 // ---- transposed copies: src[batch][R][C] -> dst[batch][C][R] --------------------------------------------------------------------------------------
@@ -369,7 +485,20 @@ template <typename T>
 void wide(const Rows& q, const void* x, int K, const void* w, const float* bias, const float* t, const void* b, int N, const Drop& drop, void* y, hipStream_t st)
 {
     if (!q.count) return;
-    hipLaunchKernelGGL((wide_kernel<T>), dim3((q.count + 63) / 64, (N + 63) / 64), dim3(256), 0, st, q, (const T*)x, K, (const T*)w, bias, t, (const T*)b, N, drop, (T*)y);
+    Wide<T> p;
+    p.q = q; p.x = (const T*)x; p.w = (const T*)w; p.b = (const T*)b; p.bias = bias; p.t = t; p.K = K; p.N = N; p.drop = drop; p.y = (T*)y;
+    auto tiles = [&](int tm, int tn) {
+        p.tiles_n = (q.count + tn - 1) / tn;
+        p.tiles = p.tiles_n * ((N + tm - 1) / tm);
+        return p.tiles;
+    };
+    const int cus = device_cus();
+    if (tiles(256, 256) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 4, 4, 2>), dim3(p.tiles), dim3(512), 0, st, p);
+    else if (tiles(128, 128) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 2, 2>), dim3(p.tiles), dim3(256), 0, st, p);
+    else {
+        tiles(64, 64);
+        hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 1, 1>), dim3(p.tiles), dim3(256), 0, st, p);
+    }
 }
 
 template <typename T>

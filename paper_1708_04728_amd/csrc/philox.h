@@ -59,6 +59,26 @@ DR_ANY unsigned drop_draw(const uint32_t (&r)[4], int j) { return j & 1 ? r[j >>
 #if defined(__HIPCC__)
 __device__ __forceinline__ uint64_t drop_place(const Drop& d) { return d.offset + (d.step ? *d.step : 0); }
 
+// Which of a block's elements are kept: bit j for element 8 block + j
+__device__ __forceinline__ unsigned kept8(const Drop& d, uint64_t place, uint64_t block)
+{
+    uint32_t r[4];
+    philox(d.seed, block, place, r);
+    unsigned bits = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) bits |= drop_draw(r, j) >= d.border ? 1u << j : 0u;
+    return bits;
+}
+// ... of sixteen from any `first` on
+__device__ __forceinline__ unsigned kept16(const Drop& d, uint64_t place, uint64_t first)
+{
+    const int shift = (int)(first & 7), blocks = shift ? 3 : 2;
+    unsigned bits = 0;
+#pragma unroll 1
+    for (int i = 0; i < blocks; ++i) bits |= kept8(d, place, (first >> 3) + i) << (8 * i);
+    return (bits >> shift) & 0xFFFFu;
+}
+
 // Dropout of the eight elements of a block (v[j] is element 8 block + j)
 __device__ __forceinline__ void drop8(const Drop& d, uint64_t place, uint64_t block, float (&v)[8])
 {

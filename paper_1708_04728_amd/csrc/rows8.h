@@ -41,6 +41,12 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8])
     *reinterpret_cast<f32x4_any*>(p) = f32x4{v[0], v[1], v[2], v[3]};
     *reinterpret_cast<f32x4_any*>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
 }
+__device__ __forceinline__ void store4(uint16_t* p, const float (&v)[4])
+{
+    typedef unsigned int u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+    *reinterpret_cast<u32x2_any*>(p) = u32x2_any{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+}
+__device__ __forceinline__ void store4(float* p, const float (&v)[4]) { *reinterpret_cast<f32x4_any*>(p) = f32x4{v[0], v[1], v[2], v[3]}; }
 // ... of which `n` exist (n <= 0: none; 8 and more: all), `none` in the place of the others
 template <typename T>
 __device__ __forceinline__ void load8(const T* p, int n, float none, float (&v)[8])
