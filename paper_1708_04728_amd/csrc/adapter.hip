@@ -8,6 +8,7 @@
 // of each adapter.  Rows are visited in the order of their adapters, so that few tiles hold rows of several; such a tile takes its adapters one after the other.
 // t and u are held in fp32 and enter bf16 products as two pieces each (16 bits of their values): with one piece the adapter's part of y would be rounded twice.
 #include <algorithm>
+#include <type_traits>
 
 #include "dr_internal.h"
 #include "philox.h"
@@ -192,9 +193,9 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
 }
 
 // ---- the wide product: y[row][o] = sum_k W[o][k] x[row][k] + bias[o] + drop'(sum_r B_a[o][r] t[row][r]) ---------------------------------------------
-// A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  128 bytes of every row of W and x are a stage: loaded
-// into registers while the stage before is multiplied, then written to the other half of LDS, 16-byte pieces in the order piece ^ (row & 7), so that neither the writes (a
-// row's eight pieces together) nor the reads (one piece of 32 rows) meet in a bank.
+// A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  128 bytes of every row of W and x are a stage, fetched
+// while the stage before is multiplied into the other half of LDS: by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or by way of registers.  A row's
+// 16-byte pieces lie in the order piece ^ (row & 7), so that neither the writes (a row's eight pieces together) nor the reads (one piece of 32 rows) meet in a bank.
 template <typename T> struct Wide {
     Rows q;
     const T *x, *w, *b;
@@ -249,7 +250,33 @@ __device__ __forceinline__ void tile_of(int block, int tiles, int tiles_n, int* 
     *n = run * 8 + (j - *m * wide);
 }
 
-template <typename T, int WM, int WN, int MB, int NB>
+// 16 bytes per lane from `base` + voff + soff to LDS: lane l's at `lds` + 16 l.  Zeros where voff lies outside the buffer.  The compiler does not see the write: the
+// caller waits for it (wait_loads) in front of the barrier behind which it is read.
+__device__ __forceinline__ void load_lds16(const u32x4& rsrc, const unsigned char* lds, unsigned voff, unsigned soff)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 ::"s"((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
+#endif
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// the workgroup's barrier alone, without the waits of a fence (a wave's own LDS reads have been consumed before it)
+__device__ __forceinline__ void meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+// A tensor as a buffer of raw bytes; NOWHERE is an offset outside of it
+constexpr unsigned NOWHERE = 0xFFFFFFF0u;
+__device__ __forceinline__ u32x4 buffer_of(const void* p, size_t bytes)
+{
+    const uint64_t a = (uint64_t)p;
+    return u32x4{(unsigned)__builtin_amdgcn_readfirstlane((unsigned)a), (unsigned)__builtin_amdgcn_readfirstlane((unsigned)(a >> 32) & 0xFFFFu),
+                 (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00020000u};
+}
+
+template <typename T, int WM, int WN, int MB, int NB, bool DMA, bool DROP>
 __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 {
     constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * 8 / THREADS, E = 16 / sizeof(T), STAGE_K = 8 * E;
@@ -269,13 +296,14 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     __syncthreads();
 
     // this thread's pieces of a stage: row and piece are the same in every stage.  Rows that do not exist repeat one that does: what comes of them is not stored
-    unsigned from[PIECES];
+    std::conditional_t<DMA, unsigned, size_t> from[PIECES];
     int at[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
         const int e = threadIdx.x + i * THREADS, r = e >> 3, c = e & 7;
         const int row = r < TM ? min(o0 + r, p.N - 1) : max(row_of[r - TM], 0);
-        from[i] = (unsigned)((size_t)row * p.K * sizeof(T)) + c * 16;
+        // (DMA: the lane's place in LDS is given, and it fetches the piece that belongs there)
+        from[i] = (decltype(from[i] + 0))((size_t)row * p.K * sizeof(T)) + (DMA ? c ^ (r & 7) : c) * 16;
         at[i] = r * 128 + ((c ^ (r & 7)) << 4);
     }
     const int stages = (p.K + STAGE_K - 1) / STAGE_K, whole = p.K / STAGE_K;
@@ -294,29 +322,70 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) *reinterpret_cast<u32x4*>(to + at[i]) = held[i];
     };
+    [[maybe_unused]] const u32x4 rw = buffer_of(p.w, (size_t)p.N * p.K * sizeof(T)), rx = buffer_of(p.x, (size_t)q.count * p.K * sizeof(T));
+    auto stream = [&](int s, unsigned char* to) {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            unsigned voff = from[i];
+            if (s >= whole) {                // (the last stage, if it is no whole one)
+                const int e = threadIdx.x + i * THREADS;
+                if (s * 128 + ((e ^ (e >> 3)) & 7) * 16 >= p.K * (int)sizeof(T)) voff = NOWHERE;
+            }
+            load_lds16(i < PIECES * TM / (TM + TN) ? rw : rx, to + __builtin_amdgcn_readfirstlane((wave + i * (THREADS / 64)) * 1024), voff, s * 128);
+        }
+    };
     f32x16 acc[MB][NB] = {};
     const int rd_m = (wm * MB * 32 + l32) * 128, rd_n = (TM + wn * NB * 32 + l32) * 128;
-    fetch(0);
-    put(lds[0]);
-    __syncthreads();
-    for (int s = 0; s < stages; ++s) {
-        if (s + 1 < stages) fetch(s + 1);
-        const unsigned char* buf = lds[s & 1];
+    // operands two steps deep: those of step k + 1 are read while step k is multiplied, the next stage's first ones behind the barrier and in front of the last step
+    u32x4 a[2][MB], b[2][NB];
+    auto read = [&](const unsigned char* buf, int k, int to) {
+        const int c = ((2 * k + h) ^ (l32 & 7)) << 4;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int c = ((2 * k + h) ^ (l32 & 7)) << 4;
-            u32x4 a[MB], b[NB];
+        for (int i = 0; i < MB; ++i) a[to][i] = *reinterpret_cast<const u32x4*>(buf + rd_m + i * 4096 + c);
 #pragma unroll
-            for (int i = 0; i < MB; ++i) a[i] = *reinterpret_cast<const u32x4*>(buf + rd_m + i * 4096 + c);
+        for (int j = 0; j < NB; ++j) b[to][j] = *reinterpret_cast<const u32x4*>(buf + rd_n + j * 4096 + c);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](int from) {
 #pragma unroll
-            for (int j = 0; j < NB; ++j) b[j] = *reinterpret_cast<const u32x4*>(buf + rd_n + j * 4096 + c);
+        for (int i = 0; i < MB; ++i)
 #pragma unroll
-            for (int i = 0; i < MB; ++i)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) acc[i][j] = mfma32<T>(a[i], b[j], acc[i][j]);
-        }
-        if (s + 1 < stages) put(lds[(s + 1) & 1]);
+            for (int j = 0; j < NB; ++j) acc[i][j] = mfma32<T>(a[from][i], b[from][j], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    if constexpr (DMA) {
+        stream(0, lds[0]);
+        wait_loads();
+        meet();
+        if (stages > 1) stream(1, lds[1]);
+    } else {
+        fetch(0);
+        put(lds[0]);
         __syncthreads();
+        if (stages > 1) fetch(1);
+    }
+    read(lds[0], 0, 0);
+    for (int s = 0; s < stages; ++s) {
+        unsigned char* const buf = lds[s & 1];
+        unsigned char* const other = lds[(s + 1) & 1];
+        read(buf, 1, 1);
+        multiply(0);
+        read(buf, 2, 0);
+        multiply(1);
+        read(buf, 3, 1);
+        multiply(0);
+        if constexpr (DMA) {
+            __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): nothing of this half is still to be read
+            wait_loads();
+            meet();
+            if (s + 2 < stages) stream(s + 2, buf);
+        } else {
+            if (s + 1 < stages) put(other);
+            __syncthreads();
+            if (s + 2 < stages) fetch(s + 2);
+        }
+        if (s + 1 < stages) read(other, 0, 0);
+        multiply(1);
     }
 
     // the adapters of this wave's rows, one after the other
@@ -327,8 +396,8 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
         id[j] = id_of[(wn * NB + j) * 32 + l32];
     }
     const int ow = o0 + wm * MB * 32;
-    const uint64_t place = p.drop.border ? drop_place(p.drop) : 0;
-    const float scale = p.drop.border ? p.drop.scale : 1.f;
+    const uint64_t place = DROP ? drop_place(p.drop) : 0;
+    const float scale = DROP ? p.drop.scale : 1.f;
     for (int a = -1;;) {
         int next = 0x7FFFFFFF;
 #pragma unroll
@@ -363,7 +432,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
                 for (int j = 0; j < NB; ++j) {
                     // this lane's row of the block: outputs 16 h .. 16 h + 15, the others from the lane that holds the same row
                     unsigned keep = 0xFFFFFFFFu;
-                    if (p.drop.border) {
+                    if constexpr (DROP) {
                         const unsigned own = kept16(p.drop, place, (uint64_t)((size_t)max(row[j], 0) * p.N + ow + i * 32 + h * 16)), other = __shfl_xor(own, 32, 64);
                         keep = h ? own << 16 | other : other << 16 | own;
                         keep >>= h * 4;
@@ -493,12 +562,15 @@ void wide(const Rows& q, const void* x, int K, const void* w, const float* bias,
         return p.tiles;
     };
     const int cus = device_cus();
-    if (tiles(256, 256) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 4, 4, 2>), dim3(p.tiles), dim3(512), 0, st, p);
-    else if (tiles(128, 128) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 2, 2>), dim3(p.tiles), dim3(256), 0, st, p);
-    else {
-        tiles(64, 64);
-        hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 1, 1>), dim3(p.tiles), dim3(256), 0, st, p);
-    }
+    const bool dma = aligned16(x) && aligned16(w) && K * sizeof(T) % 16 == 0 && (size_t)std::max(q.count, N) * K * sizeof(T) <= NOWHERE && (size_t)K * sizeof(T) < 0x7FFFFF00u;
+    auto run = [&](auto dma, auto masked) {
+        constexpr bool DMA = decltype(dma)::value, DROP = decltype(masked)::value;
+        if (tiles(256, 256) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 4, 4, 2, DMA, DROP>), dim3(p.tiles), dim3(512), 0, st, p);
+        else if (tiles(128, 128) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 2, 2, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
+        else if (tiles(64, 64)) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 1, 1, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
+    };
+    auto run_masked = [&](auto masked) { dma ? run(std::true_type(), masked) : run(std::false_type(), masked); };
+    drop.border ? run_masked(std::true_type()) : run_masked(std::false_type());
 }
 
 template <typename T>
