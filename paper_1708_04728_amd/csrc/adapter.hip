@@ -76,15 +76,6 @@ __device__ __forceinline__ void mask8(const Drop& d, uint64_t place, uint64_t fi
 #pragma unroll
     for (int j = 0; j < 8; ++j) v.keep(j, one[j] != 0.f);
 }
-// ... and of a single one
-__device__ __forceinline__ bool kept(const Drop& d, uint64_t place, uint64_t at)
-{
-    uint32_t r[4];
-    philox(d.seed, at >> 3, place, r);
-    const unsigned j = (unsigned)at & 7, w = j & 4 ? (j & 2 ? r[3] : r[2]) : (j & 2 ? r[1] : r[0]);
-    return (j & 1 ? w >> 16 : w & 0xFFFFu) >= d.border;
-}
-
 // Which row is at a position, and its adapter.  Positions walk the images in `order` (NULL: as they come).
 struct Rows {
     int count, hw;               // rows; pixels of an image
@@ -490,49 +481,161 @@ __global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ sr
 }
 
 // ---- sums over the rows of an adapter: out[a][r][c] (or [a][c][r]) = sum f[row][r] drop(v[row][c]) ---------------------------------------------------
-// A workgroup adds a share of adapter a's rows for 64 columns and 16 of the rank, its four waves every fourth row each; partial sums of several shares are added after.
+// A workgroup takes `length` positions, 512 bytes of columns (a quarter of them a wave) and up to 64 of the rank, and the adapters among those positions one after the other: a segment each.  Both
+// operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into two pieces.  A segment that is all of its
+// adapter is the result; others are partial sums, that of chunk k and adapter a in slot k + a (one of the two grows from a segment to the next), added in their order after.
 struct Sums {
-    int C, splits;
+    int C, length;
     int ranks_last;              // out[a][c][r]
-    float* out;                  // [split][adapters][..]
+    float *out, *partial;        // partial: [slot][rank][C] in the order of out
 };
-template <typename T>
-__global__ __launch_bounds__(256) void rows_kernel(const Rows q, const Sums s, const T* __restrict__ v, const float* __restrict__ f, const Drop drop)
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+// Of a block of 4 rows x 16 columns of 16 bits, whose lane i of 16 names the address of four elements (row i / 4, columns 4 (i % 4) ..): column i's four rows
+__device__ __forceinline__ u32x2 read_transposed(const unsigned char* p)
 {
-    __shared__ float red[4][16][65];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * 64 + lane;
-    const int a = blockIdx.y / s.splits, split = blockIdx.y - a * s.splits, r0 = blockIdx.z * 16;
-    const long long begin = (long long)q.starts[a] * q.hw, all = (long long)q.starts[a + 1] * q.hw - begin;
-    const int lo = (int)(begin + all * split / s.splits), hi = (int)(begin + all * (split + 1) / s.splits);
+#if defined(__HIP_DEVICE_COMPILE__)
+    return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)p));
+#else
+    return u32x2{};
+#endif
+}
+
+template <typename T, int RB>
+__global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums s, const T* __restrict__ v, const float* __restrict__ f, const Drop drop)
+{
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int UNITS = 512 / (8 * sizeof(T)), PER = 32 * UNITS / 256, CB = 512 / sizeof(T) / 64, FB = 32 * RB * 16, F_PER = FB / 256, WINDOW = 256;
+    __shared__ __attribute__((aligned(128))) unsigned char xt[2][32 * 512];
+    __shared__ __attribute__((aligned(128))) unsigned char ft[2][FB * 4];          // bf16: upper pieces, then lower ones
+    __shared__ int rows_of[WINDOW];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
+    const int c0 = blockIdx.x * (512 / (int)sizeof(T)), chunk = blockIdx.y, p0 = chunk * s.length, p1 = min(p0 + s.length, q.count), r0 = blockIdx.z * 64;
     const uint64_t place = drop.border ? drop_place(drop) : 0;
-    float acc[16] = {};
-    for (int p = lo + wave; p < hi; p += 4) {
-        int id;
-        const int row = q.row(p, &id);
-        float e = c < s.C ? Store<T>::ld(v + (size_t)row * s.C + c) : 0.f;
-        if (drop.border && !kept(drop, place, (uint64_t)((size_t)row * s.C + c))) e = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[i] = __builtin_fmaf(r0 + i < q.rank ? f[(size_t)row * q.rank + r0 + i] : 0.f, e, acc[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < 16; ++i) red[wave][i][lane] = acc[i];
-    __syncthreads();
     const float scale = drop.border ? drop.scale : 1.f;
-    for (int i = threadIdx.x; i < 1024; i += 256) {
-        const int r = r0 + (s.ranks_last ? i & 15 : i >> 6), l = s.ranks_last ? i >> 4 : i & 63, cc = blockIdx.x * 64 + l;
-        if (r >= q.rank || cc >= s.C) continue;
-        const float sum = ((red[0][r - r0][l] + red[1][r - r0][l]) + (red[2][r - r0][l] + red[3][r - r0][l])) * scale;
-        float* out = s.out + ((size_t)split * q.adapters + a) * q.rank * s.C;
-        out[s.ranks_last ? (size_t)cc * q.rank + r : (size_t)r * s.C + cc] = sum;
+    // 32-byte pieces of a row lie in the order piece ^ turn(row), so that the rows that one read takes do not meet in a bank
+    auto turn = [](int row) { return ((row & 3) | ((row >> 1) & 4)) << (BF ? 0 : 1); };
+    Operand<T> held[PER];
+    float heldf[F_PER];
+    auto fetch = [&](int st) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = threadIdx.x + i * 256, row = rows_of[st * 32 + e / UNITS], c = c0 + (e % UNITS) * 8;
+            held[i].load(v + (size_t)max(row, 0) * s.C + c, row >= 0 ? s.C - c : 0);
+        }
+#pragma unroll
+        for (int i = 0; i < F_PER; ++i) {
+            const int e = threadIdx.x + i * 256, row = rows_of[st * 32 + e / (RB * 16)], r = r0 + e % (RB * 16);
+            heldf[i] = row >= 0 && r < q.rank ? f[(size_t)row * q.rank + r] : 0.f;
+        }
+    };
+    auto put = [&](int st, int to) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int e = threadIdx.x + i * 256, r = e / UNITS, u = e % UNITS;
+            if (drop.border) mask8(drop, place, (uint64_t)((size_t)max(rows_of[st * 32 + r], 0) * s.C + c0 + u * 8), held[i]);
+            unsigned char* at = xt[to] + r * 512;
+            if constexpr (BF) *reinterpret_cast<u32x4*>(at + ((u >> 1) ^ turn(r)) * 32 + (u & 1) * 16) = held[i].v;
+            else {
+                *reinterpret_cast<f32x4*>(at + (u ^ turn(r)) * 32) = held[i].v[0];
+                *reinterpret_cast<f32x4*>(at + (u ^ turn(r)) * 32 + 16) = held[i].v[1];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < F_PER; ++i) {
+            const int e = threadIdx.x + i * 256;
+            if constexpr (BF) {
+                const uint16_t high = f32_to_bf16(heldf[i]);
+                reinterpret_cast<uint16_t*>(ft[to])[e] = high;
+                reinterpret_cast<uint16_t*>(ft[to])[FB + e] = f32_to_bf16(heldf[i] - bf16_to_f32(high));
+            } else reinterpret_cast<float*>(ft[to])[e] = heldf[i];
+        }
+    };
+    for (int p = p0; p < p1;) {
+        int a;
+        q.row(p, &a);
+        if (a < 0) break;
+        const long long begin = (long long)q.starts[a] * q.hw, finish = (long long)q.starts[a + 1] * q.hw;
+        const int end = (int)min((long long)p1, finish);
+        f32x4 acc[RB][CB] = {};
+        for (int base = p; base < end; base += WINDOW) {
+            const int n = min(WINDOW, end - base), steps = (n + 31) / 32;
+            __syncthreads();
+            int id;
+            rows_of[threadIdx.x] = (int)threadIdx.x < n ? q.row(base + threadIdx.x, &id) : -1;
+            __syncthreads();
+            fetch(0);
+            put(0, 0);
+            __syncthreads();
+            for (int st = 0; st < steps; ++st) {
+                if (st + 1 < steps) fetch(st + 1);
+                const unsigned char *x = xt[st & 1], *fs = ft[st & 1];
+                if constexpr (BF) {
+                    const int row = 8 * g + (l16 >> 2), fx = (l16 >> 2) | ((g & 1) << 2);
+                    u32x4 b[CB];
+#pragma unroll
+                    for (int j = 0; j < CB; ++j) {
+                        const unsigned char* at = x + row * 512 + (((wave * CB + j) ^ fx) << 5) + (l16 & 3) * 8;
+                        const u32x2 lo = read_transposed(at), hi = read_transposed(at + 4 * 512);
+                        b[j] = u32x4{lo[0], lo[1], hi[0], hi[1]};
+                    }
+#pragma unroll
+                    for (int i = 0; i < RB; ++i)
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            const unsigned char* at = fs + half * FB * 2 + row * (RB * 32) + i * 32 + (l16 & 3) * 8;
+                            const u32x2 lo = read_transposed(at), hi = read_transposed(at + 4 * RB * 32);
+                            const u32x4 w = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+                            for (int j = 0; j < CB; ++j) acc[i][j] = mfma(w, b[j], acc[i][j]);
+                        }
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int row = 4 * k + g, fx = (g | ((k << 1) & 4)) << 1;
+                        float b[CB];
+#pragma unroll
+                        for (int j = 0; j < CB; ++j) b[j] = *reinterpret_cast<const float*>(x + row * 512 + ((((wave * CB + j) * 2 + (l16 >> 3)) ^ fx) << 5) + (l16 & 7) * 4);
+#pragma unroll
+                        for (int i = 0; i < RB; ++i) {
+                            const float w = reinterpret_cast<const float*>(fs)[row * (RB * 16) + i * 16 + l16];
+#pragma unroll
+                            for (int j = 0; j < CB; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w, b[j], acc[i][j], 0, 0, 0);
+                        }
+                    }
+                }
+                if (st + 1 < steps) put(st + 1, (st + 1) & 1);
+                __syncthreads();
+            }
+        }
+        const bool all = begin == p && finish == end;
+        float* out = all ? s.out + (size_t)a * q.rank * s.C : s.partial + (size_t)(chunk + a) * q.rank * s.C;
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < CB; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int r = r0 + i * 16 + g * 4 + e, c = c0 + (wave * CB + j) * 16 + l16;
+                    if (r < q.rank && c < s.C) out[s.ranks_last ? (size_t)c * q.rank + r : (size_t)r * s.C + c] = acc[i][j][e] * scale;
+                }
+        p = end;
     }
 }
-__global__ __launch_bounds__(256) void join_kernel(const float* __restrict__ partial, int splits, size_t count, float* __restrict__ out)
+// Adapters whose rows lie in several chunks, and zeros for those without rows: `groups` workgroups for each adapter
+__global__ __launch_bounds__(256) void join_kernel(const Rows q, const Sums s, int groups)
 {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (i >= count) return;
-    float s = partial[i];
-    for (int k = 1; k < splits; ++k) s += partial[(size_t)k * count + i];
-    out[i] = s;
+    const int a = blockIdx.x / groups, group = blockIdx.x - a * groups;
+    const long long begin = (long long)q.starts[a] * q.hw, end = (long long)q.starts[a + 1] * q.hw;
+    const int first = (int)(begin / s.length), last = (int)((end - 1) / s.length);
+    if (end > begin && first == last) return;
+    const size_t count = (size_t)q.rank * s.C;
+    for (size_t i = group * 256u + threadIdx.x; i < count; i += groups * 256u) {
+        float sum = 0.f;
+        if (end > begin)
+            for (int k = first; k <= last; ++k) sum += s.partial[(size_t)(k + a) * count + i];
+        s.out[a * count + i] = sum;
+    }
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------------------
@@ -580,26 +683,38 @@ void transpose(const void* src, void* dst, int batch, int R, int C, hipStream_t 
     if (batch) hipLaunchKernelGGL((transpose_kernel<T>), dim3((unsigned)batch * tr * tc), dim3(256), 0, st, (const T*)src, (T*)dst, R, C, tr, tc);
 }
 
-// shares of an adapter's rows that workgroups of their own add: enough for four workgroups on every compute unit, of 64 rows and more if adapters have rows alike
-int splits_of(int rows, int adapters, int columns, int rank)
+// positions that a workgroup of the sums over rows takes: two workgroups for every compute unit, of 32 rows and more, up to 2048 chunks
+int length_of(int rows, int columns, int dtype)
 {
-    const long long groups = (long long)adapters * ((columns + 63) / 64) * ((rank + 15) / 16);
-    const int per = adapters ? rows / adapters : 0;
-    return (int)std::max<long long>(1, std::min<long long>({(1024 + groups - 1) / std::max(groups, 1ll), (long long)per / 64, 64ll}));
+    const int per = 512 / (int)elem_size(dtype), blocks = (columns + per - 1) / per, chunks = std::max(1, 512 / blocks);
+    return (int)align_up(std::max({(rows + chunks - 1) / chunks, (rows + 2047) / 2048, 1}), 32);
+}
+size_t slots_of(const AdapterShape& p, int columns)
+{
+    const int rows = p.images * p.hw, length = length_of(rows, columns, p.dtype);
+    return (size_t)(rows + length - 1) / length + p.adapters;
 }
 
+template <typename T, int RB>
+void sum_rows(const Rows& q, const Sums& s, const void* v, const float* f, const Drop& drop, hipStream_t st)
+{
+    constexpr int COLUMNS = 512 / sizeof(T);
+    hipLaunchKernelGGL((sums_kernel<T, RB>), dim3((s.C + COLUMNS - 1) / COLUMNS, (q.count + s.length - 1) / s.length, (q.rank + 63) / 64), dim3(256), 0, st, q, s, (const T*)v, f,
+                       drop);
+}
 template <typename T>
 void sum_rows(const Rows& q, const void* v, const float* f, int C, const Drop& drop, int ranks_last, float* out, float* partial, hipStream_t st)
 {
     Sums s;
-    s.C = C; s.ranks_last = ranks_last;
-    s.splits = splits_of(q.count, q.adapters, C, q.rank);
-    s.out = s.splits > 1 ? partial : out;
-    hipLaunchKernelGGL((rows_kernel<T>), dim3((C + 63) / 64, q.adapters * s.splits, (q.rank + 15) / 16), dim3(256), 0, st, q, s, (const T*)v, f, drop);
-    if (s.splits > 1) {
-        const size_t count = (size_t)q.adapters * q.rank * C;
-        hipLaunchKernelGGL(join_kernel, dim3((unsigned)((count + 255) / 256)), dim3(256), 0, st, partial, s.splits, count, out);
+    s.C = C; s.ranks_last = ranks_last; s.out = out; s.partial = partial;
+    s.length = length_of(q.count, C, sizeof(T) == 2 ? DR_BF16 : DR_F32);
+    if (q.count) {
+        if (q.rank <= 16) sum_rows<T, 1>(q, s, v, f, drop, st);
+        else if (q.rank <= 32) sum_rows<T, 2>(q, s, v, f, drop, st);
+        else sum_rows<T, 4>(q, s, v, f, drop, st);
     }
+    const int groups = (int)std::min<size_t>(64, ((size_t)q.rank * C + 1023) / 1024);
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)(q.adapters * groups)), dim3(256), 0, st, q, s, groups);
 }
 
 struct Scratch {                 // places in the workspace
@@ -618,8 +733,7 @@ Scratch scratch_of(const AdapterShape& p, bool backward)
         s.wt = take((size_t)p.in * p.out * el);
         s.at = take(factors * p.in * el);
         s.bt = take(factors * p.out * el);
-        const int rows = p.images * p.hw;
-        s.partial = take(factors * std::max((size_t)p.in * splits_of(rows, p.adapters, p.in, p.rank), (size_t)p.out * splits_of(rows, p.adapters, p.out, p.rank)) * 4);
+        s.partial = take((size_t)p.rank * std::max(slots_of(p, p.in) * p.in, slots_of(p, p.out) * p.out) * 4);
     }
     s.bytes = at;
     return s;
