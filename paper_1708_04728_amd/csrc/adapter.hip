@@ -466,6 +466,72 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
         }
 }
 
+// ---- the wide product of few rows ---------------------------------------------------------------------------------------------------------------
+// A workgroup owns 16 outputs of up to 64 rows (NB blocks of 16) and its eight waves share the contraction, so that W is read by as many compute units as there are blocks
+// of 16 outputs; operands go from memory to the matrix units, a row's 128 bytes together, U eighths of each in flight.  The sums of the waves are added in LDS, where a
+// lane adds the adapter's part of its output by itself: rank products.
+template <typename T, int NB, int U>
+__global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
+{
+    constexpr int NW = 8, PAIR = sizeof(T) == 2 ? 2 : 1, SLICE = 32 * PAIR;
+    __shared__ int row_of[NB * 16], id_of[NB * 16];
+    __shared__ __attribute__((aligned(16))) float red[NW][NB * 16][20];
+    const Rows& q = p.q;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4, p0 = blockIdx.x % p.tiles_n * (NB * 16), o0 = blockIdx.x / p.tiles_n * 16;
+    if (threadIdx.x < NB * 16) {
+        int id = -2, row = -1;
+        if (p0 + (int)threadIdx.x < q.count) row = q.row(p0 + threadIdx.x, &id);
+        row_of[threadIdx.x] = row;
+        id_of[threadIdx.x] = id;
+    }
+    __syncthreads();
+    const T* wr = p.w + (size_t)min(o0 + l16, p.N - 1) * p.K;
+    const T* xr[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) xr[j] = p.x + (size_t)max(row_of[j * 16 + l16], 0) * p.K;
+    f32x4 acc[NB] = {};
+    for (int k0 = wave * SLICE; k0 < p.K; k0 += NW * SLICE * (U / PAIR)) {
+        Operand<T> w[U], x[U][NB];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
+            w[u].load(wr + k, p.K - k);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) x[u][j].load(xr[j] + k, p.K - k);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[j] = mfma(w[u], x[u][j], acc[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4*>(&red[wave][j * 16 + l16][g * 4]) = acc[j];
+    __syncthreads();
+    const uint64_t place = p.drop.border ? drop_place(p.drop) : 0;
+    for (int i = threadIdx.x; i < NB * 256; i += 512) {
+        const int n = i >> 4, o = o0 + (i & 15), row = row_of[n], a = id_of[n];
+        if (row < 0 || o >= p.N) continue;
+        float part = 0.f;
+        if (a >= 0) {
+            const T* b = p.b + ((size_t)a * p.N + o) * q.rank;
+            const float* t = p.t + (size_t)row * q.rank;
+            for (int r = 0; r < q.rank; r += 8) {
+                float u[8], v[8];
+                load8(b + r, q.rank - r, 0.f, u);
+                load8(t + r, q.rank - r, 0.f, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) part = __builtin_fmaf(u[e], v[e], part);
+            }
+            const size_t at = (size_t)row * p.N + o;
+            if (p.drop.border) part = kept8(p.drop, place, at >> 3) >> (at & 7) & 1 ? part * p.drop.scale : 0.f;
+        }
+        float sum = red[0][n][i & 15];
+#pragma unroll
+        for (int w = 1; w < NW; ++w) sum += red[w][n][i & 15];
+        Store<T>::st(p.y + (size_t)row * p.N + o, sum + (p.bias ? p.bias[o] : 0.f) + part);
+    }
+}
+
 // ---- transposed copies: src[batch][R][C] -> dst[batch][C][R] --------------------------------------------------------------------------------------
 template <typename T>
 __global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ src, T* __restrict__ dst, int R, int C, int tiles_r, int tiles_c)
@@ -665,6 +731,13 @@ void wide(const Rows& q, const void* x, int K, const void* w, const float* bias,
         return p.tiles;
     };
     const int cus = device_cus();
+    if (tiles(64, 64) < cus / 2) {
+        constexpr int U = sizeof(T) == 2 ? 8 : 4;
+        if (q.count <= 16) { tiles(16, 16); hipLaunchKernelGGL((few_kernel<T, 1, U>), dim3(p.tiles), dim3(512), 0, st, p); }
+        else if (q.count <= 32) { tiles(16, 32); hipLaunchKernelGGL((few_kernel<T, 2, U / 2>), dim3(p.tiles), dim3(512), 0, st, p); }
+        else { tiles(16, 64); hipLaunchKernelGGL((few_kernel<T, 4, U / 2>), dim3(p.tiles), dim3(512), 0, st, p); }
+        return;
+    }
     const bool dma = aligned16(x) && aligned16(w) && K * sizeof(T) % 16 == 0 && (size_t)std::max(q.count, N) * K * sizeof(T) <= NOWHERE && (size_t)K * sizeof(T) < 0x7FFFFF00u;
     auto run = [&](auto dma, auto masked) {
         constexpr bool DMA = decltype(dma)::value, DROP = decltype(masked)::value;
