@@ -26,37 +26,67 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
 
 // Eight elements of an operand's row, as the matrix instructions take them.  A lane of group g = lane / 16 holds elements 8 g .. 8 g + 7 of a slice of 32: one
 // instruction in bf16, eight in fp32 (the j-th of them multiplies the j-th elements of the four groups).
+// load(row, k, K) reads elements k .. k + 7 of a row of K >= 8, or its last eight where it ends before, which settle() then moves to their places, with zeros behind
+// them: loads without a condition between them stay in flight together.  load_any() is for rows of any length.
 template <typename T> struct Operand;
 template <> struct Operand<uint16_t> {
     u32x4 v;
-    __device__ __forceinline__ void load(const uint16_t* p, int n)      // n: elements that exist
+    __device__ __forceinline__ void load(const uint16_t* row, int k, int K) { v = *reinterpret_cast<const u32x4_any*>(row + min(k, K - 8)); }
+    __device__ __forceinline__ void settle(int k, int K)
     {
-        if (n >= 8) v = *reinterpret_cast<const u32x4_any*>(p);
-        else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = (2 * i < n ? p[2 * i] : 0u) | (2 * i + 1 < n ? (unsigned)p[2 * i + 1] << 16 : 0u);
-        }
+        const int s = max(0, min(k - (K - 8), 8));
+        uint64_t lo = (uint64_t)v[1] << 32 | v[0], hi = (uint64_t)v[3] << 32 | v[2];
+        if (s >= 4) { lo = hi; hi = 0; }
+        const int bits = 16 * (s & 3);
+        lo = lo >> bits | (bits ? hi << (64 - bits) : 0);
+        hi >>= bits;
+        if (s == 8) lo = 0;
+        v = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
     }
+    __device__ __forceinline__ void load_any(const uint16_t* row, int k, int K)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = (k + 2 * i < K ? row[k + 2 * i] : 0u) | (k + 2 * i + 1 < K ? (unsigned)row[k + 2 * i + 1] << 16 : 0u);
+    }
+    __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
     __device__ __forceinline__ void keep(int j, bool yes)
     {
         if (!yes) v[j >> 1] &= j & 1 ? 0xFFFFu : 0xFFFF0000u;
     }
+    __device__ __forceinline__ void values(float (&e)[8]) const { unpack8(v, e); }
 };
 template <> struct Operand<float> {
     f32x4 v[2];
-    __device__ __forceinline__ void load(const float* p, int n)
+    __device__ __forceinline__ void load(const float* row, int k, int K)
     {
-        if (n >= 8) {
-            v[0] = *reinterpret_cast<const f32x4_any*>(p);
-            v[1] = *reinterpret_cast<const f32x4_any*>(p + 4);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = i < n ? p[i] : 0.f;
-        }
+        const float* p = row + min(k, K - 8);
+        v[0] = *reinterpret_cast<const f32x4_any*>(p);
+        v[1] = *reinterpret_cast<const f32x4_any*>(p + 4);
     }
+    __device__ __forceinline__ void settle(int k, int K)
+    {
+        const int s = max(0, min(k - (K - 8), 8));
+#pragma unroll
+        for (int d = 8; d >= 1; d >>= 1)
+            if (s & d) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = i + d < 8 ? v[(i + d) >> 2 & 1][(i + d) & 3] : 0.f;
+            }
+    }
+    __device__ __forceinline__ void load_any(const float* row, int k, int K)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = k + i < K ? row[k + i] : 0.f;
+    }
+    __device__ __forceinline__ void clear() { v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
     __device__ __forceinline__ void keep(int j, bool yes)
     {
         if (!yes) v[j >> 2][j & 3] = 0.f;
+    }
+    __device__ __forceinline__ void values(float (&e)[8]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e[i] = v[i >> 2][i & 3];
     }
 };
 __device__ __forceinline__ f32x4 mfma(const Operand<uint16_t>& a, const Operand<uint16_t>& b, f32x4 c) { return mfma(a.v, b.v, c); }
@@ -71,10 +101,16 @@ __device__ __forceinline__ f32x4 mfma(const Operand<float>& a, const Operand<flo
 template <typename T>
 __device__ __forceinline__ void mask8(const Drop& d, uint64_t place, uint64_t first, Operand<T>& v)
 {
-    float one[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
-    drop8_from(d, place, first, one);
+    if ((first & 7) == 0) {
+        uint32_t r[4];
+        philox(d.seed, first >> 3, place, r);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v.keep(j, one[j] != 0.f);
+        for (int j = 0; j < 8; ++j) v.keep(j, drop_draw(r, j) >= d.border);
+        return;
+    }
+    const unsigned bits = (kept8(d, place, first >> 3) | kept8(d, place, (first >> 3) + 1) << 8) >> (first & 7);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v.keep(j, bits >> j & 1);
 }
 // Which row is at a position, and its adapter.  Positions walk the images in `order` (NULL: as they come).
 struct Rows {
@@ -126,45 +162,68 @@ __global__ __launch_bounds__(1024) void order_kernel(const int* __restrict__ ids
 }
 
 // ---- a narrow product: out[row][r] = s_a sum_k v[row][k] M_a[r][k] -----------------------------------------------------------------------------
-// A workgroup takes 16 rows and the adapters among them, every `slots`-th from its own on; its waves share the contraction in slices of 32 and add up in LDS.
-template <typename T, int RB, int NW>
+// A workgroup takes 16 rows and the adapters among them, every gridDim.y-th from its own on (the i-th adapter is that of the i-th row whose adapter no row before has); its NW
+// waves share the contraction, 128 bytes of a row together and U eighths in flight, and add up in LDS.
+template <typename T, int RB, int NW, int U>
 __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
 {
-    __shared__ int row_of[16], id_of[16];
+    constexpr int PAIR = sizeof(T) == 2 ? 2 : 1, SLICE = 32 * PAIR;
     __shared__ float red[NW][RB * 16][17];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-    if (threadIdx.x < 16) {
-        const int p = blockIdx.x * 16 + threadIdx.x;
-        int id = -2, row = -1;
-        if (p < q.count) row = q.row(p, &id);
-        row_of[threadIdx.x] = row;
-        id_of[threadIdx.x] = id;
-    }
-    __syncthreads();
-    if (blockIdx.y == 0)
-        for (int i = threadIdx.x; i < 16 * q.rank; i += NW * 64)
-            if (id_of[i / q.rank] == -1) out[(size_t)row_of[i / q.rank] * q.rank + i % q.rank] = 0.f;
-    const uint64_t place = drop.border ? drop_place(drop) : 0;
-    const int row = row_of[l16];
-    const T* vr = v + (size_t)max(row, 0) * K;
-    for (int a = -1, turn = 0;; ++turn) {
-        int next = 0x7FFFFFFF;
-        for (int i = 0; i < 16; ++i) next = id_of[i] > a ? min(next, id_of[i]) : next;
-        if (next == 0x7FFFFFFF) break;
-        a = next;
-        if (turn % gridDim.y != blockIdx.y) continue;
-        f32x4 acc[RB] = {};
-        for (int k = wave * 32 + g * 8; k - g * 8 < K; k += NW * 32) {
-            Operand<T> x, w;
-            x.load(vr + k, row >= 0 ? K - k : 0);
-            if (drop.border) mask8(drop, place, (uint64_t)((size_t)max(row, 0) * K + k), x);
+    const int p = blockIdx.x * 16 + l16;
+    int id = -2, row = -1;
+    if (p < q.count) row = q.row(p, &id);
+    bool again = id < 0;
 #pragma unroll
-            for (int b = 0; b < RB; ++b) {
-                const int r = b * 16 + l16;
-                w.load(m + ((size_t)a * q.rank + min(r, q.rank - 1)) * K + k, r < q.rank ? K - k : 0);
-                acc[b] = mfma(w, x, acc[b]);
+    for (int i = 0; i < 15; ++i) again |= i < l16 && __builtin_amdgcn_readlane(id, i) == id;
+    unsigned firsts = (unsigned)__ballot(!again) & 0xFFFFu;
+    if (blockIdx.y == 0 && id == -1)
+        for (int r = wave * 4 + g; r < q.rank; r += NW * 4) out[(size_t)row * q.rank + r] = 0.f;
+    const uint64_t place = drop.border ? drop_place(drop) : 0;
+    for (int turn = 0; firsts; firsts &= firsts - 1, ++turn) {
+        if (turn % gridDim.y != blockIdx.y) continue;
+        const int first = __builtin_ctz(firsts), a = __builtin_amdgcn_readlane(id, first);
+        // (what comes of rows of other adapters is not stored: they read this adapter's first row)
+        const int mine = id == a ? row : __builtin_amdgcn_readlane(row, first);
+        const T* vr = v + (size_t)mine * K;
+        f32x4 acc[RB] = {};
+        const T* mr[RB];
+#pragma unroll
+        for (int b = 0; b < RB; ++b) mr[b] = m + ((size_t)a * q.rank + min(b * 16 + l16, q.rank - 1)) * K;
+        auto walk = [&](auto any) {
+            for (int k0 = wave * SLICE; k0 < K; k0 += NW * SLICE * (U / PAIR)) {
+                Operand<T> x[U], w[U][RB];
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
+                    if constexpr (decltype(any)::value) x[u].load_any(vr, k, K);
+                    else x[u].load(vr, k, K);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) {
+                        if constexpr (decltype(any)::value) w[u][b].load_any(mr[b], k, K);
+                        else w[u][b].load(mr[b], k, K);
+                    }
+                }
+                if (!decltype(any)::value && k0 + (U / PAIR - 1) * (NW * SLICE) + SLICE > K) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
+                        x[u].settle(k, K);
+#pragma unroll
+                        for (int b = 0; b < RB; ++b) w[u][b].settle(k, K);
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
+                    if (drop.border) mask8(drop, place, (uint64_t)((size_t)mine * K + k), x[u]);
+#pragma unroll
+                    for (int b = 0; b < RB; ++b) acc[b] = mfma(w[u][b], x[u], acc[b]);
+                }
             }
-        }
+        };
+        if (K >= 8) walk(std::false_type());
+        else walk(std::true_type());
         __syncthreads();
 #pragma unroll
         for (int b = 0; b < RB; ++b)
@@ -172,14 +231,14 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
             for (int i = 0; i < 4; ++i) red[wave][b * 16 + g * 4 + i][l16] = acc[b][i];
         __syncthreads();
         const float scale = (q.scales ? q.scales[a] : 1.f) * (drop.border ? drop.scale : 1.f);
-        for (int i = threadIdx.x; i < 16 * q.rank; i += NW * 64) {
-            const int n = i / q.rank, r = i - n * q.rank;
-            if (id_of[n] != a) continue;
-            float s = red[0][r][n];
+        // 16 lanes hold the rows, the others of the workgroup the ranks
+        if (id == a)
+            for (int r = wave * 4 + g; r < q.rank; r += NW * 4) {
+                float s = red[0][r][l16];
 #pragma unroll
-            for (int w = 1; w < NW; ++w) s += red[w][r][n];
-            out[(size_t)row_of[n] * q.rank + r] = s * scale;
-        }
+                for (int w = 1; w < NW; ++w) s += red[w][r][l16];
+                out[(size_t)row * q.rank + r] = s * scale;
+            }
     }
 }
 
@@ -489,46 +548,92 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
     const T* xr[NB];
 #pragma unroll
     for (int j = 0; j < NB; ++j) xr[j] = p.x + (size_t)max(row_of[j * 16 + l16], 0) * p.K;
-    f32x4 acc[NB] = {};
-    for (int k0 = wave * SLICE; k0 < p.K; k0 += NW * SLICE * (U / PAIR)) {
-        Operand<T> w[U], x[U][NB];
+    // this lane's outputs and the first sixteen of their rows of B_a, which are on their way while the projection is multiplied
+    constexpr int PER = (NB * 256 + 511) / 512;
+    Operand<T> early[PER][2];
+    int n[PER], a[PER];
+    const int o = o0 + (threadIdx.x & 15);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
-            w[u].load(wr + k, p.K - k);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) x[u][j].load(xr[j] + k, p.K - k);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int j = 0; j < NB; ++j) acc[j] = mfma(w[u], x[u][j], acc[j]);
+    for (int i = 0; i < PER; ++i) {
+        n[i] = (threadIdx.x >> 4) + i * 32;
+        a[i] = n[i] < NB * 16 ? id_of[n[i]] : -2;
+        if (a[i] < 0) continue;
+        const T* b = p.b + ((size_t)a[i] * p.N + min(o, p.N - 1)) * q.rank;
+        if (q.rank >= 8) {
+            early[i][0].load(b, 0, q.rank);
+            early[i][1].load(b, 8, q.rank);
+        } else early[i][0].load_any(b, 0, q.rank);
     }
+    f32x4 acc[NB] = {};
+    auto walk = [&](auto any) {
+        for (int k0 = wave * SLICE; k0 < p.K; k0 += NW * SLICE * (U / PAIR)) {
+            Operand<T> w[U], x[U][NB];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
+                if constexpr (decltype(any)::value) w[u].load_any(wr, k, p.K);
+                else w[u].load(wr, k, p.K);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    if constexpr (decltype(any)::value) x[u][j].load_any(xr[j], k, p.K);
+                    else x[u][j].load(xr[j], k, p.K);
+                }
+            }
+            if (!decltype(any)::value && k0 + (U / PAIR - 1) * (NW * SLICE) + SLICE > p.K) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
+                    w[u].settle(k, p.K);
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) x[u][j].settle(k, p.K);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[j] = mfma(w[u], x[u][j], acc[j]);
+        }
+    };
+    if (p.K >= 8) walk(std::false_type());
+    else walk(std::true_type());
 #pragma unroll
     for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4*>(&red[wave][j * 16 + l16][g * 4]) = acc[j];
+    float part[PER] = {};
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        if (a[i] < 0) continue;
+        const T* b = p.b + ((size_t)a[i] * p.N + min(o, p.N - 1)) * q.rank;
+        const float* t = p.t + (size_t)row_of[n[i]] * q.rank;
+        for (int r = 0; r < q.rank; r += 8) {
+            Operand<T> v = early[i][0];
+            Operand<float> f;
+            if (q.rank >= 8) {
+                if (r == 8) v = early[i][1];
+                if (r > 8) v.load(b, r, q.rank);
+                f.load(t, r, q.rank);
+                if (r + 8 > q.rank) {
+                    v.settle(r, q.rank);
+                    f.settle(r, q.rank);
+                }
+            } else f.load_any(t, r, q.rank);
+            float e[8], d[8];
+            v.values(e);
+            f.values(d);
+#pragma unroll
+            for (int c = 0; c < 8; ++c) part[i] = __builtin_fmaf(e[c], d[c], part[i]);
+        }
+    }
     __syncthreads();
     const uint64_t place = p.drop.border ? drop_place(p.drop) : 0;
-    for (int i = threadIdx.x; i < NB * 256; i += 512) {
-        const int n = i >> 4, o = o0 + (i & 15), row = row_of[n], a = id_of[n];
-        if (row < 0 || o >= p.N) continue;
-        float part = 0.f;
-        if (a >= 0) {
-            const T* b = p.b + ((size_t)a * p.N + o) * q.rank;
-            const float* t = p.t + (size_t)row * q.rank;
-            for (int r = 0; r < q.rank; r += 8) {
-                float u[8], v[8];
-                load8(b + r, q.rank - r, 0.f, u);
-                load8(t + r, q.rank - r, 0.f, v);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) part = __builtin_fmaf(u[e], v[e], part);
-            }
-            const size_t at = (size_t)row * p.N + o;
-            if (p.drop.border) part = kept8(p.drop, place, at >> 3) >> (at & 7) & 1 ? part * p.drop.scale : 0.f;
-        }
-        float sum = red[0][n][i & 15];
+    for (int i = 0; i < PER; ++i) {
+        if (a[i] < -1 || o >= p.N) continue;
+        const size_t at = (size_t)row_of[n[i]] * p.N + o;
+        if (p.drop.border && a[i] >= 0) part[i] = kept8(p.drop, place, at >> 3) >> (at & 7) & 1 ? part[i] * p.drop.scale : 0.f;
+        float sum = red[0][n[i]][threadIdx.x & 15];
 #pragma unroll
-        for (int w = 1; w < NW; ++w) sum += red[w][n][i & 15];
-        Store<T>::st(p.y + (size_t)row * p.N + o, sum + (p.bias ? p.bias[o] : 0.f) + part);
+        for (int w = 1; w < NW; ++w) sum += red[w][n[i]][threadIdx.x & 15];
+        Store<T>::st(p.y + at, sum + (p.bias ? p.bias[o] : 0.f) + part[i]);
     }
 }
 
@@ -587,18 +692,23 @@ __global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums s, c
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = threadIdx.x + i * 256, row = rows_of[st * 32 + e / UNITS], c = c0 + (e % UNITS) * 8;
-            held[i].load(v + (size_t)max(row, 0) * s.C + c, row >= 0 ? s.C - c : 0);
+            const T* from = v + (size_t)max(row, 0) * s.C;
+            if (s.C >= 8) held[i].load(from, c, s.C);
+            else held[i].load_any(from, c, s.C);
         }
 #pragma unroll
         for (int i = 0; i < F_PER; ++i) {
-            const int e = threadIdx.x + i * 256, row = rows_of[st * 32 + e / (RB * 16)], r = r0 + e % (RB * 16);
-            heldf[i] = row >= 0 && r < q.rank ? f[(size_t)row * q.rank + r] : 0.f;
+            const int at = threadIdx.x + i * 256, row = rows_of[st * 32 + at / (RB * 16)], r = r0 + at % (RB * 16);
+            const float e = f[(size_t)max(row, 0) * q.rank + min(r, q.rank - 1)];
+            heldf[i] = row >= 0 && r < q.rank ? e : 0.f;
         }
     };
     auto put = [&](int st, int to) {
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = threadIdx.x + i * 256, r = e / UNITS, u = e % UNITS;
+            if (s.C >= 8 && c0 + 512 / (int)sizeof(T) > s.C) held[i].settle(c0 + u * 8, s.C);
+            if (rows_of[st * 32 + r] < 0) held[i].clear();
             if (drop.border) mask8(drop, place, (uint64_t)((size_t)max(rows_of[st * 32 + r], 0) * s.C + c0 + u * 8), held[i]);
             unsigned char* at = xt[to] + r * 512;
             if constexpr (BF) *reinterpret_cast<u32x4*>(at + ((u >> 1) ^ turn(r)) * 32 + (u & 1) * 16) = held[i].v;
@@ -705,18 +815,19 @@ __global__ __launch_bounds__(256) void join_kernel(const Rows q, const Sums s, i
 }
 
 // ---- host ---------------------------------------------------------------------------------------------------------------------------------------
-constexpr int NARROW_WAVES = 8;
-
 template <typename T>
 void narrow(const Rows& q, const void* v, int K, const void* m, const Drop& drop, float* out, hipStream_t st)
 {
     if (!q.count) return;
-    const int tiles = (q.count + 15) / 16, slots = tiles < 256 ? std::min({16, q.adapters, (256 + tiles - 1) / tiles}) : 1;
-    const dim3 grid(tiles, std::max(slots, 1)), block(NARROW_WAVES * 64);
-    if (q.rank <= 16) hipLaunchKernelGGL((narrow_kernel<T, 1, NARROW_WAVES>), grid, block, 0, st, q, (const T*)v, K, (const T*)m, drop, out);
-    else if (q.rank <= 32) hipLaunchKernelGGL((narrow_kernel<T, 2, NARROW_WAVES>), grid, block, 0, st, q, (const T*)v, K, (const T*)m, drop, out);
-    else if (q.rank <= 64) hipLaunchKernelGGL((narrow_kernel<T, 4, NARROW_WAVES>), grid, block, 0, st, q, (const T*)v, K, (const T*)m, drop, out);
-    else hipLaunchKernelGGL((narrow_kernel<T, 8, 4>), grid, dim3(256), 0, st, q, (const T*)v, K, (const T*)m, drop, out);
+    constexpr int U = sizeof(T) == 2 ? 8 : 4;
+    const int tiles = (q.count + 15) / 16;
+    auto launch = [&](auto kernel, int waves, int slots) { hipLaunchKernelGGL(kernel, dim3(tiles, slots), dim3(waves * 64), 0, st, q, (const T*)v, K, (const T*)m, drop, out); };
+    // few rows: each of a tile's adapters in a workgroup of its own, and twice the waves
+    const int slots = tiles < 256 ? std::max(1, std::min({16, q.adapters, (1023 + tiles) / tiles})) : 1;
+    if (q.rank <= 16) tiles <= 64 ? launch(narrow_kernel<T, 1, 16, U>, 16, slots) : launch(narrow_kernel<T, 1, 8, U>, 8, slots);
+    else if (q.rank <= 32) launch(narrow_kernel<T, 2, 8, U / 2>, 8, slots);
+    else if (q.rank <= 64) launch(narrow_kernel<T, 4, 8, U / 2>, 8, slots);
+    else launch(narrow_kernel<T, 8, 4, 2>, 4, slots);
 }
 
 template <typename T>

@@ -87,27 +87,6 @@ __device__ __forceinline__ void drop8(const Drop& d, uint64_t place, uint64_t bl
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = drop_draw(r, j) >= d.border ? v[j] * d.scale : 0.f;
 }
-// ... of eight elements from any `first` on: two blocks where it is no multiple of eight
-__device__ __forceinline__ void drop8_from(const Drop& d, uint64_t place, uint64_t first, float (&v)[8])
-{
-    const int shift = (int)(first & 7);
-    if (shift == 0) return drop8(d, place, first >> 3, v);
-    uint32_t r[8], lo[4], hi[4];
-    philox(d.seed, first >> 3, place, lo);
-    philox(d.seed, (first >> 3) + 1, place, hi);
-    // sixteen draws in a row, moved down by `shift` of them: whole words, then a half
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { r[i] = lo[i]; r[4 + i] = hi[i]; }
-#pragma unroll
-    for (int s = 4; s >= 2; s >>= 1)
-#pragma unroll
-        for (int i = 0; i + (s >> 1) < 8; ++i) r[i] = shift & s ? r[i + (s >> 1)] : r[i];
-    const bool half = shift & 1;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) lo[i] = half ? (r[i] >> 16) | (r[i + 1] << 16) : r[i];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = drop_draw(lo, j) >= d.border ? v[j] * d.scale : 0.f;
-}
 #endif
 
 }  // namespace dr

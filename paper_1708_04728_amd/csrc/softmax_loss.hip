@@ -100,57 +100,101 @@ __global__ __launch_bounds__(PER < 256 ? 256 : PER) void loss_kernel(const Loss 
         const T* zr = z + (size_t)row * q.C;
         const int label = q.labels[row];
         const bool has = (unsigned)label < (unsigned)q.C;
-        float v[NV][8];
-        if (has) {
-            const float z_t = Store<T>::ld(zr + label);
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < NV; ++i) load8(zr + (i * PER + lane) * 8, q.C - (i * PER + lane) * 8, -INFINITY, v[i]);
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = fmaxf(top, v[i][j]);
-            RowSums s;
-            s.top = top = reduce<PER>(top, red, larger);
-            float sum = 0.f, shifted = 0.f;
-            if (q.smoothing != 0.f) {
-#pragma unroll
-                for (int i = 0; i < NV; ++i)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) shifted += (i * PER + lane) * 8 + j < q.C ? v[i][j] - top : 0.f;
-            }
-#pragma unroll
-            for (int i = 0; i < NV; ++i)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    // (places behind the row: -inf less a finite maximum; where the maximum is not finite the row is NaN anyway)
-                    v[i][j] = exp_of(v[i][j] - top);
-                    sum += v[i][j];
-                }
-            s.sum = reduce<PER>(sum, red, add);
-            s.shifted = q.smoothing != 0.f ? reduce<PER>(shifted, red, add) : 0.f;
-            if (lane == 0) q.row_loss[row] = row_loss_of(q, s, z_t);
-            if (dz) {
-                const float scale = g / s.sum, less = g * (q.smoothing / (float)q.C), at_label = g * (1.f - q.smoothing);
-#pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int c = (i * PER + lane) * 8;
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * scale - (c + j == label ? less + at_label : less);
-                    store8(dz + (size_t)row * q.C + c, q.C - c, v[i]);
-                }
-            }
-        } else {
+        // A lane's eight places, the row's last eight where it ends before them: those of them that another lane has too (the first `twice`) are left out of the sums, and
+        // written by both with the same bits.  Loads without a condition between them stay in flight together.
+        auto start = [&](int i) { return min((i * PER + lane) * 8, q.C - 8); };
+        auto twice = [&](int i) { return min((i * PER + lane) * 8 - start(i), 8); };
+        auto ragged = [&](int i) { return (i + 1) * PER * 8 > q.C; };
+        if (!has) {
             if (lane == 0) q.row_loss[row] = 0.f;
             if (dz) {
                 const float zero[8] = {};
 #pragma unroll
-                for (int i = 0; i < NV; ++i) {
-                    const int c = (i * PER + lane) * 8;
-                    store8(dz + (size_t)row * q.C + c, q.C - c, zero);
-                }
+                for (int i = 0; i < NV; ++i)
+                    if ((i * PER + lane) * 8 < q.C) store8(dz + (size_t)row * q.C + start(i), zero);
+            }
+            continue;
+        }
+        float v[NV][8];
+        const float z_t = Store<T>::ld(zr + label);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) load8(zr + start(i), v[i]);
+        float top = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, v[i][j]);
+        RowSums s;
+        s.top = top = reduce<PER>(top, red, larger);
+        float sum = 0.f, shifted = 0.f;
+        if (q.smoothing != 0.f) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) shifted += !ragged(i) || j >= twice(i) ? v[i][j] - top : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = exp_of(v[i][j] - top);
+            if (ragged(i)) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += j >= twice(i) ? v[i][j] : 0.f;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += v[i][j];
             }
         }
+        s.sum = reduce<PER>(sum, red, add);
+        s.shifted = q.smoothing != 0.f ? reduce<PER>(shifted, red, add) : 0.f;
+        if (lane == 0) q.row_loss[row] = row_loss_of(q, s, z_t);
+        if (dz) {
+            const float scale = g / s.sum, less = g * (q.smoothing / (float)q.C), at_label = g * (1.f - q.smoothing);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = start(i);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * scale - (c + j == label ? less + at_label : less);
+                if ((i * PER + lane) * 8 < q.C) store8(dz + (size_t)row * q.C + c, v[i]);
+            }
+        }
+    }
+}
+
+// Fewer than eight classes: a lane a row
+template <typename T>
+__global__ __launch_bounds__(256) void loss_short_kernel(const Loss q, const T* z, T* dz)
+{
+    __shared__ int redi[16];
+    float g = 1.f;
+    if (q.mean && dz) {
+        const int n = q.counted ? *q.counted : count_labels(q.labels, q.rows, q.C, 256, redi);
+        g = n > 0 ? 1.f / (float)n : 0.f;
+    }
+    for (int row = blockIdx.x * 256 + threadIdx.x; row < q.rows; row += gridDim.x * 256) {
+        const int label = q.labels[row];
+        const bool has = (unsigned)label < (unsigned)q.C;
+        float v[8];
+        load8(z + (size_t)row * q.C, q.C, -INFINITY, v);
+        RowSums s = {-INFINITY, 0.f, 0.f};
+        float z_t = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s.top = fmaxf(s.top, v[j]);
+            z_t = j == label ? v[j] : z_t;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j < q.C) s.shifted += v[j] - s.top;
+            v[j] = j < q.C ? exp_of(v[j] - s.top) : 0.f;
+            s.sum += v[j];
+        }
+        q.row_loss[row] = has ? row_loss_of(q, s, z_t) : 0.f;
+        if (!dz) continue;
+        const float scale = g / s.sum, less = g * (q.smoothing / (float)q.C), at_label = g * (1.f - q.smoothing);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = has ? v[j] * scale - (j == label ? less + at_label : less) : 0.f;
+        store8(dz + (size_t)row * q.C, q.C, v);
     }
 }
 
@@ -238,7 +282,8 @@ void launch_rows(const Loss& q, const void* z, void* dz, hipStream_t st)
 template <typename T>
 void launch(const Loss& q, const void* z, void* dz, hipStream_t st)
 {
-    if (q.C <= 512) launch_rows<T, 64, 1>(q, z, dz, st);
+    if (q.C < 8) hipLaunchKernelGGL((loss_short_kernel<T>), dim3(std::min((q.rows + 255) / 256, 4096)), dim3(256), 0, st, q, (const T*)z, (T*)dz);
+    else if (q.C <= 512) launch_rows<T, 64, 1>(q, z, dz, st);
     else if (q.C <= 1024) launch_rows<T, 64, 2>(q, z, dz, st);
     else if (q.C <= 2048) launch_rows<T, 256, 1>(q, z, dz, st);
     else if (q.C <= 4096) launch_rows<T, 256, 2>(q, z, dz, st);
