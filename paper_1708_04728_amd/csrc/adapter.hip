@@ -161,13 +161,145 @@ __global__ __launch_bounds__(1024) void order_kernel(const int* __restrict__ ids
     }
 }
 
+// 16 bytes of a row, of which `n` elements exist (zeros behind them)
+__device__ __forceinline__ u32x4 piece(const char* p) { return *reinterpret_cast<const u32x4_any*>(p); }
+template <typename T>
+__device__ __forceinline__ u32x4 piece(const char* p, int n)
+{
+    constexpr int E = 16 / sizeof(T);
+    if (n >= E) return piece(p);
+    u32x4 v = {0, 0, 0, 0};
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) v[i >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) v[i] = reinterpret_cast<const unsigned*>(p)[i];
+    }
+    return v;
+}
+
+// ---- products of few rows or few ranks: a wave by itself ----------------------------------------------------------------------------------------
+// Rows of two matrices, A blocks of 16 of the one and B of the other, 128 bytes of a row at a time: loads in which eight lanes take a row's 128 bytes (lanes that take a row
+// each, as the matrix instructions want them, are served one row a cycle: four times as long), D slices of them in flight in registers, through the wave's own LDS,
+// in the order piece ^ (row & 7), to the operands.  Waves of a workgroup share the contraction: wave w takes slices w, w + NW, ...
+struct Piece { u32x4 v; };
+template <typename T> __device__ __forceinline__ void load_piece(Piece& e, const T* row, int k, int K)      // the row's last ones where it ends before (K >= 16 bytes)
+{
+    constexpr int E = 16 / sizeof(T);
+    e.v = *reinterpret_cast<const u32x4_any*>(row + min(k, K - E));
+}
+template <typename T> __device__ __forceinline__ void load_piece_any(Piece& e, const T* row, int k, int K) { e.v = piece<T>((const char*)(row + k), K - k); }
+// ... then moved to their places, zeros behind them
+template <typename T> __device__ __forceinline__ void settle_piece(Piece& e, int k, int K)
+{
+    constexpr int E = 16 / sizeof(T);
+    const int s = max(0, min(k - (K - E), E)) * (int)sizeof(T);
+    uint64_t lo = (uint64_t)e.v[1] << 32 | e.v[0], hi = (uint64_t)e.v[3] << 32 | e.v[2];
+    if (s >= 8) { lo = hi; hi = 0; }
+    const int bits = 8 * (s & 7);
+    lo = lo >> bits | (bits ? hi << (64 - bits) : 0);
+    hi >>= bits;
+    if (s == 16) lo = 0;
+    e.v = u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+// Which elements of the piece that starts at element `first` dropout keeps: sets the others to zero (what is kept is scaled where the sums are, exactly)
+__device__ __forceinline__ void mask_piece(const Drop& d, uint64_t place, uint64_t first, Piece& e, uint16_t)
+{
+    unsigned bits = kept8(d, place, first >> 3);
+    if (first & 7) bits = (bits | kept8(d, place, (first >> 3) + 1) << 8) >> (first & 7);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.v[i] &= (bits >> (2 * i) & 1 ? 0xFFFFu : 0u) | (bits >> (2 * i + 1) & 1 ? 0xFFFF0000u : 0u);
+}
+__device__ __forceinline__ void mask_piece(const Drop& d, uint64_t place, uint64_t first, Piece& e, float)
+{
+    unsigned bits = kept8(d, place, first >> 3);
+    if ((first & 7) > 4) bits |= kept8(d, place, (first >> 3) + 1) << 8;
+    bits >>= first & 7;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.v[i] = bits >> i & 1 ? e.v[i] : 0u;
+}
+template <typename T> __device__ __forceinline__ f32x4 mfma16(u32x4 a, u32x4 b, f32x4 c)
+{
+    if constexpr (sizeof(T) == 2) return mfma(a, b, c);
+    else {
+        const f32x4 p = __builtin_bit_cast(f32x4, a), q = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(p[i], q[i], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// ra(i), rb(i): row of the first and of the second matrix that lane / 8 loads for rows 8 i .. 8 i + 7 of its blocks.  lds: (A + B) x 2 KiB of the wave's own.
+template <typename T, int A, int B, int D, int NW, bool DROP, class RA, class RB_>
+__device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ rb, int K, int wave, unsigned char* lds, const Drop& drop, uint64_t place, f32x4 (&acc)[A][B])
+{
+    constexpr int E = 16 / sizeof(T), SLICE = 8 * E, N = 2 * (A + B);
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4, r8 = lane >> 3, c = lane & 7, slices = (K + SLICE - 1) / SLICE;
+    const T* from[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) from[i] = i < 2 * A ? a + (size_t)ra(i) * K : b + (size_t)rb(i - 2 * A) * K;
+    const bool tiny = K < E;
+    Piece held[D][N];
+    auto load = [&](int s, Piece (&h)[N]) {
+        const int k = s * SLICE + c * E;
+        if (!tiny) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_piece(h[i], from[i], k, K);
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) load_piece_any(h[i], from[i], k, K);
+        }
+    };
+    auto put = [&](int s, Piece (&h)[N]) {
+        const int k = s * SLICE + c * E;
+        if ((s + 1) * SLICE > K && !tiny) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) settle_piece<T>(h[i], k, K);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (DROP && i >= 2 * A) mask_piece(drop, place, (uint64_t)((size_t)rb(i - 2 * A) * K + k), h[i], T());
+            *reinterpret_cast<u32x4*>(lds + (i * 8 + r8) * 128 + ((c ^ r8) << 4)) = h[i].v;
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+        if (wave + d * NW < slices) load(wave + d * NW, held[d]);
+    for (int s0 = wave; s0 < slices; s0 += NW * D) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int s = s0 + d * NW;
+            if (s >= slices) break;
+            put(s, held[d]);
+            asm volatile("" ::: "memory");              // (the wave's own LDS, written and read in order)
+            if (s + D * NW < slices) load(s + D * NW, held[d]);
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                u32x4 x[B];
+#pragma unroll
+                for (int j = 0; j < B; ++j) x[j] = *reinterpret_cast<const u32x4*>(lds + (A * 16 + j * 16 + l16) * 128 + (((t * 4 + g) ^ (l16 & 7)) << 4));
+#pragma unroll
+                for (int i = 0; i < A; ++i) {
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + (i * 16 + l16) * 128 + (((t * 4 + g) ^ (l16 & 7)) << 4));
+#pragma unroll
+                    for (int j = 0; j < B; ++j) acc[i][j] = mfma16<T>(w, x[j], acc[i][j]);
+                }
+            }
+            asm volatile("" ::: "memory");
+        }
+    }
+}
+
 // ---- a narrow product: out[row][r] = s_a sum_k v[row][k] M_a[r][k] -----------------------------------------------------------------------------
 // A workgroup takes 16 rows and the adapters among them, every gridDim.y-th from its own on (the i-th adapter is that of the i-th row whose adapter no row before has); its NW
-// waves share the contraction, 128 bytes of a row together and U eighths in flight, and add up in LDS.
-template <typename T, int RB, int NW, int U>
+// waves share the contraction and add up in LDS.
+template <typename T, int RB, int NW, int D>
 __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
 {
-    constexpr int PAIR = sizeof(T) == 2 ? 2 : 1, SLICE = 32 * PAIR;
+    __shared__ __attribute__((aligned(128))) unsigned char lds[NW][(RB + 1) * 2048];
     __shared__ float red[NW][RB * 16][17];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
     const int p = blockIdx.x * 16 + l16;
@@ -184,51 +316,18 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
         if (turn % gridDim.y != blockIdx.y) continue;
         const int first = __builtin_ctz(firsts), a = __builtin_amdgcn_readlane(id, first);
         // (what comes of rows of other adapters is not stored: they read this adapter's first row)
-        const int mine = id == a ? row : __builtin_amdgcn_readlane(row, first);
-        const T* vr = v + (size_t)mine * K;
-        f32x4 acc[RB] = {};
-        const T* mr[RB];
-#pragma unroll
-        for (int b = 0; b < RB; ++b) mr[b] = m + ((size_t)a * q.rank + min(b * 16 + l16, q.rank - 1)) * K;
-        auto walk = [&](auto any) {
-            for (int k0 = wave * SLICE; k0 < K; k0 += NW * SLICE * (U / PAIR)) {
-                Operand<T> x[U], w[U][RB];
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
-                    if constexpr (decltype(any)::value) x[u].load_any(vr, k, K);
-                    else x[u].load(vr, k, K);
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) {
-                        if constexpr (decltype(any)::value) w[u][b].load_any(mr[b], k, K);
-                        else w[u][b].load(mr[b], k, K);
-                    }
-                }
-                if (!decltype(any)::value && k0 + (U / PAIR - 1) * (NW * SLICE) + SLICE > K) {
-#pragma unroll
-                    for (int u = 0; u < U; ++u) {
-                        const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
-                        x[u].settle(k, K);
-#pragma unroll
-                        for (int b = 0; b < RB; ++b) w[u][b].settle(k, K);
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
-                    if (drop.border) mask8(drop, place, (uint64_t)((size_t)mine * K + k), x[u]);
-#pragma unroll
-                    for (int b = 0; b < RB; ++b) acc[b] = mfma(w[u][b], x[u], acc[b]);
-                }
-            }
-        };
-        if (K >= 8) walk(std::false_type());
-        else walk(std::true_type());
+        const int mine = id == a ? row : __builtin_amdgcn_readlane(row, first), low = __shfl(mine, lane >> 3, 64), high = __shfl(mine, 8 + (lane >> 3), 64);
+        f32x4 acc[RB][1] = {};
+        auto ra = [&](int i) { return min(i * 8 + (lane >> 3), q.rank - 1); };
+        auto rb = [&](int i) { return i ? high : low; };
+        const T* ma = m + (size_t)a * q.rank * K;
+        if (drop.border) wave_product<T, RB, 1, D, NW, true>(ma, ra, v, rb, K, wave, lds[wave], drop, place, acc);
+        else wave_product<T, RB, 1, D, NW, false>(ma, ra, v, rb, K, wave, lds[wave], drop, place, acc);
         __syncthreads();
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) red[wave][b * 16 + g * 4 + i][l16] = acc[b][i];
+            for (int i = 0; i < 4; ++i) red[wave][b * 16 + g * 4 + i][l16] = acc[b][0][i];
         __syncthreads();
         const float scale = (q.scales ? q.scales[a] : 1.f) * (drop.border ? drop.scale : 1.f);
         // 16 lanes hold the rows, the others of the workgroup the ranks
@@ -269,26 +368,6 @@ template <> __device__ __forceinline__ f32x16 mfma32<float>(u32x4 a, u32x4 b, f3
 #pragma unroll
     for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(p[i], q[i], c, 0, 0, 0);
     return c;
-}
-
-// 16 bytes of a row, of which `n` elements exist (zeros behind them)
-__device__ __forceinline__ u32x4 piece(const char* p) { return *reinterpret_cast<const u32x4_any*>(p); }
-template <typename T>
-__device__ __forceinline__ u32x4 piece(const char* p, int n)
-{
-    constexpr int E = 16 / sizeof(T);
-    if (n >= E) return piece(p);
-    u32x4 v = {0, 0, 0, 0};
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < n) v[i >> 1] |= (unsigned)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i & 1));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < n) v[i] = reinterpret_cast<const unsigned*>(p)[i];
-    }
-    return v;
 }
 
 // The tiles that the 8 dies' workgroups (dealt out in turn) see are neighbours: die d takes the d-th run of the list, which goes down runs of 8 tiles of rows.
@@ -527,12 +606,12 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 
 // ---- the wide product of few rows ---------------------------------------------------------------------------------------------------------------
 // A workgroup owns 16 outputs of up to 64 rows (NB blocks of 16) and its eight waves share the contraction, so that W is read by as many compute units as there are blocks
-// of 16 outputs; operands go from memory to the matrix units, a row's 128 bytes together, U eighths of each in flight.  The sums of the waves are added in LDS, where a
-// lane adds the adapter's part of its output by itself: rank products.
-template <typename T, int NB, int U>
+// of 16 outputs.  The sums of the waves are added in LDS, where a lane adds the adapter's part of its output by itself: rank products.
+template <typename T, int NB, int D>
 __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
 {
-    constexpr int NW = 8, PAIR = sizeof(T) == 2 ? 2 : 1, SLICE = 32 * PAIR;
+    constexpr int NW = 8;
+    __shared__ __attribute__((aligned(128))) unsigned char lds[NW][(NB + 1) * 2048];
     __shared__ int row_of[NB * 16], id_of[NB * 16];
     __shared__ __attribute__((aligned(16))) float red[NW][NB * 16][20];
     const Rows& q = p.q;
@@ -544,10 +623,6 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
         id_of[threadIdx.x] = id;
     }
     __syncthreads();
-    const T* wr = p.w + (size_t)min(o0 + l16, p.N - 1) * p.K;
-    const T* xr[NB];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) xr[j] = p.x + (size_t)max(row_of[j * 16 + l16], 0) * p.K;
     // this lane's outputs and the first sixteen of their rows of B_a, which are on their way while the projection is multiplied
     constexpr int PER = (NB * 256 + 511) / 512;
     Operand<T> early[PER][2];
@@ -564,40 +639,11 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
             early[i][1].load(b, 8, q.rank);
         } else early[i][0].load_any(b, 0, q.rank);
     }
-    f32x4 acc[NB] = {};
-    auto walk = [&](auto any) {
-        for (int k0 = wave * SLICE; k0 < p.K; k0 += NW * SLICE * (U / PAIR)) {
-            Operand<T> w[U], x[U][NB];
+    f32x4 acc[1][NB] = {};
+    wave_product<T, 1, NB, D, NW, false>(p.w, [&](int i) { return min(o0 + i * 8 + (lane >> 3), p.N - 1); }, p.x, [&](int i) { return max(row_of[i * 8 + (lane >> 3)], 0); }, p.K,
+                                         wave, lds[wave], p.drop, 0, acc);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
-                if constexpr (decltype(any)::value) w[u].load_any(wr, k, p.K);
-                else w[u].load(wr, k, p.K);
-#pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    if constexpr (decltype(any)::value) x[u][j].load_any(xr[j], k, p.K);
-                    else x[u][j].load(xr[j], k, p.K);
-                }
-            }
-            if (!decltype(any)::value && k0 + (U / PAIR - 1) * (NW * SLICE) + SLICE > p.K) {
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int k = k0 + u / PAIR * (NW * SLICE) + g * (8 * PAIR) + u % PAIR * 8;
-                    w[u].settle(k, p.K);
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) x[u][j].settle(k, p.K);
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int j = 0; j < NB; ++j) acc[j] = mfma(w[u], x[u][j], acc[j]);
-        }
-    };
-    if (p.K >= 8) walk(std::false_type());
-    else walk(std::true_type());
-#pragma unroll
-    for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4*>(&red[wave][j * 16 + l16][g * 4]) = acc[j];
+    for (int j = 0; j < NB; ++j) *reinterpret_cast<f32x4*>(&red[wave][j * 16 + l16][g * 4]) = acc[0][j];
     float part[PER] = {};
 #pragma unroll
     for (int i = 0; i < PER; ++i) {
@@ -819,15 +865,14 @@ template <typename T>
 void narrow(const Rows& q, const void* v, int K, const void* m, const Drop& drop, float* out, hipStream_t st)
 {
     if (!q.count) return;
-    constexpr int U = sizeof(T) == 2 ? 8 : 4;
     const int tiles = (q.count + 15) / 16;
     auto launch = [&](auto kernel, int waves, int slots) { hipLaunchKernelGGL(kernel, dim3(tiles, slots), dim3(waves * 64), 0, st, q, (const T*)v, K, (const T*)m, drop, out); };
-    // few rows: each of a tile's adapters in a workgroup of its own, and twice the waves
+    // few rows: each of a tile's adapters in a workgroup of its own
     const int slots = tiles < 256 ? std::max(1, std::min({16, q.adapters, (1023 + tiles) / tiles})) : 1;
-    if (q.rank <= 16) tiles <= 64 ? launch(narrow_kernel<T, 1, 16, U>, 16, slots) : launch(narrow_kernel<T, 1, 8, U>, 8, slots);
-    else if (q.rank <= 32) launch(narrow_kernel<T, 2, 8, U / 2>, 8, slots);
-    else if (q.rank <= 64) launch(narrow_kernel<T, 4, 8, U / 2>, 8, slots);
-    else launch(narrow_kernel<T, 8, 4, 2>, 4, slots);
+    if (q.rank <= 16) launch(narrow_kernel<T, 1, 8, 4>, 8, slots);
+    else if (q.rank <= 32) launch(narrow_kernel<T, 2, 8, 3>, 8, slots);
+    else if (q.rank <= 64) launch(narrow_kernel<T, 4, 8, 2>, 8, slots);
+    else launch(narrow_kernel<T, 8, 4, 1>, 4, slots);
 }
 
 template <typename T>
@@ -843,10 +888,9 @@ void wide(const Rows& q, const void* x, int K, const void* w, const float* bias,
     };
     const int cus = device_cus();
     if (tiles(64, 64) < cus / 2) {
-        constexpr int U = sizeof(T) == 2 ? 8 : 4;
-        if (q.count <= 16) { tiles(16, 16); hipLaunchKernelGGL((few_kernel<T, 1, U>), dim3(p.tiles), dim3(512), 0, st, p); }
-        else if (q.count <= 32) { tiles(16, 32); hipLaunchKernelGGL((few_kernel<T, 2, U / 2>), dim3(p.tiles), dim3(512), 0, st, p); }
-        else { tiles(16, 64); hipLaunchKernelGGL((few_kernel<T, 4, U / 2>), dim3(p.tiles), dim3(512), 0, st, p); }
+        if (q.count <= 16) { tiles(16, 16); hipLaunchKernelGGL((few_kernel<T, 1, 4>), dim3(p.tiles), dim3(512), 0, st, p); }
+        else if (q.count <= 32) { tiles(16, 32); hipLaunchKernelGGL((few_kernel<T, 2, 3>), dim3(p.tiles), dim3(512), 0, st, p); }
+        else { tiles(16, 64); hipLaunchKernelGGL((few_kernel<T, 4, 2>), dim3(p.tiles), dim3(512), 0, st, p); }
         return;
     }
     const bool dma = aligned16(x) && aligned16(w) && K * sizeof(T) % 16 == 0 && (size_t)std::max(q.count, N) * K * sizeof(T) <= NOWHERE && (size_t)K * sizeof(T) < 0x7FFFFF00u;
