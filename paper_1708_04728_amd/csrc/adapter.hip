@@ -184,7 +184,7 @@ __device__ __forceinline__ u32x4 piece(const char* p, int n)
 // ---- products of few rows or few ranks: a wave by itself ----------------------------------------------------------------------------------------
 // Rows of two matrices, A blocks of 16 of the one and B of the other, 128 bytes of a row at a time: loads in which eight lanes take a row's 128 bytes (lanes that take a row
 // each, as the matrix instructions want them, are served one row a cycle: four times as long), D slices of them in flight in registers, through the wave's own LDS,
-// in the order piece ^ (row & 7), to the operands.  Waves of a workgroup share the contraction: wave w takes slices w, w + NW, ...
+// in the order piece ^ (row / 2 & 7) (sixteen rows' pieces then lie in all 64 banks), to the operands.  Waves of a workgroup share the contraction: wave w takes slices w, w + NW, ...
 struct Piece { u32x4 v; };
 template <typename T> __device__ __forceinline__ void load_piece(Piece& e, const T* row, int k, int K)      // the row's last ones where it ends before (K >= 16 bytes)
 {
@@ -262,7 +262,7 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             if (DROP && i >= 2 * A) mask_piece(drop, place, (uint64_t)((size_t)rb(i - 2 * A) * K + k), h[i], T());
-            *reinterpret_cast<u32x4*>(lds + (i * 8 + r8) * 128 + ((c ^ r8) << 4)) = h[i].v;
+            *reinterpret_cast<u32x4*>(lds + (i * 8 + r8) * 128 + ((c ^ (r8 >> 1) ^ (i & 1) << 2) << 4)) = h[i].v;
         }
     };
 #pragma unroll
@@ -280,10 +280,10 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
             for (int t = 0; t < 2; ++t) {
                 u32x4 x[B];
 #pragma unroll
-                for (int j = 0; j < B; ++j) x[j] = *reinterpret_cast<const u32x4*>(lds + (A * 16 + j * 16 + l16) * 128 + (((t * 4 + g) ^ (l16 & 7)) << 4));
+                for (int j = 0; j < B; ++j) x[j] = *reinterpret_cast<const u32x4*>(lds + (A * 16 + j * 16 + l16) * 128 + (((t * 4 + g) ^ (l16 >> 1)) << 4));
 #pragma unroll
                 for (int i = 0; i < A; ++i) {
-                    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + (i * 16 + l16) * 128 + (((t * 4 + g) ^ (l16 & 7)) << 4));
+                    const u32x4 w = *reinterpret_cast<const u32x4*>(lds + (i * 16 + l16) * 128 + (((t * 4 + g) ^ (l16 >> 1)) << 4));
 #pragma unroll
                     for (int j = 0; j < B; ++j) acc[i][j] = mfma16<T>(w, x[j], acc[i][j]);
                 }
@@ -342,9 +342,9 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
 }
 
 // ---- the wide product: y[row][o] = sum_k W[o][k] x[row][k] + bias[o] + drop'(sum_r B_a[o][r] t[row][r]) ---------------------------------------------
-// A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  128 bytes of every row of W and x are a stage, fetched
-// while the stage before is multiplied into the other half of LDS: by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or by way of registers.  A row's
-// 16-byte pieces lie in the order piece ^ (row & 7), so that neither the writes (a row's eight pieces together) nor the reads (one piece of 32 rows) meet in a bank.
+// A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  64 bytes of every row of W and x are a stage, of which
+// LDS holds four: one that is multiplied and three on their way, by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or one by way of registers.  A
+// row's 16-byte pieces lie in the order piece ^ (row / 4 & 3): the same piece of sixteen rows is then in all 64 banks.
 template <typename T> struct Wide {
     Rows q;
     const T *x, *w, *b;
@@ -388,7 +388,7 @@ __device__ __forceinline__ void load_lds16(const u32x4& rsrc, const unsigned cha
                  ::"s"((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
 #endif
 }
-__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }      // but the last N
 // the workgroup's barrier alone, without the waits of a fence (a wave's own LDS reads have been consumed before it)
 __device__ __forceinline__ void meet()
 {
@@ -408,8 +408,8 @@ __device__ __forceinline__ u32x4 buffer_of(const void* p, size_t bytes)
 template <typename T, int WM, int WN, int MB, int NB, bool DMA, bool DROP>
 __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 {
-    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * 8 / THREADS, E = 16 / sizeof(T), STAGE_K = 8 * E;
-    __shared__ __attribute__((aligned(128))) unsigned char lds[2][(TM + TN) * 128];
+    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * 4 / THREADS, E = 16 / sizeof(T), STAGE_K = 4 * E;
+    __shared__ __attribute__((aligned(128))) unsigned char lds[4][(TM + TN) * 64];
     __shared__ int row_of[TN], id_of[TN];
     const Rows& q = p.q;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
@@ -429,22 +429,22 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     int at[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int e = threadIdx.x + i * THREADS, r = e >> 3, c = e & 7;
+        const int e = threadIdx.x + i * THREADS, r = e >> 2, c = e & 3;
         const int row = r < TM ? min(o0 + r, p.N - 1) : max(row_of[r - TM], 0);
         // (DMA: the lane's place in LDS is given, and it fetches the piece that belongs there)
-        from[i] = (decltype(from[i] + 0))((size_t)row * p.K * sizeof(T)) + (DMA ? c ^ (r & 7) : c) * 16;
-        at[i] = r * 128 + ((c ^ (r & 7)) << 4);
+        from[i] = (decltype(from[i] + 0))((size_t)row * p.K * sizeof(T)) + (DMA ? c ^ (r >> 2 & 3) : c) * 16;
+        at[i] = r * 64 + ((c ^ (r >> 2 & 3)) << 4);
     }
     const int stages = (p.K + STAGE_K - 1) / STAGE_K, whole = p.K / STAGE_K;
     u32x4 held[PIECES];
     auto fetch = [&](int s) {
-        const char *w = (const char*)p.w + (size_t)s * 128, *x = (const char*)p.x + (size_t)s * 128;
+        const char *w = (const char*)p.w + (size_t)s * 64, *x = (const char*)p.x + (size_t)s * 64;
         if (s < whole) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) held[i] = piece((i < PIECES * TM / (TM + TN) ? w : x) + from[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) held[i] = piece<T>((i < PIECES * TM / (TM + TN) ? w : x) + from[i], p.K - s * STAGE_K - (int)((threadIdx.x + i * THREADS) & 7) * E);
+            for (int i = 0; i < PIECES; ++i) held[i] = piece<T>((i < PIECES * TM / (TM + TN) ? w : x) + from[i], p.K - s * STAGE_K - (int)((threadIdx.x + i * THREADS) & 3) * E);
         }
     };
     auto put = [&](unsigned char* to) {
@@ -458,21 +458,29 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
             unsigned voff = from[i];
             if (s >= whole) {                // (the last stage, if it is no whole one)
                 const int e = threadIdx.x + i * THREADS;
-                if (s * 128 + ((e ^ (e >> 3)) & 7) * 16 >= p.K * (int)sizeof(T)) voff = NOWHERE;
+                if (s * 64 + ((e ^ (e >> 4)) & 3) * 16 >= p.K * (int)sizeof(T)) voff = NOWHERE;
             }
-            load_lds16(i < PIECES * TM / (TM + TN) ? rw : rx, to + __builtin_amdgcn_readfirstlane((wave + i * (THREADS / 64)) * 1024), voff, s * 128);
+            load_lds16(i < PIECES * TM / (TM + TN) ? rw : rx, to + __builtin_amdgcn_readfirstlane((wave + i * (THREADS / 64)) * 1024), voff, s * 64);
         }
     };
-    f32x16 acc[MB][NB] = {};
-    const int rd_m = (wm * MB * 32 + l32) * 128, rd_n = (TM + wn * NB * 32 + l32) * 128;
+    f32x16 acc[MB][NB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float from_bias = p.bias ? p.bias[min(o0 + wm * MB * 32 + i * 32 + (e >> 2) * 8 + h * 4 + (e & 3), p.N - 1)] : 0.f;
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j][e] = from_bias;
+        }
+    const int rd_m = (wm * MB * 32 + l32) * 64, rd_n = (TM + wn * NB * 32 + l32) * 64;
     // operands two steps deep: those of step k + 1 are read while step k is multiplied, the next stage's first ones behind the barrier and in front of the last step
     u32x4 a[2][MB], b[2][NB];
     auto read = [&](const unsigned char* buf, int k, int to) {
-        const int c = ((2 * k + h) ^ (l32 & 7)) << 4;
+        const int c = ((2 * k + h) ^ (l32 >> 2 & 3)) << 4;
 #pragma unroll
-        for (int i = 0; i < MB; ++i) a[to][i] = *reinterpret_cast<const u32x4*>(buf + rd_m + i * 4096 + c);
+        for (int i = 0; i < MB; ++i) a[to][i] = *reinterpret_cast<const u32x4*>(buf + rd_m + i * 2048 + c);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) b[to][j] = *reinterpret_cast<const u32x4*>(buf + rd_n + j * 4096 + c);
+        for (int j = 0; j < NB; ++j) b[to][j] = *reinterpret_cast<const u32x4*>(buf + rd_n + j * 2048 + c);
         __builtin_amdgcn_sched_barrier(0);
     };
     auto multiply = [&](int from) {
@@ -483,10 +491,11 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
         __builtin_amdgcn_sched_barrier(0);
     };
     if constexpr (DMA) {
-        stream(0, lds[0]);
-        wait_loads();
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            if (s < stages) stream(s, lds[s]);
+        wait_loads<0>();
         meet();
-        if (stages > 1) stream(1, lds[1]);
     } else {
         fetch(0);
         put(lds[0]);
@@ -495,25 +504,21 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     }
     read(lds[0], 0, 0);
     for (int s = 0; s < stages; ++s) {
-        unsigned char* const buf = lds[s & 1];
-        unsigned char* const other = lds[(s + 1) & 1];
-        read(buf, 1, 1);
-        multiply(0);
-        read(buf, 2, 0);
-        multiply(1);
-        read(buf, 3, 1);
+        unsigned char* const next = lds[(s + 1) & 3];
+        read(lds[s & 3], 1, 1);
         multiply(0);
         if constexpr (DMA) {
-            __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): nothing of this half is still to be read
-            wait_loads();
+            __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): nothing of this stage is still to be read
+            if (s + 3 < stages) wait_loads<2 * PIECES>();    // the next stage has landed, the two behind it may be on their way
+            else wait_loads<0>();
             meet();
-            if (s + 2 < stages) stream(s + 2, buf);
+            if (s + 4 < stages) stream(s + 4, lds[s & 3]);
         } else {
-            if (s + 1 < stages) put(other);
+            if (s + 1 < stages) put(next);
             __syncthreads();
             if (s + 2 < stages) fetch(s + 2);
         }
-        if (s + 1 < stages) read(other, 0, 0);
+        if (s + 1 < stages) read(next, 0, 0);
         multiply(1);
     }
 
@@ -578,30 +583,41 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
             }
         }
     }
+    // 32 rows at a time through the wave's own part of LDS, so that a store writes a row's outputs together (16 bytes of 32 rows each would take L2 a request apiece)
+    constexpr int ROW = MB * 32 * sizeof(T), IN_ROW = ROW / 16, SPREAD = ROW < 256 ? 256 / ROW : 1;
+    static_assert(WM * WN * 32 * ROW <= (int)sizeof(lds), "a wave's rows");
+    unsigned char* const mine = &lds[0][0] + wave * 32 * ROW;
+    __syncthreads();
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+    for (int j = 0; j < NB; ++j) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int o = ow + i * 32 + e * 8 + h * 4;
-            float add[4] = {};
-            if (p.bias) {
+        for (int i = 0; i < MB; ++i)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) add[c] = p.bias[min(o + c, p.N - 1)];
-            }
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                if (row[j] < 0) continue;
-                T* to = p.y + (size_t)row[j] * p.N + o;
+            for (int e = 0; e < 4; ++e) {
                 float v[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = acc[i][j][e * 4 + c] + add[c];
-                if (o + 4 <= p.N) store4(to, v);
-                else
+                for (int c = 0; c < 4; ++c) v[c] = acc[i][j][e * 4 + c];
+                const int in = (i * 32 + e * 8 + h * 4) * (int)sizeof(T);
+                store4(reinterpret_cast<T*>(mine + l32 * ROW + (((in >> 4) ^ (l32 / SPREAD & (IN_ROW - 1))) << 4) + (in & 15)), v);
+            }
+        asm volatile("" ::: "memory");              // (the wave's own LDS, written and read in order)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
-                        if (o + c < p.N) Store<T>::st(to + c, v[c]);
+        for (int k = 0; k < 32 * IN_ROW / 64; ++k) {
+            const int e = lane + k * 64, r = e / IN_ROW, c = e % IN_ROW, o = ow + c * E, to_row = row_of[(wn * NB + j) * 32 + r];
+            const u32x4 v = *reinterpret_cast<const u32x4*>(mine + r * ROW + ((c ^ (r / SPREAD & (IN_ROW - 1))) << 4));
+            if (to_row < 0) continue;
+            T* to = p.y + (size_t)to_row * p.N + o;
+            if (o + E <= p.N) *reinterpret_cast<u32x4_any*>(to) = v;
+            else {
+                T part[E];
+                __builtin_memcpy(part, &v, 16);
+#pragma unroll
+                for (int u = 0; u < E; ++u)
+                    if (o + u < p.N) to[u] = part[u];
             }
         }
+        asm volatile("" ::: "memory");
+    }
 }
 
 // ---- the wide product of few rows ---------------------------------------------------------------------------------------------------------------
