@@ -342,9 +342,9 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
 }
 
 // ---- the wide product: y[row][o] = sum_k W[o][k] x[row][k] + bias[o] + drop'(sum_r B_a[o][r] t[row][r]) ---------------------------------------------
-// A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  64 bytes of every row of W and x are a stage, of which
-// LDS holds four: one that is multiplied and three on their way, by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or one by way of registers.  A
-// row's 16-byte pieces lie in the order piece ^ (row / 4 & 3): the same piece of sixteen rows is then in all 64 banks.
+// A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  PB pieces of 16 bytes of every row of W and x are a
+// stage, of which LDS holds NS: one that is multiplied and others on their way, by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or one by way of
+// registers.  A row's pieces lie in the order piece ^ (row PB / 16): the same piece of sixteen rows is then in all 64 banks.
 template <typename T> struct Wide {
     Rows q;
     const T *x, *w, *b;
@@ -405,11 +405,12 @@ __device__ __forceinline__ u32x4 buffer_of(const void* p, size_t bytes)
                  (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00020000u};
 }
 
-template <typename T, int WM, int WN, int MB, int NB, bool DMA, bool DROP>
+template <typename T, int WM, int WN, int MB, int NB, int PB, int NS, bool DMA, bool DROP>
 __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 {
-    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * 4 / THREADS, E = 16 / sizeof(T), STAGE_K = 4 * E;
-    __shared__ __attribute__((aligned(128))) unsigned char lds[4][(TM + TN) * 64];
+    constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * PB / THREADS, E = 16 / sizeof(T), STAGE_K = PB * E;
+    constexpr int PITCH = PB * 16, WITH = 16 / PB;        // bytes of a row; rows to all 64 banks
+    __shared__ __attribute__((aligned(128))) unsigned char lds[NS][(TM + TN) * PITCH];
     __shared__ int row_of[TN], id_of[TN];
     const Rows& q = p.q;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
@@ -429,22 +430,22 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     int at[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int e = threadIdx.x + i * THREADS, r = e >> 2, c = e & 3;
+        const int e = threadIdx.x + i * THREADS, r = e / PB, c = e % PB;
         const int row = r < TM ? min(o0 + r, p.N - 1) : max(row_of[r - TM], 0);
         // (DMA: the lane's place in LDS is given, and it fetches the piece that belongs there)
-        from[i] = (decltype(from[i] + 0))((size_t)row * p.K * sizeof(T)) + (DMA ? c ^ (r >> 2 & 3) : c) * 16;
-        at[i] = r * 64 + ((c ^ (r >> 2 & 3)) << 4);
+        from[i] = (decltype(from[i] + 0))((size_t)row * p.K * sizeof(T)) + (DMA ? c ^ (r / WITH & (PB - 1)) : c) * 16;
+        at[i] = r * PITCH + ((c ^ (r / WITH & (PB - 1))) << 4);
     }
     const int stages = (p.K + STAGE_K - 1) / STAGE_K, whole = p.K / STAGE_K;
     u32x4 held[PIECES];
     auto fetch = [&](int s) {
-        const char *w = (const char*)p.w + (size_t)s * 64, *x = (const char*)p.x + (size_t)s * 64;
+        const char *w = (const char*)p.w + (size_t)s * PITCH, *x = (const char*)p.x + (size_t)s * PITCH;
         if (s < whole) {
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) held[i] = piece((i < PIECES * TM / (TM + TN) ? w : x) + from[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) held[i] = piece<T>((i < PIECES * TM / (TM + TN) ? w : x) + from[i], p.K - s * STAGE_K - (int)((threadIdx.x + i * THREADS) & 3) * E);
+            for (int i = 0; i < PIECES; ++i) held[i] = piece<T>((i < PIECES * TM / (TM + TN) ? w : x) + from[i], p.K - s * STAGE_K - (int)((threadIdx.x + i * THREADS) % PB) * E);
         }
     };
     auto put = [&](unsigned char* to) {
@@ -458,9 +459,9 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
             unsigned voff = from[i];
             if (s >= whole) {                // (the last stage, if it is no whole one)
                 const int e = threadIdx.x + i * THREADS;
-                if (s * 64 + ((e ^ (e >> 4)) & 3) * 16 >= p.K * (int)sizeof(T)) voff = NOWHERE;
+                if (s * PITCH + ((e ^ (e / PB / WITH)) & (PB - 1)) * 16 >= p.K * (int)sizeof(T)) voff = NOWHERE;
             }
-            load_lds16(i < PIECES * TM / (TM + TN) ? rw : rx, to + __builtin_amdgcn_readfirstlane((wave + i * (THREADS / 64)) * 1024), voff, s * 64);
+            load_lds16(i < PIECES * TM / (TM + TN) ? rw : rx, to + __builtin_amdgcn_readfirstlane((wave + i * (THREADS / 64)) * 1024), voff, s * PITCH);
         }
     };
     f32x16 acc[MB][NB];
@@ -472,15 +473,15 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 #pragma unroll
             for (int j = 0; j < NB; ++j) acc[i][j][e] = from_bias;
         }
-    const int rd_m = (wm * MB * 32 + l32) * 64, rd_n = (TM + wn * NB * 32 + l32) * 64;
+    const int rd_m = (wm * MB * 32 + l32) * PITCH, rd_n = (TM + wn * NB * 32 + l32) * PITCH;
     // operands two steps deep: those of step k + 1 are read while step k is multiplied, the next stage's first ones behind the barrier and in front of the last step
     u32x4 a[2][MB], b[2][NB];
     auto read = [&](const unsigned char* buf, int k, int to) {
-        const int c = ((2 * k + h) ^ (l32 >> 2 & 3)) << 4;
+        const int c = ((2 * k + h) ^ (l32 / WITH & (PB - 1))) << 4;
 #pragma unroll
-        for (int i = 0; i < MB; ++i) a[to][i] = *reinterpret_cast<const u32x4*>(buf + rd_m + i * 2048 + c);
+        for (int i = 0; i < MB; ++i) a[to][i] = *reinterpret_cast<const u32x4*>(buf + rd_m + i * 32 * PITCH + c);
 #pragma unroll
-        for (int j = 0; j < NB; ++j) b[to][j] = *reinterpret_cast<const u32x4*>(buf + rd_n + j * 2048 + c);
+        for (int j = 0; j < NB; ++j) b[to][j] = *reinterpret_cast<const u32x4*>(buf + rd_n + j * 32 * PITCH + c);
         __builtin_amdgcn_sched_barrier(0);
     };
     auto multiply = [&](int from) {
@@ -492,7 +493,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     };
     if constexpr (DMA) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
+        for (int s = 0; s < NS; ++s)
             if (s < stages) stream(s, lds[s]);
         wait_loads<0>();
         meet();
@@ -504,15 +505,18 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     }
     read(lds[0], 0, 0);
     for (int s = 0; s < stages; ++s) {
-        unsigned char* const next = lds[(s + 1) & 3];
-        read(lds[s & 3], 1, 1);
-        multiply(0);
+        unsigned char *const here = lds[s % NS], *const next = lds[(s + 1) % NS];
+#pragma unroll
+        for (int k = 0; k < PB / 2 - 1; ++k) {
+            read(here, k + 1, (k + 1) & 1);
+            multiply(k & 1);
+        }
         if constexpr (DMA) {
             __builtin_amdgcn_s_waitcnt(0xC07F);            // lgkmcnt(0): nothing of this stage is still to be read
-            if (s + 3 < stages) wait_loads<2 * PIECES>();    // the next stage has landed, the two behind it may be on their way
+            if (s + NS - 1 < stages) wait_loads<(NS - 2) * PIECES>();    // the next stage has landed, those behind it may be on their way
             else wait_loads<0>();
             meet();
-            if (s + 4 < stages) stream(s + 4, lds[s & 3]);
+            if (s + NS < stages) stream(s + NS, here);
         } else {
             if (s + 1 < stages) put(next);
             __syncthreads();
@@ -912,9 +916,9 @@ void wide(const Rows& q, const void* x, int K, const void* w, const float* bias,
     const bool dma = aligned16(x) && aligned16(w) && K * sizeof(T) % 16 == 0 && (size_t)std::max(q.count, N) * K * sizeof(T) <= NOWHERE && (size_t)K * sizeof(T) < 0x7FFFFF00u;
     auto run = [&](auto dma, auto masked) {
         constexpr bool DMA = decltype(dma)::value, DROP = decltype(masked)::value;
-        if (tiles(256, 256) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 4, 4, 2, DMA, DROP>), dim3(p.tiles), dim3(512), 0, st, p);
-        else if (tiles(128, 128) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 2, 2, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
-        else if (tiles(64, 64)) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 1, 1, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
+        if (tiles(256, 256) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 4, 4, 2, 8, 2, DMA, DROP>), dim3(p.tiles), dim3(512), 0, st, p);
+        else if (tiles(128, 128) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 2, 2, 8, 2, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
+        else if (tiles(64, 64)) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 1, 1, 8, 4, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
     };
     auto run_masked = [&](auto masked) { dma ? run(std::true_type(), masked) : run(std::false_type(), masked); };
     drop.border ? run_masked(std::true_type()) : run_masked(std::false_type());
