@@ -97,21 +97,17 @@ __device__ __forceinline__ f32x4 mfma(const Operand<float>& a, const Operand<flo
     return c;
 }
 
-// Which of the eight elements from `first` on dropout keeps: sets the others to zero (what is kept is scaled where the sums are, exactly)
+// Which of the eight elements from `first` on dropout keeps, a bit each; sets the others to zero (what is kept is scaled where the sums are, exactly)
 template <typename T>
-__device__ __forceinline__ void mask8(const Drop& d, uint64_t place, uint64_t first, Operand<T>& v)
+__device__ __forceinline__ unsigned mask8(const Drop& d, uint64_t place, uint64_t first, Operand<T>& v)
 {
-    if ((first & 7) == 0) {
-        uint32_t r[4];
-        philox(d.seed, first >> 3, place, r);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v.keep(j, drop_draw(r, j) >= d.border);
-        return;
-    }
-    const unsigned bits = (kept8(d, place, first >> 3) | kept8(d, place, (first >> 3) + 1) << 8) >> (first & 7);
+    unsigned bits = kept8(d, place, first >> 3);
+    if (first & 7) bits = ((bits | kept8(d, place, (first >> 3) + 1) << 8) >> (first & 7)) & 0xFFu;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v.keep(j, bits >> j & 1);
+    return bits;
 }
+
 // Which row is at a position, and its adapter.  Positions walk the images in `order` (NULL: as they come).
 struct Rows {
     int count, hw;               // rows; pixels of an image
@@ -128,37 +124,122 @@ struct Rows {
     }
 };
 
-// ---- order of the images by adapter ---------------------------------------------------------------------------------------------------------
-// Workgroup a writes the images of adapter a (the last one those without) in the order in which they come: first how many belong before them, then which they are.
-__global__ __launch_bounds__(1024) void order_kernel(const int* __restrict__ ids, int n, int adapters, int* __restrict__ order, int* __restrict__ starts)
+// ---- what the products start from: the order of the images by adapter, and transposed copies ------------------------------------------------------
+// Order: workgroup a writes the images of adapter a (the last one those without) in the order in which they come: first how many belong before them, then which they
+// are.  A wave takes a quarter of the ids, four of a lane at a time.
+// Copies: src[batch][R][C] -> dst[batch][C][R], 64 x 64 elements a workgroup.
+struct Copy { const void* src; void* dst; int R, C, tiles_r, tiles_c, first, last; };      // workgroups first .. last - 1
+struct Prepare {
+    const int* ids;
+    int n, adapters, orders;     // orders: workgroups of the order (0: none)
+    int *order, *starts;
+    Copy copy[3];
+};
+__device__ __forceinline__ void put_in_order(const Prepare& p, int a, int* red)
 {
-    __shared__ int red[16];
-    const int a = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    auto key = [&](int i) { const int id = ids[i]; return (unsigned)id < (unsigned)adapters ? id : adapters; };
-    int before = 0;
-    for (int i = threadIdx.x; i < n; i += 1024) before += key(i) < a;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int share = ((p.n + 1023) / 1024) * 256, lo = min(wave * share, p.n), hi = min(lo + share, p.n);
+    constexpr int AHEAD = 8;     // runs of 256 ids whose loads are in flight together
+    auto load = [&](int i0, int (&key)[AHEAD][4]) {
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) before += __shfl_xor(before, d, 64);
-    if (lane == 0) red[wave] = before;
-    __syncthreads();
-    int base = 0;
-    for (int w = 0; w < 16; ++w) base += red[w];
-    if (threadIdx.x == 0) starts[a] = base;
-    if (a == adapters && threadIdx.x == 0) starts[a + 1] = n;
-    for (int i0 = 0; i0 < n; i0 += 1024) {
-        const int i = i0 + threadIdx.x;
-        const bool mine = i < n && key(i) == a;
-        const unsigned long long set = __ballot(mine);
-        __syncthreads();
-        if (lane == 0) red[wave] = __popcll(set);
-        __syncthreads();
-        int at = base;
-        for (int w = 0; w < 16; ++w) {
-            at += w < wave ? red[w] : 0;
-            base += red[w];
-        }
-        if (mine) order[at + __popcll(set & ((1ull << lane) - 1))] = i;
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) key[u][j] = p.ids[min(i0 + u * 256 + lane * 4 + j, p.n - 1)];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) key[u][j] = i0 + u * 256 + lane * 4 + j < hi ? min((unsigned)key[u][j], (unsigned)p.adapters) : 0x7FFFFFFF;
+    };
+    int before = 0, own = 0;
+    for (int i0 = lo; i0 < hi; i0 += AHEAD * 256) {
+        int key[AHEAD][4];
+        load(i0, key);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                before += key[u][j] < a;
+                own += key[u][j] == a;
+            }
     }
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) {
+        before += __shfl_xor(before, d, 64);
+        own += __shfl_xor(own, d, 64);
+    }
+    if (lane == 0) {
+        red[wave] = before;
+        red[4 + wave] = own;
+    }
+    __syncthreads();
+    const int base = red[0] + red[1] + red[2] + red[3];
+    if (threadIdx.x == 0) {
+        p.starts[a] = base;
+        if (a == p.adapters) p.starts[a + 1] = p.n;
+    }
+    int at = base;
+    for (int w = 0; w < wave; ++w) at += red[4 + w];
+    if (red[4 + wave] == 0) return;
+    const unsigned long long below = (1ull << lane) - 1;
+    for (int i0 = lo; i0 < hi; i0 += AHEAD * 256) {
+        int key[AHEAD][4];
+        load(i0, key);
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            int mine = at;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned long long set = __ballot(key[u][j] == a);
+                mine += __popcll(set & below);
+                at += __popcll(set);
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (key[u][j] == a) p.order[mine++] = i0 + u * 256 + lane * 4 + j;
+        }
+    }
+}
+template <typename T>
+__global__ __launch_bounds__(256) void prepare_kernel(const Prepare p)
+{
+    constexpr int E = 16 / sizeof(T);
+    constexpr int PITCH = 64 + 4 / (int)sizeof(T);           // an odd number of words: a column is in as many banks as it has rows
+    __shared__ __attribute__((aligned(16))) T tile[64][PITCH];
+    __shared__ int red[8];
+    const int block = blockIdx.x;
+    if (block < p.orders) return put_in_order(p, block, red);
+    const int which = block < p.copy[0].last ? 0 : block < p.copy[1].last ? 1 : 2;
+    auto of = [&](auto field) { return which == 0 ? p.copy[0].*field : which == 1 ? p.copy[1].*field : p.copy[2].*field; };
+    const Copy c = {of(&Copy::src), of(&Copy::dst), of(&Copy::R), of(&Copy::C), of(&Copy::tiles_r), of(&Copy::tiles_c), of(&Copy::first), 0};
+    const int i = block - c.first, per = c.tiles_r * c.tiles_c, b = i / per, j = i - b * per, r0 = j / c.tiles_c * 64, c0 = (j - j / c.tiles_c * c.tiles_c) * 64;
+    const T* src = (const T*)c.src + (size_t)b * c.R * c.C;
+    T* dst = (T*)c.dst + (size_t)b * c.R * c.C;
+    if (r0 + 64 <= c.R && c0 + 64 <= c.C) {
+#pragma unroll
+        for (int k = 0; k < 16 / E; ++k) {
+            const int e = threadIdx.x + k * 256, r = e / (64 / E), o = e % (64 / E) * E;
+            const u32x4 v = *reinterpret_cast<const u32x4_any*>(src + (size_t)(r0 + r) * c.C + c0 + o);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) reinterpret_cast<unsigned*>(&tile[r][o])[u] = v[u];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < 16 / E; ++k) {
+            const int e = threadIdx.x + k * 256, r = e / (64 / E), o = e % (64 / E) * E;
+            T v[E];
+#pragma unroll
+            for (int u = 0; u < E; ++u) v[u] = tile[o + u][r];
+            u32x4 w;
+            __builtin_memcpy(&w, v, 16);
+            *reinterpret_cast<u32x4_any*>(dst + (size_t)(c0 + r) * c.R + r0 + o) = w;
+        }
+        return;
+    }
+    for (int e = threadIdx.x; e < 4096; e += 256)
+        if (r0 + e / 64 < c.R && c0 + e % 64 < c.C) tile[e / 64][e % 64] = src[(size_t)(r0 + e / 64) * c.C + c0 + e % 64];
+    __syncthreads();
+    for (int e = threadIdx.x; e < 4096; e += 256)
+        if (c0 + e / 64 < c.C && r0 + e % 64 < c.R) dst[(size_t)(c0 + e / 64) * c.R + r0 + e % 64] = tile[e % 64][e / 64];
 }
 
 // 16 bytes of a row, of which `n` elements exist (zeros behind them)
@@ -351,6 +432,7 @@ template <typename T> struct Wide {
     const float *bias, *t;
     int K, N;
     Drop drop;
+    const uint8_t* bits;         // drop's mask, if the sums over rows have left it, or NULL
     T* y;
     int tiles_n, tiles;          // tiles of rows; all tiles
 };
@@ -384,8 +466,9 @@ __device__ __forceinline__ void tile_of(int block, int tiles, int tiles_n, int* 
 __device__ __forceinline__ void load_lds16(const u32x4& rsrc, const unsigned char* lds, unsigned voff, unsigned soff)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 ::"s"((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory", "m0");
+    unsigned m0;                 // (put back: the compiler may hold something in it)
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "s"((unsigned)(uintptr_t)(__attribute__((address_space(3))) const unsigned char*)lds), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
 #endif
 }
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }      // but the last N
@@ -405,7 +488,8 @@ __device__ __forceinline__ u32x4 buffer_of(const void* p, size_t bytes)
                  (unsigned)__builtin_amdgcn_readfirstlane((unsigned)bytes), 0x00020000u};
 }
 
-template <typename T, int WM, int WN, int MB, int NB, int PB, int NS, bool DMA, bool DROP>
+enum { NO_MASK = 0, MASK_DRAWN = 1, MASK_BITS = 2 };
+template <typename T, int WM, int WN, int MB, int NB, int PB, int NS, bool DMA, int DROP>
 __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 {
     constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * PB / THREADS, E = 16 / sizeof(T), STAGE_K = PB * E;
@@ -534,7 +618,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
         id[j] = id_of[(wn * NB + j) * 32 + l32];
     }
     const int ow = o0 + wm * MB * 32;
-    const uint64_t place = DROP ? drop_place(p.drop) : 0;
+    const uint64_t place = DROP == MASK_DRAWN ? drop_place(p.drop) : 0;
     const float scale = DROP ? p.drop.scale : 1.f;
     for (int a = -1;;) {
         int next = 0x7FFFFFFF;
@@ -571,8 +655,14 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
                     // this lane's row of the block: outputs 16 h .. 16 h + 15, the others from the lane that holds the same row
                     unsigned keep = 0xFFFFFFFFu;
                     if constexpr (DROP) {
-                        const unsigned own = kept16(p.drop, place, (uint64_t)((size_t)max(row[j], 0) * p.N + ow + i * 32 + h * 16)), other = __shfl_xor(own, 32, 64);
-                        keep = h ? own << 16 | other : other << 16 | own;
+                        const size_t from = (size_t)max(row[j], 0) * p.N + min(ow + i * 32, p.N - 1);
+                        if constexpr (DROP == MASK_BITS) {
+                            typedef unsigned int u32_any __attribute__((aligned(1)));
+                            keep = *reinterpret_cast<const u32_any*>(p.bits + (from >> 3));
+                        } else {
+                            const unsigned own = kept16(p.drop, place, from + h * 16), other = __shfl_xor(own, 32, 64);
+                            keep = h ? own << 16 | other : other << 16 | own;
+                        }
                         keep >>= h * 4;
                     }
                     f32x16 part = {};          // of its own: rows of other adapters must not meet this one's numbers, not even times zero
@@ -703,28 +793,21 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
     }
 }
 
-// ---- transposed copies: src[batch][R][C] -> dst[batch][C][R] --------------------------------------------------------------------------------------
-template <typename T>
-__global__ __launch_bounds__(256) void transpose_kernel(const T* __restrict__ src, T* __restrict__ dst, int R, int C, int tiles_r, int tiles_c)
-{
-    __shared__ T tile[32][33];
-    const int b = blockIdx.x / (tiles_r * tiles_c), i = blockIdx.x - b * (tiles_r * tiles_c), r0 = i / tiles_c * 32, c0 = (i - i / tiles_c * tiles_c) * 32;
-    const int l = threadIdx.x & 31, h = threadIdx.x >> 5;
-    for (int k = h; k < 32; k += 8)
-        if (r0 + k < R && c0 + l < C) tile[k][l] = src[((size_t)b * R + r0 + k) * C + c0 + l];
-    __syncthreads();
-    for (int k = h; k < 32; k += 8)
-        if (c0 + k < C && r0 + l < R) dst[((size_t)b * C + c0 + k) * R + r0 + l] = tile[l][k];
-}
-
 // ---- sums over the rows of an adapter: out[a][r][c] (or [a][c][r]) = sum f[row][r] drop(v[row][c]) ---------------------------------------------------
 // A workgroup takes `length` positions, 512 bytes of columns (a quarter of them a wave) and up to 64 of the rank, and the adapters among those positions one after the other: a segment each.  Both
 // operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into two pieces.  A segment that is all of its
 // adapter is the result; others are partial sums, that of chunk k and adapter a in slot k + a (one of the two grows from a segment to the next), added in their order after.
-struct Sums {
-    int C, length;
-    int ranks_last;              // out[a][c][r]
+struct Sum {
+    const void* v;
+    const float* f;
+    int C, ranks_last;           // ranks_last: out[a][c][r]
+    Drop drop;                   // (of the first part)
+    uint8_t* bits;               // which elements of v's rows were kept, a bit each, for the wide product (C % 8 == 0), or NULL
     float *out, *partial;        // partial: [slot][rank][C] in the order of out
+};
+struct Sums {                    // of x and of dy, in one launch
+    Sum part[2];
+    int length, blocks;          // blocks of columns of the first part
 };
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
@@ -739,7 +822,7 @@ __device__ __forceinline__ u32x2 read_transposed(const unsigned char* p)
 }
 
 template <typename T, int RB>
-__global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums s, const T* __restrict__ v, const float* __restrict__ f, const Drop drop)
+__global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums both)
 {
     constexpr bool BF = sizeof(T) == 2;
     constexpr int UNITS = 512 / (8 * sizeof(T)), PER = 32 * UNITS / 256, CB = 512 / sizeof(T) / 64, FB = 32 * RB * 16, F_PER = FB / 256, WINDOW = 256;
@@ -747,7 +830,16 @@ __global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums s, c
     __shared__ __attribute__((aligned(128))) unsigned char ft[2][FB * 4];          // bf16: upper pieces, then lower ones
     __shared__ int rows_of[WINDOW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-    const int c0 = blockIdx.x * (512 / (int)sizeof(T)), chunk = blockIdx.y, p0 = chunk * s.length, p1 = min(p0 + s.length, q.count), r0 = blockIdx.z * 64;
+    const bool second = (int)blockIdx.x >= both.blocks;
+    auto of = [&](auto field) { return second ? both.part[1].*field : both.part[0].*field; };
+    Sum s;
+    s.C = of(&Sum::C); s.ranks_last = of(&Sum::ranks_last); s.bits = of(&Sum::bits); s.out = of(&Sum::out); s.partial = of(&Sum::partial);
+    const T* const __restrict__ v = (const T*)of(&Sum::v);
+    const float* const __restrict__ f = of(&Sum::f);
+    Drop drop = both.part[0].drop;           // (dy is not dropped)
+    if (second) drop.border = 0;
+    const int c0 = (blockIdx.x - ((int)blockIdx.x >= both.blocks ? both.blocks : 0)) * (512 / (int)sizeof(T)), chunk = blockIdx.y, p0 = chunk * both.length;
+    const int p1 = min(p0 + both.length, q.count), r0 = blockIdx.z * 64;
     const uint64_t place = drop.border ? drop_place(drop) : 0;
     const float scale = drop.border ? drop.scale : 1.f;
     // 32-byte pieces of a row lie in the order piece ^ turn(row), so that the rows that one read takes do not meet in a bank
@@ -775,7 +867,11 @@ __global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums s, c
             const int e = threadIdx.x + i * 256, r = e / UNITS, u = e % UNITS;
             if (s.C >= 8 && c0 + 512 / (int)sizeof(T) > s.C) held[i].settle(c0 + u * 8, s.C);
             if (rows_of[st * 32 + r] < 0) held[i].clear();
-            if (drop.border) mask8(drop, place, (uint64_t)((size_t)max(rows_of[st * 32 + r], 0) * s.C + c0 + u * 8), held[i]);
+            if (drop.border) {
+                const int row = rows_of[st * 32 + r], c = c0 + u * 8;
+                const unsigned bits = mask8(drop, place, (uint64_t)((size_t)max(row, 0) * s.C + c), held[i]);
+                if (s.bits && r0 == 0 && row >= 0 && c < s.C) s.bits[((size_t)row * s.C + c) >> 3] = (uint8_t)bits;
+            }
             unsigned char* at = xt[to] + r * 512;
             if constexpr (BF) *reinterpret_cast<u32x4*>(at + ((u >> 1) ^ turn(r)) * 32 + (u & 1) * 16) = held[i].v;
             else {
@@ -864,19 +960,32 @@ __global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums s, c
         p = end;
     }
 }
-// Adapters whose rows lie in several chunks, and zeros for those without rows: `groups` workgroups for each adapter
-__global__ __launch_bounds__(256) void join_kernel(const Rows q, const Sums s, int groups)
+// Adapters whose rows lie in several chunks, and zeros for those without rows: `groups` workgroups for each adapter of each part
+__global__ __launch_bounds__(256) void join_kernel(const Rows q, const Sums both, int groups)
 {
+    const Sum& s = both.part[blockIdx.y];
+    if (!s.out) return;
     const int a = blockIdx.x / groups, group = blockIdx.x - a * groups;
     const long long begin = (long long)q.starts[a] * q.hw, end = (long long)q.starts[a + 1] * q.hw;
-    const int first = (int)(begin / s.length), last = (int)((end - 1) / s.length);
+    const int first = (int)(begin / both.length), last = (int)((end - 1) / both.length);
     if (end > begin && first == last) return;
     const size_t count = (size_t)q.rank * s.C;
-    for (size_t i = group * 256u + threadIdx.x; i < count; i += groups * 256u) {
-        float sum = 0.f;
-        if (end > begin)
-            for (int k = first; k <= last; ++k) sum += s.partial[(size_t)(k + a) * count + i];
-        s.out[a * count + i] = sum;
+    for (size_t i = (group * 256u + threadIdx.x) * 4; i < count; i += groups * 1024u) {
+        float sum[4] = {};
+        const int n = (int)min(count - i, (size_t)4);
+        if (end > begin && n == 4) {
+#pragma unroll 8
+            for (int k = first; k <= last; ++k) {
+                const f32x4 v = *reinterpret_cast<const f32x4_any*>(s.partial + (size_t)(k + a) * count + i);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += v[e];
+            }
+        } else if (end > begin)
+            for (int k = first; k <= last; ++k)
+                for (int e = 0; e < n; ++e) sum[e] += s.partial[(size_t)(k + a) * count + i + e];
+        if (n == 4) store4(s.out + a * count + i, sum);
+        else
+            for (int e = 0; e < n; ++e) s.out[a * count + i + e] = sum[e];
     }
 }
 
@@ -896,10 +1005,12 @@ void narrow(const Rows& q, const void* v, int K, const void* m, const Drop& drop
 }
 
 template <typename T>
-void wide(const Rows& q, const void* x, int K, const void* w, const float* bias, const float* t, const void* b, int N, const Drop& drop, void* y, hipStream_t st)
+void wide(const Rows& q, const void* x, int K, const void* w, const float* bias, const float* t, const void* b, int N, const Drop& drop, const uint8_t* bits,
+          void* y, hipStream_t st)
 {
     if (!q.count) return;
     Wide<T> p;
+    p.bits = bits;
     p.q = q; p.x = (const T*)x; p.w = (const T*)w; p.b = (const T*)b; p.bias = bias; p.t = t; p.K = K; p.N = N; p.drop = drop; p.y = (T*)y;
     auto tiles = [&](int tm, int tn) {
         p.tiles_n = (q.count + tn - 1) / tn;
@@ -915,73 +1026,65 @@ void wide(const Rows& q, const void* x, int K, const void* w, const float* bias,
     }
     const bool dma = aligned16(x) && aligned16(w) && K * sizeof(T) % 16 == 0 && (size_t)std::max(q.count, N) * K * sizeof(T) <= NOWHERE && (size_t)K * sizeof(T) < 0x7FFFFF00u;
     auto run = [&](auto dma, auto masked) {
-        constexpr bool DMA = decltype(dma)::value, DROP = decltype(masked)::value;
+        constexpr bool DMA = decltype(dma)::value;
+        constexpr int DROP = decltype(masked)::value;
         if (tiles(256, 256) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 4, 4, 2, 8, 2, DMA, DROP>), dim3(p.tiles), dim3(512), 0, st, p);
         else if (tiles(128, 128) >= cus) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 2, 2, 8, 2, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
         else if (tiles(64, 64)) hipLaunchKernelGGL((tiled_kernel<T, 2, 2, 1, 1, 8, 4, DMA, DROP>), dim3(p.tiles), dim3(256), 0, st, p);
     };
     auto run_masked = [&](auto masked) { dma ? run(std::true_type(), masked) : run(std::false_type(), masked); };
-    drop.border ? run_masked(std::true_type()) : run_masked(std::false_type());
+    if (!drop.border) run_masked(std::integral_constant<int, NO_MASK>());
+    else if (bits) run_masked(std::integral_constant<int, MASK_BITS>());
+    else run_masked(std::integral_constant<int, MASK_DRAWN>());
 }
 
-template <typename T>
-void transpose(const void* src, void* dst, int batch, int R, int C, hipStream_t st)
+constexpr int columns_of(int dtype) { return 512 / (dtype == DR_BF16 ? 2 : 4); }
+// positions that a workgroup of the sums over rows takes: four workgroups for every compute unit, of 32 rows and more, up to 2048 chunks
+int length_of(const AdapterShape& p)
 {
-    const int tr = (R + 31) / 32, tc = (C + 31) / 32;
-    if (batch) hipLaunchKernelGGL((transpose_kernel<T>), dim3((unsigned)batch * tr * tc), dim3(256), 0, st, (const T*)src, (T*)dst, R, C, tr, tc);
-}
-
-// positions that a workgroup of the sums over rows takes: two workgroups for every compute unit, of 32 rows and more, up to 2048 chunks
-int length_of(int rows, int columns, int dtype)
-{
-    const int per = 512 / (int)elem_size(dtype), blocks = (columns + per - 1) / per, chunks = std::max(1, 512 / blocks);
+    const int rows = p.images * p.hw, per = columns_of(p.dtype), blocks = (p.in + per - 1) / per + (p.out + per - 1) / per, chunks = std::max(1, 1024 / blocks);
     return (int)align_up(std::max({(rows + chunks - 1) / chunks, (rows + 2047) / 2048, 1}), 32);
 }
-size_t slots_of(const AdapterShape& p, int columns)
+size_t slots_of(const AdapterShape& p)
 {
-    const int rows = p.images * p.hw, length = length_of(rows, columns, p.dtype);
+    const int rows = p.images * p.hw, length = length_of(p);
     return (size_t)(rows + length - 1) / length + p.adapters;
 }
 
-template <typename T, int RB>
-void sum_rows(const Rows& q, const Sums& s, const void* v, const float* f, const Drop& drop, hipStream_t st)
+template <typename T>
+void sum_rows(const Rows& q, const Sums& s, hipStream_t st)
 {
     constexpr int COLUMNS = 512 / sizeof(T);
-    hipLaunchKernelGGL((sums_kernel<T, RB>), dim3((s.C + COLUMNS - 1) / COLUMNS, (q.count + s.length - 1) / s.length, (q.rank + 63) / 64), dim3(256), 0, st, q, s, (const T*)v, f,
-                       drop);
-}
-template <typename T>
-void sum_rows(const Rows& q, const void* v, const float* f, int C, const Drop& drop, int ranks_last, float* out, float* partial, hipStream_t st)
-{
-    Sums s;
-    s.C = C; s.ranks_last = ranks_last; s.out = out; s.partial = partial;
-    s.length = length_of(q.count, C, sizeof(T) == 2 ? DR_BF16 : DR_F32);
+    auto blocks = [&](int i) { return s.part[i].out ? (s.part[i].C + COLUMNS - 1) / COLUMNS : 0; };
+    const dim3 grid(blocks(0) + blocks(1), (q.count + s.length - 1) / s.length, (q.rank + 63) / 64);
     if (q.count) {
-        if (q.rank <= 16) sum_rows<T, 1>(q, s, v, f, drop, st);
-        else if (q.rank <= 32) sum_rows<T, 2>(q, s, v, f, drop, st);
-        else sum_rows<T, 4>(q, s, v, f, drop, st);
+        if (q.rank <= 16) hipLaunchKernelGGL((sums_kernel<T, 1>), grid, dim3(256), 0, st, q, s);
+        else if (q.rank <= 32) hipLaunchKernelGGL((sums_kernel<T, 2>), grid, dim3(256), 0, st, q, s);
+        else hipLaunchKernelGGL((sums_kernel<T, 4>), grid, dim3(256), 0, st, q, s);
     }
-    const int groups = (int)std::min<size_t>(64, ((size_t)q.rank * C + 1023) / 1024);
-    hipLaunchKernelGGL(join_kernel, dim3((unsigned)(q.adapters * groups)), dim3(256), 0, st, q, s, groups);
+    const int groups = (int)std::min<size_t>(64, ((size_t)q.rank * std::max(s.part[0].C, s.part[1].C) + 1023) / 1024);
+    hipLaunchKernelGGL(join_kernel, dim3((unsigned)(q.adapters * groups), 2), dim3(256), 0, st, q, s, groups);
 }
 
 struct Scratch {                 // places in the workspace
-    size_t order, starts, inner, wt, at, bt, partial, bytes;
+    size_t order, starts, inner, wt, at, bt, partial[2], bits, bytes;
 };
 Scratch scratch_of(const AdapterShape& p, bool backward)
 {
     Scratch s = {};
     size_t at = 0;
     auto take = [&](size_t bytes) { const size_t here = at; at += align_up(bytes, 256); return here; };
-    const size_t el = elem_size(p.dtype), factors = (size_t)p.adapters * p.rank;
+    const size_t el = elem_size(p.dtype), factors = (size_t)p.adapters * p.rank, rows = (size_t)p.images * p.hw;
     s.order = take((size_t)p.images * 4);
     s.starts = take(((size_t)p.adapters + 2) * 4);
-    s.inner = take((size_t)p.images * p.hw * p.rank * 4);
+    s.inner = take(rows * p.rank * 4);
     if (backward) {
         s.wt = take((size_t)p.in * p.out * el);
         s.at = take(factors * p.in * el);
         s.bt = take(factors * p.out * el);
-        s.partial = take((size_t)p.rank * std::max(slots_of(p, p.in) * p.in, slots_of(p, p.out) * p.out) * 4);
+        s.partial[0] = take((size_t)p.rank * slots_of(p) * p.in * 4);
+        s.partial[1] = take((size_t)p.rank * slots_of(p) * p.out * 4);
+        s.bits = take(p.in % 8 == 0 ? rows * p.in / 8 + 64 : 0);         // (words that begin in the last row's bytes)
     }
     s.bytes = at;
     return s;
@@ -997,9 +1100,18 @@ Rows rows_of(const AdapterShape& p, const AdapterArgs& g, char* ws, const Scratc
     return q;
 }
 
-void put_in_order(const AdapterShape& p, const AdapterArgs& g, char* ws, const Scratch& s, hipStream_t st)
+Prepare ordering(const AdapterShape& p, const AdapterArgs& g, char* ws, const Scratch& s)
 {
-    hipLaunchKernelGGL(order_kernel, dim3(p.adapters + 1), dim3(1024), 0, st, g.ids, p.images, p.adapters, (int*)(ws + s.order), (int*)(ws + s.starts));
+    Prepare r = {};
+    r.ids = g.ids; r.n = p.images; r.adapters = p.adapters; r.orders = p.adapters + 1;
+    r.order = (int*)(ws + s.order); r.starts = (int*)(ws + s.starts);
+    for (Copy& c : r.copy) c.first = c.last = r.orders;
+    return r;
+}
+template <typename T>
+void prepare(const Prepare& r, hipStream_t st)
+{
+    hipLaunchKernelGGL((prepare_kernel<T>), dim3(r.copy[2].last), dim3(256), 0, st, r);
 }
 
 template <typename T>
@@ -1007,11 +1119,11 @@ void forward(const AdapterShape& p, const AdapterArgs& g, const void* x, void* y
 {
     const Scratch s = scratch_of(p, false);
     const bool sorted = p.images > 64 && p.hw < 64 && p.adapters > 1;      // few images, or images as long as a tile: as they come
-    if (sorted) put_in_order(p, g, ws, s, st);
+    if (sorted) prepare<T>(ordering(p, g, ws, s), st);
     const Rows q = rows_of(p, g, ws, s, sorted);
     float* t = inner ? inner : (float*)(ws + s.inner);
     if (p.adapters || inner) narrow<T>(q, x, p.in, g.a, drop, t, st);
-    wide<T>(q, x, p.in, g.w, g.bias, t, g.b, p.out, make_drop(0.f, 0, 0, nullptr), y, st);
+    wide<T>(q, x, p.in, g.w, g.bias, t, g.b, p.out, make_drop(0.f, 0, 0, nullptr), nullptr, y, st);
 }
 
 template <typename T>
@@ -1020,20 +1132,36 @@ void backward(const AdapterShape& p, const AdapterArgs& g, const void* dy, const
 {
     const Scratch s = scratch_of(p, true);
     const Drop none = make_drop(0.f, 0, 0, nullptr);
-    put_in_order(p, g, ws, s, st);
+    Prepare r = ordering(p, g, ws, s);
+    if (p.images == 0) r.n = 0;
+    int copies = 0, first = r.orders;
+    auto copy = [&](const void* src, size_t dst, int batch, int R, int C) {
+        Copy& c = r.copy[copies++];
+        c.src = src; c.dst = ws + dst; c.R = R; c.C = C;
+        c.tiles_r = (R + 63) / 64; c.tiles_c = (C + 63) / 64;
+        c.first = first;
+        for (int i = copies - 1; i < 3; ++i) r.copy[i].last = first + batch * c.tiles_r * c.tiles_c;
+        first = c.last;
+    };
+    if (p.images) {
+        if (p.adapters && (dx || da)) copy(g.b, s.bt, p.adapters, p.out, p.rank);
+        if (dx) copy(g.w, s.wt, 1, p.out, p.in);
+        if (p.adapters && dx) copy(g.a, s.at, p.adapters, p.rank, p.in);
+    }
+    prepare<T>(r, st);
     const Rows q = rows_of(p, g, ws, s, true);
     float* u = (float*)(ws + s.inner);
-    if (p.adapters && (dx || da)) {
-        transpose<T>(g.b, ws + s.bt, p.adapters, p.out, p.rank, st);
-        narrow<T>(q, dy, p.out, ws + s.bt, none, u, st);
+    if (p.adapters && (dx || da)) narrow<T>(q, dy, p.out, ws + s.bt, none, u, st);
+    uint8_t* bits = drop.border && p.adapters && da && dx && p.in % 8 == 0 ? (uint8_t*)(ws + s.bits) : nullptr;
+    if (p.adapters && (da || db)) {
+        Sums both = {};
+        both.part[0] = Sum{x, u, p.in, 0, drop, bits, da, (float*)(ws + s.partial[0])};
+        both.part[1] = Sum{dy, inner, p.out, 1, none, nullptr, db, (float*)(ws + s.partial[1])};
+        both.length = length_of(p);
+        both.blocks = da ? (p.in + columns_of(p.dtype) - 1) / columns_of(p.dtype) : 0;
+        sum_rows<T>(q, both, st);
     }
-    if (dx) {
-        transpose<T>(g.w, ws + s.wt, 1, p.out, p.in, st);
-        transpose<T>(g.a, ws + s.at, p.adapters, p.rank, p.in, st);
-        wide<T>(q, dy, p.out, ws + s.wt, nullptr, u, ws + s.at, p.in, drop, dx, st);
-    }
-    if (p.adapters && da) sum_rows<T>(q, x, u, p.in, drop, 0, da, (float*)(ws + s.partial), st);
-    if (p.adapters && db) sum_rows<T>(q, dy, inner, p.out, none, 1, db, (float*)(ws + s.partial), st);
+    if (dx) wide<T>(q, dy, p.out, ws + s.wt, nullptr, u, ws + s.at, p.in, drop, bits, dx, st);
 }
 
 long long product_bytes(const AdapterShape& p, bool backward)

@@ -28,7 +28,11 @@ __device__ __forceinline__ u32x4 pack8(const float (&v)[8])
     return t;
 }
 
-__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) { unpack8(*reinterpret_cast<const u32x4_any*>(p), v); }
+__device__ __forceinline__ void load8(const uint16_t* p, float (&v)[8]) 
+{
+    const u32x4 t = *reinterpret_cast<const u32x4_any*>(p);
+    unpack8(t, v);
+}
 __device__ __forceinline__ void load8(const float* p, float (&v)[8])
 {
     const f32x4 a = *reinterpret_cast<const f32x4_any*>(p), b = *reinterpret_cast<const f32x4_any*>(p + 4);
