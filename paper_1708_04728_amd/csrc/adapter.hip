@@ -496,8 +496,9 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     constexpr int PITCH = PB * 16, WITH = 16 / PB;        // bytes of a row; rows to all 64 banks
     __shared__ __attribute__((aligned(128))) unsigned char lds[NS][(TM + TN) * PITCH];
     __shared__ int row_of[TN], id_of[TN];
+    __shared__ __attribute__((aligned(16))) float bias_of[TM];
     const Rows& q = p.q;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5, wm = wave % WM, wn = wave / WM;
     int tm, tn;
     tile_of(blockIdx.x, p.tiles, p.tiles_n, &tm, &tn);
     const int o0 = tm * TM, p0 = tn * TN;
@@ -507,6 +508,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
         row_of[i] = row;
         id_of[i] = id;
     }
+    for (int i = threadIdx.x; i < TM; i += THREADS) bias_of[i] = p.bias ? p.bias[min(o0 + i, p.N - 1)] : 0.f;
     __syncthreads();
 
     // this thread's pieces of a stage: row and piece are the same in every stage.  Rows that do not exist repeat one that does: what comes of them is not stored
@@ -545,7 +547,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
                 const int e = threadIdx.x + i * THREADS;
                 if (s * PITCH + ((e ^ (e / PB / WITH)) & (PB - 1)) * 16 >= p.K * (int)sizeof(T)) voff = NOWHERE;
             }
-            load_lds16(i < PIECES * TM / (TM + TN) ? rw : rx, to + __builtin_amdgcn_readfirstlane((wave + i * (THREADS / 64)) * 1024), voff, s * PITCH);
+            load_lds16(i < PIECES * TM / (TM + TN) ? rw : rx, to + (wave + i * (THREADS / 64)) * 1024, voff, s * PITCH);
         }
     };
     f32x16 acc[MB][NB];
@@ -553,7 +555,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            const float from_bias = p.bias ? p.bias[min(o0 + wm * MB * 32 + i * 32 + (e >> 2) * 8 + h * 4 + (e & 3), p.N - 1)] : 0.f;
+            const float from_bias = bias_of[(wm * MB + i) * 32 + (e >> 2) * 8 + h * 4 + (e & 3)];
 #pragma unroll
             for (int j = 0; j < NB; ++j) acc[i][j][e] = from_bias;
         }
