@@ -642,18 +642,14 @@ def muon_step(params, ws, lr, momentum=0.95, weight_decay=0.0, steps=5, coeffici
 
 def _on_device(*ts):
     """Refuses tensors that are not on the current device (None: nothing is passed)."""
-    current = -1
+    current = None
     for t in ts:
-        if t is None:
-            continue
-        if isinstance(t, NHWC):
-            t = t.t
-        if not t.is_cuda:
-            raise ValueError("tensors of a call lie on the current device")
-        if current < 0:
-            current = torch.cuda.current_device() if _device is None else _device()
-        if t.get_device() != current:
-            raise ValueError("tensors of a call lie on the current device")
+        if t is not None:
+            device = t.get_device()                      # (-1: the host)
+            if device != current:
+                if current is not None or device < 0 or device != (torch.cuda.current_device() if _device is None else _device()):
+                    raise ValueError("tensors of a call lie on the current device")
+                current = device
 
 
 def dropout_desc(p, seed, offset=0, step=None):
@@ -724,84 +720,112 @@ def softmax_loss_grad(z, labels, dz, loss, ws, smoothing=0.0, mean=True, row_los
     return dz
 
 
-def _adapted(x, a, b):
-    """dr_tensor of x, a (rows, channels) or NHWC tensor, and dr_adapters of the adapters a (count, rank, c_in), b (count, c_out, rank)."""
-    if isinstance(x, NHWC):
-        n, h, w, c = x.t.shape
-        t, layout = x.t, DR_NHWC
+# what the shapes of a call's tensors come to: dr_tensor of the input, dr_adapters, dr_tensor of the output, images, pixels
+_adapter_shapes = {}
+
+
+def _adapted(x, a, b, y=None, w=None):
+    """(dr_tensor, dr_adapters, dr_tensor of y or None, images, pixels) of x, a (rows, channels) or NHWC tensor, the adapters a (count, rank, c_in), b (count, c_out, rank), the
+    output y and the projection w, and x's plain tensor."""
+    maps = x.__class__ is NHWC
+    tx, ty = x.t if maps else x, y.t if y.__class__ is NHWC else y
+    dtype = tx.dtype
+    if dtype not in _DTYPES or a.dtype is not dtype or b.dtype is not dtype:
+        raise TypeError("input, projection and adapters share a dtype, fp32 or bf16")
+    if not (tx.is_contiguous() and a.is_contiguous() and b.is_contiguous()):
+        raise ValueError("tensor must be contiguous")
+    if ty is not None:
+        if ty.dtype is not dtype or (y.__class__ is NHWC) is not maps:
+            raise ValueError("the output has the input's pixels, order and dtype and c_out channels")
+        if not ty.is_contiguous():
+            raise ValueError("tensor must be contiguous")
+    if w is not None and (w.dtype is not dtype or not w.is_contiguous()):
+        raise ValueError("the projection is a contiguous (c_out, c_in) tensor of the input's dtype")
+    key = (maps, dtype, tx.shape, a.shape, b.shape, None if ty is None else ty.shape, None if w is None else w.shape)
+    got = _adapter_shapes.get(key)
+    if got is None:
+        if len(_adapter_shapes) > 1000:
+            _adapter_shapes.clear()
+        got = _adapter_shapes[key] = _adapter_shape(maps, tx, a, b, ty, w)
+    return got, tx, ty
+
+
+def _adapter_shape(maps, x, a, b, y, w):
+    if maps:
+        n, h, wd, c = x.shape
     elif x.dim() == 2:
-        (n, c), h, w = x.shape, 1, 1
-        t, layout = x, DR_NCHW
+        (n, c), h, wd = x.shape, 1, 1
     else:
         raise ValueError("adapters take (rows, channels) or NHWC tensors")
     if a.dim() != 3 or b.dim() != 3 or a.shape[0] != b.shape[0] or a.shape[1] != b.shape[2]:
         raise ValueError("adapters are (count, rank, c_in) and (count, c_out, rank)")
-    if a.dtype is not t.dtype or b.dtype is not t.dtype:
-        raise TypeError("input, projection and adapters share a dtype")
-    if not (t.is_contiguous() and a.is_contiguous() and b.is_contiguous()):
-        raise ValueError("tensor must be contiguous")
-    if max(t.numel(), a.numel(), b.numel()) > _MOST_ELEMENTS:
-        raise ValueError(_TOO_MANY)
     count, rank, cin = a.shape
-    return dr_tensor(n, c, h, w, _dtype_code(t), layout), dr_adapters(count, rank, cin, b.shape[1])
-
-
-def _projected(xd, ad, x, y, w):
-    """dr_tensor of the projection's output y; checks w."""
-    if w is not None and (w.dtype is not x.dtype or tuple(w.shape) not in ((ad.c_out, ad.c_in), (ad.c_out, ad.c_in, 1, 1)) or not w.is_contiguous()):
+    cout = b.shape[1]
+    if w is not None and tuple(w.shape) not in ((cout, cin), (cout, cin, 1, 1)):
         raise ValueError("the projection is a contiguous (c_out, c_in) tensor of the input's dtype")
-    t = y.t if isinstance(y, NHWC) else y
-    if isinstance(y, NHWC) is not (xd.layout == DR_NHWC) or t.dtype is not x.dtype or tuple(t.shape) != ((xd.n, xd.h, xd.w, ad.c_out) if xd.layout == DR_NHWC else (xd.n, ad.c_out)):
+    if y is not None and tuple(y.shape) != ((n, h, wd, cout) if maps else (n, cout)):
         raise ValueError("the output has the input's pixels, order and dtype and c_out channels")
-    if not t.is_contiguous():
-        raise ValueError("tensor must be contiguous")
-    if t.numel() > _MOST_ELEMENTS:
+    if max(t.numel() for t in (x, a, b, y, w) if t is not None) > _MOST_ELEMENTS:
         raise ValueError(_TOO_MANY)
-    return dr_tensor(xd.n, ad.c_out, xd.h, xd.w, xd.dtype, xd.layout)
+    layout, code = (DR_NHWC if maps else DR_NCHW), _dtype_code(x)
+    return dr_tensor(n, c, h, wd, code, layout), dr_adapters(count, rank, cin, cout), dr_tensor(n, cout, h, wd, code, layout), n, n * h * wd
+
+
+_FLOATS = "bias, scales, inner, da and db are contiguous fp32 tensors: entries per output channel, per adapter, rank entries per pixel, and the adapters' shapes"
+
+
+def _floats(t, n):
+    """Pointer of a contiguous fp32 tensor of n entries (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous():
+        raise ValueError(_FLOATS)
+    return t.data_ptr()
 
 
 def adapter_fwd_workspace_bytes(x, a, b):
     n = C.c_size_t(0)
-    _check(lib().dr_adapter_fwd_workspace_bytes(*_adapted(x, a, b), C.byref(n)))
+    (xd, ad, *_), _, _ = _adapted(x, a, b)
+    _check(lib().dr_adapter_fwd_workspace_bytes(xd, ad, C.byref(n)))
     return n.value
 
 
 def adapter_fwd(x, w, bias, a, b, ids, y, ws, scales=None, drop=None, inner=None, stream=None):
     """y = projection w (c_out, c_in) of x plus bias plus the adapter b[ids] a[ids] of every image (or row) of x; an id outside the adapters adds nothing.  x: (rows, c_in) or
     NHWC; ids: int32, one per row or image; scales: fp32 per adapter; drop: dropout_desc(...) of what the adapters read; inner: fp32, rank values per pixel, for adapter_bwd."""
-    xd, ad = _adapted(x, a, b)
-    yd = _projected(xd, ad, x, y, w)
     if w is None:
         raise ValueError("no projection")
-    for t, n in ((bias, ad.c_out), (scales, ad.count), (inner, xd.n * xd.h * xd.w * ad.rank)):
-        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
-            raise ValueError("bias, scales and inner are contiguous fp32 tensors: entries per output channel, per adapter, and rank entries per pixel")
-    _on_device(x, w, bias, a, b, ids, y, ws, scales, inner)
-    _check(lib().dr_adapter_fwd(xd, _ptr(x), ad, w.data_ptr(), _ptr(bias), a.data_ptr(), b.data_ptr(), _ptr(scales), _ints(ids, xd.n, "ids"), drop, yd, _ptr(y), _ptr(inner),
-                                _ptr(ws), _nbytes(ws), _stream(stream)))
+    (xd, ad, yd, images, pixels), tx, ty = _adapted(x, a, b, y, w)
+    pbias, pscales, pinner, pids = _floats(bias, ad.c_out), _floats(scales, ad.count), _floats(inner, pixels * ad.rank), _ints(ids, images, "ids")
+    _on_device(tx, w, bias, a, b, ids, ty, ws, scales, inner)
+    rc = lib().dr_adapter_fwd(xd, tx.data_ptr(), ad, w.data_ptr(), pbias, a.data_ptr(), b.data_ptr(), pscales, pids, drop, yd, ty.data_ptr(), pinner, _ptr(ws), _nbytes(ws),
+                              _stream(stream))
+    if rc:
+        _check(rc)
     return y
 
 
 def adapter_bwd_workspace_bytes(x, a, b):
     n = C.c_size_t(0)
-    _check(lib().dr_adapter_bwd_workspace_bytes(*_adapted(x, a, b), C.byref(n)))
+    (xd, ad, *_), _, _ = _adapted(x, a, b)
+    _check(lib().dr_adapter_bwd_workspace_bytes(xd, ad, C.byref(n)))
     return n.value
 
 
 def adapter_bwd(dy, x, w, a, b, ids, inner, dx, da, db, ws, scales=None, drop=None, stream=None):
     """dx (like x), da, db (fp32, like a and b; each of the three may be None) from dy and the forward pass's x, ids, inner and dropout."""
-    xd, ad = _adapted(x, a, b)
-    yd = _projected(xd, ad, x, dy, w)
+    (xd, ad, yd, images, pixels), tx, tdy = _adapted(x, a, b, dy, w)
+    tdx = None
     if dx is not None:
-        t, u = (v.t if isinstance(v, NHWC) else v for v in (x, dx))
-        if isinstance(x, NHWC) is not isinstance(dx, NHWC) or t.dtype is not u.dtype or t.shape != u.shape or not u.is_contiguous():
+        tdx = dx.t if dx.__class__ is NHWC else dx
+        if dx.__class__ is not x.__class__ and NHWC in (dx.__class__, x.__class__) or tdx.dtype is not tx.dtype or tdx.shape != tx.shape or not tdx.is_contiguous():
             raise ValueError("dx has the input's shape, order and dtype and is contiguous")
-    for t, n in ((scales, ad.count), (inner, xd.n * xd.h * xd.w * ad.rank), (da, a.numel()), (db, b.numel())):
-        if t is not None and (t.dtype is not torch.float32 or t.numel() != n or not t.is_contiguous()):
-            raise ValueError("scales, inner, da and db are contiguous fp32 tensors: entries per adapter, rank entries per pixel, and the adapters' shapes")
-    _on_device(dy, x, w, a, b, ids, inner, dx, da, db, ws, scales)
-    _check(lib().dr_adapter_bwd(yd, _ptr(dy), xd, _ptr(x), ad, _ptr(w), a.data_ptr(), b.data_ptr(), _ptr(scales), _ints(ids, xd.n, "ids"), drop, _ptr(inner), _ptr(dx), _ptr(da),
-                                _ptr(db), _ptr(ws), _nbytes(ws), _stream(stream)))
+    pscales, pinner, pda, pdb, pids = _floats(scales, ad.count), _floats(inner, pixels * ad.rank), _floats(da, a.numel()), _floats(db, b.numel()), _ints(ids, images, "ids")
+    _on_device(tdy, tx, w, a, b, ids, inner, tdx, da, db, ws, scales)
+    rc = lib().dr_adapter_bwd(yd, tdy.data_ptr(), xd, tx.data_ptr(), ad, _ptr(w), a.data_ptr(), b.data_ptr(), pscales, pids, drop, pinner, _ptr(tdx), pda, pdb, _ptr(ws),
+                              _nbytes(ws), _stream(stream))
+    if rc:
+        _check(rc)
     return dx, da, db
 
 

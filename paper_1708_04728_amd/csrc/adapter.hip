@@ -24,6 +24,18 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// Eight 16-bit elements, of which those without a bit become zero (their bits times 0 or 1)
+__device__ __forceinline__ void keep_halves(u32x4& v, unsigned bits)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned two = bits >> (2 * i) & 3, word = v[i], times = (two | two << 15) & 0x00010001u;      // (a cast of v[i] itself would read v[0])
+        const u16x2 kept = __builtin_bit_cast(u16x2, word) * __builtin_bit_cast(u16x2, times);
+        v[i] = __builtin_bit_cast(unsigned, kept);
+    }
+}
+
 // Eight elements of an operand's row, as the matrix instructions take them.  A lane of group g = lane / 16 holds elements 8 g .. 8 g + 7 of a slice of 32: one
 // instruction in bf16, eight in fp32 (the j-th of them multiplies the j-th elements of the four groups).
 // load(row, k, K) reads elements k .. k + 7 of a row of K >= 8, or its last eight where it ends before, which settle() then moves to their places, with zeros behind
@@ -49,10 +61,7 @@ template <> struct Operand<uint16_t> {
         for (int i = 0; i < 4; ++i) v[i] = (k + 2 * i < K ? row[k + 2 * i] : 0u) | (k + 2 * i + 1 < K ? (unsigned)row[k + 2 * i + 1] << 16 : 0u);
     }
     __device__ __forceinline__ void clear() { v = u32x4{0, 0, 0, 0}; }
-    __device__ __forceinline__ void keep(int j, bool yes)
-    {
-        if (!yes) v[j >> 1] &= j & 1 ? 0xFFFFu : 0xFFFF0000u;
-    }
+    __device__ __forceinline__ void keep(unsigned bits) { keep_halves(v, bits); }
     __device__ __forceinline__ void values(float (&e)[8]) const { unpack8(v, e); }
 };
 template <> struct Operand<float> {
@@ -79,9 +88,10 @@ template <> struct Operand<float> {
         for (int i = 0; i < 8; ++i) v[i >> 2][i & 3] = k + i < K ? row[k + i] : 0.f;
     }
     __device__ __forceinline__ void clear() { v[0] = v[1] = f32x4{0.f, 0.f, 0.f, 0.f}; }
-    __device__ __forceinline__ void keep(int j, bool yes)
+    __device__ __forceinline__ void keep(unsigned bits)
     {
-        if (!yes) v[j >> 2][j & 3] = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j >> 2][j & 3] = bits >> j & 1 ? v[j >> 2][j & 3] : 0.f;
     }
     __device__ __forceinline__ void values(float (&e)[8]) const
     {
@@ -97,15 +107,11 @@ __device__ __forceinline__ f32x4 mfma(const Operand<float>& a, const Operand<flo
     return c;
 }
 
-// Which of the eight elements from `first` on dropout keeps, a bit each; sets the others to zero (what is kept is scaled where the sums are, exactly)
-template <typename T>
-__device__ __forceinline__ unsigned mask8(const Drop& d, uint64_t place, uint64_t first, Operand<T>& v)
+// Which of the eight elements from `first` on dropout keeps, a bit each
+__device__ __forceinline__ unsigned kept8_from(const Drop& d, uint64_t place, uint64_t first)
 {
-    unsigned bits = kept8(d, place, first >> 3);
-    if (first & 7) bits = ((bits | kept8(d, place, (first >> 3) + 1) << 8) >> (first & 7)) & 0xFFu;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v.keep(j, bits >> j & 1);
-    return bits;
+    const unsigned bits = kept8(d, place, first >> 3);
+    return first & 7 ? ((bits | kept8(d, place, (first >> 3) + 1) << 8) >> (first & 7)) & 0xFFu : bits;
 }
 
 // Which row is at a position, and its adapter.  Positions walk the images in `order` (NULL: as they come).
@@ -289,10 +295,8 @@ template <typename T> __device__ __forceinline__ void settle_piece(Piece& e, int
 // Which elements of the piece that starts at element `first` dropout keeps: sets the others to zero (what is kept is scaled where the sums are, exactly)
 __device__ __forceinline__ void mask_piece(const Drop& d, uint64_t place, uint64_t first, Piece& e, uint16_t)
 {
-    unsigned bits = kept8(d, place, first >> 3);
-    if (first & 7) bits = (bits | kept8(d, place, (first >> 3) + 1) << 8) >> (first & 7);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) e.v[i] &= (bits >> (2 * i) & 1 ? 0xFFFFu : 0u) | (bits >> (2 * i + 1) & 1 ? 0xFFFF0000u : 0u);
+    const unsigned bits = kept8_from(d, place, first);
+    keep_halves(e.v, bits);
 }
 __device__ __forceinline__ void mask_piece(const Drop& d, uint64_t place, uint64_t first, Piece& e, float)
 {
@@ -824,7 +828,7 @@ __device__ __forceinline__ u32x2 read_transposed(const unsigned char* p)
 }
 
 template <typename T, int RB>
-__global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums both)
+__global__ __launch_bounds__(256, RB == 1 ? 4 : 1) void sums_kernel(const Rows q, const Sums both)
 {
     constexpr bool BF = sizeof(T) == 2;
     constexpr int UNITS = 512 / (8 * sizeof(T)), PER = 32 * UNITS / 256, CB = 512 / sizeof(T) / 64, FB = 32 * RB * 16, F_PER = FB / 256, WINDOW = 256;
@@ -847,8 +851,9 @@ __global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums both
     // 32-byte pieces of a row lie in the order piece ^ turn(row), so that the rows that one read takes do not meet in a bank
     auto turn = [](int row) { return ((row & 3) | ((row >> 1) & 4)) << (BF ? 0 : 1); };
     Operand<T> held[PER];
+    unsigned kept[PER];
     float heldf[F_PER];
-    auto fetch = [&](int st) {
+    auto fetch = [&](int st) {               // (masks are drawn while the loads are on their way)
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
             const int e = threadIdx.x + i * 256, row = rows_of[st * 32 + e / UNITS], c = c0 + (e % UNITS) * 8;
@@ -862,6 +867,14 @@ __global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums both
             const float e = f[(size_t)max(row, 0) * q.rank + min(r, q.rank - 1)];
             heldf[i] = row >= 0 && r < q.rank ? e : 0.f;
         }
+        if (drop.border) {
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                const int e = threadIdx.x + i * 256, row = rows_of[st * 32 + e / UNITS], c = c0 + (e % UNITS) * 8;
+                kept[i] = kept8_from(drop, place, (uint64_t)((size_t)max(row, 0) * s.C + c));
+                if (s.bits && r0 == 0 && row >= 0 && c < s.C) s.bits[((size_t)row * s.C + c) >> 3] = (uint8_t)kept[i];
+            }
+        }
     };
     auto put = [&](int st, int to) {
 #pragma unroll
@@ -869,11 +882,7 @@ __global__ __launch_bounds__(256) void sums_kernel(const Rows q, const Sums both
             const int e = threadIdx.x + i * 256, r = e / UNITS, u = e % UNITS;
             if (s.C >= 8 && c0 + 512 / (int)sizeof(T) > s.C) held[i].settle(c0 + u * 8, s.C);
             if (rows_of[st * 32 + r] < 0) held[i].clear();
-            if (drop.border) {
-                const int row = rows_of[st * 32 + r], c = c0 + u * 8;
-                const unsigned bits = mask8(drop, place, (uint64_t)((size_t)max(row, 0) * s.C + c), held[i]);
-                if (s.bits && r0 == 0 && row >= 0 && c < s.C) s.bits[((size_t)row * s.C + c) >> 3] = (uint8_t)bits;
-            }
+            if (drop.border) held[i].keep(kept[i]);
             unsigned char* at = xt[to] + r * 512;
             if constexpr (BF) *reinterpret_cast<u32x4*>(at + ((u >> 1) ^ turn(r)) * 32 + (u & 1) * 16) = held[i].v;
             else {

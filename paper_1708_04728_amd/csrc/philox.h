@@ -59,15 +59,26 @@ DR_ANY unsigned drop_draw(const uint32_t (&r)[4], int j) { return j & 1 ? r[j >>
 #if defined(__HIPCC__)
 __device__ __forceinline__ uint64_t drop_place(const Drop& d) { return d.offset + (d.step ? *d.step : 0); }
 
-// Which of a block's elements are kept: bit j for element 8 block + j
-__device__ __forceinline__ unsigned kept8(const Drop& d, uint64_t place, uint64_t block)
+// Which of a block's elements are kept: 1 or 0 in the half of a word that held the element's draw (border >= 1)
+__device__ __forceinline__ void kept_halves(const Drop& d, uint64_t place, uint64_t block, uint32_t (&m)[4])
 {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
     uint32_t r[4];
     philox(d.seed, block, place, r);
-    unsigned bits = 0;
+    const unsigned short last = (unsigned short)(d.border - 1);          // the last draw that is dropped
 #pragma unroll
-    for (int j = 0; j < 8; ++j) bits |= drop_draw(r, j) >= d.border ? 1u << j : 0u;
-    return bits;
+    for (int i = 0; i < 4; ++i) {
+        const u16x2 beyond = __builtin_elementwise_sub_sat(__builtin_bit_cast(u16x2, r[i]), u16x2{last, last});
+        m[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_min(beyond, u16x2{1, 1}));
+    }
+}
+// ... bit j for element 8 block + j
+__device__ __forceinline__ unsigned kept8(const Drop& d, uint64_t place, uint64_t block)
+{
+    uint32_t m[4];
+    kept_halves(d, place, block, m);
+    const unsigned t = m[0] | m[1] << 2 | m[2] << 4 | m[3] << 6;         // even elements in bits 0, 2, .., odd ones in 16, 18, ..
+    return (t | t >> 15) & 0xFFu;
 }
 // ... of sixteen from any `first` on
 __device__ __forceinline__ unsigned kept16(const Drop& d, uint64_t place, uint64_t first)

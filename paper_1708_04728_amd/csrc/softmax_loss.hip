@@ -14,16 +14,8 @@ namespace {
 
 constexpr int COUNT_ROWS = 2048;         // most labels that every workgroup counts for itself
 
-// exp(d) for d <= 0 to about one unit in the last place: d log2(e) in two parts, the lower one after the exponential.  -inf gives 0, a NaN stays one.
-__device__ __forceinline__ float exp_of(float d)
-{
-    constexpr float L2E = 1.44269502162933349609375f, LOW = 1.92596299112661746887e-8f, LN2 = 0.693147180559945f;
-    d = d < -200.f ? -200.f : d;
-    const float t = d * L2E;
-    const float r = __builtin_fmaf(d, L2E, -t) + d * LOW;
-    const float e = __builtin_amdgcn_exp2f(t);
-    return __builtin_fmaf(e, r * LN2, e);
-}
+// exp(d) for d <= 0: off by |d| 2^-24 of itself, as much as the rounding of d = z - top is, which is below e^-d d 2^-24 of the sum.  -inf gives 0, a NaN stays one.
+__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * 1.44269502162933349609375f); }
 
 template <int THREADS, class F>
 __device__ __forceinline__ float reduce(float v, float* red, F f)
@@ -85,7 +77,7 @@ __device__ __forceinline__ float row_loss_of(const Loss& q, const RowSums& s, fl
 
 // PER lanes a row, NV blocks of eight elements a lane; workgroups of max(PER, 256) threads walk the rows
 template <typename T, int PER, int NV>
-__global__ __launch_bounds__(PER < 256 ? 256 : PER) void loss_kernel(const Loss q, const T* z, T* dz)
+__global__ __launch_bounds__(PER < 256 ? 256 : PER, 4) void loss_kernel(const Loss q, const T* z, T* dz)
 {
     constexpr int THREADS = PER < 256 ? 256 : PER, TEAMS = THREADS / PER;
     __shared__ float red[16];
@@ -154,7 +146,11 @@ __global__ __launch_bounds__(PER < 256 ? 256 : PER) void loss_kernel(const Loss 
             for (int i = 0; i < NV; ++i) {
                 const int c = start(i);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * scale - (c + j == label ? less + at_label : less);
+                for (int j = 0; j < 8; ++j) v[i][j] = __builtin_fmaf(v[i][j], scale, -less);
+                if ((unsigned)(label - c) < 8u) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[i][j] -= c + j == label ? at_label : 0.f;
+                }
                 if ((i * PER + lane) * 8 < q.C) store8(dz + (size_t)row * q.C + c, v[i]);
             }
         }
@@ -288,7 +284,7 @@ void launch(const Loss& q, const void* z, void* dz, hipStream_t st)
     else if (q.C <= 2048) launch_rows<T, 256, 1>(q, z, dz, st);
     else if (q.C <= 4096) launch_rows<T, 256, 2>(q, z, dz, st);
     else if (q.C <= 8192) launch_rows<T, 256, 4>(q, z, dz, st);
-    else if (q.C <= 16384) launch_rows<T, 1024, 2>(q, z, dz, st);
+    else if (q.C <= 16384) launch_rows<T, 512, 4>(q, z, dz, st);
     else if (q.C <= 32768) launch_rows<T, 1024, 4>(q, z, dz, st);
     else if (q.C <= 65536) launch_rows<T, 1024, 8>(q, z, dz, st);
     else hipLaunchKernelGGL((loss_long_kernel<T>), dim3(std::min(q.rows, 4096)), dim3(1024), 0, st, q, (const T*)z, (T*)dz);
