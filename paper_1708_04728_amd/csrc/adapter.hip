@@ -801,7 +801,8 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
 
 // ---- sums over the rows of an adapter: out[a][r][c] (or [a][c][r]) = sum f[row][r] drop(v[row][c]) ---------------------------------------------------
 // A workgroup takes `length` positions, 512 bytes of columns (a quarter of them a wave) and up to 64 of the rank, and the adapters among those positions one after the other: a segment each.  Both
-// operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into two pieces.  A segment that is all of its
+// operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into three
+// pieces (all its bits: the sums are fp32).  A segment that is all of its
 // adapter is the result; others are partial sums, that of chunk k and adapter a in slot k + a (one of the two grows from a segment to the next), added in their order after.
 struct Sum {
     const void* v;
@@ -833,7 +834,7 @@ __global__ __launch_bounds__(256, RB == 1 ? 4 : 1) void sums_kernel(const Rows q
     constexpr bool BF = sizeof(T) == 2;
     constexpr int UNITS = 512 / (8 * sizeof(T)), PER = 32 * UNITS / 256, CB = 512 / sizeof(T) / 64, FB = 32 * RB * 16, F_PER = FB / 256, WINDOW = 256;
     __shared__ __attribute__((aligned(128))) unsigned char xt[2][32 * 512];
-    __shared__ __attribute__((aligned(128))) unsigned char ft[2][FB * 4];          // bf16: upper pieces, then lower ones
+    __shared__ __attribute__((aligned(128))) unsigned char ft[2][FB * (BF ? 6 : 4)];          // bf16: upper pieces, then middle and lower ones
     __shared__ int rows_of[WINDOW];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
     const bool second = (int)blockIdx.x >= both.blocks;
@@ -895,8 +896,11 @@ __global__ __launch_bounds__(256, RB == 1 ? 4 : 1) void sums_kernel(const Rows q
             const int e = threadIdx.x + i * 256;
             if constexpr (BF) {
                 const uint16_t high = f32_to_bf16(heldf[i]);
+                const float rest = heldf[i] - bf16_to_f32(high);
+                const uint16_t middle = f32_to_bf16(rest);
                 reinterpret_cast<uint16_t*>(ft[to])[e] = high;
-                reinterpret_cast<uint16_t*>(ft[to])[FB + e] = f32_to_bf16(heldf[i] - bf16_to_f32(high));
+                reinterpret_cast<uint16_t*>(ft[to])[FB + e] = middle;
+                reinterpret_cast<uint16_t*>(ft[to])[2 * FB + e] = f32_to_bf16(rest - bf16_to_f32(middle));
             } else reinterpret_cast<float*>(ft[to])[e] = heldf[i];
         }
     };
@@ -931,8 +935,8 @@ __global__ __launch_bounds__(256, RB == 1 ? 4 : 1) void sums_kernel(const Rows q
 #pragma unroll
                     for (int i = 0; i < RB; ++i)
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            const unsigned char* at = fs + half * FB * 2 + row * (RB * 32) + i * 32 + (l16 & 3) * 8;
+                        for (int third = 0; third < 3; ++third) {
+                            const unsigned char* at = fs + third * FB * 2 + row * (RB * 32) + i * 32 + (l16 & 3) * 8;
                             const u32x2 lo = read_transposed(at), hi = read_transposed(at + 4 * RB * 32);
                             const u32x4 w = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
