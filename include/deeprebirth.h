@@ -292,8 +292,8 @@ int dr_dropout_fwd(const dr_tensor* d, const void* x, const dr_dropout* drop, vo
  * mean != 0: L = sum l / N and g = 1 / N over the N rows that have a label; else L = sum l, g = 1.  A label outside
  * 0 .. c - 1 is none: the row's l and dz are 0 whatever its logits (N = 0: L = 0).  Logits of -inf have probability 0; a row with
  * a label that holds a NaN, +inf or nothing but -inf becomes NaN.  labels: n device ints.  dz (may be NULL, may be z), loss: one device
- * float (may be NULL), row_loss: n device floats, the l (may be NULL).  0 <= smoothing <= 1.  ws: device scratch of at least
- * dr_softmax_loss_workspace_bytes, 256-byte aligned.  Sums are added in a fixed order. */
+ * float (may be NULL), row_loss: n device floats, the l (may be NULL).  0 <= smoothing <= 1.  n and c at most 2^30.  ws: device
+ * scratch of at least dr_softmax_loss_workspace_bytes, 256-byte aligned.  Sums are added in a fixed order. */
 int dr_softmax_loss_workspace_bytes(const dr_tensor* d, size_t* bytes);
 int dr_softmax_loss_grad(const dr_tensor* d, const void* z, const int* labels, float smoothing, int mean, void* dz, float* loss, float* row_loss, void* ws,
                          size_t ws_bytes, void* stream);
@@ -305,7 +305,9 @@ int dr_softmax_loss_grad(const dr_tensor* d, const void* z, const int* labels, f
  * 1x1), fp32 or bf16; W: c_out x c_in, A: count x rank x c_in, B: count x c_out x rank, dense, of the same type.  bias, scales: fp32,
  * c_out and count entries (NULL: zeros, ones).  ids: one device int per image of x.  drop (NULL or p = 0: none): dropout of x in
  * front of A only.  inner: fp32, rank values per pixel, that the gradient reads (NULL: not stored).  Sums, inner among them, are held in
- * fp32.  1 <= rank <= DR_MAX_ADAPTER_RANK, 0 <= count <= DR_MAX_ADAPTERS (0: A, B and ids may be NULL).  Tensors do not overlap.
+ * fp32.  1 <= rank <= DR_MAX_ADAPTER_RANK, 0 <= count <= DR_MAX_ADAPTERS (0: A, B and ids may be NULL), at most 2^26 pixels, and
+ * count times max(c_in, c_out) / 64 at most 2^22.  Tensors do not overlap.  One adapter's, pixel's or gradient's infinities and NaN reach no
+ * other's results.
  * ws: device scratch of at least dr_adapter_fwd_workspace_bytes, 256-byte aligned. */
 #define DR_MAX_ADAPTER_RANK 128
 #define DR_MAX_ADAPTERS 16384

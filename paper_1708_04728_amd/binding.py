@@ -674,7 +674,7 @@ def dropout_fwd(x, drop, y, stream=None):
     count = tx.numel()
     if count > _MOST_ELEMENTS:
         raise ValueError(_TOO_MANY)
-    _on_device(tx, ty)
+    _on_device(tx, ty, getattr(drop, "keep", None))
     _check(lib().dr_dropout_fwd(dr_tensor(1, count, 1, 1, _dtype_code(tx), DR_NCHW), tx.data_ptr(), drop, ty.data_ptr(), _stream(stream)))
     return y
 
@@ -797,7 +797,7 @@ def adapter_fwd(x, w, bias, a, b, ids, y, ws, scales=None, drop=None, inner=None
         raise ValueError("no projection")
     (xd, ad, yd, images, pixels), tx, ty = _adapted(x, a, b, y, w)
     pbias, pscales, pinner, pids = _floats(bias, ad.c_out), _floats(scales, ad.count), _floats(inner, pixels * ad.rank), _ints(ids, images, "ids")
-    _on_device(tx, w, bias, a, b, ids, ty, ws, scales, inner)
+    _on_device(tx, w, bias, a, b, ids, ty, ws, scales, inner, getattr(drop, "keep", None))
     rc = lib().dr_adapter_fwd(xd, tx.data_ptr(), ad, w.data_ptr(), pbias, a.data_ptr(), b.data_ptr(), pscales, pids, drop, yd, ty.data_ptr(), pinner, _ptr(ws), _nbytes(ws),
                               _stream(stream))
     if rc:
@@ -821,7 +821,7 @@ def adapter_bwd(dy, x, w, a, b, ids, inner, dx, da, db, ws, scales=None, drop=No
         if dx.__class__ is not x.__class__ and NHWC in (dx.__class__, x.__class__) or tdx.dtype is not tx.dtype or tdx.shape != tx.shape or not tdx.is_contiguous():
             raise ValueError("dx has the input's shape, order and dtype and is contiguous")
     pscales, pinner, pda, pdb, pids = _floats(scales, ad.count), _floats(inner, pixels * ad.rank), _floats(da, a.numel()), _floats(db, b.numel()), _ints(ids, images, "ids")
-    _on_device(tdy, tx, w, a, b, ids, inner, tdx, da, db, ws, scales)
+    _on_device(tdy, tx, w, a, b, ids, inner, tdx, da, db, ws, scales, getattr(drop, "keep", None))
     rc = lib().dr_adapter_bwd(yd, tdy.data_ptr(), xd, tx.data_ptr(), ad, _ptr(w), a.data_ptr(), b.data_ptr(), pscales, pids, drop, pinner, _ptr(tdx), pda, pdb, _ptr(ws),
                               _nbytes(ws), _stream(stream))
     if rc:

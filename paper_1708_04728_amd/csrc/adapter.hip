@@ -118,13 +118,13 @@ __device__ __forceinline__ unsigned kept8_from(const Drop& d, uint64_t place, ui
 struct Rows {
     int count, hw;               // rows; pixels of an image
     int adapters, rank;
-    const int* ids;              // of every image
+    const int* ids;              // of every image (NULL: none has an adapter)
     const int* order;
     const int* starts;           // adapter a's images are order[starts[a]] .. order[starts[a + 1] - 1] (read by the sums over rows)
     const float* scales;
     __device__ __forceinline__ int row(int p, int* id) const
     {
-        const int slot = p / hw, img = order ? order[slot] : slot, a = ids[img];
+        const int slot = p / hw, img = order ? order[slot] : slot, a = ids ? ids[img] : -1;
         *id = (unsigned)a < (unsigned)adapters ? a : -1;
         return img * hw + (p - slot * hw);
     }
@@ -273,6 +273,12 @@ __device__ __forceinline__ u32x4 piece(const char* p, int n)
 // each, as the matrix instructions want them, are served one row a cycle: four times as long), D slices of them in flight in registers, through the wave's own LDS,
 // in the order piece ^ (row / 2 & 7) (sixteen rows' pieces then lie in all 64 banks), to the operands.  Waves of a workgroup share the contraction: wave w takes slices w, w + NW, ...
 struct Piece { u32x4 v; };
+// What the wave's lanes have written to its own LDS is what they read behind this (the wave's LDS accesses run in order: nothing to wait for)
+__device__ __forceinline__ void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 template <typename T> __device__ __forceinline__ void load_piece(Piece& e, const T* row, int k, int K)      // the row's last ones where it ends before (K >= 16 bytes)
 {
     constexpr int E = 16 / sizeof(T);
@@ -359,7 +365,7 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
             const int s = s0 + d * NW;
             if (s >= slices) break;
             put(s, held[d]);
-            asm volatile("" ::: "memory");              // (the wave's own LDS, written and read in order)
+            wave_fence();
             if (s + D * NW < slices) load(s + D * NW, held[d]);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -373,7 +379,7 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
                     for (int j = 0; j < B; ++j) acc[i][j] = mfma16<T>(w, x[j], acc[i][j]);
                 }
             }
-            asm volatile("" ::: "memory");
+            wave_fence();
         }
     }
 }
@@ -700,7 +706,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
                 const int in = (i * 32 + e * 8 + h * 4) * (int)sizeof(T);
                 store4(reinterpret_cast<T*>(mine + l32 * ROW + (((in >> 4) ^ (l32 / SPREAD & (IN_ROW - 1))) << 4) + (in & 15)), v);
             }
-        asm volatile("" ::: "memory");              // (the wave's own LDS, written and read in order)
+        wave_fence();
 #pragma unroll
         for (int k = 0; k < 32 * IN_ROW / 64; ++k) {
             const int e = lane + k * 64, r = e / IN_ROW, c = e % IN_ROW, o = ow + c * E, to_row = row_of[(wn * NB + j) * 32 + r];
@@ -716,7 +722,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
                     if (o + u < p.N) to[u] = part[u];
             }
         }
-        asm volatile("" ::: "memory");
+        wave_fence();
     }
 }
 
@@ -1109,7 +1115,7 @@ Rows rows_of(const AdapterShape& p, const AdapterArgs& g, char* ws, const Scratc
 {
     Rows q;
     q.count = p.images * p.hw; q.hw = p.hw; q.adapters = p.adapters; q.rank = p.rank;
-    q.ids = g.ids; q.scales = g.scales;
+    q.ids = p.adapters ? g.ids : nullptr; q.scales = g.scales;
     q.order = sorted ? (const int*)(ws + s.order) : nullptr;
     q.starts = (const int*)(ws + s.starts);
     return q;
@@ -1126,7 +1132,7 @@ Prepare ordering(const AdapterShape& p, const AdapterArgs& g, char* ws, const Sc
 template <typename T>
 void prepare(const Prepare& r, hipStream_t st)
 {
-    hipLaunchKernelGGL((prepare_kernel<T>), dim3(r.copy[2].last), dim3(256), 0, st, r);
+    if (r.copy[2].last) hipLaunchKernelGGL((prepare_kernel<T>), dim3(r.copy[2].last), dim3(256), 0, st, r);
 }
 
 template <typename T>
@@ -1148,8 +1154,9 @@ void backward(const AdapterShape& p, const AdapterArgs& g, const void* dy, const
     const Scratch s = scratch_of(p, true);
     const Drop none = make_drop(0.f, 0, 0, nullptr);
     Prepare r = ordering(p, g, ws, s);
-    if (p.images == 0) r.n = 0;
+    if (!p.adapters) r.orders = 0;
     int copies = 0, first = r.orders;
+    for (Copy& c : r.copy) c.first = c.last = first;
     auto copy = [&](const void* src, size_t dst, int batch, int R, int C) {
         Copy& c = r.copy[copies++];
         c.src = src; c.dst = ws + dst; c.R = R; c.C = C;
@@ -1164,7 +1171,7 @@ void backward(const AdapterShape& p, const AdapterArgs& g, const void* dy, const
         if (p.adapters && dx) copy(g.a, s.at, p.adapters, p.rank, p.in);
     }
     prepare<T>(r, st);
-    const Rows q = rows_of(p, g, ws, s, true);
+    const Rows q = rows_of(p, g, ws, s, p.adapters > 0);
     float* u = (float*)(ws + s.inner);
     if (p.adapters && (dx || da)) narrow<T>(q, dy, p.out, ws + s.bt, none, u, st);
     uint8_t* bits = drop.border && p.adapters && da && dx && p.in % 8 == 0 ? (uint8_t*)(ws + s.bits) : nullptr;

@@ -1595,11 +1595,15 @@ int dr_dropout_fwd(const dr_tensor* d, const void* x, const dr_dropout* drop, vo
     return launch_dropout(d->dtype, x, p, y, tensor_elems(*d), (hipStream_t)stream);
 }
 
+// rows, classes and channels that kernels count in 32 bits, and a little beyond the last
+constexpr int MOST = 1 << 30;
+
 static int check_logits(const char* who, const dr_tensor* d)
 {
     DR_TRY(check_tensor(who, "d", d));
     if (d->h != 1 || d->w != 1) return fail(DR_ERR_SHAPE, "%s: logits must be {n, c, 1, 1}", who);
     if (d->c < 1) return fail(DR_ERR_SHAPE, "%s: no classes", who);
+    if (d->n > MOST || d->c > MOST) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^30 rows or classes", who);
     return DR_OK;
 }
 
@@ -1635,6 +1639,9 @@ static int check_adapters(const char* who, const dr_tensor* xd, const dr_adapter
     const double pixels = (double)xd->n * xd->h * xd->w, most = std::max(ad->c_in, ad->c_out), factors = (double)ad->count * ad->rank;
     if (pixels * std::max(most, (double)ad->rank) >= 2147483648.0 || (double)ad->c_in * ad->c_out >= 2147483648.0 || factors * most >= 2147483648.0)
         return fail(DR_ERR_UNSUPPORTED, "%s: a tensor of more than 2^31-1 elements", who);
+    if (pixels > (1 << 26) || most > MOST) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^26 pixels or 2^30 channels", who);
+    // (blocks of 64 x 64 of A and B, a workgroup each)
+    if (ad->count * ceil(most / 64) * 2 > (1 << 23)) return fail(DR_ERR_UNSUPPORTED, "%s: %d adapters of %.0f channels", who, ad->count, most);
     p->images = pixels > 0 ? xd->n : 0;
     p->hw = pixels > 0 ? xd->h * xd->w : 1;
     p->in = ad->c_in; p->out = ad->c_out; p->adapters = ad->count; p->rank = ad->rank; p->dtype = xd->dtype;

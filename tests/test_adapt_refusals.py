@@ -33,6 +33,7 @@ def test_softmax_loss_refuses():
     call = lambda d=tensor(5, 7), z=FAKE, labels=FAKE, e=0.0, ws=FAKE, n=need.value: L.dr_softmax_loss_grad(d, z, labels, e, 1, FAKE, FAKE, FAKE, ws, n, None)
     assert call(d=None) == B.DR_ERR_NULL and call(z=None) == B.DR_ERR_NULL and call(labels=None) == B.DR_ERR_NULL
     assert call(d=tensor(5, 7, 1, 2)) == B.DR_ERR_SHAPE and call(d=tensor(5, 0)) == B.DR_ERR_SHAPE and call(d=tensor(5, 7, dtype=9)) == B.DR_ERR_UNSUPPORTED
+    assert call(d=tensor((1 << 30) + 1, 1)) == B.DR_ERR_UNSUPPORTED and call(d=tensor(1, (1 << 30) + 1)) == B.DR_ERR_UNSUPPORTED
     for e in (-0.1, 1.5, float("nan")):
         assert call(e=e) == B.DR_ERR_SHAPE and "smoothing" in B.last_error()
     assert call(ws=None) == B.DR_ERR_WORKSPACE and call(n=need.value - 1) == B.DR_ERR_WORKSPACE and call(ws=C.c_void_p(4096 + 16)) == B.DR_ERR_WORKSPACE
@@ -53,6 +54,9 @@ def test_adapters_refuse():
         assert size(tensor(1 << 20, 8), B.dr_adapters(2, 4, 8, 1 << 12), need) == B.DR_ERR_UNSUPPORTED
         assert size(tensor(3, 1 << 16), B.dr_adapters(2, 4, 1 << 16, 1 << 15), need) == B.DR_ERR_UNSUPPORTED
         assert size(tensor(3, 1 << 12), B.dr_adapters(1 << 13, 64, 1 << 12, 8), need) == B.DR_ERR_UNSUPPORTED
+        assert size(tensor((1 << 26) + 1, 8), B.dr_adapters(2, 4, 8, 8), need) == B.DR_ERR_UNSUPPORTED and size(tensor(1 << 26, 8), B.dr_adapters(2, 4, 8, 8), need) == B.DR_OK
+        assert size(tensor(1, 1 << 17), B.dr_adapters(1 << 12, 1, 1 << 17, 8), need) == B.DR_ERR_UNSUPPORTED
+        assert size(tensor(0, 8, 1 << 20, 1 << 20), ad, need) == B.DR_OK                  # (no pixels, whatever the map)
     assert L.dr_adapter_fwd_workspace_bytes(xd, ad, need) == B.DR_OK and need.value > 0
     names = ("x", "w", "a", "b", "ids", "y")
     def fwd(xd=xd, ad=ad, yd=yd, drop=None, ws=FAKE, n=need.value, **p):

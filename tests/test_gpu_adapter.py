@@ -135,6 +135,51 @@ def test_against_the_formulas(n, h, w, cin, cout, rank, count, p, dtype):
     f.check()
 
 
+LARGE = [  # rows, c_in, c_out, rank, adapters, p: tiles of 128 and of 256 in both directions, aligned rows and others, a last stage that is no whole one
+    (2048, 136, 2048, 16, 5, 0.1, "bf16"), (1500, 133, 1999, 20, 3, 0.4, "bf16"), (4096, 264, 4096, 16, 8, 0.1, "bf16"), (4100, 131, 4100, 5, 3, 0.0, "bf16"),
+    (2000, 136, 2100, 16, 5, 0.4, "f32"), (4096, 72, 4096, 33, 4, 0.0, "f32"), (4097, 67, 4101, 8, 2, 0.4, "f32")]
+
+
+@pytest.mark.parametrize("rows,cin,cout,rank,count,p,dtype", LARGE)
+@pytest.mark.parametrize("turned", [False, True])
+def test_large_tiles(rows, cin, cout, rank, count, p, dtype, turned):
+    """y of a projection to many channels, and (turned) dx of one from many; the same formulas and bounds, in 64 bits on the device."""
+    cin, cout = (cout, cin) if turned else (cin, cout)
+    rng = np.random.default_rng(case_seed((rows, cin, cout, rank, count, p, dtype)))
+    dt, ut = (torch.bfloat16, 2.0 ** -8) if dtype == "bf16" else (torch.float32, U)
+    pieces = 2.0 ** -17 if dtype == "bf16" else 0.0
+    num = lambda *s: torch.from_numpy(rng.standard_normal(s, dtype=np.float32)).to(dt).cuda()
+    x, w, a, b, dy, bias = num(rows, cin), num(cout, cin), num(count, rank, cin), num(count, cout, rank), num(rows, cout), num(cout).float()
+    ids = torch.from_numpy(rng.integers(-1, count, rows).astype(np.int32)).cuda()
+    drop = B.dropout_desc(p, 77, 3) if p else None
+    y, dx, inner = torch.empty_like(dy), torch.empty_like(x), torch.empty((rows, rank), device="cuda")
+    da, db = torch.empty(a.shape, device="cuda"), torch.empty(b.shape, device="cuda")
+    ws = torch.empty(max(B.adapter_fwd_workspace_bytes(x, a, b), B.adapter_bwd_workspace_bytes(x, a, b)), dtype=torch.uint8, device="cuda")
+    B.adapter_fwd(x, w, bias, a, b, ids, y, ws, drop=drop, inner=inner)
+    B.adapter_bwd(dy, x, w, a, b, ids, inner, dx, da, db, ws, drop=drop)
+    only, _, _ = B.adapter_bwd(dy, x, w, a, b, ids, None, torch.empty_like(x), None, None, ws, drop=drop)      # the mask drawn in the product itself
+    assert torch.equal(only, dx)
+    m = torch.from_numpy(O.mask((rows, cin), p, 77, 3)).cuda()
+    chosen = (ids[:, None] == torch.arange(count, device="cuda")).double()
+    xd, wd, ad, bd, dyd = (t.double() for t in (x, w, a.view(-1, cin), b.permute(0, 2, 1).reshape(-1, cout), dy))
+    own = chosen.repeat_interleave(rank, 1)
+    def check(what, got, ref, tol):
+        assert note(what + " / bound", ((got.double() - ref).abs() / tol).max().item(), 1.0)
+    if not turned:
+        t, st = own * ((xd * m) @ ad.t()), own * ((xd.abs() * m) @ ad.abs().t())
+        ref = xd @ wd.t() + bias.double() + t @ bd
+        off = (chain(cin) + 4 * U) * st + pieces * t.abs()
+        check("y", y, ref, chain(cin + rank) * (xd.abs() @ wd.abs().t() + bias.double().abs() + st @ bd.abs()) + off @ bd.abs() + ut * ref.abs() + 1e-37)
+    else:
+        u, su = own * (dyd @ bd.t()), own * (dyd.abs() @ bd.abs().t())
+        ref = dyd @ wd + m * (u @ ad)
+        through = m * (su @ ad.abs())
+        check("dx", dx, ref, chain(cout + rank) * (dyd.abs() @ wd.abs() + through) + (chain(cout) + 4 * U + pieces) * through + ut * ref.abs() + 1e-37)
+        da_ref, s_da = u.t() @ (xd * m), su.t() @ (xd.abs() * m)
+        most = int(chosen.sum(0).max().item())
+        check("da", da.view(-1, cin), da_ref, (chain(most) + chain(cout) + 6 * U) * s_da + 1e-37)
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("offset", [1, 3, 8])
 def test_tensors_at_any_address(dtype, offset):
@@ -185,6 +230,24 @@ def test_rows_as_a_matrix_and_no_rows():
     assert np.abs(y.double().cpu().numpy() - ref).max() < chain(72) * 72 * 25 and (f.inner == 0).all()
     B.adapter_bwd(dy, x, f.gw, a, b, f.gids, f.inner, dx, f.da[:0], f.db[:0], f.ws)
     assert np.abs(dx.double().cpu().numpy() - f.wide(f.dy) @ f.wt.double().numpy()).max() < chain(40) * 40 * 25
+
+
+@pytest.mark.parametrize("n", [5, 400])
+def test_a_projection_without_adapters_asks_for_none(n):
+    """count = 0 with A, B and ids NULL, by the C entry points."""
+    import ctypes as C
+    f = Case(n, 1, 1, 72, 136, 8, 0, "f32", ids=[-1] * n).gpu()
+    xd, yd, ad = B.dr_tensor(n, 72, 1, 1, 0, 1), B.dr_tensor(n, 136, 1, 1, 0, 1), B.dr_adapters(0, 8, 72, 136)
+    L, p, need, stream = B.lib(), B._ptr, C.c_size_t(0), torch.cuda.current_stream().cuda_stream
+    for size in (L.dr_adapter_fwd_workspace_bytes, L.dr_adapter_bwd_workspace_bytes):
+        assert size(xd, ad, need) == B.DR_OK and need.value <= f.ws.numel()
+    assert L.dr_adapter_fwd(xd, p(f.gx), ad, p(f.gw), p(f.gbias), None, None, None, None, None, yd, p(f.y), p(f.inner), p(f.ws), f.ws.numel(), stream) == B.DR_OK
+    assert L.dr_adapter_bwd(yd, p(f.gdy), xd, p(f.gx), ad, p(f.gw), None, None, None, None, None, None, p(f.dx), p(f.da), p(f.db), p(f.ws), f.ws.numel(), stream) == B.DR_OK
+    w = f.wt.double().numpy()
+    y, dx = f.wide(f.x) @ w.T + f.bias.double().numpy(), f.wide(f.dy) @ w
+    f.close("y", f.y, y, chain(72) * (np.abs(f.wide(f.x)) @ np.abs(w).T + np.abs(f.bias.double().numpy())) + U * np.abs(y))
+    f.close("dx", f.dx, dx, chain(136) * (np.abs(f.wide(f.dy)) @ np.abs(w)) + U * np.abs(dx))
+    assert (f.inner == 0).all()
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
