@@ -6,7 +6,11 @@
 //
 // Both are a narrow product (t, u: rows x rank), a wide one whose contraction runs over the projection and then over the rank, and for the gradient two sums over the rows
 // of each adapter.  Rows are visited in the order of their adapters, so that few tiles hold rows of several; such a tile takes its adapters one after the other.
-// t and u are held in fp32 and enter bf16 products as two pieces each (16 bits of their values): with one piece the adapter's part of y would be rounded twice.
+// t and u are held in fp32 and enter bf16 products as two pieces each (16 bits of their values): with one piece the adapter's part of y would be rounded twice.  The sums
+// over rows, whose results are fp32, take three.
+//
+// 8192 rows of 4096 channels to 4096 in bf16, eight adapters of rank 16, dropout: forward 285 us (order 7, narrow 33, wide 243: 1.13 PFLOP/s, where the library's
+// product alone takes 217), gradient 380 (order and copies 18, narrow 20, sums 57 + 6, wide 280).
 #include <algorithm>
 #include <type_traits>
 
@@ -36,9 +40,7 @@ __device__ __forceinline__ void keep_halves(u32x4& v, unsigned bits)
     }
 }
 
-// Eight elements of an operand's row, as the matrix instructions take them.  A lane of group g = lane / 16 holds elements 8 g .. 8 g + 7 of a slice of 32: one
-// instruction in bf16, eight in fp32 (the j-th of them multiplies the j-th elements of the four groups).
-// load(row, k, K) reads elements k .. k + 7 of a row of K >= 8, or its last eight where it ends before, which settle() then moves to their places, with zeros behind
+// Eight elements of a row.  load(row, k, K) reads elements k .. k + 7 of a row of K >= 8, or its last eight where it ends before, which settle() then moves to their places, with zeros behind
 // them: loads without a condition between them stay in flight together.  load_any() is for rows of any length.
 template <typename T> struct Operand;
 template <> struct Operand<uint16_t> {
@@ -99,14 +101,6 @@ template <> struct Operand<float> {
         for (int i = 0; i < 8; ++i) e[i] = v[i >> 2][i & 3];
     }
 };
-__device__ __forceinline__ f32x4 mfma(const Operand<uint16_t>& a, const Operand<uint16_t>& b, f32x4 c) { return mfma(a.v, b.v, c); }
-__device__ __forceinline__ f32x4 mfma(const Operand<float>& a, const Operand<float>& b, f32x4 c)
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i >> 2][i & 3], b.v[i >> 2][i & 3], c, 0, 0, 0);
-    return c;
-}
-
 // Which of the eight elements from `first` on dropout keeps, a bit each
 __device__ __forceinline__ unsigned kept8_from(const Drop& d, uint64_t place, uint64_t first)
 {
@@ -133,7 +127,8 @@ struct Rows {
 // ---- what the products start from: the order of the images by adapter, and transposed copies ------------------------------------------------------
 // Order: workgroup a writes the images of adapter a (the last one those without) in the order in which they come: first how many belong before them, then which they
 // are.  A wave takes a quarter of the ids, four of a lane at a time.
-// Copies: src[batch][R][C] -> dst[batch][C][R], 64 x 64 elements a workgroup.
+// Copies: src[batch][R][C] -> dst[batch][C][R], 64 x 64 elements a workgroup.  Of W, A and B for the gradient, whose products run over the other dimension: 18 us of 380 at
+// 4096 x 4096 in bf16, most of it W's 64 MB; one launch with the order, where four took 53.
 struct Copy { const void* src; void* dst; int R, C, tiles_r, tiles_c, first, last; };      // workgroups first .. last - 1
 struct Prepare {
     const int* ids;
@@ -386,7 +381,8 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
 
 // ---- a narrow product: out[row][r] = s_a sum_k v[row][k] M_a[r][k] -----------------------------------------------------------------------------
 // A workgroup takes 16 rows and the adapters among them, every gridDim.y-th from its own on (the i-th adapter is that of the i-th row whose adapter no row before has); its NW
-// waves share the contraction and add up in LDS.
+// waves share the contraction and add up in LDS.  Bound by memory (8192 rows of 4096 in bf16: 20 us, 3.4 TB/s of v, and M_a again from L2 for every 16 rows), with dropout by
+// the vector instructions that draw the mask (33 us); 64 rows with an adapter each 8.2 us.
 template <typename T, int RB, int NW, int D>
 __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
 {
@@ -436,6 +432,10 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
 // A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  PB pieces of 16 bytes of every row of W and x are a
 // stage, of which LDS holds NS: one that is multiplied and others on their way, by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or one by way of
 // registers.  A row's pieces lie in the order piece ^ (row PB / 16): the same piece of sixteen rows is then in all 64 banks.
+// 8192 x 4096 x 4096 bf16 241 us without adapters (1.14 PFLOP/s; stages of 64 bytes four deep 253, bank conflicts and 8-byte stores from registers 272, by way of registers
+// 315); a step of 4096 in the contraction costs what 1.29 PFLOP/s cost, the rest (35 us in two rounds of tiles) is first loads, adapters and stores.  Four waves of 128 x 128
+// would read a third less from LDS, but the compiler then moves accumulators between register files (933 us).  2000 rows 68 us, 512 28, 128 21; fp32 8192 x 1024 x 1024
+// 145 us (119 TFLOP/s of 157 that the fp32 instruction has).
 template <typename T> struct Wide {
     Rows q;
     const T *x, *w, *b;
@@ -729,6 +729,7 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
 // ---- the wide product of few rows ---------------------------------------------------------------------------------------------------------------
 // A workgroup owns 16 outputs of up to 64 rows (NB blocks of 16) and its eight waves share the contraction, so that W is read by as many compute units as there are blocks
 // of 16 outputs.  The sums of the waves are added in LDS, where a lane adds the adapter's part of its output by itself: rank products.
+// 64 rows of 4096 to 4096 in bf16: 13 us, 33.5 MB of W at 2.6 TB/s beside x again for each block (134 MB from L2); tiles of 64 x 64 take 27 there.
 template <typename T, int NB, int D>
 __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
 {
@@ -806,10 +807,11 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
 }
 
 // ---- sums over the rows of an adapter: out[a][r][c] (or [a][c][r]) = sum f[row][r] drop(v[row][c]) ---------------------------------------------------
-// A workgroup takes `length` positions, 512 bytes of columns (a quarter of them a wave) and up to 64 of the rank, and the adapters among those positions one after the other: a segment each.  Both
-// operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into three
-// pieces (all its bits: the sums are fp32).  A segment that is all of its
-// adapter is the result; others are partial sums, that of chunk k and adapter a in slot k + a (one of the two grows from a segment to the next), added in their order after.
+// A workgroup takes `length` positions, 512 bytes of columns (a quarter of them a wave) and up to 64 of the rank, and the adapters among those positions one after the
+// other: a segment each.  Both operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into three pieces
+// (all its bits: the sums are fp32).  A segment that is all of its adapter is the result; others are partial sums, that of chunk k and adapter a in slot k + a (one of the
+// two grows from a segment to the next), added in their order after.
+// 8192 rows of 4096 + 4096 columns in bf16, rank 16: 57 us for 134 MB, bound by the vector instructions that draw x's mask (44 without) and move both operands through LDS.
 struct Sum {
     const void* v;
     const float* f;
@@ -1039,6 +1041,8 @@ void wide(const Rows& q, const void* x, int K, const void* w, const float* bias,
         return p.tiles;
     };
     const int cus = device_cus();
+    // fewer tiles of 64 x 64 than half the compute units: blocks of 16 outputs (128 rows of 1024 to 1000 in fp32 25 -> 13 us; 64 rows of 4096 to 4096 in bf16 27 -> 13;
+    // 128 rows of 4096 to 4096, 128 tiles, 21 in tiles and 2 x 13 so)
     if (tiles(64, 64) < cus / 2) {
         if (q.count <= 16) { tiles(16, 16); hipLaunchKernelGGL((few_kernel<T, 1, 4>), dim3(p.tiles), dim3(512), 0, st, p); }
         else if (q.count <= 32) { tiles(16, 32); hipLaunchKernelGGL((few_kernel<T, 2, 3>), dim3(p.tiles), dim3(512), 0, st, p); }
@@ -1139,7 +1143,8 @@ template <typename T>
 void forward(const AdapterShape& p, const AdapterArgs& g, const void* x, void* y, float* inner, const Drop& drop, char* ws, hipStream_t st)
 {
     const Scratch s = scratch_of(p, false);
-    const bool sorted = p.images > 64 && p.hw < 64 && p.adapters > 1;      // few images, or images as long as a tile: as they come
+    // few images, or images as long as a tile: as they come (a tile then holds few adapters, and the order's launch is 4-8 us)
+    const bool sorted = p.images > 64 && p.hw < 64 && p.adapters > 1;
     if (sorted) prepare<T>(ordering(p, g, ws, s), st);
     const Rows q = rows_of(p, g, ws, s, sorted);
     float* t = inner ? inner : (float*)(ws + s.inner);

@@ -9,7 +9,8 @@
 namespace dr {
 namespace {
 
-// A lane takes blocks of eight elements, U of them 256 apart, all loaded before the first is used.
+// A lane takes blocks of eight elements, U of them 256 apart, all loaded before the first is used.  Bound by memory: 128 x 192 x 56 x 56 in bf16 58 us, 5.3 TB/s; a block's
+// ten rounds of two 32 x 32-bit products are ~560 cycles of a wave for 512 elements, half of what memory takes for them.
 template <typename T, int U>
 __global__ __launch_bounds__(256) void dropout_kernel(const Drop drop, const T* x, T* y, unsigned count)
 {

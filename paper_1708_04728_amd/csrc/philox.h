@@ -32,7 +32,7 @@ DR_ANY void philox(uint64_t seed, uint64_t block, uint64_t place, uint32_t (&r)[
 }
 
 // An element is dropped where its 16 bits are below the border, with probability border / 65536: p to within 2^-17.  Sixteen bits rather than 32, because a block of
-// ten rounds (~130 cycles of a lane) then serves eight elements.
+// ten rounds (about 140 instruction slots of a lane, 80 of them in 32-bit products) then serves eight elements: four would make a bf16 tensor's dropout wait for it.
 constexpr int DROP_BITS = 65536;
 inline unsigned drop_border(float p) { return (unsigned)((double)p * DROP_BITS + 0.5); }
 inline float drop_scale(unsigned border) { return border >= DROP_BITS ? 0.f : (float)((double)DROP_BITS / (DROP_BITS - (int)border)); }

@@ -3,7 +3,8 @@
 //   l = log sum exp z - (1 - e) z_t - e / C sum z,   dz = g (exp(z - log sum exp z) - (1 - e) [j = t] - e / C),   g = 1 or 1 / (rows with a label)
 //
 // A row is read once: its lanes hold it in registers from the maximum to the gradient.  Sums are in fp32 over a lane's elements, then over lanes in a fixed order; the
-// loss of all rows is added in double.
+// loss of all rows is added in double.  Bound by memory where rows are many (8192 x 32768 bf16 223 us, 4.8 TB/s; 353 with loads behind conditions, 276 with exponentials of
+// eight instructions, 294 with 512 lanes of 64 elements, whose registers spill), by launches where they are few (128 x 1000: 4.4 + 2.2 us).
 #include <algorithm>
 
 #include "dr_internal.h"
