@@ -632,6 +632,15 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
     const int ow = o0 + wm * MB * 32;
     const uint64_t place = DROP == MASK_DRAWN ? drop_place(p.drop) : 0;
     const float scale = DROP ? p.drop.scale : 1.f;
+    [[maybe_unused]] unsigned kept_bits[MB][NB];
+    if constexpr (DROP == MASK_BITS) {
+        typedef unsigned int u32_any __attribute__((aligned(1)));
+#pragma unroll
+        for (int i = 0; i < MB; ++i)
+#pragma unroll
+            for (int j = 0; j < NB; ++j)
+                kept_bits[i][j] = *reinterpret_cast<const u32_any*>(p.bits + (((size_t)max(row[j], 0) * p.N + min(ow + i * 32, p.N - 1)) >> 3));
+    }
     for (int a = -1;;) {
         int next = 0x7FFFFFFF;
 #pragma unroll
@@ -643,39 +652,41 @@ __global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
         a = next;
         constexpr int STEP = 2 * E;
         for (int r0 = 0; r0 < q.rank; r0 += STEP) {
+            // (what comes of rows of other adapters is not taken, so their t need not be left out)
             const int r = r0 + h * E;
-            u32x4 high[NB], low[NB];
+            const bool all = r0 + STEP <= q.rank;
+            u32x4 high[NB], low[NB], factor[MB];
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                const char* at = (const char*)(p.b + ((size_t)a * p.N + min(ow + i * 32 + l32, p.N - 1)) * q.rank + r);
+                factor[i] = all ? piece(at) : piece<T>(at, q.rank - r);
+            }
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
+                const float* at = p.t + (size_t)max(row[j], 0) * q.rank + r;
                 float e[8];
-                load8(p.t + (size_t)max(row[j], 0) * q.rank + r, id[j] == a ? min(q.rank - r, E) : 0, 0.f, e);
                 if constexpr (sizeof(T) == 2) {
                     float up[8];
+                    if (all) load8(at, e);
+                    else load8(at, q.rank - r, 0.f, e);
                     high[j] = pack8(e);
                     unpack8(high[j], up);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) e[c] -= up[c];
                     low[j] = pack8(e);
-                } else high[j] = __builtin_bit_cast(u32x4, f32x4{e[0], e[1], e[2], e[3]});
+                } else high[j] = all ? piece((const char*)at) : piece<T>((const char*)at, q.rank - r);
             }
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
-                const int o = min(ow + i * 32 + l32, p.N - 1);
-                const u32x4 v = piece<T>((const char*)(p.b + ((size_t)a * p.N + o) * q.rank + r), q.rank - r);
+                const u32x4 v = factor[i];
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
                     // this lane's row of the block: outputs 16 h .. 16 h + 15, the others from the lane that holds the same row
                     unsigned keep = 0xFFFFFFFFu;
-                    if constexpr (DROP) {
-                        const size_t from = (size_t)max(row[j], 0) * p.N + min(ow + i * 32, p.N - 1);
-                        if constexpr (DROP == MASK_BITS) {
-                            typedef unsigned int u32_any __attribute__((aligned(1)));
-                            keep = *reinterpret_cast<const u32_any*>(p.bits + (from >> 3));
-                        } else {
-                            const unsigned own = kept16(p.drop, place, from + h * 16), other = __shfl_xor(own, 32, 64);
-                            keep = h ? own << 16 | other : other << 16 | own;
-                        }
-                        keep >>= h * 4;
+                    if constexpr (DROP == MASK_BITS) keep = kept_bits[i][j] >> (h * 4);
+                    if constexpr (DROP == MASK_DRAWN) {
+                        const unsigned own = kept16(p.drop, place, (size_t)max(row[j], 0) * p.N + min(ow + i * 32, p.N - 1) + h * 16), other = __shfl_xor(own, 32, 64);
+                        keep = (h ? own << 16 | other : other << 16 | own) >> (h * 4);
                     }
                     f32x16 part = {};          // of its own: rows of other adapters must not meet this one's numbers, not even times zero
                     part = mfma32<T>(v, high[j], part);
