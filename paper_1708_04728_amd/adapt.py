@@ -73,7 +73,7 @@ def main(batch=128, c=1024, classes=1000, tasks=4, rank=8, steps=100):
         x = normal(batch, c).abs()
         ids = torch.randint(0, tasks, (batch,), device="cuda", generator=gen, dtype=torch.int32)
         labels = B.adapter_fwd(x, w, bias, a, b, ids, y, ws).argmax(1).int()
-        model.step(x, ids, labels, 1.0)
+        model.step(x, ids, labels, 0.05)
         if i % 20 == 0 or i + 1 == steps:
             print("step %3d  loss %.4f" % (i, model.loss.item()))
 

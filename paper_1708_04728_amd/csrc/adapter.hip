@@ -383,8 +383,8 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
 // A workgroup takes 16 rows and the adapters among them, every gridDim.y-th from its own on (the i-th adapter is that of the i-th row whose adapter no row before has); its NW
 // waves share the contraction and add up in LDS.  Bound by memory (8192 rows of 4096 in bf16: 20 us, 3.4 TB/s of v, and M_a again from L2 for every 16 rows), with dropout by
 // the vector instructions that draw the mask (33 us); 64 rows with an adapter each 8.2 us.
-template <typename T, int RB, int NW, int D>
-__global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
+template <typename T, int RB, int NW, int D, bool DROP>
+__global__ __launch_bounds__(NW * 64, RB == 1 && sizeof(T) == 2 ? 4 : 1) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
 {
     __shared__ __attribute__((aligned(128))) unsigned char lds[NW][(RB + 1) * 2048];
     __shared__ float red[NW][RB * 16][17];
@@ -398,7 +398,7 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
     unsigned firsts = (unsigned)__ballot(!again) & 0xFFFFu;
     if (blockIdx.y == 0 && id == -1)
         for (int r = wave * 4 + g; r < q.rank; r += NW * 4) out[(size_t)row * q.rank + r] = 0.f;
-    const uint64_t place = drop.border ? drop_place(drop) : 0;
+    const uint64_t place = DROP ? drop_place(drop) : 0;
     for (int turn = 0; firsts; firsts &= firsts - 1, ++turn) {
         if (turn % gridDim.y != blockIdx.y) continue;
         const int first = __builtin_ctz(firsts), a = __builtin_amdgcn_readlane(id, first);
@@ -408,15 +408,14 @@ __global__ __launch_bounds__(NW * 64) void narrow_kernel(const Rows q, const T* 
         auto ra = [&](int i) { return min(i * 8 + (lane >> 3), q.rank - 1); };
         auto rb = [&](int i) { return i ? high : low; };
         const T* ma = m + (size_t)a * q.rank * K;
-        if (drop.border) wave_product<T, RB, 1, D, NW, true>(ma, ra, v, rb, K, wave, lds[wave], drop, place, acc);
-        else wave_product<T, RB, 1, D, NW, false>(ma, ra, v, rb, K, wave, lds[wave], drop, place, acc);
+        wave_product<T, RB, 1, D, NW, DROP>(ma, ra, v, rb, K, wave, lds[wave], drop, place, acc);
         __syncthreads();
 #pragma unroll
         for (int b = 0; b < RB; ++b)
 #pragma unroll
             for (int i = 0; i < 4; ++i) red[wave][b * 16 + g * 4 + i][l16] = acc[b][0][i];
         __syncthreads();
-        const float scale = (q.scales ? q.scales[a] : 1.f) * (drop.border ? drop.scale : 1.f);
+        const float scale = (q.scales ? q.scales[a] : 1.f) * (DROP ? drop.scale : 1.f);
         // 16 lanes hold the rows, the others of the workgroup the ranks
         if (id == a)
             for (int r = wave * 4 + g; r < q.rank; r += NW * 4) {
@@ -1031,11 +1030,15 @@ void narrow(const Rows& q, const void* v, int K, const void* m, const Drop& drop
     const int tiles = (q.count + 15) / 16;
     auto launch = [&](auto kernel, int waves, int slots) { hipLaunchKernelGGL(kernel, dim3(tiles, slots), dim3(waves * 64), 0, st, q, (const T*)v, K, (const T*)m, drop, out); };
     // few rows: each of a tile's adapters in a workgroup of its own
-    const int slots = tiles < 256 ? std::max(1, std::min({16, q.adapters, (1023 + tiles) / tiles})) : 1;
-    if (q.rank <= 16) launch(narrow_kernel<T, 1, 8, 4>, 8, slots);
-    else if (q.rank <= 32) launch(narrow_kernel<T, 2, 8, 3>, 8, slots);
-    else if (q.rank <= 64) launch(narrow_kernel<T, 4, 8, 2>, 8, slots);
-    else launch(narrow_kernel<T, 8, 4, 1>, 4, slots);
+    const int slots = tiles < 256 ? std::max(1, std::min({16, q.adapters, (255 + tiles) / tiles})) : 1;
+    auto run = [&](auto masked) {
+        constexpr bool DROP = decltype(masked)::value;
+        if (q.rank <= 16) launch(narrow_kernel<T, 1, 8, 4, DROP>, 8, slots);
+        else if (q.rank <= 32) launch(narrow_kernel<T, 2, 8, 3, DROP>, 8, slots);
+        else if (q.rank <= 64) launch(narrow_kernel<T, 4, 8, 2, DROP>, 8, slots);
+        else launch(narrow_kernel<T, 8, 4, 1, DROP>, 4, slots);
+    };
+    drop.border ? run(std::true_type()) : run(std::false_type());
 }
 
 template <typename T>
