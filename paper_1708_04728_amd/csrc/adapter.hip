@@ -9,8 +9,8 @@
 // t and u are held in fp32 and enter bf16 products as two pieces each (16 bits of their values): with one piece the adapter's part of y would be rounded twice.  The sums
 // over rows, whose results are fp32, take three.
 //
-// 8192 rows of 4096 channels to 4096 in bf16, eight adapters of rank 16, dropout: forward 285 us (order 7, narrow 33, wide 243: 1.13 PFLOP/s, where the library's
-// product alone takes 217), gradient 380 (order and copies 18, narrow 20, sums 57 + 6, wide 280).
+// 8192 rows of 4096 channels to 4096 in bf16, eight adapters of rank 16, dropout: forward 266 us (order 7, narrow 26, wide 232: 1.18 PFLOP/s, where the library's
+// product alone takes 217), gradient 341 (order and copies 18, narrow 17, sums 58 + 6, wide 246).
 #include <algorithm>
 #include <type_traits>
 
@@ -127,7 +127,7 @@ struct Rows {
 // ---- what the products start from: the order of the images by adapter, and transposed copies ------------------------------------------------------
 // Order: workgroup a writes the images of adapter a (the last one those without) in the order in which they come: first how many belong before them, then which they
 // are.  A wave takes a quarter of the ids, four of a lane at a time.
-// Copies: src[batch][R][C] -> dst[batch][C][R], 64 x 64 elements a workgroup.  Of W, A and B for the gradient, whose products run over the other dimension: 18 us of 380 at
+// Copies: src[batch][R][C] -> dst[batch][C][R], 64 x 64 elements a workgroup.  Of W, A and B for the gradient, whose products run over the other dimension: 18 us of 341 at
 // 4096 x 4096 in bf16, most of it W's 64 MB; one launch with the order, where four took 53.
 struct Copy { const void* src; void* dst; int R, C, tiles_r, tiles_c, first, last; };      // workgroups first .. last - 1
 struct Prepare {
@@ -381,8 +381,8 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
 
 // ---- a narrow product: out[row][r] = s_a sum_k v[row][k] M_a[r][k] -----------------------------------------------------------------------------
 // A workgroup takes 16 rows and the adapters among them, every gridDim.y-th from its own on (the i-th adapter is that of the i-th row whose adapter no row before has); its NW
-// waves share the contraction and add up in LDS.  Bound by memory (8192 rows of 4096 in bf16: 20 us, 3.4 TB/s of v, and M_a again from L2 for every 16 rows), with dropout by
-// the vector instructions that draw the mask (33 us); 64 rows with an adapter each 8.2 us.
+// waves share the contraction and add up in LDS.  Bound by memory (8192 rows of 4096 in bf16: 17 us, 3.9 TB/s of v, and M_a again from L2 for every 16 rows), with dropout by
+// the vector instructions that draw the mask (26 us; 33 where registers leave a compute unit one workgroup); 64 rows with an adapter each 6.5 us.
 template <typename T, int RB, int NW, int D, bool DROP>
 __global__ __launch_bounds__(NW * 64, RB == 1 && sizeof(T) == 2 ? 4 : 1) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
 {
@@ -431,7 +431,7 @@ __global__ __launch_bounds__(NW * 64, RB == 1 && sizeof(T) == 2 ? 4 : 1) void na
 // A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  PB pieces of 16 bytes of every row of W and x are a
 // stage, of which LDS holds NS: one that is multiplied and others on their way, by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or one by way of
 // registers.  A row's pieces lie in the order piece ^ (row PB / 16): the same piece of sixteen rows is then in all 64 banks.
-// 8192 x 4096 x 4096 bf16 241 us without adapters (1.14 PFLOP/s; stages of 64 bytes four deep 253, bank conflicts and 8-byte stores from registers 272, by way of registers
+// 8192 x 4096 x 4096 bf16 232 us with adapters (1.18 PFLOP/s; before registers stopped spilling 241 without them; stages of 64 bytes four deep 253, bank conflicts and 8-byte stores from registers 272, by way of registers
 // 315); a step of 4096 in the contraction costs what 1.29 PFLOP/s cost, the rest (35 us in two rounds of tiles) is first loads, adapters and stores.  Four waves of 128 x 128
 // would read a third less from LDS, but the compiler then moves accumulators between register files (933 us).  2000 rows 68 us, 512 28, 128 21; fp32 8192 x 1024 x 1024
 // 145 us (119 TFLOP/s of 157 that the fp32 instruction has).
@@ -821,7 +821,7 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
 // other: a segment each.  Both operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into three pieces
 // (all its bits: the sums are fp32).  A segment that is all of its adapter is the result; others are partial sums, that of chunk k and adapter a in slot k + a (one of the
 // two grows from a segment to the next), added in their order after.
-// 8192 rows of 4096 + 4096 columns in bf16, rank 16: 57 us for 134 MB, bound by the vector instructions that draw x's mask (44 without) and move both operands through LDS.
+// 8192 rows of 4096 + 4096 columns in bf16, rank 16: 58 us for 134 MB, bound by the vector instructions that draw x's mask (44 without) and move both operands through LDS.
 struct Sum {
     const void* v;
     const float* f;
@@ -1029,7 +1029,7 @@ void narrow(const Rows& q, const void* v, int K, const void* m, const Drop& drop
     if (!q.count) return;
     const int tiles = (q.count + 15) / 16;
     auto launch = [&](auto kernel, int waves, int slots) { hipLaunchKernelGGL(kernel, dim3(tiles, slots), dim3(waves * 64), 0, st, q, (const T*)v, K, (const T*)m, drop, out); };
-    // few rows: each of a tile's adapters in a workgroup of its own
+    // few rows: each of a tile's adapters in a workgroup of its own, while there are compute units (maps of five adapters, 232 tiles: 6.3 us with 2, 8.5 with 5)
     const int slots = tiles < 256 ? std::max(1, std::min({16, q.adapters, (255 + tiles) / tiles})) : 1;
     auto run = [&](auto masked) {
         constexpr bool DROP = decltype(masked)::value;
