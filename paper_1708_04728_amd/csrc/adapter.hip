@@ -433,8 +433,8 @@ __global__ __launch_bounds__(NW * 64, RB == 1 && sizeof(T) == 2 ? 4 : 1) void na
 // registers.  A row's pieces lie in the order piece ^ (row PB / 16): the same piece of sixteen rows is then in all 64 banks.
 // 8192 x 4096 x 4096 bf16 232 us with adapters (1.18 PFLOP/s; before registers stopped spilling 241 without them; stages of 64 bytes four deep 253, bank conflicts and 8-byte stores from registers 272, by way of registers
 // 315); a step of 4096 in the contraction costs what 1.29 PFLOP/s cost, the rest (35 us in two rounds of tiles) is first loads, adapters and stores.  Four waves of 128 x 128
-// would read a third less from LDS, but the compiler then moves accumulators between register files (933 us).  2000 rows 68 us, 512 28, 128 21; fp32 8192 x 1024 x 1024
-// 145 us (119 TFLOP/s of 157 that the fp32 instruction has).
+// would read a third less from LDS, but the compiler then moves accumulators between register files (933 us).  2000 rows 66 us, 512 28, 128 19; fp32 8192 x 1024 x 1024
+// 131 us (131 TFLOP/s of 157 that the fp32 instruction has; 145 where accumulators in registers of their own leave a compute unit one workgroup).
 template <typename T> struct Wide {
     Rows q;
     const T *x, *w, *b;
@@ -499,7 +499,7 @@ __device__ __forceinline__ u32x4 buffer_of(const void* p, size_t bytes)
 
 enum { NO_MASK = 0, MASK_DRAWN = 1, MASK_BITS = 2 };
 template <typename T, int WM, int WN, int MB, int NB, int PB, int NS, bool DMA, int DROP>
-__global__ __launch_bounds__(WM * WN * 64) void tiled_kernel(const Wide<T> p)
+__global__ __launch_bounds__(WM * WN * 64, 2) void tiled_kernel(const Wide<T> p)
 {
     constexpr int TM = 32 * MB * WM, TN = 32 * NB * WN, THREADS = WM * WN * 64, PIECES = (TM + TN) * PB / THREADS, E = 16 / sizeof(T), STAGE_K = PB * E;
     constexpr int PITCH = PB * 16, WITH = 16 / PB;        // bytes of a row; rows to all 64 banks
