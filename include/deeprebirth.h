@@ -308,7 +308,7 @@ int dr_softmax_loss_grad(const dr_tensor* d, const void* z, const int* labels, f
  * fp32.  1 <= rank <= DR_MAX_ADAPTER_RANK, 0 <= count <= DR_MAX_ADAPTERS (0: A, B and ids may be NULL), at most 2^26 pixels, and
  * count times max(c_in, c_out) / 64 at most 2^22.  Tensors do not overlap.  One adapter's, pixel's or gradient's infinities and NaN reach no
  * other's results.
- * ws: device scratch of at least dr_adapter_fwd_workspace_bytes, 256-byte aligned. */
+ * ws: device scratch of at least dr_adapter_fwd_workspace_bytes, 256-byte aligned; what serves a batch serves every smaller one (of n in xd). */
 #define DR_MAX_ADAPTER_RANK 128
 #define DR_MAX_ADAPTERS 16384
 typedef struct { int count, rank, c_in, c_out; } dr_adapters;

@@ -1078,16 +1078,22 @@ void wide(const Rows& q, const void* x, int K, const void* w, const float* bias,
 }
 
 constexpr int columns_of(int dtype) { return 512 / (dtype == DR_BF16 ? 2 : 4); }
-// positions that a workgroup of the sums over rows takes: four workgroups for every compute unit, of 32 rows and more, up to 2048 chunks
+// The sums over rows: positions come in chunks, at most as many as give each compute unit four workgroups (512, as there are two blocks of columns or more), of 32 positions
+// and more.  A chunk's length is a whole number of 32, so a few rows more can make fewer chunks: scratch is for the most that any batch up to this one has.
+int most_chunks(const AdapterShape& p)
+{
+    const int per = columns_of(p.dtype), blocks = (p.in + per - 1) / per + (p.out + per - 1) / per;
+    return std::max(1, 1024 / blocks);
+}
 int length_of(const AdapterShape& p)
 {
-    const int rows = p.images * p.hw, per = columns_of(p.dtype), blocks = (p.in + per - 1) / per + (p.out + per - 1) / per, chunks = std::max(1, 1024 / blocks);
-    return (int)align_up(std::max({(rows + chunks - 1) / chunks, (rows + 2047) / 2048, 1}), 32);
+    const int rows = p.images * p.hw, chunks = most_chunks(p);
+    return (int)align_up(std::max((rows + chunks - 1) / chunks, 1), 32);
 }
 size_t slots_of(const AdapterShape& p)
 {
-    const int rows = p.images * p.hw, length = length_of(p);
-    return (size_t)(rows + length - 1) / length + p.adapters;
+    const int rows = p.images * p.hw;
+    return (size_t)std::min(most_chunks(p), (rows + 31) / 32) + p.adapters;
 }
 
 template <typename T>
