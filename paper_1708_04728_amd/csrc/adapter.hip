@@ -6,8 +6,7 @@
 //
 // Both are a narrow product (t, u: rows x rank), a wide one whose contraction runs over the projection and then over the rank, and for the gradient two sums over the rows
 // of each adapter.  Rows are visited in the order of their adapters, so that few tiles hold rows of several; such a tile takes its adapters one after the other.
-// t and u are held in fp32 and enter bf16 products as two pieces each (16 bits of their values): with one piece the adapter's part of y would be rounded twice.  The sums
-// over rows, whose results are fp32, take three.
+// t and u are held in fp32 and enter bf16 products as three pieces each, all their bits: an output in which the projection and the adapter nearly cancel shows them.
 //
 // 8192 rows of 4096 channels to 4096 in bf16, eight adapters of rank 16, dropout: forward 266 us (order 7, narrow 26, wide 232: 1.18 PFLOP/s, where the library's
 // product alone takes 217), gradient 341 (order and copies 18, narrow 17, sums 58 + 6, wide 246).
@@ -241,6 +240,17 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Prepare p)
     __syncthreads();
     for (int e = threadIdx.x; e < 4096; e += 256)
         if (c0 + e / 64 < c.C && r0 + e % 64 < c.R) dst[(size_t)(c0 + e / 64) * c.R + r0 + e % 64] = tile[e % 64][e / 64];
+}
+
+// The upper bf16 pieces of eight numbers, which are left with the rest: three hold all 24 bits
+__device__ __forceinline__ u32x4 take_piece(float (&e)[8])
+{
+    const u32x4 v = pack8(e);
+    float up[8];
+    unpack8(v, up);
+#pragma unroll
+    for (int c = 0; c < 8; ++c) e[c] -= up[c];
+    return v;
 }
 
 // 16 bytes of a row, of which `n` elements exist (zeros behind them)
@@ -654,7 +664,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void tiled_kernel(const Wide<T> p)
             // (what comes of rows of other adapters is not taken, so their t need not be left out)
             const int r = r0 + h * E;
             const bool all = r0 + STEP <= q.rank;
-            u32x4 high[NB], low[NB], factor[MB];
+            u32x4 high[NB], middle[NB], low[NB], factor[MB];
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
                 const char* at = (const char*)(p.b + ((size_t)a * p.N + min(ow + i * 32 + l32, p.N - 1)) * q.rank + r);
@@ -663,15 +673,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void tiled_kernel(const Wide<T> p)
 #pragma unroll
             for (int j = 0; j < NB; ++j) {
                 const float* at = p.t + (size_t)max(row[j], 0) * q.rank + r;
-                float e[8];
                 if constexpr (sizeof(T) == 2) {
-                    float up[8];
+                    float e[8];
                     if (all) load8(at, e);
                     else load8(at, q.rank - r, 0.f, e);
-                    high[j] = pack8(e);
-                    unpack8(high[j], up);
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) e[c] -= up[c];
+                    high[j] = take_piece(e);
+                    middle[j] = take_piece(e);
                     low[j] = pack8(e);
                 } else high[j] = all ? piece((const char*)at) : piece<T>((const char*)at, q.rank - r);
             }
@@ -689,7 +696,10 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void tiled_kernel(const Wide<T> p)
                     }
                     f32x16 part = {};          // of its own: rows of other adapters must not meet this one's numbers, not even times zero
                     part = mfma32<T>(v, high[j], part);
-                    if constexpr (sizeof(T) == 2) part = mfma32<T>(v, low[j], part);
+                    if constexpr (sizeof(T) == 2) {
+                        part = mfma32<T>(v, middle[j], part);
+                        part = mfma32<T>(v, low[j], part);
+                    }
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const bool mine = id[j] == a && (keep >> ((e >> 2) * 8 + (e & 3)) & 1);
