@@ -242,14 +242,38 @@ __global__ __launch_bounds__(256) void prepare_kernel(const Prepare p)
         if (c0 + e / 64 < c.C && r0 + e % 64 < c.R) dst[(size_t)(c0 + e / 64) * c.R + r0 + e % 64] = tile[e % 64][e / 64];
 }
 
-// The upper bf16 pieces of eight numbers, which are left with the rest: three hold all 24 bits
-__device__ __forceinline__ u32x4 take_piece(float (&e)[8])
+// A number's upper 16 bits, a bf16 of its first 8 significant ones; `e` is left with the rest (none of an infinity).  Cut, not rounded: three pieces hold all 24 bits, none is
+// infinite unless the number is, and all have its sign.
+__device__ __forceinline__ uint16_t cut(float& e)
 {
-    const u32x4 v = pack8(e);
-    float up[8];
-    unpack8(v, up);
+    const unsigned bits = __float_as_uint(e);
+    const float upper = __uint_as_float(bits & 0xFFFF0000u);
+    e = e == upper ? 0.f : e - upper;
+    return (uint16_t)(bits >> 16);
+}
+__device__ __forceinline__ u32x4 cut8(float (&e)[8])
+{
+    u32x4 v;
 #pragma unroll
-    for (int c = 0; c < 8; ++c) e[c] -= up[c];
+    for (int i = 0; i < 4; ++i) {
+        const unsigned low = cut(e[2 * i]);
+        v[i] = low | (unsigned)cut(e[2 * i + 1]) << 16;
+    }
+    return v;
+}
+// What the lower pieces are multiplied by: infinities (and NaN) as bf16's largest number of their sign.  The upper piece alone meets them: a lower one may be zero, and zero times an
+// infinity would make a NaN of what is infinite.  (As signed numbers the positive ones beyond 0x7F7F, as unsigned ones those beyond 0xFF7F.)
+__device__ __forceinline__ u32x4 finite8(u32x4 v)
+{
+    typedef short i16x2 __attribute__((ext_vector_type(2)));
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned word = v[i];
+        const i16x2 above = __builtin_elementwise_min(__builtin_bit_cast(i16x2, word), i16x2{0x7F7F, 0x7F7F});
+        const u16x2 both = __builtin_elementwise_min(__builtin_bit_cast(u16x2, above), u16x2{0xFF7F, 0xFF7F});
+        v[i] = __builtin_bit_cast(unsigned, both);
+    }
     return v;
 }
 
@@ -677,14 +701,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void tiled_kernel(const Wide<T> p)
                     float e[8];
                     if (all) load8(at, e);
                     else load8(at, q.rank - r, 0.f, e);
-                    high[j] = take_piece(e);
-                    middle[j] = take_piece(e);
-                    low[j] = pack8(e);
+                    high[j] = cut8(e);
+                    middle[j] = cut8(e);
+                    low[j] = cut8(e);
                 } else high[j] = all ? piece((const char*)at) : piece<T>((const char*)at, q.rank - r);
             }
 #pragma unroll
             for (int i = 0; i < MB; ++i) {
-                const u32x4 v = factor[i];
+                const u32x4 v = factor[i], vf = sizeof(T) == 2 ? finite8(v) : v;
 #pragma unroll
                 for (int j = 0; j < NB; ++j) {
                     // this lane's row of the block: outputs 16 h .. 16 h + 15, the others from the lane that holds the same row
@@ -697,8 +721,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void tiled_kernel(const Wide<T> p)
                     f32x16 part = {};          // of its own: rows of other adapters must not meet this one's numbers, not even times zero
                     part = mfma32<T>(v, high[j], part);
                     if constexpr (sizeof(T) == 2) {
-                        part = mfma32<T>(v, middle[j], part);
-                        part = mfma32<T>(v, low[j], part);
+                        part = mfma32<T>(vf, middle[j], part);
+                        part = mfma32<T>(vf, low[j], part);
                     }
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
@@ -923,12 +947,9 @@ __global__ __launch_bounds__(256, RB == 1 ? 4 : 1) void sums_kernel(const Rows q
         for (int i = 0; i < F_PER; ++i) {
             const int e = threadIdx.x + i * 256;
             if constexpr (BF) {
-                const uint16_t high = f32_to_bf16(heldf[i]);
-                const float rest = heldf[i] - bf16_to_f32(high);
-                const uint16_t middle = f32_to_bf16(rest);
-                reinterpret_cast<uint16_t*>(ft[to])[e] = high;
-                reinterpret_cast<uint16_t*>(ft[to])[FB + e] = middle;
-                reinterpret_cast<uint16_t*>(ft[to])[2 * FB + e] = f32_to_bf16(rest - bf16_to_f32(middle));
+                float rest = heldf[i];
+#pragma unroll
+                for (int third = 0; third < 3; ++third) reinterpret_cast<uint16_t*>(ft[to])[third * FB + e] = cut(rest);
             } else reinterpret_cast<float*>(ft[to])[e] = heldf[i];
         }
     };
@@ -961,15 +982,20 @@ __global__ __launch_bounds__(256, RB == 1 ? 4 : 1) void sums_kernel(const Rows q
                         b[j] = u32x4{lo[0], lo[1], hi[0], hi[1]};
                     }
 #pragma unroll
-                    for (int i = 0; i < RB; ++i)
+                    for (int third = 0; third < 3; ++third) {
+                        if (third == 1) {
 #pragma unroll
-                        for (int third = 0; third < 3; ++third) {
+                            for (int j = 0; j < CB; ++j) b[j] = finite8(b[j]);
+                        }
+#pragma unroll
+                        for (int i = 0; i < RB; ++i) {
                             const unsigned char* at = fs + third * FB * 2 + row * (RB * 32) + i * 32 + (l16 & 3) * 8;
                             const u32x2 lo = read_transposed(at), hi = read_transposed(at + 4 * RB * 32);
                             const u32x4 w = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
                             for (int j = 0; j < CB; ++j) acc[i][j] = mfma(w, b[j], acc[i][j]);
                         }
+                    }
                 } else {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
