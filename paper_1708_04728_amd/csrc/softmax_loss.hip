@@ -75,15 +75,16 @@ struct Loss {
     float smoothing;
     int mean;
     const int* counted;          // rows with a label, or NULL: every workgroup counts them
+    float share;                 // a power of two of at most 1 / (2 C): so much of a row's numbers adds up to no more than the largest of them
     float* row_loss;
 };
 
 // what one row's gradient and loss need beside its exponentials
-struct RowSums { float top, sum, shifted; };       // max z, sum exp(z - top), sum (z - top)
+struct RowSums { float top, sum, shifted; };       // max z, sum exp(z - top), sum (z - top) share
 
 __device__ __forceinline__ float row_loss_of(const Loss& q, const RowSums& s, float z_t)
 {
-    const float about = q.smoothing != 0.f ? q.smoothing * (s.shifted / (float)q.C) : 0.f;
+    const float about = q.smoothing != 0.f ? q.smoothing * s.shifted / ((float)q.C * q.share) : 0.f;
     return logf(s.sum) - (1.f - q.smoothing) * (z_t - s.top) - about;
 }
 
@@ -135,7 +136,7 @@ __global__ __launch_bounds__(PER < 256 ? 256 : PER, 4) void loss_kernel(const Lo
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) shifted += !ragged(i) || j >= twice(i) ? v[i][j] - top : 0.f;
+                for (int j = 0; j < 8; ++j) shifted += !ragged(i) || j >= twice(i) ? __builtin_fmaf(v[i][j], q.share, -top * q.share) : 0.f;
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
@@ -193,7 +194,7 @@ __global__ __launch_bounds__(256) void loss_short_kernel(const Loss q, const T* 
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            if (j < q.C) s.shifted += v[j] - s.top;
+            if (j < q.C) s.shifted += __builtin_fmaf(v[j], q.share, -s.top * q.share);
             v[j] = j < q.C ? exp_of<T>(v[j] - s.top) : 0.f;
             s.sum += v[j];
         }
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(1024) void loss_long_kernel(const Loss q, const T* 
                 sum *= exp_of<T>(top - from);
                 if (q.smoothing != 0.f) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) shifted += c + j < q.C ? v[j] : 0.f;
+                    for (int j = 0; j < 8; ++j) shifted += c + j < q.C ? v[j] * q.share : 0.f;
                 }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum += exp_of<T>(v[j] - from);
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(1024) void loss_long_kernel(const Loss q, const T* 
             }
             s.top = reduce<1024>(top, red, larger);
             s.sum = reduce<1024>(top == -INFINITY ? (s.top == -INFINITY ? NAN : sum) : sum * exp_of<T>(top - s.top), red, add);
-            s.shifted = q.smoothing != 0.f ? reduce<1024>(shifted, red, add) - (float)q.C * s.top : 0.f;
+            s.shifted = q.smoothing != 0.f ? reduce<1024>(shifted, red, add) - (float)q.C * q.share * s.top : 0.f;
             if (threadIdx.x == 0) q.row_loss[row] = row_loss_of(q, s, z_t);
             __syncthreads();                                                    // (dz may be z: the label's logit has been read)
         } else if (threadIdx.x == 0) q.row_loss[row] = 0.f;
@@ -311,6 +312,8 @@ int launch_softmax_loss_grad(int dtype, int rows, int classes, const void* z, co
 {
     TraceScope trace("softmax_loss", nullptr, (long long)rows * classes, st, (long long)rows * classes * (long long)elem_size(dtype) * (dz ? 2 : 1));
     Loss q;
+    q.share = 0.5f;
+    for (unsigned c = 1; c < (unsigned)classes; c *= 2) q.share *= 0.5f;
     q.rows = rows; q.C = classes; q.labels = labels; q.smoothing = smoothing; q.mean = mean;
     q.row_loss = row_loss ? row_loss : (float*)((char*)ws + 256);
     q.counted = nullptr;
