@@ -53,3 +53,15 @@ def test_masks_of_the_lowest_value(classes, dtype):
     ut = 2.0 ** -8 if dtype == torch.bfloat16 else U
     # probabilities are good to 1e-4 of themselves (logits below 8 beside a sum of at most 70003 terms), the smoothing's part and the result round
     assert note("gradient / bound", np.max(np.abs(dz - grad) / (1e-4 * (grad + 1) * (grad > 0) + (ut + 1e-5) * np.abs(grad) + 1e-6 * e)), 1.0)
+
+
+@pytest.mark.parametrize("classes", CLASSES)
+def test_a_label_as_far_below_as_its_part_allows(classes):
+    z = torch.zeros((2, classes))
+    z[:, 0], z[:, 1] = 3e38, -3e38
+    e = float(np.float32(0.75))                                   # 6e38 from the largest: beyond fp32, its quarter is not
+    ref, tol, _ = expect(z, [0, 1], e)
+    ok = np.abs(ref) < 3.3e38
+    row, _ = run(z.cuda(), [0, 1], e)
+    assert ok[0] and note("row loss / bound", np.max((np.abs(row - ref) / tol)[ok]), 1.0)
+    assert np.isinf(row[~ok]).all()
