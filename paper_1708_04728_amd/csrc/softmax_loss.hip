@@ -86,7 +86,8 @@ __device__ __forceinline__ float row_loss_of(const Loss& q, const RowSums& s, fl
 {
     const float about = q.smoothing != 0.f ? q.smoothing * s.shifted / ((float)q.C * q.share) : 0.f;
     // (halves: their difference is a number wherever both are)
-    return logf(s.sum) - 2.f * ((1.f - q.smoothing) * (0.5f * z_t - 0.5f * s.top)) - about;
+    const float label = q.smoothing != 1.f ? 2.f * ((1.f - q.smoothing) * (0.5f * z_t - 0.5f * s.top)) : 0.f;
+    return logf(s.sum) - label - about;
 }
 
 // PER lanes a row, NV blocks of eight elements a lane; workgroups of max(PER, 256) threads walk the rows

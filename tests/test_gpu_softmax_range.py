@@ -65,3 +65,15 @@ def test_a_label_as_far_below_as_its_part_allows(classes):
     row, _ = run(z.cuda(), [0, 1], e)
     assert ok[0] and note("row loss / bound", np.max((np.abs(row - ref) / tol)[ok]), 1.0)
     assert np.isinf(row[~ok]).all()
+
+
+@pytest.mark.parametrize("classes", CLASSES)
+def test_smoothing_of_one_asks_nothing_of_the_label(classes):
+    """(1 - e) z_t is no part of the loss then, whatever the label's logit: with a masked class the mean is infinite, and so is the loss."""
+    z = torch.zeros((2, classes))
+    z[0, 1] = -float("inf")
+    row, dz = run(z.cuda(), [1, 1], 1.0)
+    assert row[0] == np.inf and abs(row[1] - np.log(classes)) < 1e-5
+    ref = np.full(classes, 1 / (classes - 1) - 1 / classes)
+    ref[1] = -1 / classes
+    assert np.abs(dz[0] - ref).max() < 1e-6 and np.abs(dz[1]).max() < 1e-6
