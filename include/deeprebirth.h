@@ -305,7 +305,7 @@ int dr_softmax_loss_grad(const dr_tensor* d, const void* z, const int* labels, f
  * 1x1), fp32 or bf16; W: c_out x c_in, A: count x rank x c_in, B: count x c_out x rank, dense, of the same type.  bias, scales: fp32,
  * c_out and count entries (NULL: zeros, ones).  ids: one device int per image of x.  drop (NULL or p = 0: none): dropout of x in
  * front of A only.  inner: fp32, rank values per pixel, that the gradient reads (NULL: not stored).  Sums, inner among them, are held in
- * fp32.  1 <= rank <= DR_MAX_ADAPTER_RANK, 0 <= count <= DR_MAX_ADAPTERS (0: A, B and ids may be NULL), at most 2^26 pixels, and
+ * fp32.  1 <= rank <= DR_MAX_ADAPTER_RANK, 0 <= count <= DR_MAX_ADAPTERS (0: A, B and ids may be NULL), at most 2^26 pixels, 2^29 channels, and
  * count times max(c_in, c_out) / 64 at most 2^22.  Tensors do not overlap.  One adapter's, pixel's or gradient's infinities and NaN reach no
  * other's results.
  * ws: device scratch of at least dr_adapter_fwd_workspace_bytes, 256-byte aligned; what serves a batch serves every smaller one (of n in xd). */

@@ -1639,7 +1639,8 @@ static int check_adapters(const char* who, const dr_tensor* xd, const dr_adapter
     const double pixels = (double)xd->n * xd->h * xd->w, most = std::max(ad->c_in, ad->c_out), factors = (double)ad->count * ad->rank;
     if (pixels * std::max(most, (double)ad->rank) >= 2147483648.0 || (double)ad->c_in * ad->c_out >= 2147483648.0 || factors * most >= 2147483648.0)
         return fail(DR_ERR_UNSUPPORTED, "%s: a tensor of more than 2^31-1 elements", who);
-    if (pixels > (1 << 26) || most > MOST) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^26 pixels or 2^30 channels", who);
+    // (a launch has fewer than 2^32 threads: 256 for every 64 x 64 of W)
+    if (pixels > (1 << 26) || most > MOST / 2) return fail(DR_ERR_UNSUPPORTED, "%s: more than 2^26 pixels or 2^29 channels", who);
     // (blocks of 64 x 64 of A and B, a workgroup each)
     if (ad->count * ceil(most / 64) * 2 > (1 << 23)) return fail(DR_ERR_UNSUPPORTED, "%s: %d adapters of %.0f channels", who, ad->count, most);
     p->images = pixels > 0 ? xd->n : 0;

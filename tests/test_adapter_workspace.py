@@ -20,3 +20,12 @@ def test_a_larger_batch_asks_for_no_less(cin, cout, rank, count, hw, most, dtype
     for size in (L.dr_adapter_fwd_workspace_bytes, L.dr_adapter_bwd_workspace_bytes):
         asked = [need(size, rows, cin, cout, rank, count, dtype, hw) for rows in range(most)]
         assert [i for i in range(1, most) if asked[i] < asked[i - 1]] == []
+
+
+def test_channels_beyond_a_launch_are_refused():
+    L = B.lib()
+    n = C.c_size_t(0)
+    for size in (L.dr_adapter_fwd_workspace_bytes, L.dr_adapter_bwd_workspace_bytes):
+        for cin, cout in ((1, 1 << 30), (1 << 30, 1), (1, (1 << 29) + 1)):
+            assert size(B.dr_tensor(1, cin, 1, 1, B.DR_F32, B.DR_NHWC), B.dr_adapters(0, 1, cin, cout), n) == B.DR_ERR_UNSUPPORTED and "2^29" in B.last_error()
+        assert size(B.dr_tensor(1, 1, 1, 1, B.DR_F32, B.DR_NHWC), B.dr_adapters(0, 1, 1, 1 << 29), n) == B.DR_OK
