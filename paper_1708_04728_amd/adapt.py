@@ -8,8 +8,9 @@ correction B A of them.  A step on a batch whose images belong to any of the tas
     backward    to every task's A and B (and to x)                 dr_adapter_bwd
     descent     A and B along their gradients                      dr_sgd_step
 
-every one of them a kernel of the library on the caller's stream, on buffers made once.  ``python -m paper_1708_04728_amd.adapt`` learns adapters of a slimmed
-GoogLeNet's classifier on synthetic features and prints the loss.
+every one of them a kernel of the library on the caller's stream, on buffers made once; a batch may have fewer rows than they were made for.  Parameters are fp32.
+``python -m paper_1708_04728_amd.adapt`` learns adapters of a classifier of GoogLeNet's size (1024 features to 1000 classes, random weights) on synthetic features and
+prints the loss.
 """
 from __future__ import annotations
 

@@ -8,8 +8,9 @@
 // of each adapter.  Rows are visited in the order of their adapters, so that few tiles hold rows of several; such a tile takes its adapters one after the other.
 // t and u are held in fp32 and enter bf16 products as three pieces each, all their bits: an output in which the projection and the adapter nearly cancel shows them.
 //
-// 8192 rows of 4096 channels to 4096 in bf16, eight adapters of rank 16, dropout: forward 266 us (order 7, narrow 26, wide 232: 1.18 PFLOP/s, where the library's
-// product alone takes 217), gradient 341 (order and copies 18, narrow 17, sums 58 + 6, wide 246).
+// 8192 rows of 4096 channels to 4096 in bf16, eight adapters of rank 16, dropout: forward 267 us, gradient 346.  Their kernels under the profiler, shortest and average of 20:
+// order 7.5 and 8.4, narrow 26 and 32, wide 234 and 264 (1.17 and 1.04 PFLOP/s; the library's product alone takes 217); order and copies 18 and 19, narrow 17 and 19, sums 62 and 70 with
+// 6 for their join, wide 249 and 275.
 #include <algorithm>
 #include <type_traits>
 
@@ -126,7 +127,7 @@ struct Rows {
 // ---- what the products start from: the order of the images by adapter, and transposed copies ------------------------------------------------------
 // Order: workgroup a writes the images of adapter a (the last one those without) in the order in which they come: first how many belong before them, then which they
 // are.  A wave takes a quarter of the ids, four of a lane at a time.
-// Copies: src[batch][R][C] -> dst[batch][C][R], 64 x 64 elements a workgroup.  Of W, A and B for the gradient, whose products run over the other dimension: 18 us of 341 at
+// Copies: src[batch][R][C] -> dst[batch][C][R], 64 x 64 elements a workgroup.  Of W, A and B for the gradient, whose products run over the other dimension: 18 us of 346 at
 // 4096 x 4096 in bf16, most of it W's 64 MB; one launch with the order, where four took 53.
 struct Copy { const void* src; void* dst; int R, C, tiles_r, tiles_c, first, last; };      // workgroups first .. last - 1
 struct Prepare {
@@ -415,8 +416,8 @@ __device__ __forceinline__ void wave_product(const T* a, RA ra, const T* b, RB_ 
 
 // ---- a narrow product: out[row][r] = s_a sum_k v[row][k] M_a[r][k] -----------------------------------------------------------------------------
 // A workgroup takes 16 rows and the adapters among them, every gridDim.y-th from its own on (the i-th adapter is that of the i-th row whose adapter no row before has); its NW
-// waves share the contraction and add up in LDS.  Bound by memory (8192 rows of 4096 in bf16: 17 us, 3.9 TB/s of v, and M_a again from L2 for every 16 rows), with dropout by
-// the vector instructions that draw the mask (26 us; 33 where registers leave a compute unit one workgroup); 64 rows with an adapter each 6.5 us.
+// waves share the contraction and add up in LDS.  Bound by memory (8192 rows of 4096 in bf16: 17-19 us, 3.5-3.9 TB/s of v, and M_a again from L2 for every 16 rows), with dropout by
+// the vector instructions that draw the mask (26-32 us; 33 at its shortest where registers leave a compute unit one workgroup); 64 rows with an adapter each 7-8 us.
 template <typename T, int RB, int NW, int D, bool DROP>
 __global__ __launch_bounds__(NW * 64, RB == 1 && sizeof(T) == 2 ? 4 : 1) void narrow_kernel(const Rows q, const T* __restrict__ v, int K, const T* __restrict__ m, const Drop drop, float* __restrict__ out)
 {
@@ -465,10 +466,12 @@ __global__ __launch_bounds__(NW * 64, RB == 1 && sizeof(T) == 2 ? 4 : 1) void na
 // A workgroup of WM x WN waves owns TM = 32 MB WM outputs of TN = 32 NB WN rows, a wave MB x NB blocks of 32 x 32.  PB pieces of 16 bytes of every row of W and x are a
 // stage, of which LDS holds NS: one that is multiplied and others on their way, by loads that write LDS (DMA: rows of whole, aligned 16-byte pieces), or one by way of
 // registers.  A row's pieces lie in the order piece ^ (row PB / 16): the same piece of sixteen rows is then in all 64 banks.
-// 8192 x 4096 x 4096 bf16 232 us with adapters (1.18 PFLOP/s; before registers stopped spilling 241 without them; stages of 64 bytes four deep 253, bank conflicts and 8-byte stores from registers 272, by way of registers
+// 8192 x 4096 x 4096 bf16 234 us with adapters, the shortest of 20 launches as are the figures behind it (1.17 PFLOP/s, 1.04 on average; before registers stopped spilling 241 without adapters; stages of 64 bytes four deep 253, bank conflicts and 8-byte stores from registers 272, by way of registers
 // 315); a step of 4096 in the contraction costs what 1.29 PFLOP/s cost, the rest (35 us in two rounds of tiles) is first loads, adapters and stores.  Four waves of 128 x 128
 // would read a third less from LDS, but the compiler then moves accumulators between register files (933 us).  2000 rows 66 us, 512 28, 128 19; fp32 8192 x 1024 x 1024
 // 131 us (131 TFLOP/s of 157 that the fp32 instruction has; 145 where accumulators in registers of their own leave a compute unit one workgroup).
+// A mask drawn here (no da, or c_in no multiple of 8) is drawn again for every adapter and step of rank of a wave, and the tile of 256 x 256 then spills about 100 registers: with dropout the
+// gradient to x alone takes 321 us, 260 without; 8192 rows to 4100 channels 515.
 template <typename T> struct Wide {
     Rows q;
     const T *x, *w, *b;
@@ -855,7 +858,7 @@ __global__ __launch_bounds__(512) void few_kernel(const Wide<T> p)
 // other: a segment each.  Both operands are contracted over rows, so they go through LDS, 32 rows at a time: bf16 is read from there transposed, f cut into three pieces
 // (all its bits: the sums are fp32).  A segment that is all of its adapter is the result; others are partial sums, that of chunk k and adapter a in slot k + a (one of the
 // two grows from a segment to the next), added in their order after.
-// 8192 rows of 4096 + 4096 columns in bf16, rank 16: 58 us for 134 MB, bound by the vector instructions that draw x's mask (44 without) and move both operands through LDS.
+// 8192 rows of 4096 + 4096 columns in bf16, rank 16: 62-70 us for 134 MB, bound by the vector instructions that draw x's mask (58 and 44 without it, before lower pieces met infinities as numbers) and move both operands through LDS.
 struct Sum {
     const void* v;
     const float* f;

@@ -4,7 +4,8 @@
 //
 // A row is read once: its lanes hold it in registers from the maximum to the gradient.  Sums are in fp32 over a lane's elements, then over lanes in a fixed order; the
 // loss of all rows is added in double.  Bound by memory where rows are many (8192 x 32768 bf16 223 us, 4.8 TB/s; 353 with loads behind conditions, 276 with exponentials of
-// eight instructions, 294 with 512 lanes of 64 elements, whose registers spill), by launches where they are few (128 x 1000: 4.4 + 2.2 us).
+// eight instructions, 294 with 512 lanes of 64 elements, whose registers spill), by launches where they are few (128 x 1000: 4.5 + 2.5 us), by the one workgroup that counts labels and the one that adds losses where
+// they are many and short (2^20 x 16: 876 us).
 #include <algorithm>
 
 #include "dr_internal.h"
@@ -289,7 +290,8 @@ void launch_rows(const Loss& q, const void* z, void* dz, hipStream_t st)
     hipLaunchKernelGGL((loss_kernel<T, PER, NV>), dim3(std::min(groups, 8192)), dim3(THREADS), 0, st, q, (const T*)z, (T*)dz);
 }
 
-// The fewest lanes that hold a row in at most 32 elements each
+// The fewest lanes that hold a row in at most 32 elements each; in 64 above 32768 classes, where 1024 lanes are all there are and some registers spill (2048 x 50001 bf16 178 us, fp32 208; read
+// twice, 2048 x 65537 bf16 162)
 template <typename T>
 void launch(const Loss& q, const void* z, void* dz, hipStream_t st)
 {
