@@ -16,10 +16,10 @@ namespace {
 
 constexpr int COUNT_ROWS = 2048;         // most labels that every workgroup counts for itself
 
-// exp(d) for d <= 0: 2^p with p = d log2 e, whose rounding puts it off by |d| 2^-24 of itself.  fp32 gradients show that (70 of their last bits at d = -80), so in fp32 what the rounding
-// lost, d - p ln 2, is put back: off by (3 + |d| / 20) 2^-24.  bf16 ones are rounded at 2^-9, and the sum, where exp(d) counts for p_j of it, is off by
-// sum p_j |d_j| 2^-24 <= ln C 2^-24 (their mean is the entropy less ln of the sum), a tenth of what its additions may round away; three instructions more cost
-// 8192 x 32768 classes 13 us of 229 there, and nothing in fp32.
+// exp(d) for d <= 0: 2^p with p = d log2 e, whose rounding and that of log2 e put it off by up to 1.3 |d| 2^-24 of itself.  fp32 gradients show that (70 x 2^-24 at d = -80), so in fp32 what
+// is lost, d - p ln 2, is put back: off by (3 + |d| / 20) 2^-24.  bf16 ones are rounded at 2^-8, and the sum, of which exp(d_j) is the share p_j, is off by
+// 1.3 sum p_j |d_j| 2^-24 <= 1.3 ln C 2^-24 (sum p_j |d_j| is the entropy less ln of the sum), 14 x 2^-24 at 65536 classes, where its additions may round away up to 90: three
+// instructions more cost 8192 x 32768 classes 13 us of 229 there, and nothing in fp32.
 // -inf gives 0, a NaN stays one; below 2^-126 zero, where the instruction ends: a sum, which is 1 at least, does not see it, and a gradient that small is 0.
 template <typename T>
 __device__ __forceinline__ float exp_of(float d)
